@@ -385,6 +385,176 @@ scalify_status scalify_layernorm_bwd(const scalify_scaled_array* dy, const scali
                                      float* pre_out, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
+/* Scaled RMS norm forward with the residual's addition and an output in 8 bits
+ * (or F16) with its scales. Per row r of x (R x D):
+ *   residual R': scaled add (Section 3.2, Algorithm 3): e_h = max(e(s_x), e(s_r)),
+ *     h = fl32(x_d 2^(e(s_x) - e_h) + r_d 2^(e(s_r) - e_h)); sum_out.data =
+ *     RNE(h) in sum_out.dtype, *sum_out.scale = 2^e_h. With sum_out the stored
+ *     (rounded) value is what the norm sees, so that scalify_rmsnorm_bwd, which
+ *     reads it, is the gradient of this very function. No residual: h = x_d
+ *     (x.scale is not read, as in scalify_layernorm_fwd).
+ *   The normalization is scale invariant up to its eps, so the data is
+ *   normalized (Appendix C.2):
+ *   y = h / sqrt(sum_j h[r,j]^2 / D + eps) * gamma  (0 for a zero row, also with eps = 0)
+ *   out.data = RNE(y 2^-e), *out.scale = 1, where
+ *     e = 0, or, with row_scale (device fp32 [R]), e_r = clamp(floor(log2 amax_r) -
+ *     target_log2, -127, 127) of the row's amax over non-NaN |y| (0 when that is 0 or
+ *     Inf) and row_scale[r] = 2^e_r: the a_channel_scale of a scalify_matmul whose a
+ *     is out; or, with block_scale, the same per 32 columns of a row, as E8M0 bytes
+ *     e + 127 in the packed order of scalify_mx_pack_block_scales (rows = R, K = D;
+ *     padding written as 127): the a_block_scale of that matmul (or, with out
+ *     read through trans, its b_block_scale).
+ * x.dtype: any scalify_dtype; residual, sum_out and out: E4M3, E5M2 or F16 (out
+ * 8-bit with block_scale). All R x D with the layout rules of
+ * scalify_layernorm_fwd, 1 <= D <= 8192 (any D when R = 0). residual, sum_out,
+ * gamma (device fp32 [D], NULL = 1), row_scale, block_scale (4-byte aligned,
+ * scalify_mx_packed_bytes(R, D) bytes) and pre_out (device fp32 [R][D]: y) are
+ * optional (NULL). sum_out needs a residual (SCALIFY_ERR_NULL), row_scale and
+ * block_scale exclude each other (SCALIFY_ERR_VALUE). out and sum_out may each be
+ * the very same matrix as x or residual (same data, element size and ld) but must
+ * not otherwise overlap them or each other; with a residual an output's scale
+ * must not be the memory of an input's scale or the other output's
+ * (SCALIFY_ERR_LAYOUT). saturate applies to both casts. Squares of F32 inputs
+ * of any magnitude stay in range (the row is divided by a power of two first).
+ * Sums are fp32 in a fixed order: reruns are bit-identical. */
+scalify_status scalify_rmsnorm_fwd(const scalify_scaled_array* x,
+                                   const scalify_scaled_array* residual, const float* gamma,
+                                   float eps, scalify_scaled_array* sum_out,
+                                   scalify_scaled_array* out, float* row_scale,
+                                   uint8_t* block_scale, int32_t target_log2, int32_t saturate,
+                                   float* pre_out, void* stream);
+
+/* Bytes of device workspace scalify_rmsnorm_bwd needs: a 256-byte header plus,
+ * in fp32, 4 numbers per row and up to 1024 partial rows of dgamma. 0 for
+ * invalid sizes (D > 8192). */
+size_t scalify_rmsnorm_bwd_workspace_size(int64_t R, int64_t D);
+
+/* Input gradient of scalify_rmsnorm_fwd's norm with respect to the data of x,
+ * the array that was normalized (sum_out, or x without a residual), plus the
+ * gradient that reaches that array itself (dsum, from the residual stream),
+ * with the dynamic rescale. Per row (inv = 1 / sqrt(mean(x_d^2) + eps), g =
+ * dy_d * gamma):
+ *   dn = inv (g - x_d inv^2 mean(g x_d)), scale s_dy / s_x
+ *   dsum: scaled add: e = max(e(s_dy) - e(s_x), e(s_ds)),
+ *     dx = fl32(dn 2^(e(s_dy) - e(s_x) - e) + ds_d 2^(e(s_ds) - e)); else dx = dn
+ *   AMAX: e_r = floor(log2 amax |dx|) - target_log2 (0 for amax 0 / Inf / all
+ *   NaN); NONE: e_r = 0. e_out = clamp(e + e_r, -127, 127), dx.data = RNE(dx
+ *   2^(e - e_out)), *dx.scale = 2^e_out.
+ *   dgamma[j] = sum_r dy_d[r,j] x_d[r,j] inv (optional device fp32 [D]; its true
+ *   value is this times s_dy).
+ * By the sum rule dx is the gradient of x and of the residual alike. dsum's
+ * gradient is with respect to the sum's true value, dn's (as in
+ * scalify_layernorm_bwd) to the data over its scale; both carry true values.
+ * dy and x: any scalify_dtype; dsum and dx: E4M3, E5M2 or F16; all R x D with
+ * the layout rules of scalify_layernorm_fwd; dx may be the very same matrix as
+ * dy, x or dsum but must not otherwise overlap them, and dx.scale may be the
+ * memory of an input's scale. amax_out: optional device fp32, the amax of |dx|;
+ * pre_out: optional device fp32 [R][D], dx before the rescale. workspace: at
+ * least scalify_rmsnorm_bwd_workspace_size(R, D) bytes, 256-byte aligned, not
+ * shared with a concurrent call. Deterministic on one device (fixed-order
+ * sums; their grouping depends on the device's number of compute units). */
+scalify_status scalify_rmsnorm_bwd(const scalify_scaled_array* dy, const scalify_scaled_array* x,
+                                   const scalify_scaled_array* dsum, const float* gamma, float eps,
+                                   scalify_scaled_array* dx, float* dgamma, int32_t rescale,
+                                   int32_t target_log2, int32_t saturate, float* amax_out,
+                                   float* pre_out, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/* Attention over ScaledArrays. The matrices are those that the layer's GEMMs
+ * write and read: rows are tokens, columns heads * head_dim (head h at columns h *
+ * head_dim ...), any ld, so that q, k and v may be column ranges of one matrix. */
+typedef struct {
+    int32_t heads;       /* query heads */
+    int32_t kv_heads;    /* key and value heads: heads is a multiple; query head h reads key head
+                            h / (heads / kv_heads) */
+    int32_t head_dim;    /* a multiple of 16 in [16, 128] */
+    int32_t causal;      /* 1: query i of a sequence of L_q queries and L_k keys sees the keys
+                            j <= i + L_k - L_q (the last query sees all of them) */
+    int64_t batch;       /* sequences */
+    float softmax_scale; /* alpha > 0, finite: the scores are alpha * q . k of the true values */
+    const int64_t* q_start; /* optional device [batch + 1], not decreasing: sequence b has the rows
+                            q_start[b] ... q_start[b + 1] - 1 of q; NULL: rows / batch each.
+                            Rows that belong to no sequence are left as they were */
+    const int64_t* k_start; /* likewise the rows of k and v; NULL: rows / batch each */
+    const int64_t* k_len;   /* optional device [batch]: only the first k_len[b] of sequence b's
+                            rows of k and v are keys (a cache that is not full) */
+    int64_t max_q;       /* with q_start: no sequence has more queries (0: any number). Rows
+                            past it are left as they were */
+    int64_t max_k;       /* with k_start: no sequence has more rows of k (0: any number); the
+                            backward leaves rows past it as they were. With k_len, the most
+                            keys of a sequence, if that is known (0: it is not): a hint for how
+                            the work is split */
+} scalify_attention_opts;
+
+/* Bytes of device workspace scalify_attention_fwd needs for rows_q rows of q and
+ * rows_k rows of k. 0 where the call needs none, and for invalid arguments. */
+size_t scalify_attention_fwd_workspace_size(int64_t rows_q, int64_t rows_k,
+                                            const scalify_attention_opts* opts);
+
+/* Attention forward: per sequence and query head
+ *   S_ij = alpha s_q s_k sum_d q_id k_jd (admitted pairs), P = softmax_j(S), O = P v.
+ * A row of P has the sum 1, so a result's data lies in the range of v's data:
+ * *out.scale = *v.scale (clamped to the E8M0 range) and out.data = RNE(sum_j P_ij
+ * v_jd), saturating when `saturate`. lse (optional device fp32 [heads][rows of
+ * q]): log sum_j exp(S_ij), which the backward reads. A query that sees no key
+ * gives zeros and lse = -Inf. What a mask or k_len hides has no effect, whatever
+ * it holds (Inf, NaN); an admitted NaN gives NaN.
+ * Scores, statistics and sums are fp32. The probabilities that multiply v are
+ * rounded to F16 as 2^14 P relative to the row's running maximum (half a step:
+ * 2^-11 of each; exact products with any v, and no loss down to P = 2^-28).
+ * q, k, v: E4M3, E5M2 or F16, any mix of q with k and v, k and v any mix; out:
+ * E4M3, E5M2 or F16. q and out: [rows of q][heads * head_dim], k and v: [rows of
+ * k][kv_heads * head_dim]; trans = 0; data 16-byte aligned, every ld a multiple
+ * of 16 elements (8 for F16) with 128 rows below 2^31 bytes. out must not overlap q, k
+ * or v (other columns of rows of the same pitch in bytes are no overlap);
+ * out.scale may be v's but not q's or k's. At most 2^30 rows, 2^30 queries times
+ * heads that share a key head per sequence, and 2^31 - 1 workgroups (SCALIFY_ERR_SHAPE).
+ * The values of q_start, k_start and k_len are not errors: they are clamped to
+ * the matrices' rows. workspace: scalify_attention_fwd_workspace_size bytes (may be
+ * NULL when that is 0), 256-byte aligned, not shared with a concurrent call.
+ * Few queries, single tokens among them, take a kernel that splits the keys.
+ * Deterministic: reruns are bit-identical. */
+scalify_status scalify_attention_fwd(const scalify_scaled_array* q, const scalify_scaled_array* k,
+                                     const scalify_scaled_array* v, scalify_scaled_array* out,
+                                     float* lse, const scalify_attention_opts* opts,
+                                     int32_t saturate, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/* Bytes of device workspace scalify_attention_bwd needs: a 256-byte header, 2
+ * fp32 numbers per query row and head and 1 per key row and head, and with AMAX
+ * the fp32 gradients. 0 for invalid arguments. */
+size_t scalify_attention_bwd_workspace_size(int64_t rows_q, int64_t rows_k,
+                                            const scalify_attention_opts* opts, int32_t rescale);
+
+/* Gradients of scalify_attention_fwd for the upstream gradient dO = dout, from the
+ * forward's inputs and its stored results out and lse: with S as above
+ *   P_ij = exp(S_ij - lse_i), delta_i = sum_d dO_id O_id, dP_ij = sum_d dO_id v_jd,
+ *   dS = P (dP - delta), dV = P^T dO, dQ = alpha dS k, dK = alpha dS^T q
+ * (a key head's gradients are summed over the query heads that share it), as
+ * ScaledArrays with the propagated scales dv: s_do, dq: s_do s_v s_k, dk: s_do s_v
+ * s_q. Each has its own rescale, as in scalify_layernorm_bwd:
+ *   AMAX: e_r = floor(log2 amax of its data) - target_log2 (0 for amax 0 / Inf / all
+ *   NaN), NONE: e_r = 0; e_out = clamp(propagated + e_r, -127, 127).
+ * amax_out: optional device fp32 [3], the statistics of dq, dk and dv.
+ * Rows of k past k_len get zeros. P is rounded to F16 as above, dS to F16 times a
+ * power of two that a bound of its largest magnitude in the sequence and head,
+ * 2 max |dO_i| max |v_j|, gives.
+ * dout, q, k, v: E4M3, E5M2 or F16; out: F16 (delta needs more than 8-bit codes
+ * keep); dq, dk, dv: E4M3, E5M2 or F16. Shapes, layouts and limits as in the
+ * forward; sequences must not share rows. dq, dk and dv must not overlap an
+ * input or each other (other columns of rows of the same pitch are no overlap),
+ * nor their scales (SCALIFY_ERR_LAYOUT). workspace: 256-byte aligned, at least
+ * scalify_attention_bwd_workspace_size bytes, not shared with a concurrent call.
+ * Deterministic: no sum depends on the order in which workgroups run. */
+scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
+                                     const scalify_scaled_array* q, const scalify_scaled_array* k,
+                                     const scalify_scaled_array* v, const scalify_scaled_array* out,
+                                     const float* lse, scalify_scaled_array* dq,
+                                     scalify_scaled_array* dk, scalify_scaled_array* dv,
+                                     const scalify_attention_opts* opts, int32_t rescale,
+                                     int32_t target_log2, int32_t saturate, float* amax_out,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
 /* Human-readable name of a status code (static string). */
 const char* scalify_status_string(int32_t status);
 

@@ -53,13 +53,23 @@ class CMatmulOpts(ctypes.Structure):
                 ("b_block_scale", ctypes.c_void_p)]
 
 
+class CAttentionOpts(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("batch", ctypes.c_int64), ("softmax_scale", ctypes.c_float),
+                ("q_start", ctypes.c_void_p), ("k_start", ctypes.c_void_p), ("k_len", ctypes.c_void_p),
+                ("max_q", ctypes.c_int64), ("max_k", ctypes.c_int64)]
+
+
 EXPORTED = ("scalify_matmul_scale_log2", "scalify_matmul_workspace_size",
             "scalify_matmul_workspace_size_opts", "scalify_matmul",
             "scalify_rescale_workspace_size", "scalify_rescale", "scalify_cast",
             "scalify_set_scaling", "scalify_status_string", "scalify_layernorm_fwd",
             "scalify_layernorm_bwd_workspace_size", "scalify_layernorm_bwd",
             "scalify_mx_packed_bytes", "scalify_mx_pack_block_scales",
-            "scalify_matmul_noalloc")
+            "scalify_matmul_noalloc", "scalify_rmsnorm_fwd",
+            "scalify_rmsnorm_bwd_workspace_size", "scalify_rmsnorm_bwd",
+            "scalify_attention_fwd_workspace_size", "scalify_attention_fwd",
+            "scalify_attention_bwd_workspace_size", "scalify_attention_bwd")
 
 _lib = None
 
@@ -108,6 +118,25 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.scalify_layernorm_bwd.argtypes = [P(CScaledArray), P(CScaledArray), vp, f32, P(CScaledArray),
                                           vp, vp, i32, i32, i32, vp, vp, vp, ctypes.c_size_t, vp]
     lib.scalify_layernorm_bwd.restype = ctypes.c_int
+    lib.scalify_rmsnorm_fwd.argtypes = [P(CScaledArray), P(CScaledArray), vp, f32, P(CScaledArray),
+                                        P(CScaledArray), vp, vp, i32, i32, vp, vp]
+    lib.scalify_rmsnorm_fwd.restype = ctypes.c_int
+    lib.scalify_rmsnorm_bwd_workspace_size.argtypes = [i64, i64]
+    lib.scalify_rmsnorm_bwd_workspace_size.restype = ctypes.c_size_t
+    lib.scalify_rmsnorm_bwd.argtypes = [P(CScaledArray), P(CScaledArray), P(CScaledArray), vp, f32,
+                                        P(CScaledArray), vp, i32, i32, i32, vp, vp, vp,
+                                        ctypes.c_size_t, vp]
+    lib.scalify_rmsnorm_bwd.restype = ctypes.c_int
+    A = P(CScaledArray)
+    lib.scalify_attention_fwd_workspace_size.argtypes = [i64, i64, P(CAttentionOpts)]
+    lib.scalify_attention_fwd_workspace_size.restype = ctypes.c_size_t
+    lib.scalify_attention_fwd.argtypes = [A, A, A, A, vp, P(CAttentionOpts), i32, vp, ctypes.c_size_t, vp]
+    lib.scalify_attention_fwd.restype = ctypes.c_int
+    lib.scalify_attention_bwd_workspace_size.argtypes = [i64, i64, P(CAttentionOpts), i32]
+    lib.scalify_attention_bwd_workspace_size.restype = ctypes.c_size_t
+    lib.scalify_attention_bwd.argtypes = [A, A, A, A, A, vp, A, A, A, P(CAttentionOpts), i32, i32, i32, vp,
+                                          vp, ctypes.c_size_t, vp]
+    lib.scalify_attention_bwd.restype = ctypes.c_int
     lib.scalify_status_string.argtypes = [i32]
     lib.scalify_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -374,6 +403,138 @@ def scalify_layernorm_bwd(dy: ScaledArray, x: ScaledArray, dx: ScaledArray, *,
                                    _ptr_or_none(pre_out), ws.data_ptr(), ws.numel(),
                                    _stream_handle(stream))
     _check(st, "scalify_layernorm_bwd")
+
+
+def _struct_or_none(x: Optional[ScaledArray]):
+    return ctypes.byref(x.c_struct()) if x is not None else None
+
+
+def scalify_rmsnorm_fwd(x: ScaledArray, out: ScaledArray, *, residual: ScaledArray = None,
+                        sum_out: ScaledArray = None, gamma: torch.Tensor = None, eps: float = 1e-5,
+                        row_scale: torch.Tensor = None, block_scale: torch.Tensor = None,
+                        target_log2: int = 0, saturate: bool = True, pre_out: torch.Tensor = None,
+                        stream=None) -> None:
+    """Scaled RMS norm forward with the residual's scaled add; see
+    scalify_rmsnorm_fwd in include/scalify.h. `sum_out` receives the sum (the
+    residual stream), `row_scale` (contiguous fp32 [R]) or `block_scale` (uint8,
+    scalify_mx_packed_bytes(R, D) bytes) the output's power-of-two scales, as
+    scalify_matmul's a_channel_scale / a_block_scale take them."""
+    R, D = x.shape
+    if row_scale is not None and (row_scale.dtype != torch.float32 or not row_scale.is_contiguous() or
+                                  row_scale.numel() != R):
+        raise ValueError("row_scale: contiguous fp32 [R]")
+    if block_scale is not None and (block_scale.dtype != torch.uint8 or not block_scale.is_contiguous() or
+                                    block_scale.numel() != scalify_mx_packed_bytes(R, D)):
+        raise ValueError("block_scale: contiguous uint8 [scalify_mx_packed_bytes(R, D)]")
+    st = load_library().scalify_rmsnorm_fwd(
+        _struct_or_none(x), _struct_or_none(residual), _ptr_or_none(gamma), float(eps),
+        _struct_or_none(sum_out), _struct_or_none(out), _ptr_or_none(row_scale),
+        _ptr_or_none(block_scale), int(target_log2), int(bool(saturate)), _ptr_or_none(pre_out),
+        _stream_handle(stream))
+    _check(st, "scalify_rmsnorm_fwd")
+
+
+def scalify_rmsnorm_bwd_workspace_size(R: int, D: int) -> int:
+    return int(load_library().scalify_rmsnorm_bwd_workspace_size(R, D))
+
+
+def scalify_rmsnorm_bwd(dy: ScaledArray, x: ScaledArray, dx: ScaledArray, *, dsum: ScaledArray = None,
+                        gamma: torch.Tensor = None, eps: float = 1e-5, rescale: int = RESCALE_AMAX,
+                        target_log2: int = 0, saturate: bool = True, dgamma: torch.Tensor = None,
+                        amax_out: torch.Tensor = None, pre_out: torch.Tensor = None,
+                        ws: torch.Tensor = None, stream=None) -> None:
+    """RMS norm input gradient, plus the gradient `dsum` that reaches the
+    normalized array itself, with its dynamic rescale; see scalify_rmsnorm_bwd
+    in include/scalify.h."""
+    lib = load_library()
+    R, D = x.shape
+    if ws is None:
+        ws = _call_workspace(max(scalify_rmsnorm_bwd_workspace_size(R, D), 1), x.data.device, stream)
+    st = lib.scalify_rmsnorm_bwd(
+        _struct_or_none(dy), _struct_or_none(x), _struct_or_none(dsum), _ptr_or_none(gamma), float(eps),
+        _struct_or_none(dx), _ptr_or_none(dgamma), int(rescale), int(target_log2), int(bool(saturate)),
+        _ptr_or_none(amax_out), _ptr_or_none(pre_out), ws.data_ptr(), ws.numel(), _stream_handle(stream))
+    _check(st, "scalify_rmsnorm_bwd")
+
+
+def attention_opts(q: ScaledArray, heads: int, *, kv_heads: int = None, batch: int = 1, causal: bool = False,
+                   softmax_scale: float = None, q_start: torch.Tensor = None, k_start: torch.Tensor = None,
+                   k_len: torch.Tensor = None, max_q: int = 0, max_k: int = 0) -> CAttentionOpts:
+    """scalify_attention_opts of a call (include/scalify.h). softmax_scale
+    defaults to 1 / sqrt(head_dim); q_start, k_start ([batch + 1]) and k_len
+    ([batch]) are contiguous int64 device tensors."""
+    D = q.shape[1] // heads if heads > 0 and q.shape[1] % heads == 0 else 0
+    for t, n in ((q_start, batch + 1), (k_start, batch + 1), (k_len, batch)):
+        if t is not None and (t.dtype != torch.int64 or not t.is_contiguous() or t.numel() != n):
+            raise ValueError("q_start, k_start: contiguous int64 [batch + 1]; k_len: [batch]")
+    if softmax_scale is None:
+        softmax_scale = D ** -0.5 if D else 1.0
+    return CAttentionOpts(int(heads), int(heads if kv_heads is None else kv_heads), D, int(bool(causal)), int(batch),
+                          float(softmax_scale), _ptr_or_none(q_start), _ptr_or_none(k_start), _ptr_or_none(k_len),
+                          int(max_q), int(max_k))
+
+
+def _check_lse(lse: Optional[torch.Tensor], rows: int, heads: int):
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != rows * heads):
+        raise ValueError("lse: contiguous fp32 [heads, rows of q]")
+
+
+def _call_workspace(nbytes: int, device, stream) -> Optional[torch.Tensor]:
+    """A workspace that lives until the call's work on `stream` is done."""
+    if nbytes == 0:
+        return None
+    ws = workspace(nbytes, device)
+    if stream is not None:
+        ws.record_stream(stream)
+    return ws
+
+
+def scalify_attention_fwd_workspace_size(rows_q: int, rows_k: int, opts: CAttentionOpts) -> int:
+    return int(load_library().scalify_attention_fwd_workspace_size(rows_q, rows_k, ctypes.byref(opts)))
+
+
+def scalify_attention_fwd(q: ScaledArray, k: ScaledArray, v: ScaledArray, out: ScaledArray, *, heads: int,
+                          lse: torch.Tensor = None, saturate: bool = True, ws: torch.Tensor = None,
+                          stream=None, **opts) -> None:
+    """Attention forward; see scalify_attention_fwd in include/scalify.h. q and
+    out: [rows, heads * head_dim], k and v: [rows, kv_heads * head_dim]; lse: an
+    optional fp32 [heads, rows of q] device tensor. Further arguments: those of
+    attention_opts."""
+    lib = load_library()
+    o = attention_opts(q, heads, **opts)
+    _check_lse(lse, q.shape[0], heads)
+    if ws is None:
+        ws = _call_workspace(scalify_attention_fwd_workspace_size(q.shape[0], k.shape[0], o), q.data.device, stream)
+    st = lib.scalify_attention_fwd(_struct_or_none(q), _struct_or_none(k), _struct_or_none(v), _struct_or_none(out),
+                                   _ptr_or_none(lse), ctypes.byref(o), int(bool(saturate)), _ptr_or_none(ws),
+                                   ws.numel() if ws is not None else 0, _stream_handle(stream))
+    _check(st, "scalify_attention_fwd")
+
+
+def scalify_attention_bwd_workspace_size(rows_q: int, rows_k: int, opts: CAttentionOpts,
+                                         rescale: int = RESCALE_AMAX) -> int:
+    return int(load_library().scalify_attention_bwd_workspace_size(rows_q, rows_k, ctypes.byref(opts), int(rescale)))
+
+
+def scalify_attention_bwd(dout: ScaledArray, q: ScaledArray, k: ScaledArray, v: ScaledArray, out: ScaledArray,
+                          lse: torch.Tensor, dq: ScaledArray, dk: ScaledArray, dv: ScaledArray, *, heads: int,
+                          rescale: int = RESCALE_AMAX, target_log2: int = 0, saturate: bool = True,
+                          amax_out: torch.Tensor = None, ws: torch.Tensor = None, stream=None, **opts) -> None:
+    """Attention gradients with their rescales; see scalify_attention_bwd in
+    include/scalify.h. out and lse: what the forward stored; amax_out: an
+    optional fp32 [3] device tensor. Further arguments: those of attention_opts."""
+    lib = load_library()
+    o = attention_opts(q, heads, **opts)
+    _check_lse(lse, q.shape[0], heads)
+    if ws is None:
+        ws = _call_workspace(scalify_attention_bwd_workspace_size(q.shape[0], k.shape[0], o, rescale),
+                             q.data.device, stream)
+    st = lib.scalify_attention_bwd(_struct_or_none(dout), _struct_or_none(q), _struct_or_none(k), _struct_or_none(v),
+                                   _struct_or_none(out), _ptr_or_none(lse), _struct_or_none(dq), _struct_or_none(dk),
+                                   _struct_or_none(dv), ctypes.byref(o), int(rescale), int(target_log2),
+                                   int(bool(saturate)), _ptr_or_none(amax_out), _ptr_or_none(ws),
+                                   ws.numel() if ws is not None else 0, _stream_handle(stream))
+    _check(st, "scalify_attention_bwd")
 
 
 def empty_scaled(rows: int, cols: int, fmt: int, device, ld: int = None) -> ScaledArray:

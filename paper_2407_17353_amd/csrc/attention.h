@@ -1,0 +1,59 @@
+// Internal interface of the attention kernels (attention_*.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace scalify {
+
+struct AttnParams {
+  // [rows][heads * D], rows ld elements apart; formats; scales (NULL = 1)
+  const void *q, *k, *v;
+  int64_t ldq, ldk, ldv;
+  int q_fmt, k_fmt, v_fmt;
+  const float *s_q, *s_k, *s_v;
+  int64_t rows_q, rows_k, batch;
+  int H, Hkv, G, D;          // G = H / Hkv query heads share a key head
+  int causal;
+  float alpha;
+  const int64_t *q_start, *k_start, *k_len;  // or NULL
+  int64_t max_q, max_k;      // bounds of a sequence's rows
+  void* out;                 // forward: codes; backward: the stored output (F16)
+  int64_t ldo;
+  int out_fmt;
+  float* out_scale;          // (backward: of the stored output, read)
+  float* lse;                // [H][rows_q]: written (or NULL) / read
+  int sat;
+  // forward, keys of a sequence split over `splits` workgroups
+  int splits;
+  float* part_o;             // [splits][rows_q][H][D] unnormalised
+  float2* part_ml;           // [splits][rows_q][H] running maximum and sum
+  // backward
+  const void* dout;
+  int64_t lddo;
+  int do_fmt;
+  const float* s_do;
+  float *delta, *nd2;        // [H][rows_q]: sum dO O, sum dO^2
+  float* nv2;                // [Hkv][rows_k]: sum v^2
+  void *dq, *dk, *dv;        // codes (no rescale)
+  int64_t lddq, lddk, lddv;
+  int dq_fmt, dk_fmt, dv_fmt;
+  float *dq_scale, *dk_scale, *dv_scale;
+  float *dq32, *dk32, *dv32; // dynamic rescale: fp32 gradients [rows][heads * D], else NULL
+  uint32_t* amax;            // the three statistics
+  float* amax_out;           // optional [3]
+  int mode, target;
+};
+
+constexpr int kAttnMaxD = 128;
+// Splits of a sequence's keys for the forward, 1 where the grid fills the
+// device without, and whether a workgroup's four waves share 32 query columns
+// (few queries) or hold 128.
+struct AttnPlan {
+  int splits;
+  bool narrow;
+};
+AttnPlan attention_plan(int64_t batch, int Hkv, int G, int64_t max_q, int64_t max_k);
+hipError_t launch_attention_fwd(const AttnParams& p, const AttnPlan& plan, hipStream_t s);
+hipError_t launch_attention_bwd(const AttnParams& p, hipStream_t s);
+
+}  // namespace scalify

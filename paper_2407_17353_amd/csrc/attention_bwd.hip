@@ -1,0 +1,490 @@
+// Attention backward, which recomputes the probabilities from the stored
+// log-sum-exp:
+//   P = exp(S - lse), dP = dO v^T, dS = P (dP - delta), delta = rowsum(dO O),
+//   dV = P^T dO, dK = alpha dS^T q, dQ = alpha dS k.
+//
+// Three kernels: delta and the rows' norms; dK and dV, a workgroup holding 128
+// keys and walking the queries (of every head that shares the key head) that see
+// them; dQ, a workgroup holding 128 query columns and walking the keys. Scores and
+// dP are formed twice (seven products where five would do), but no workgroup adds
+// to another's result: no fp32 atomics whose order would change the bits, and no
+// fp32 gradient in memory unless a rescale needs one.
+//
+// F16 operands of the second products: P as 2^14 P, dS as 2^E dS with the power of
+// two that its bound allows, |dS| <= P (|dP| + |delta|) <= 2 max|dO_i| max|v_j|
+// (Cauchy-Schwarz; delta_i is a mean of dP_ij): 2^E dS <= 2^15, so 29 binades below
+// the bound are normal F16 numbers.
+#include "attention_dev.h"
+#include "kernels.h"
+
+namespace scalify {
+
+// delta, |dO_i|^2 and |v_j|^2: 16 lanes a row of a head, eight columns each.
+__global__ __launch_bounds__(256) void attn_rows_kernel(AttnParams p) {
+  const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+  const int lane = threadIdx.x & 15;
+  const int64_t nq = p.rows_q * p.H, nk = p.rows_k * p.Hkv;
+  if (blockIdx.x == 0 && threadIdx.x < 3) p.amax[threadIdx.x] = 0u;
+  if (item >= nq + nk) return;
+  const bool query = item < nq;
+  const int heads = query ? p.H : p.Hkv;
+  const int64_t i = query ? item : item - nq, row = i / heads;
+  const int head = (int)(i - row * heads), col = head * p.D + 8 * lane;
+  float dot = 0.0f, sq = 0.0f;
+  if (8 * lane < p.D) {
+    if (query) {
+      const h8 d = __builtin_bit_cast(h8, load_f16x8(p.do_fmt, p.dout, row * p.lddo + col));
+      const h8 o = __builtin_bit_cast(h8, load_f16x8(p.out_fmt, p.out, row * p.ldo + col));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dot = fmaf((float)d[e], (float)o[e], dot);
+        sq = fmaf((float)d[e], (float)d[e], sq);
+      }
+    } else {
+      const h8 v = __builtin_bit_cast(h8, load_f16x8(p.v_fmt, p.v, row * p.ldv + col));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sq = fmaf((float)v[e], (float)v[e], sq);
+    }
+  }
+#pragma unroll
+  for (int off = 8; off > 0; off >>= 1) {
+    dot += __shfl_xor(dot, off, 16);
+    sq += __shfl_xor(sq, off, 16);
+  }
+  if (lane != 0) return;
+  if (query) {
+    // in units of dO's and v's data, as dP is
+    p.delta[head * p.rows_q + row] = __builtin_ldexpf(dot, pow2_exponent(p.out_scale) - pow2_exponent(p.s_v));
+    p.nd2[head * p.rows_q + row] = sq;
+  } else {
+    p.nv2[head * p.rows_k + row] = sq;
+  }
+}
+
+// E for the largest |dO_i|^2 and |v_j|^2.
+__device__ __forceinline__ int ds_exponent(float nd2, float nv2) {
+  const float n = nd2 * nv2;
+  if (!(n > 0.0f) || !(n < 3.0e38f)) return 0;
+  return 14 - ((floor_log2_bits(__float_as_uint(n)) + 2) >> 1);
+}
+
+// Largest finite value of n floats, over the workgroup (256 threads).
+__device__ __forceinline__ float block_max(const float* x, int64_t n, float (&red)[4]) {
+  float a = 0.0f;
+  for (int64_t i = threadIdx.x; i < n; i += 256) {
+    const float v = x[i];
+    if (v < 3.0e38f) a = fmaxf(a, v);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) a = fmaxf(a, __shfl_xor(a, off, 64));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
+  __syncthreads();
+  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
+
+__device__ __forceinline__ void fold_amax(uint32_t* word, float a) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) a = fmaxf(a, __shfl_xor(a, off, 64));
+  if ((threadIdx.x & 63) == 0)
+    __hip_atomic_fetch_max(word, __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// One gradient row's block of 32 columns times f, to codes or fp32; returns the
+// largest magnitude.
+template <int DP>
+__device__ __forceinline__ float store_block(const f16v& acc, float f, int d, int h, int D, float* f32, void* codes, int fmt,
+                                             int64_t e32, int64_t e, int shift, bool sat) {
+  float a = 0.0f;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int n = 32 * d + 8 * g + 4 * h;
+    if (n >= D) continue;
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[i] = acc[4 * g + i] * f;
+      a = fmaxf(a, fabsf(y[i]));  // (fmaxf skips NaN)
+    }
+    if (f32) *(float4*)(f32 + e32 + n) = make_float4(y[0], y[1], y[2], y[3]);
+    else store4_any(fmt, codes, e + n, y, shift, sat);
+  }
+  return a;
+}
+
+// Exponents of the propagated scales of dq, dk, dv.
+__device__ __forceinline__ void grad_exponents(const AttnParams& p, int (&e)[3]) {
+  const int eo = pow2_exponent(p.s_do), ev = pow2_exponent(p.s_v);
+  e[0] = eo + ev + pow2_exponent(p.s_k);
+  e[1] = eo + ev + pow2_exponent(p.s_q);
+  e[2] = eo;
+}
+
+// dK and dV of 128 keys, 32 a wave: scores and dP are formed with a key a lane
+// (rows: queries), which makes them the operands of the second products as they
+// stand. K and v rows stay in registers, tiles of 64 queries (q, dO) go through
+// two LDS buffers.
+template <int DP>
+__global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tiles) {
+  constexpr int TQ = 64, KS = DP / 16, DB = DP / 32, BUF = TQ * DP * 2;
+  __shared__ __align__(16) uint8_t lds[4 * BUF];
+  __shared__ __align__(16) float row_l[2][TQ], row_d[2][TQ];
+  __shared__ int odd[2];
+  __shared__ float red[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const Place at = attn_place(p);
+  const int tile = (int)at.rest;  // (the first keys are seen by the most queries)
+  const Seq sq = load_seq(p, at.b);
+  const int kext = (int)min((int64_t)sq.kext, p.max_k);
+  const int j0 = tile * 128;
+  if (j0 >= kext) return;
+  const int behind = sq.lk - sq.lq;
+  const int key = j0 + 32 * wave + (lane & 31);
+  const bool have = key < sq.lk;
+  const int first = !have ? 0x7FFFFFFF : (p.causal ? key - behind : 0);  // first query that sees this key
+  const int64_t krow = sq.k0 + key;
+  h8 kf[KS], vf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    kf[ks] = row_chunk(p.k_fmt, p.k, krow * p.ldk + (int64_t)at.hk * p.D, ks, h, p.D, have);
+    vf[ks] = row_chunk(p.v_fmt, p.v, krow * p.ldv + (int64_t)at.hk * p.D, ks, h, p.D, have);
+  }
+  // queries that see any of the keys, in whole tiles
+  const int q_lo = p.causal ? max(0, j0 - behind) / TQ * TQ : 0;
+  const int nt = j0 < sq.lk && q_lo < sq.lq ? (sq.lq - q_lo + TQ - 1) / TQ : 0;
+  const int steps = nt * p.G;
+
+  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+  float nd2 = 0.0f;
+  for (int g = 0; g < p.G; ++g)
+    nd2 = fmaxf(nd2, block_max(p.nd2 + (int64_t)(at.hk * p.G + g) * p.rows_q + sq.q0 + q_lo, max(0, sq.lq - q_lo), red));
+  const float nv2 = block_max(p.nv2 + (int64_t)at.hk * p.rows_k + sq.k0 + j0, max(0, min(128, sq.lk - j0)), red);
+  const int E = ds_exponent(nd2, nv2);
+  const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2);
+
+  f16v ak[DB], av[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) ak[d] = av[d] = f16v{};
+  TileLoader<TQ, DP, 256> lq, ld;
+  float l_next = 0.0f, d_next = 0.0f;
+  auto fetch = [&](int step) {
+    const int g = step / nt, t = q_lo + (step - g * nt) * TQ, head = at.hk * p.G + g;
+    lq.init(p.q, sq.q0 * p.ldq + (int64_t)head * p.D, p.ldq, p.D, p.q_fmt);
+    ld.init(p.dout, sq.q0 * p.lddo + (int64_t)head * p.D, p.lddo, p.D, p.do_fmt);
+    lq.load(t, sq.lq);
+    ld.load(t, sq.lq);
+    if (threadIdx.x < TQ) {
+      // a row without keys, or past the end: exp2(score - Inf) = 0
+      const int i = t + (int)threadIdx.x;
+      const float l = i < sq.lq ? p.lse[(int64_t)head * p.rows_q + sq.q0 + i] : neg_inf();
+      l_next = l == neg_inf() ? __builtin_inff() : fmaf(l, kLog2e, -kProbLog2);
+      d_next = i < sq.lq ? p.delta[(int64_t)head * p.rows_q + sq.q0 + i] * c2 : 0.0f;
+    }
+  };
+  auto put = [&](int step) {
+    uint8_t* b = lds + (step & 1) * 2 * BUF;
+    lq.store(b);
+    ld.store(b + BUF);
+    if (threadIdx.x < TQ) {
+      row_l[step & 1][threadIdx.x] = l_next;
+      row_d[step & 1][threadIdx.x] = d_next;
+    }
+    const int t = q_lo + (step % nt) * TQ;
+    // (a tile that every key of the workgroup sees whole has no masked pairs)
+    if (t + TQ > sq.lq || j0 + 128 > sq.lk || (p.causal && t + behind < j0 + 127)) {
+      mark_not_finite(lq, &odd[step & 1], step);
+      mark_not_finite(ld, &odd[step & 1], step);
+    }
+  };
+  if (steps > 0) {
+    fetch(0);
+    __syncthreads();  // (odd is cleared)
+    put(0);
+    if (steps > 1) fetch(1);
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int step = 0; step < steps; ++step) {
+    uint8_t* const qt = lds + (step & 1) * 2 * BUF;
+    uint8_t* const dt = qt + BUF;
+    const int t = q_lo + (step % nt) * TQ;
+    const bool is_odd = __builtin_amdgcn_readfirstlane(odd[step & 1]) == step;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int i0 = t + 32 * b;
+      if (!is_odd && !__any(i0 + 31 >= first)) continue;  // (no key of this wave is seen)
+      f16v s = {}, dp = {};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mfma(row_operand<DP>(qt, 32 * b, ks, lane), kf[ks], s);
+        dp = mfma(row_operand<DP>(dt, 32 * b, ks, lane), vf[ks], dp);
+      }
+      float pr[16], ds[16];
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const float4 L = *(const float4*)&row_l[step & 1][32 * b + 8 * r4 + 4 * h];
+        const float4 Dl = *(const float4*)&row_d[step & 1][32 * b + 8 * r4 + 4 * h];
+        const float lv[4] = {L.x, L.y, L.z, L.w}, dv[4] = {Dl.x, Dl.y, Dl.z, Dl.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * r4 + i;
+          pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c1, -lv[i]));
+          ds[r] = pr[r] * fmaf(dp[r], c2, -dv[i]);
+        }
+      }
+      if (__any(i0 < first) || i0 + 32 > sq.lq) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int i = i0 + result_row(r, h);
+          if (i < first || i >= sq.lq) pr[r] = ds[r] = 0.0f;
+        }
+      }
+      if (is_odd) {
+        // dO's values that are not finite: added pair by pair (an admitted P is
+        // positive). Those of q need no more than to be taken out: their scores, and
+        // so dS, are NaN where they are admitted.
+#pragma unroll 1
+        for (int j = 0; j < 32; ++j) {
+          if (i0 + j < first || i0 + j >= sq.lq) continue;
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const u2 w = *(const u2*)(dt + tile_off<DP>(32 * b + j, 4 * d + g) + 8 * h);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) av[d][4 * g + i] += odd_part((w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 32 * DP / 8; i += 256) {
+          h8* a = (h8*)(qt + 32 * b * DP * 2) + i;
+          h8* c = (h8*)(dt + 32 * b * DP * 2) + i;
+          *a = finite_part(*a);
+          *c = finite_part(*c);
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const h8 pf = to_operand(pr, g), sf = to_operand(ds, g);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          av[d] = mfma(col_operand<DP>(dt, 32 * b + 16 * g, d, lane), pf, av[d]);
+          ak[d] = mfma(col_operand<DP>(qt, 32 * b + 16 * g, d, lane), sf, ak[d]);
+        }
+      }
+    }
+    if (step + 1 < steps) {
+      put(step + 1);
+      if (step + 2 < steps) fetch(step + 2);
+    }
+    __syncthreads();
+  }
+  int e[3];
+  grad_exponents(p, e);
+  float mk = 0.0f, mv = 0.0f;
+  if (key < kext) {
+    const float fk = __builtin_ldexpf(p.alpha, -E), fv = pow2_float(-(int)kProbLog2);
+    const int64_t c = (int64_t)at.hk * p.D, e32 = krow * p.Hkv * p.D + c;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      mk = fmaxf(mk, store_block<DP>(ak[d], fk, d, h, p.D, p.dk32, p.dk, p.dk_fmt, e32, krow * p.lddk + c,
+                                     clamp_e8m0(e[1]) - e[1], p.sat != 0));
+      mv = fmaxf(mv, store_block<DP>(av[d], fv, d, h, p.D, p.dv32, p.dv, p.dv_fmt, e32, krow * p.lddv + c,
+                                     clamp_e8m0(e[2]) - e[2], p.sat != 0));
+    }
+  }
+  fold_amax(p.amax + 1, mk);
+  fold_amax(p.amax + 2, mv);
+}
+
+// dQ of 128 query columns, 32 a wave, a query a lane: the forward's walk over
+// tiles of 64 keys, with q and dO rows in registers.
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles) {
+  constexpr int TK = 64, KS = DP / 16, DB = DP / 32, BUF = TK * DP * 2;
+  __shared__ __align__(16) uint8_t lds[2 * BUF];
+  __shared__ int odd;
+  __shared__ float red[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const Place at = attn_place(p);
+  const int tile = tiles - 1 - (int)at.rest;
+  const Seq sq = load_seq(p, at.b);
+  const int64_t ncols = (int64_t)sq.lq * p.G, col0 = (int64_t)tile * 128;
+  if (col0 >= ncols) return;
+  const int64_t col = col0 + 32 * wave + (lane & 31);
+  const bool live = col < ncols;
+  const int pos = (int)(col / p.G), head = at.hk * p.G + (int)(col - (int64_t)pos * p.G);
+  const int64_t qrow = sq.q0 + pos;
+  const int behind = sq.lk - sq.lq;
+  const int last = !live ? 0x7FFFFFFF : (p.causal ? min(pos + behind, sq.lk - 1) : sq.lk - 1);
+  const int last0 = p.causal ? min((int)(col0 / p.G) + behind, sq.lk - 1) : sq.lk - 1;
+  h8 qf[KS], df[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    qf[ks] = row_chunk(p.q_fmt, p.q, qrow * p.ldq + (int64_t)head * p.D, ks, h, p.D, live);
+    df[ks] = row_chunk(p.do_fmt, p.dout, qrow * p.lddo + (int64_t)head * p.D, ks, h, p.D, live);
+  }
+  const int64_t last_col = col0 + 128 < ncols ? col0 + 127 : ncols - 1;
+  const int end = p.causal ? max(0, min(sq.lk, (int)(last_col / p.G) + behind + 1)) : sq.lk;
+
+  // the columns' norms: a lane each (128 of the workgroup's threads read one)
+  if (threadIdx.x == 0) odd = -1;
+  const float nv2 = block_max(p.nv2 + (int64_t)at.hk * p.rows_k + sq.k0, end, red);
+  float nd2 = 0.0f;
+  if (live) nd2 = p.nd2[(int64_t)head * p.rows_q + qrow];
+  if (!(nd2 < 3.0e38f)) nd2 = 0.0f;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) nd2 = fmaxf(nd2, __shfl_xor(nd2, off, 64));
+  const int E = ds_exponent(nd2, nv2);  // (of this wave)
+  const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2);
+  float L = __builtin_inff(), Dl = 0.0f;
+  if (live) {
+    const float l = p.lse[(int64_t)head * p.rows_q + qrow];
+    L = l == neg_inf() ? __builtin_inff() : fmaf(l, kLog2e, -kProbLog2);
+    Dl = p.delta[(int64_t)head * p.rows_q + qrow] * c2;
+  }
+  f16v acc[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) acc[d] = f16v{};
+  uint8_t* const kt = lds;
+  uint8_t* const vt = lds + BUF;
+  TileLoader<TK, DP, 256> lk, lv;
+  lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
+  lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
+  if (end > 0) {
+    lk.load(0, end);
+    lv.load(0, end);
+  }
+#pragma unroll 1
+  for (int t = 0; t < end; t += TK) {
+    lk.store(kt);
+    lv.store(vt);
+    if (t + TK - 1 > last0) mark_not_finite(lk, &odd, t);
+    __syncthreads();
+    if (t + TK < end) {
+      lk.load(t + TK, end);
+      lv.load(t + TK, end);
+    }
+    const bool is_odd = __builtin_amdgcn_readfirstlane(odd) == t;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      f16v s = {}, dp = {};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mfma(row_operand<DP>(kt, 32 * b, ks, lane), qf[ks], s);
+        dp = mfma(row_operand<DP>(vt, 32 * b, ks, lane), df[ks], dp);
+      }
+      float ds[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c1, -L)) * fmaf(dp[r], c2, -Dl);
+      if (__any(t + 32 * b + 31 > last)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (t + 32 * b + result_row(r, h) > last) ds[r] = 0.0f;
+      }
+      if (is_odd) {
+        // (where they are admitted the scores, and so dS, are NaN)
+        __syncthreads();
+        for (int i = threadIdx.x; i < 32 * DP / 8; i += 256) {
+          h8* a = (h8*)(kt + 32 * b * DP * 2) + i;
+          *a = finite_part(*a);
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const h8 sf = to_operand(ds, g);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[d] = mfma(col_operand<DP>(kt, 32 * b + 16 * g, d, lane), sf, acc[d]);
+      }
+    }
+    __syncthreads();
+  }
+  int e[3];
+  grad_exponents(p, e);
+  float mq = 0.0f;
+  if (live) {
+    const float f = __builtin_ldexpf(p.alpha, -E);
+    const int64_t c = (int64_t)head * p.D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+      mq = fmaxf(mq, store_block<DP>(acc[d], f, d, h, p.D, p.dq32, p.dq, p.dq_fmt, qrow * p.H * p.D + c,
+                                     qrow * p.lddq + c, clamp_e8m0(e[0]) - e[0], p.sat != 0));
+  }
+  fold_amax(p.amax, mq);
+}
+
+// The dynamic rescale's cast of the three fp32 gradients (blockIdx.y), 16 rows of a
+// sequence a workgroup, and the scales and statistics of either mode.
+constexpr int ATTN_CAST_ROWS = 16;
+
+__global__ __launch_bounds__(256) void attn_grads_kernel(AttnParams p, int64_t tiles) {
+  const int which = blockIdx.y;
+  int e[3];
+  grad_exponents(p, e);
+  const int base = e[which];
+  const uint32_t amax = p.amax[which];
+  const int e_out = clamp_e8m0(base + (p.mode == 1 ? rescale_exponent(amax, p.target) : 0));
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *(which == 0 ? p.dq_scale : which == 1 ? p.dk_scale : p.dv_scale) = pow2_float(e_out);
+    if (p.amax_out) p.amax_out[which] = __uint_as_float(amax);
+  }
+  if (p.mode != 1) return;
+  const int64_t b = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+  const Seq sq = load_seq(p, b);
+  const int64_t rows = which == 0 ? sq.lq : min((int64_t)sq.kext, p.max_k);
+  const int64_t r0 = tile * ATTN_CAST_ROWS;
+  if (r0 >= rows) return;
+  const int64_t row0 = (which == 0 ? sq.q0 : sq.k0) + r0;
+  const int n = (int)min((int64_t)ATTN_CAST_ROWS, rows - r0);
+  const int cols = (which == 0 ? p.H : p.Hkv) * p.D;  // (a multiple of 16)
+  const float* src = which == 0 ? p.dq32 : which == 1 ? p.dk32 : p.dv32;
+  void* dst = which == 0 ? p.dq : which == 1 ? p.dk : p.dv;
+  const int64_t ld = which == 0 ? p.lddq : which == 1 ? p.lddk : p.lddv;
+  const int fmt = which == 0 ? p.dq_fmt : which == 1 ? p.dk_fmt : p.dv_fmt;
+  const int shift = e_out - base;
+  const bool fast = shift >= kFastShiftMinSub && shift <= kFastShiftMax, sat = p.sat != 0;
+  const float scale = fast ? pow2_float(shift) : 1.0f;
+  const int chunks = cols / 16;
+  for (int i = threadIdx.x; i < n * chunks; i += 256) {
+    const int r = i / chunks, c = 16 * (i - r * chunks);
+    uint32_t u[16], w[8];
+    load16<kF32>(src, (row0 + r) * cols + c, u);
+    const int64_t o = (row0 + r) * ld + c;
+    if (fmt == kF16) {
+      encode16<kF16>(u, shift, scale, fast, sat, w);
+      store_words16<kF16>(dst, o, w);
+    } else if (fmt == kE4M3) {
+      encode16<kE4M3>(u, shift, scale, fast, sat, w);
+      store_words16<kE4M3>(dst, o, w);
+    } else {
+      encode16<kE5M2>(u, shift, scale, fast, sat, w);
+      store_words16<kE5M2>(dst, o, w);
+    }
+  }
+}
+
+template <int DP>
+static void launch(const AttnParams& p, hipStream_t s) {
+  const int64_t heads = p.batch * p.Hkv;
+  const int kt = (int)((p.max_k + 127) / 128), qt = (int)((p.max_q * p.G + 127) / 128);
+  if (p.rows_k > 0 && kt > 0)
+    hipLaunchKernelGGL((attn_dkv_kernel<DP>), dim3((unsigned)(heads * kt)), dim3(256), 0, s, p, kt);
+  if (p.rows_q > 0 && qt > 0)
+    hipLaunchKernelGGL((attn_dq_kernel<DP>), dim3((unsigned)(heads * qt)), dim3(256), 0, s, p, qt);
+}
+
+hipError_t launch_attention_bwd(const AttnParams& p, hipStream_t s) {
+  const int64_t items = p.rows_q * p.H + p.rows_k * p.Hkv;
+  hipLaunchKernelGGL(attn_rows_kernel, dim3((unsigned)(items > 16 ? (items + 15) / 16 : 1)), dim3(256), 0, s, p);
+  if (p.D <= 64) launch<64>(p, s);
+  else launch<128>(p, s);
+  const int64_t most = p.max_q > p.max_k ? p.max_q : p.max_k;
+  int64_t tiles = p.mode == 1 ? (most + ATTN_CAST_ROWS - 1) / ATTN_CAST_ROWS : 0;
+  if (tiles < 1) tiles = 1;
+  hipLaunchKernelGGL(attn_grads_kernel, dim3((unsigned)(p.mode == 1 ? p.batch * tiles : 1), 3), dim3(256), 0, s, p, tiles);
+  return hipGetLastError();
+}
+
+}  // namespace scalify

@@ -1,0 +1,308 @@
+// Device helpers of the attention kernels: sequences, tiles of keys (or
+// queries) in LDS, and the matrix operands read from them.
+//
+// All products run on the F16 matrix instruction (32 x 32 x 16, fp32 sums):
+// every E4M3 and E5M2 value is an F16 value, so 8-bit operands are decoded
+// exactly on their way into LDS.
+//
+// Operand order. The instruction's result gives a lane one column (lane & 31)
+// and, of its half h = lane >> 5, rows 8 (r / 4) + 4 h + r % 4 in register r; its
+// operands give a lane one row or column and the eight consecutive k of its half.
+// A product whose k runs over another's rows therefore takes that result without
+// any exchange between lanes, if the other operand's k are permuted alike: of 16
+// rows, half 0 holds 0-3 and 8-11, half 1 holds 4-7 and 12-15. The transposing
+// LDS read gives just that: each 16 lanes read four rows of 16 columns and every
+// lane receives its column's four values, so two reads make an operand.
+#pragma once
+#include "attention.h"
+#include "codec.h"
+#include "ew_util.h"
+
+#include <type_traits>
+
+namespace scalify {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+#define ATTN_LDS __attribute__((address_space(3)))
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+// Probabilities are kept as 2^14 p (at most 2^14): in F16 the normal range then
+// reaches down to p = 2^-28, where 2^-14, a uniform row over 16384 keys, would be
+// its end.
+constexpr float kProbLog2 = 14.0f;
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+
+// A sequence's rows. Device arrays are not checked by the host: whatever they
+// hold, the rows stay inside the matrices.
+struct Seq {
+  int64_t q0, k0;
+  int lq, lk, kext;  // queries, keys, key rows of the sequence (keys past lk are padding)
+};
+
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
+  return x < lo ? lo : (x > hi ? hi : x);
+}
+
+__device__ __forceinline__ Seq load_seq(const AttnParams& p, int64_t b) {
+  Seq s;
+  int64_t q1, k1;
+  if (p.q_start) {
+    s.q0 = clamp64(p.q_start[b], 0, p.rows_q);
+    q1 = clamp64(p.q_start[b + 1], s.q0, p.rows_q);
+  } else {
+    const int64_t n = p.rows_q / p.batch;
+    s.q0 = b * n;
+    q1 = s.q0 + n;
+  }
+  if (p.k_start) {
+    s.k0 = clamp64(p.k_start[b], 0, p.rows_k);
+    k1 = clamp64(p.k_start[b + 1], s.k0, p.rows_k);
+  } else {
+    const int64_t n = p.rows_k / p.batch;
+    s.k0 = b * n;
+    k1 = s.k0 + n;
+  }
+  const int64_t lq = q1 - s.q0;
+  s.lq = (int)(lq < p.max_q ? lq : p.max_q);
+  s.kext = (int)(k1 - s.k0);
+  s.lk = p.k_len ? (int)clamp64(p.k_len[b], 0, s.kext) : s.kext;
+  return s;
+}
+
+// Byte offset of 16-byte chunk c of a row in an LDS tile of DP columns. Chunks
+// are permuted within a row so that neither reading the same chunk of
+// consecutive rows (16 bytes a lane) nor four neighbouring chunks of four rows
+// (the transposing read) meets a bank twice.
+template <int DP>
+__device__ __forceinline__ int tile_off(int row, int c) {
+  const int f = DP == 128 ? (((row & 3) << 2) | ((row >> 2) & 3)) : ((((row >> 1) & 1) << 2) | ((row >> 2) & 3));
+  return row * (DP * 2) + ((c ^ f) << 4);
+}
+
+__device__ __forceinline__ int fmt_bytes(int fmt) { return fmt == kF16 ? 2 : 1; }
+
+// Eight codes of a format, as they were loaded (16 or 8 bytes), as F16.
+__device__ __forceinline__ u4 to_f16x8(int fmt, u4 w) {
+  if (fmt == kF16) return w;
+  u4 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    h2 lo, hi;
+    if (fmt == kE4M3) {
+      lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, true);
+    } else {
+      lo = __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w[i], 1.0f, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w[i], 1.0f, true);
+    }
+    r[2 * i] = __builtin_bit_cast(uint32_t, lo);
+    r[2 * i + 1] = __builtin_bit_cast(uint32_t, hi);
+  }
+  return r;
+}
+
+// Eight consecutive codes at element e of base, as F16.
+__device__ __forceinline__ u4 load_f16x8(int fmt, const void* base, int64_t e) {
+  if (fmt == kF16) return *(const u4*)((const uint16_t*)base + e);
+  const u2 v = *(const u2*)((const uint8_t*)base + e);
+  return to_f16x8(fmt, u4{v[0], v[1], 0u, 0u});
+}
+
+// Rows of a matrix on their way into an LDS tile of ROWS x DP: loaded ahead
+// into registers, eight columns a chunk. The buffer's range check makes rows
+// past the end, and the columns past D, read as zeros.
+template <int ROWS, int DP, int THREADS>
+struct TileLoader {
+  static constexpr int CH = DP / 8, N = ROWS * CH / THREADS;
+  u4 r[N];
+  int voff0, step;  // chunk i of a thread: voff0 + i step
+  const uint8_t* base;
+  int64_t pitch;
+  int bytes_d, fmt;
+
+  // first: element of row 0 (of the sequence) and column 0 (of the head)
+  __device__ __forceinline__ void init(const void* data, int64_t first, int64_t ld, int D, int format) {
+    const int es = fmt_bytes(format);
+    fmt = format;
+    base = (const uint8_t*)data + first * es;
+    pitch = ld * es;
+    bytes_d = D * es;
+    const int row = (int)threadIdx.x / CH, ch = (int)threadIdx.x % CH;
+    step = THREADS / CH * (int)pitch;
+    // (past the end of any buffer: a tile's rows span less than 2^31 bytes)
+    voff0 = ch * 8 < D ? row * (int)pitch + ch * 8 * es : (int)0x80000000;
+  }
+  // rows row0 .. row0 + ROWS - 1, those from `end` on zero
+  __device__ __forceinline__ void load(int64_t row0, int64_t end) {
+    const int64_t n = end - row0 < ROWS ? end - row0 : ROWS;
+    const uint32_t bytes = n > 0 ? (uint32_t)((n - 1) * pitch) + (uint32_t)bytes_d : 0u;
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(base + row0 * pitch), 0, (int)bytes, 0x00027000);
+    if (fmt == kF16) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, voff0 + i * step, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const u2 v = __builtin_amdgcn_raw_buffer_load_b64(rs, voff0 + i * step, 0, 0);
+        r[i] = u4{v[0], v[1], 0u, 0u};
+      }
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t* lds) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (int)threadIdx.x + i * THREADS;
+      *(u4*)(lds + tile_off<DP>(c / CH, c % CH)) = to_f16x8(fmt, r[i]);
+    }
+  }
+};
+
+// Operand with one row of the tile a lane (rows row0 + (lane & 31)), k = columns
+// 16 ks + 8 h ...
+template <int DP>
+__device__ __forceinline__ h8 row_operand(const uint8_t* lds, int row0, int ks, int lane) {
+  return *(const h8*)(lds + row0 * (DP * 2) + (tile_off<DP>(lane & 31, lane >> 5) ^ (ks << 5)));
+}
+
+// Operand with one column of the tile a lane (columns 32 db + (lane & 31)), k = rows
+// row0 .. row0 + 15 in the order of a result's registers. row0: a multiple of 16.
+template <int DP>
+__device__ __forceinline__ h8 col_operand(const uint8_t* lds, int row0, int db, int lane) {
+  const int h = lane >> 5, x = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const int row = 4 * h + ((lane & 15) >> 2);
+  const int a0 = (tile_off<DP>(row, x) ^ (db << 6)) + 8 * (lane & 1);
+  const int a1 = (tile_off<DP>(row + 8, x) ^ (db << 6)) + 8 * (lane & 1);
+  const uint8_t* t = lds + row0 * (DP * 2);
+  const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ATTN_LDS s4*)(t + a0));
+  const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ATTN_LDS s4*)(t + a1));
+  typedef short s8 __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(h8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// The same from global memory, a row a lane held in registers for the whole
+// kernel: chunk ks of a row that starts at element e (columns from D on zero).
+__device__ __forceinline__ h8 row_chunk(int fmt, const void* base, int64_t e, int ks, int h, int D, bool ok) {
+  u4 v = {0u, 0u, 0u, 0u};
+  const int col = 16 * ks + 8 * h;
+  if (ok && col < D) v = load_f16x8(fmt, base, e + col);
+  return __builtin_bit_cast(h8, v);
+}
+
+__device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// Registers 8 g ... 8 g + 7 of a result as an operand (round to nearest even).
+__device__ __forceinline__ h8 to_operand(const float (&x)[16], int g) {
+  h8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (_Float16)x[8 * g + i];
+  return r;
+}
+
+// Row of a result held in register r of a lane of half h.
+__device__ __forceinline__ int result_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// The other half's value (lane ^ 32).
+__device__ __forceinline__ float other_half(float x, int h) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(h ? r[0] : r[1]);
+}
+
+// Whether an operand holds an infinity or NaN.
+__device__ __forceinline__ bool not_finite(h8 v) {
+  const u4 w = __builtin_bit_cast(u4, v);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m = max(m, w[i] & 0x7C000000u);
+    m = max(m, (w[i] << 16) & 0x7C000000u);
+  }
+  return m == 0x7C000000u;
+}
+
+// v with infinities and NaN replaced by 0.
+__device__ __forceinline__ h8 finite_part(h8 v) {
+  u4 w = __builtin_bit_cast(u4, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((w[i] & 0x7C000000u) == 0x7C000000u) w[i] &= 0xFFFFu;
+    if ((w[i] & 0x7C00u) == 0x7C00u) w[i] &= 0xFFFF0000u;
+  }
+  return __builtin_bit_cast(h8, w);
+}
+
+// A pair that the mask does not admit has weight 0, and 0 * Inf must add
+// nothing. Only tiles that a mask cuts hold such pairs next to admitted ones. A
+// tile of those that holds an infinity or NaN is marked while it is stored
+// (`flag`: the tile's number, so it needs no clearing); its finite part is then
+// multiplied as usual, and the rest added pair by pair.
+template <int ROWS, int DP, int THREADS>
+__device__ __forceinline__ void mark_not_finite(const TileLoader<ROWS, DP, THREADS>& t, int* flag, int number) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < t.N; ++i) bad |= not_finite(__builtin_bit_cast(h8, to_f16x8(t.fmt, t.r[i])));
+  if (bad) *flag = number;
+}
+
+__device__ __forceinline__ float f16_bits(uint32_t b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)b); }
+
+// v where it is an infinity or NaN, else 0.
+__device__ __forceinline__ float odd_part(uint32_t b) { return (b & 0x7C00u) == 0x7C00u ? f16_bits(b) : 0.0f; }
+
+// Four consecutive values of a row, cast to a format with a shift, at element e.
+__device__ __forceinline__ void store4_any(int fmt, void* base, int64_t e, const float (&y)[4], int shift, bool sat) {
+  const bool fast = shift >= kFastShiftMinSub && shift <= kFastShiftMax;
+  uint32_t u[4];
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u[i] = __float_as_uint(y[i]);
+    nan |= is_nan_bits(u[i]);
+  }
+  const bool hw = fast && !nan;
+  if (fmt == kF16) {
+    u2 w;
+    const float inv = fast ? pow2_float(-shift) : 1.0f;
+    w[0] = hw ? cast2_f16_hw(u[0], u[1], inv, sat) : cast2_exact_f16(u[0], u[1], shift, sat);
+    w[1] = hw ? cast2_f16_hw(u[2], u[3], inv, sat) : cast2_exact_f16(u[2], u[3], shift, sat);
+    *(u2*)((uint16_t*)base + e) = w;
+  } else if (fmt == kE4M3) {
+    *(uint32_t*)((uint8_t*)base + e) = hw ? cast4_fp8_hw<kE4M3>(u[0], u[1], u[2], u[3], pow2_float(shift), sat)
+                                          : cast4_exact_fp8<kE4M3>(u[0], u[1], u[2], u[3], shift, sat);
+  } else {
+    *(uint32_t*)((uint8_t*)base + e) = hw ? cast4_fp8_hw<kE5M2>(u[0], u[1], u[2], u[3], pow2_float(shift), sat)
+                                          : cast4_exact_fp8<kE5M2>(u[0], u[1], u[2], u[3], shift, sat);
+  }
+}
+
+// Factor of the scores in powers of two: alpha s_q s_k log2 e.
+__device__ __forceinline__ float score_factor(const AttnParams& p) {
+  return __builtin_ldexpf(p.alpha * kLog2e, pow2_exponent(p.s_q) + pow2_exponent(p.s_k));
+}
+
+// Position in the grid: (sequence, key head) runs fastest, so that a head's
+// workgroups meet on one XCD (workgroups go to the eight XCDs in turn) where
+// batch * key heads is a multiple of 8, and its keys stay in that XCD's L2.
+struct Place {
+  int64_t b;
+  int hk;
+  int64_t rest;
+};
+__device__ __forceinline__ Place attn_place(const AttnParams& p) {
+  const int64_t heads = p.batch * p.Hkv, id = blockIdx.x;
+  Place w;
+  const int64_t bh = id % heads;
+  w.rest = id / heads;
+  w.b = bh / p.Hkv;
+  w.hk = (int)(bh % p.Hkv);
+  return w;
+}
+
+}  // namespace scalify

@@ -12,10 +12,12 @@
 #include <mutex>
 
 #include "../../include/scalify.h"
+#include "attention.h"
 #include "gemm_choice.h"
 #include "kernels.h"
 #include "layernorm.h"
 #include "mid_gemm.h"
+#include "rmsnorm.h"
 #include "wave_gemm.h"
 
 using namespace scalify;
@@ -226,6 +228,133 @@ scalify_status current_scratch(void** ptr) {
 size_t layernorm_bwd_ws(int64_t R, int64_t D) {
   if (R < 0 || D < 0 || D > kLayerNormMaxD || R > kMaxDim) return 0;
   return kHeaderBytes + (size_t)layernorm_ws_floats(R, D) * sizeof(float);
+}
+
+size_t rmsnorm_bwd_ws(int64_t R, int64_t D) {
+  if (R < 0 || D < 0 || D > kLayerNormMaxD || R > kMaxDim) return 0;
+  return kHeaderBytes + (size_t)rmsnorm_ws_floats(R, D) * sizeof(float);
+}
+
+// Two outputs of one call (different formats allowed) must not overlap at all.
+bool rows_overlap(const scalify_scaled_array* a, const scalify_scaled_array* b, int64_t R, int64_t D) {
+  if (R == 0 || D == 0) return false;
+  const uintptr_t a0 = (uintptr_t)a->data, b0 = (uintptr_t)b->data;
+  const uintptr_t a1 = a0 + (uintptr_t)(((R - 1) * a->ld + D) * elem_bytes(a->dtype));
+  const uintptr_t b1 = b0 + (uintptr_t)(((R - 1) * b->ld + D) * elem_bytes(b->dtype));
+  return a0 < b1 && b0 < a1;
+}
+
+// ---- attention
+
+// Sizes of a call, from its options and the rows of q and k.
+scalify_status check_attention(const scalify_attention_opts* o, int64_t rows_q, int64_t rows_k) {
+  if (!o) return SCALIFY_ERR_NULL;
+  if (rows_q < 0 || rows_k < 0 || rows_q > kMaxDim || rows_k > kMaxDim) return SCALIFY_ERR_SHAPE;
+  if (o->heads < 1 || o->kv_heads < 1 || o->heads % o->kv_heads != 0 || o->heads > 65536) return SCALIFY_ERR_SHAPE;
+  if (o->head_dim < 16 || o->head_dim > kAttnMaxD || o->head_dim % 16 != 0) return SCALIFY_ERR_SHAPE;
+  if (o->batch < 1 || o->batch > kMaxDim || o->max_q < 0 || o->max_k < 0) return SCALIFY_ERR_SHAPE;
+  if (!o->q_start && rows_q % o->batch != 0) return SCALIFY_ERR_SHAPE;
+  if (!o->k_start && rows_k % o->batch != 0) return SCALIFY_ERR_SHAPE;
+  if (o->causal != 0 && o->causal != 1) return SCALIFY_ERR_VALUE;
+  if (!(o->softmax_scale > 0.0f) || !(o->softmax_scale < 3.0e38f)) return SCALIFY_ERR_VALUE;
+  return SCALIFY_OK;
+}
+
+// Bounds of a sequence's rows.
+int64_t most_rows(const int64_t* start, int64_t rows, int64_t batch, int64_t most) {
+  if (!start) return rows / batch;
+  return most > 0 && most < rows ? most : rows;
+}
+
+// The sizes a launch goes by. SCALIFY_ERR_SHAPE where a count leaves its range.
+struct AttnSizes {
+  int64_t max_q, max_k, keys;
+  int G;
+};
+scalify_status attention_sizes(const scalify_attention_opts* o, int64_t rows_q, int64_t rows_k, AttnSizes* z) {
+  const scalify_status st = check_attention(o, rows_q, rows_k);
+  if (st != SCALIFY_OK) return st;
+  z->G = o->heads / o->kv_heads;
+  z->max_q = most_rows(o->q_start, rows_q, o->batch, o->max_q);
+  z->max_k = most_rows(o->k_start, rows_k, o->batch, o->max_k);
+  z->keys = o->k_len && o->max_k > 0 && o->max_k < z->max_k ? o->max_k : z->max_k;
+  if (z->max_q * z->G > kMaxDim) return SCALIFY_ERR_SHAPE;
+  // (workgroups of the smallest tile, 8 columns, and of the splits)
+  const int64_t heads = o->batch * o->kv_heads;
+  const int64_t wide = heads * ((z->max_q * z->G + 7) / 8);
+  const int64_t tall = heads * ((z->max_k + 31) / 32);
+  if (heads > 0x7FFFFFFF || wide > 0x7FFFFFFF || tall > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
+  return SCALIFY_OK;
+}
+
+size_t attention_fwd_ws(const scalify_attention_opts* o, int64_t rows_q, const AttnSizes& z) {
+  const AttnPlan plan = attention_plan(o->batch, o->kv_heads, z.G, z.max_q, z.keys);
+  if (plan.splits < 2 || rows_q == 0) return 0;
+  return (size_t)plan.splits * (size_t)rows_q * (size_t)o->heads * (size_t)(o->head_dim + 2) * sizeof(float);
+}
+
+// Workspace of the backward in floats: header, delta, norms, fp32 gradients.
+size_t attention_bwd_ws(const scalify_attention_opts* o, int64_t rows_q, int64_t rows_k, int32_t rescale) {
+  const size_t q = (size_t)rows_q * o->heads, k = (size_t)rows_k * o->kv_heads;
+  size_t n = kHeaderBytes + (size_t)round_up((int64_t)(2 * q + k), 4) * sizeof(float);
+  if (rescale == SCALIFY_RESCALE_AMAX) n += (q + 2 * k) * (size_t)o->head_dim * sizeof(float);
+  return n;
+}
+
+// A matrix of [rows][heads * head_dim].
+scalify_status check_tokens(const scalify_scaled_array* x, int64_t rows, int64_t cols) {
+  if (x->rows != rows || x->cols != cols) return SCALIFY_ERR_SHAPE;
+  if (x->trans != 0) return SCALIFY_ERR_LAYOUT;
+  if (rows == 0) return SCALIFY_OK;
+  if (x->data == nullptr) return SCALIFY_ERR_NULL;
+  if (x->ld < cols) return SCALIFY_ERR_SHAPE;
+  if ((x->ld * elem_bytes(x->dtype)) % 16 != 0 || !aligned16(x->data)) return SCALIFY_ERR_ALIGN;
+  if (x->ld >= ((int64_t)1 << 31) / 128 / elem_bytes(x->dtype)) return SCALIFY_ERR_SHAPE;
+  return SCALIFY_OK;
+}
+
+// Whether two matrices share an element's memory: not if their bytes lie apart,
+// or if they are other columns of rows of the same pitch.
+bool tokens_overlap(const scalify_scaled_array* a, const scalify_scaled_array* b) {
+  if (a->rows == 0 || b->rows == 0 || a->cols == 0 || b->cols == 0) return false;
+  const uint64_t a0 = (uintptr_t)a->data, b0 = (uintptr_t)b->data;
+  const uint64_t aw = (uint64_t)(a->cols * elem_bytes(a->dtype)), bw = (uint64_t)(b->cols * elem_bytes(b->dtype));
+  const uint64_t ap = (uint64_t)(a->ld * elem_bytes(a->dtype)), bp = (uint64_t)(b->ld * elem_bytes(b->dtype));
+  const uint64_t a1 = a0 + (uint64_t)(a->rows - 1) * ap + aw, b1 = b0 + (uint64_t)(b->rows - 1) * bp + bw;
+  if (!(a0 < b1 && b0 < a1)) return false;
+  if (ap != bp) return true;
+  const uint64_t d = b0 >= a0 ? (b0 - a0) % ap : (ap - (a0 - b0) % ap) % ap;  // b's first column after a's
+  return !(d >= aw && d + bw <= ap);
+}
+
+void attention_params(AttnParams* p, const scalify_scaled_array* q, const scalify_scaled_array* k,
+                      const scalify_scaled_array* v, const scalify_attention_opts* o, const AttnSizes& z) {
+  p->q = q->data;
+  p->k = k->data;
+  p->v = v->data;
+  p->ldq = q->ld;
+  p->ldk = k->ld;
+  p->ldv = v->ld;
+  p->q_fmt = q->dtype;
+  p->k_fmt = k->dtype;
+  p->v_fmt = v->dtype;
+  p->s_q = q->scale;
+  p->s_k = k->scale;
+  p->s_v = v->scale;
+  p->rows_q = q->rows;
+  p->rows_k = k->rows;
+  p->batch = o->batch;
+  p->H = o->heads;
+  p->Hkv = o->kv_heads;
+  p->G = z.G;
+  p->D = o->head_dim;
+  p->causal = o->causal;
+  p->alpha = o->softmax_scale;
+  p->q_start = o->q_start;
+  p->k_start = o->k_start;
+  p->k_len = o->k_len;
+  p->max_q = z.max_q;
+  p->max_k = z.max_k;
 }
 
 }  // namespace
@@ -647,6 +776,277 @@ scalify_status scalify_layernorm_bwd(const scalify_scaled_array* dy, const scali
   if (launch_layernorm_bwd(p, dx->dtype, (hipStream_t)stream) != hipSuccess)
     return SCALIFY_ERR_HIP;
   return SCALIFY_OK;
+}
+
+scalify_status scalify_rmsnorm_fwd(const scalify_scaled_array* x,
+                                   const scalify_scaled_array* residual, const float* gamma,
+                                   float eps, scalify_scaled_array* sum_out,
+                                   scalify_scaled_array* out, float* row_scale,
+                                   uint8_t* block_scale, int32_t target_log2, int32_t saturate,
+                                   float* pre_out, void* stream) {
+  if (!x || !out || !out->scale) return SCALIFY_ERR_NULL;
+  if (sum_out && (!residual || !sum_out->scale)) return SCALIFY_ERR_NULL;
+  if (!is_any(x->dtype) || !is_out(out->dtype) || (residual && !is_out(residual->dtype)) ||
+      (sum_out && !is_out(sum_out->dtype)) || (block_scale && !is_fp8(out->dtype)))
+    return SCALIFY_ERR_DTYPE;
+  if (row_scale && block_scale) return SCALIFY_ERR_VALUE;
+  if (target_log2 < -1000 || target_log2 > 1000) return SCALIFY_ERR_VALUE;
+  if (!(eps >= 0.0f) || !(eps < 3.0e38f)) return SCALIFY_ERR_VALUE;
+  const int64_t R = x->rows, D = x->cols;
+  if (R < 0 || D < 0 || R > kMaxDim) return SCALIFY_ERR_SHAPE;
+  if (R > 0 && (D < 1 || D > kLayerNormMaxD)) return SCALIFY_ERR_SHAPE;
+  if (!aligned16(gamma) || !aligned16(pre_out)) return SCALIFY_ERR_ALIGN;
+  if (((uintptr_t)row_scale & 3u) || ((uintptr_t)block_scale & 3u)) return SCALIFY_ERR_ALIGN;
+  scalify_status st;
+  if ((st = check_rows(x, R, D)) != SCALIFY_OK) return st;
+  if ((st = check_rows(out, R, D)) != SCALIFY_OK) return st;
+  if (rows_conflict(x, out, R, D)) return SCALIFY_ERR_LAYOUT;
+  if (residual) {
+    if ((st = check_rows(residual, R, D)) != SCALIFY_OK) return st;
+    if (rows_conflict(residual, out, R, D)) return SCALIFY_ERR_LAYOUT;
+    if (out->scale == x->scale || out->scale == residual->scale) return SCALIFY_ERR_LAYOUT;
+  }
+  if (sum_out) {
+    if ((st = check_rows(sum_out, R, D)) != SCALIFY_OK) return st;
+    if (rows_conflict(x, sum_out, R, D) || rows_conflict(residual, sum_out, R, D) ||
+        rows_overlap(out, sum_out, R, D))
+      return SCALIFY_ERR_LAYOUT;
+    if (sum_out->scale == x->scale || sum_out->scale == residual->scale || sum_out->scale == out->scale)
+      return SCALIFY_ERR_LAYOUT;
+  }
+  RmsParams p = {};
+  p.x = x->data;
+  p.ldx = x->ld;
+  p.x_fmt = x->dtype;
+  p.s_x = x->scale;
+  p.has_res = residual != nullptr;
+  if (residual) {
+    p.res = residual->data;
+    p.ldr = residual->ld;
+    p.res_fmt = residual->dtype;
+    p.s_res = residual->scale;
+  }
+  p.gamma = gamma;
+  if (sum_out) {
+    p.sum = sum_out->data;
+    p.lds = sum_out->ld;
+    p.sum_fmt = sum_out->dtype;
+    p.sum_scale = sum_out->scale;
+  }
+  p.out = out->data;
+  p.ldo = out->ld;
+  p.out_fmt = out->dtype;
+  p.out_scale = out->scale;
+  p.row_scale = row_scale;
+  p.block_scale = block_scale;
+  p.pre_out = pre_out;
+  p.R = R;
+  p.D = (int)D;
+  p.eps = eps;
+  p.sat = saturate != 0;
+  p.target = target_log2;
+  return launch_rmsnorm_fwd(p, (hipStream_t)stream) == hipSuccess ? SCALIFY_OK : SCALIFY_ERR_HIP;
+}
+
+size_t scalify_rmsnorm_bwd_workspace_size(int64_t R, int64_t D) { return rmsnorm_bwd_ws(R, D); }
+
+scalify_status scalify_rmsnorm_bwd(const scalify_scaled_array* dy, const scalify_scaled_array* x,
+                                   const scalify_scaled_array* dsum, const float* gamma, float eps,
+                                   scalify_scaled_array* dx, float* dgamma, int32_t rescale,
+                                   int32_t target_log2, int32_t saturate, float* amax_out,
+                                   float* pre_out, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
+  if (!dy || !x || !dx || !dx->scale) return SCALIFY_ERR_NULL;
+  if (!is_any(dy->dtype) || !is_any(x->dtype) || !is_out(dx->dtype) || (dsum && !is_out(dsum->dtype)))
+    return SCALIFY_ERR_DTYPE;
+  if (rescale != SCALIFY_RESCALE_NONE && rescale != SCALIFY_RESCALE_AMAX) return SCALIFY_ERR_VALUE;
+  if (target_log2 < -1000 || target_log2 > 1000) return SCALIFY_ERR_VALUE;
+  if (!(eps >= 0.0f) || !(eps < 3.0e38f)) return SCALIFY_ERR_VALUE;
+  const int64_t R = x->rows, D = x->cols;
+  if (R < 0 || D < 0 || R > kMaxDim) return SCALIFY_ERR_SHAPE;
+  if (D > kLayerNormMaxD || (R > 0 && D < 1)) return SCALIFY_ERR_SHAPE;
+  if (!aligned16(gamma) || !aligned16(dgamma) || !aligned16(pre_out)) return SCALIFY_ERR_ALIGN;
+  scalify_status st;
+  if ((st = check_rows(x, R, D)) != SCALIFY_OK) return st;
+  if ((st = check_rows(dy, R, D)) != SCALIFY_OK) return st;
+  if ((st = check_rows(dx, R, D)) != SCALIFY_OK) return st;
+  if (rows_conflict(dx, dy, R, D) || rows_conflict(dx, x, R, D)) return SCALIFY_ERR_LAYOUT;
+  if (dsum) {
+    if ((st = check_rows(dsum, R, D)) != SCALIFY_OK) return st;
+    if (rows_conflict(dx, dsum, R, D)) return SCALIFY_ERR_LAYOUT;
+  }
+  const size_t need = rmsnorm_bwd_ws(R, D);
+  if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u))
+    return SCALIFY_ERR_WORKSPACE;
+  RmsParams p = {};
+  p.x = x->data;
+  p.ldx = x->ld;
+  p.x_fmt = x->dtype;
+  p.s_x = x->scale;
+  p.dy = dy->data;
+  p.lddy = dy->ld;
+  p.dy_fmt = dy->dtype;
+  p.s_dy = dy->scale;
+  p.has_res = dsum != nullptr;
+  if (dsum) {
+    p.res = dsum->data;
+    p.ldr = dsum->ld;
+    p.res_fmt = dsum->dtype;
+    p.s_res = dsum->scale;
+  }
+  p.gamma = gamma;
+  p.out = dx->data;
+  p.ldo = dx->ld;
+  p.out_fmt = dx->dtype;
+  p.out_scale = dx->scale;
+  p.pre_out = pre_out;
+  p.R = R;
+  p.D = (int)D;
+  p.eps = eps;
+  p.sat = saturate != 0;
+  p.target = target_log2;
+  p.mode = rescale == SCALIFY_RESCALE_AMAX ? 1 : 0;
+  p.hdr = (uint32_t*)workspace;
+  p.tag = next_tag();
+  p.partial = (float*)((uint8_t*)workspace + kHeaderBytes);
+  p.amax_out = amax_out;
+  p.dgamma = dgamma;
+  return launch_rmsnorm_bwd(p, (hipStream_t)stream) == hipSuccess ? SCALIFY_OK : SCALIFY_ERR_HIP;
+}
+
+size_t scalify_attention_fwd_workspace_size(int64_t rows_q, int64_t rows_k,
+                                            const scalify_attention_opts* opts) {
+  AttnSizes z;
+  if (attention_sizes(opts, rows_q, rows_k, &z) != SCALIFY_OK) return 0;
+  return attention_fwd_ws(opts, rows_q, z);
+}
+
+scalify_status scalify_attention_fwd(const scalify_scaled_array* q, const scalify_scaled_array* k,
+                                     const scalify_scaled_array* v, scalify_scaled_array* out,
+                                     float* lse, const scalify_attention_opts* opts,
+                                     int32_t saturate, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  if (!q || !k || !v || !out || !opts || !out->scale) return SCALIFY_ERR_NULL;
+  if (!is_out(q->dtype) || !is_out(k->dtype) || !is_out(v->dtype) || !is_out(out->dtype))
+    return SCALIFY_ERR_DTYPE;
+  AttnSizes z;
+  scalify_status st = attention_sizes(opts, q->rows, k->rows, &z);
+  if (st != SCALIFY_OK) return st;
+  const int64_t cq = (int64_t)opts->heads * opts->head_dim, ck = (int64_t)opts->kv_heads * opts->head_dim;
+  if ((st = check_tokens(q, q->rows, cq)) != SCALIFY_OK) return st;
+  if ((st = check_tokens(k, k->rows, ck)) != SCALIFY_OK) return st;
+  if ((st = check_tokens(v, k->rows, ck)) != SCALIFY_OK) return st;
+  if ((st = check_tokens(out, q->rows, cq)) != SCALIFY_OK) return st;
+  if (((uintptr_t)lse & 3u) != 0) return SCALIFY_ERR_ALIGN;
+  if (((uintptr_t)opts->q_start | (uintptr_t)opts->k_start | (uintptr_t)opts->k_len) & 7u) return SCALIFY_ERR_ALIGN;
+  if (tokens_overlap(out, q) || tokens_overlap(out, k) || tokens_overlap(out, v)) return SCALIFY_ERR_LAYOUT;
+  if (out->scale == q->scale || out->scale == k->scale) return SCALIFY_ERR_LAYOUT;
+  const size_t need = attention_fwd_ws(opts, q->rows, z);
+  if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)))
+    return SCALIFY_ERR_WORKSPACE;
+  const AttnPlan plan = attention_plan(opts->batch, opts->kv_heads, z.G, z.max_q, z.keys);
+  AttnParams p = {};
+  attention_params(&p, q, k, v, opts, z);
+  p.out = out->data;
+  p.ldo = out->ld;
+  p.out_fmt = out->dtype;
+  p.out_scale = out->scale;
+  p.lse = lse;
+  p.sat = saturate != 0;
+  p.splits = plan.splits;
+  p.part_o = (float*)workspace;
+  p.part_ml = (float2*)((float*)workspace + (size_t)plan.splits * (size_t)q->rows * (size_t)cq);
+  return launch_attention_fwd(p, plan, (hipStream_t)stream) == hipSuccess ? SCALIFY_OK : SCALIFY_ERR_HIP;
+}
+
+size_t scalify_attention_bwd_workspace_size(int64_t rows_q, int64_t rows_k,
+                                            const scalify_attention_opts* opts, int32_t rescale) {
+  AttnSizes z;
+  if (attention_sizes(opts, rows_q, rows_k, &z) != SCALIFY_OK) return 0;
+  if (rescale != SCALIFY_RESCALE_NONE && rescale != SCALIFY_RESCALE_AMAX) return 0;
+  return attention_bwd_ws(opts, rows_q, rows_k, rescale);
+}
+
+scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
+                                     const scalify_scaled_array* q, const scalify_scaled_array* k,
+                                     const scalify_scaled_array* v, const scalify_scaled_array* out,
+                                     const float* lse, scalify_scaled_array* dq,
+                                     scalify_scaled_array* dk, scalify_scaled_array* dv,
+                                     const scalify_attention_opts* opts, int32_t rescale,
+                                     int32_t target_log2, int32_t saturate, float* amax_out,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dout || !q || !k || !v || !out || !dq || !dk || !dv || !opts) return SCALIFY_ERR_NULL;
+  if (!dq->scale || !dk->scale || !dv->scale) return SCALIFY_ERR_NULL;
+  const scalify_scaled_array* const in[5] = {dout, q, k, v, out};
+  scalify_scaled_array* const grad[3] = {dq, dk, dv};
+  for (const scalify_scaled_array* x : in)
+    if (!is_out(x->dtype)) return SCALIFY_ERR_DTYPE;
+  for (const scalify_scaled_array* x : grad)
+    if (!is_out(x->dtype)) return SCALIFY_ERR_DTYPE;
+  if (out->dtype != SCALIFY_F16) return SCALIFY_ERR_DTYPE;
+  if (rescale != SCALIFY_RESCALE_NONE && rescale != SCALIFY_RESCALE_AMAX) return SCALIFY_ERR_VALUE;
+  if (target_log2 < -1000 || target_log2 > 1000) return SCALIFY_ERR_VALUE;
+  AttnSizes z;
+  scalify_status st = attention_sizes(opts, q->rows, k->rows, &z);
+  if (st != SCALIFY_OK) return st;
+  const int64_t cq = (int64_t)opts->heads * opts->head_dim, ck = (int64_t)opts->kv_heads * opts->head_dim;
+  // workgroups of the row statistics (16 rows of a head) and of the casts (16 rows)
+  if ((q->rows * opts->heads + k->rows * opts->kv_heads) / 16 > 0x7FFFFFF0 ||
+      opts->batch * (((z.max_q > z.max_k ? z.max_q : z.max_k) + 15) / 16) > 0x7FFFFFFF)
+    return SCALIFY_ERR_SHAPE;
+  for (const scalify_scaled_array* x : {dout, q, (const scalify_scaled_array*)out, (const scalify_scaled_array*)dq})
+    if ((st = check_tokens(x, q->rows, cq)) != SCALIFY_OK) return st;
+  for (const scalify_scaled_array* x : {k, v, (const scalify_scaled_array*)dk, (const scalify_scaled_array*)dv})
+    if ((st = check_tokens(x, k->rows, ck)) != SCALIFY_OK) return st;
+  if (!lse && q->rows > 0) return SCALIFY_ERR_NULL;
+  if (((uintptr_t)lse & 3u) != 0) return SCALIFY_ERR_ALIGN;
+  if (((uintptr_t)opts->q_start | (uintptr_t)opts->k_start | (uintptr_t)opts->k_len) & 7u) return SCALIFY_ERR_ALIGN;
+  for (int i = 0; i < 3; ++i) {
+    for (const scalify_scaled_array* x : in)
+      if (tokens_overlap(grad[i], x) || grad[i]->scale == x->scale) return SCALIFY_ERR_LAYOUT;
+    for (int j = 0; j < i; ++j)
+      if (tokens_overlap(grad[i], grad[j]) || grad[i]->scale == grad[j]->scale) return SCALIFY_ERR_LAYOUT;
+  }
+  const size_t need = attention_bwd_ws(opts, q->rows, k->rows, rescale);
+  if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)) return SCALIFY_ERR_WORKSPACE;
+  AttnParams p = {};
+  attention_params(&p, q, k, v, opts, z);
+  p.out = out->data;
+  p.ldo = out->ld;
+  p.out_fmt = out->dtype;
+  p.out_scale = out->scale;
+  p.lse = (float*)lse;
+  p.sat = saturate != 0;
+  p.dout = dout->data;
+  p.lddo = dout->ld;
+  p.do_fmt = dout->dtype;
+  p.s_do = dout->scale;
+  const size_t nq = (size_t)q->rows * opts->heads, nk = (size_t)k->rows * opts->kv_heads;
+  p.amax = (uint32_t*)workspace;
+  p.delta = (float*)((uint8_t*)workspace + kHeaderBytes);
+  p.nd2 = p.delta + nq;
+  p.nv2 = p.nd2 + nq;
+  if (rescale == SCALIFY_RESCALE_AMAX) {
+    p.dq32 = p.delta + round_up((int64_t)(2 * nq + nk), 4);
+    p.dk32 = p.dq32 + nq * (size_t)opts->head_dim;
+    p.dv32 = p.dk32 + nk * (size_t)opts->head_dim;
+  }
+  p.dq = dq->data;
+  p.dk = dk->data;
+  p.dv = dv->data;
+  p.lddq = dq->ld;
+  p.lddk = dk->ld;
+  p.lddv = dv->ld;
+  p.dq_fmt = dq->dtype;
+  p.dk_fmt = dk->dtype;
+  p.dv_fmt = dv->dtype;
+  p.dq_scale = dq->scale;
+  p.dk_scale = dk->scale;
+  p.dv_scale = dv->scale;
+  p.amax_out = amax_out;
+  p.mode = rescale == SCALIFY_RESCALE_AMAX ? 1 : 0;
+  p.target = target_log2;
+  return launch_attention_bwd(p, (hipStream_t)stream) == hipSuccess ? SCALIFY_OK : SCALIFY_ERR_HIP;
 }
 
 }  // extern "C"

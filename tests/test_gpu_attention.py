@@ -1,0 +1,439 @@
+"""GPU parity of attention over ScaledArrays, forward and backward, through the
+C ABI, against the plain 64-bit forms in tests/layer_refs.py, whose bounds count
+the F16 rounding of the probabilities and of dS, the fp32 sums and the cast."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2407_17353_amd import binding as sc
+from tests import layer_refs as lr
+from tests.helpers import say
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F16, E4M3, E5M2 = sc.F16, sc.E4M3, sc.E5M2
+
+
+def _i64(x):
+    return torch.tensor(x, dtype=torch.int64, device=DEV) if x is not None else None
+
+
+def _inputs(case, seed=1):
+    H, Hkv, D = case["H"], case["Hkv"], case["D"]
+    q = lr.values(case["Tq"], H * D, case["fq"], seed, case.get("sq", 1.0))
+    k = lr.values(case["Tk"], Hkv * D, case["fk"], seed + 1)
+    v = lr.values(case["Tk"], Hkv * D, case["fv"], seed + 2)
+    return q, k, v
+
+
+def _opts(case):
+    return {"heads": case["H"], "kv_heads": case["Hkv"], "batch": case["B"], "causal": case["causal"],
+            "softmax_scale": case["alpha"], "q_start": _i64(case.get("q_start")), "k_start": _i64(case.get("k_start")),
+            "k_len": _i64(case.get("k_len")), "max_q": case.get("max_q", 0), "max_k": case.get("max_k", 0)}
+
+
+def _seqs(case):
+    return lr.spans(case["B"], case["Tq"], case["Tk"], case.get("q_start"), case.get("k_start"), case.get("k_len"))
+
+
+def _case(name, H=2, Hkv=None, D=64, B=1, Lq=None, Lk=None, fq=F16, fk=F16, fv=None, fo=F16, causal=True, **kw):
+    c = {"name": name, "H": H, "Hkv": Hkv or H, "D": D, "B": B, "fq": fq, "fk": fk, "fv": fk if fv is None else fv,
+         "fo": fo, "causal": causal, "eq": 1, "ek": -2, "ev": 3, "alpha": 2.0 / math.sqrt(D)}
+    c["Tq"], c["Tk"] = (Lq or 0) * B, (Lk or 0) * B
+    c.update(kw)
+    return c
+
+
+CASES = [
+    _case("one_token_one_key", Lq=1, Lk=1),
+    _case("square", Lq=64, Lk=64, D=64),
+    _case("square_128", Lq=128, Lk=128, D=128, causal=False),
+    _case("odd", Lq=77, Lk=131, D=128, B=2),
+    _case("odd_plain", Lq=131, Lk=77, D=64, causal=False),
+    _case("rows_without_keys", Lq=150, Lk=70, D=64),
+    _case("rows_without_keys_128", Lq=70, Lk=3, D=128, H=4, Hkv=2),
+    _case("no_keys", Lq=5, Lk=0, D=64),
+    _case("shared", Lq=45, Lk=200, H=8, Hkv=2, D=128),
+    _case("one_kv_head", Lq=33, Lk=97, H=5, Hkv=1, D=48),
+    _case("D16", Lq=65, Lk=65, D=16),
+    _case("D80", Lq=100, Lk=100, D=80, fk=E4M3),
+    _case("D112_8bit", Lq=90, Lk=190, D=112, fq=E4M3, fk=E4M3, fv=E5M2, fo=E4M3),
+    _case("e5m2", Lq=40, Lk=40, D=64, fq=E5M2, fk=E5M2, fo=E5M2),
+    _case("mixed", Lq=70, Lk=300, D=96, fq=F16, fk=F16, fv=E4M3),
+    _case("long", Lq=200, Lk=1500, H=2, Hkv=1, D=128),
+    _case("token", Lq=1, Lk=700, H=8, Hkv=2, D=128, causal=True),
+    _case("token_long", Lq=1, Lk=5000, H=4, Hkv=4, D=64, causal=False),
+    _case("tokens_5", Lq=5, Lk=1000, H=8, Hkv=2, D=128, B=3, fk=E4M3, fo=E4M3),
+    _case("tokens_more_than_keys", Lq=6, Lk=3, H=4, Hkv=2, D=64, B=2),
+    _case("cache", Lq=1, Lk=600, H=4, Hkv=2, D=128, B=4, fk=E4M3, k_len=[600, 0, 1, 333], max_k=600),
+    _case("cache_chunk", Lq=40, Lk=900, H=4, Hkv=2, D=64, B=3, k_len=[900, 17, 65]),
+    _case("packed", B=4, H=4, Hkv=2, D=128, Tq=300, Tk=300, q_start=[0, 100, 101, 101, 300], k_start=[0, 100, 101, 101, 300]),
+    _case("packed_max", B=3, H=2, D=64, Tq=260, Tk=400, q_start=[3, 90, 150, 255], k_start=[5, 200, 201, 390],
+          k_len=[150, 1, 189], max_q=105, max_k=195, causal=False),
+    _case("peaked", Lq=60, Lk=260, D=128, sq=8.0),
+]
+
+
+def run_fwd(case, q, k, v, out=None, lse=True, ld=None, **kw):
+    Q, K, V = (lr.scaled(t, f, e, ld=ld) for t, f, e in ((q, case["fq"], case["eq"]), (k, case["fk"], case["ek"]),
+                                                        (v, case["fv"], case["ev"])))
+    out = out or lr.empty(case["Tq"], case["H"] * case["D"], case["fo"])
+    lse = torch.full((case["H"], case["Tq"]), 7.0, device=DEV) if lse else None
+    sc.scalify_attention_fwd(Q, K, V, out, lse=lse, **_opts(case), **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def covered(case):
+    rows = torch.zeros(case["Tq"], dtype=torch.bool)
+    for q0, a, _, _ in _seqs(case):
+        rows[q0:q0 + a] = True
+    return rows
+
+
+def check_fwd(case, q, k, v, out, lse):
+    o, eo, l, el = lr.attention(q.to(lr.F64), k.to(lr.F64), v.to(lr.F64), case["H"], case["Hkv"],
+                                case["alpha"] * 2.0 ** (case["eq"] + case["ek"]), _seqs(case), case["causal"], case["fo"])
+    rows = covered(case)
+    got = lr.data(out)
+    bad = ((got - o).abs() > eo) & rows[:, None]
+    assert not bad.any(), (case["name"], int(bad.sum()), float(((got - o).abs() / eo)[rows].max()))
+    assert lr.log2_of(out) == case["ev"]
+    untouched = lr.codes(out)[~rows.numpy()]
+    assert (untouched == (0x5A5A if case["fo"] == F16 else 0x5A)).all()
+    if lse is not None:
+        m = lse.cpu().to(lr.F64)
+        assert torch.equal(torch.isinf(m[:, rows]), torch.isinf(l[:, rows]))
+        f = torch.isfinite(l) & rows
+        assert ((m - l).abs()[f] <= el[f]).all(), (case["name"], float(((m - l).abs()[f] / el[f]).max()))
+        assert (m[:, ~rows] == 7.0).all()
+    return o, l
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: c["name"])
+def test_forward(case):
+    say(f"attention fwd {case['name']}")
+    q, k, v = _inputs(case)
+    out, lse = run_fwd(case, q, k, v)
+    check_fwd(case, q, k, v, out, lse)
+    again, lse2 = run_fwd(case, q, k, v)
+    assert np.array_equal(lr.codes(out), lr.codes(again)) and torch.equal(lse, lse2)
+
+
+def test_interleaved_columns_and_large_ld():
+    """q, k and v as column ranges of one F16 matrix, and out as another range of it."""
+    case = _case("qkv", Lq=90, Lk=90, H=4, Hkv=2, D=64)
+    q, k, v = _inputs(case)
+    H, Hkv, D, T = 4, 2, 64, 90
+    cq, ck = H * D, Hkv * D
+    st = torch.full((T, 2 * cq + 2 * ck + 8), float("nan"), dtype=torch.float16)
+    at = [0, cq, cq + ck, cq + 2 * ck, 2 * cq + 2 * ck]
+    for t, a in ((q, at[0]), (k, at[1]), (v, at[2])):
+        st[:, a:a + t.shape[1]] = t
+    st = st.view(torch.int16).to(DEV)
+    part = [sc.ScaledArray(st[:, at[i]:at[i + 1]], F16, sc.scale_tensor(e, DEV)) for i, e in enumerate((1, -2, 3, 0))]
+    lse = torch.empty((H, T), device=DEV)
+    sc.scalify_attention_fwd(*part, lse=lse, **_opts(case))
+    torch.cuda.synchronize()
+    check_fwd(case, q, k, v, part[3], lse)
+    plain, _ = run_fwd(case, q, k, v)
+    assert np.array_equal(lr.codes(part[3]), lr.codes(plain))
+
+
+@pytest.mark.parametrize("D,Lq,Lk,B", [(64, 150, 150, 1), (128, 70, 200, 1), (128, 1, 700, 1), (64, 5, 300, 2)])
+def test_values_that_a_mask_hides(D, Lq, Lk, B):
+    """Infinities and NaN in the padding of a cache and in rows that only later
+    queries see reach no row that does not see them; those that do get them."""
+    lens = [Lk - 7 - 20 * b for b in range(B)]
+    case = _case("hidden", H=2, Hkv=1, D=D, B=B, Lq=Lq, Lk=Lk, k_len=lens)
+    q, k, v = _inputs(case)
+    clean, _ = run_fwd(case, q, k, v)
+    k2, v2 = k.clone(), v.clone()
+    for b in range(B):
+        k2[b * Lk + lens[b]:(b + 1) * Lk] = float("nan")
+        v2[b * Lk + lens[b]:(b + 1) * Lk] = float("inf")
+    out, lse = run_fwd(case, q, k2, v2)
+    assert np.array_equal(lr.codes(out), lr.codes(clean))
+    # (rows of the last sequence that the last four queries alone see)
+    if Lq > 4:
+        end = (B - 1) * Lk + lens[-1]
+        v2[end - 1, 3] = float("inf")
+        v2[end - 2, 5] = float("-inf")
+        v2[end - 3, 7] = float("nan")
+        v2[end - 4, 9], v2[end - 3, 9] = float("inf"), float("-inf")
+        out, lse = run_fwd(case, q, k2, v2)
+        got, want = lr.data(out), lr.data(clean)
+        T = case["Tq"]
+        assert np.array_equal(lr.codes(out)[:T - 4], lr.codes(clean)[:T - 4])
+        for h in range(2):
+            c = h * D
+            big = 65504.0  # (saturating cast of +-Inf)
+            assert got[T - 1, c + 3] == big and got[T - 2, c + 3] == want[T - 2, c + 3]
+            assert (got[T - 2:, c + 5] == -big).all() and got[T - 3, c + 5] == want[T - 3, c + 5]
+            assert got[T - 3:, c + 7].isnan().all() and got[T - 4, c + 7] == want[T - 4, c + 7]
+            assert got[T - 4, c + 9] == big and got[T - 3:, c + 9].isnan().all()
+    # a NaN key that only the last query sees
+    if Lq > 1:
+        k3 = k.clone()
+        k3[(B - 1) * Lk + lens[-1] - 1] = float("nan")
+        out, _ = run_fwd(case, q, k3, v)
+        T = case["Tq"]
+        assert np.array_equal(lr.codes(out)[:T - 1], lr.codes(clean)[:T - 1])
+        assert lr.data(out)[T - 1].isnan().all()
+
+
+def test_starts_and_lengths_are_clamped():
+    """Whatever the device arrays hold, the call stays in the matrices."""
+    case = _case("clamped", H=2, D=64, B=3, Tq=50, Tk=60, causal=False, q_start=[-5, 20, 10, 10 ** 12],
+                 k_start=[-(10 ** 15), 30, 30, 10 ** 15], k_len=[10 ** 15, 5, 10])
+    q, k, v = _inputs(case)
+    out, lse = run_fwd(case, q, k, v)
+    as_clamped = dict(case, q_start=[0, 20, 20, 50], k_start=[0, 30, 30, 60], k_len=[30, 0, 10])
+    # (starts are clamped one by one: sequence 1 is 20 .. max(10, 20), sequence 2 is 10 .. 50)
+    got = lr.data(out)
+    o, eo, _, _ = lr.attention(q.to(lr.F64), k.to(lr.F64), v.to(lr.F64), 2, 2, case["alpha"] / 2,
+                               [(0, 20, 0, 30), (10, 40, 30, 10)], False, F16)
+    assert ((got[20:] - o[20:]).abs() <= eo[20:]).all() and as_clamped["B"] == 3
+
+
+def test_another_stream_and_capture():
+    """A captured and replayed call of each kind (split keys, shared tiles)
+    gives the eager result on every replay, with eager calls between; and two
+    captured calls may share a workspace when they run one after the other."""
+    for name in ("token", "shared"):
+        case = next(c for c in CASES if c["name"] == name)
+        q, k, v = _inputs(case)
+        Q, K, V = (lr.scaled(t, F16, e) for t, e in ((q, 1), (k, -2), (v, 3)))
+        o = sc.attention_opts(Q, **{k2: v2 for k2, v2 in _opts(case).items()})
+        ws = sc.workspace(sc.scalify_attention_fwd_workspace_size(case["Tq"], case["Tk"], o), DEV)
+        want, _ = run_fwd(case, q, k, v)
+        out = [lr.empty(case["Tq"], case["H"] * case["D"], F16) for _ in range(2)]
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        graphs = []
+        for x in out:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                sc.scalify_attention_fwd(Q, K, V, x, ws=ws, **_opts(case))
+            graphs.append(g)
+        for _ in range(3):
+            ws.fill_(0xFF)
+            for x, g in zip(out, graphs):
+                x.data.fill_(0)
+                g.replay()
+            torch.cuda.synchronize()
+            assert all(np.array_equal(lr.codes(x), lr.codes(want)) for x in out)
+            eager, _ = run_fwd(case, q, k, v, ws=ws)
+            assert np.array_equal(lr.codes(eager), lr.codes(want))
+        # on a stream of the caller's, without a workspace of the caller's
+        x = lr.empty(case["Tq"], case["H"] * case["D"], F16)
+        s.wait_stream(torch.cuda.current_stream())
+        sc.scalify_attention_fwd(Q, K, V, x, stream=s, **_opts(case))
+        s.synchronize()
+        assert np.array_equal(lr.codes(x), lr.codes(want))
+
+
+# ---------------------------------------------------------------- backward
+
+BWD = [dict(c, fo=F16) for c in CASES if c["name"] in
+       ("one_token_one_key", "square", "square_128", "odd", "odd_plain", "rows_without_keys", "rows_without_keys_128",
+        "no_keys", "shared", "one_kv_head", "D16", "D80", "D112_8bit", "mixed", "cache_chunk", "packed", "packed_max",
+        "peaked", "long")]
+
+
+def _bwd_inputs(case, fdo=F16, seed=9, heavy=False):
+    q, k, v = _inputs(case)
+    rows = -10 * torch.rand(case["Tq"], generator=torch.Generator().manual_seed(seed)) if heavy else None
+    do = lr.values(case["Tq"], case["H"] * case["D"], fdo, seed, rows=rows)
+    return q, k, v, do
+
+
+def run_bwd(case, q, k, v, do, fdo=F16, fg=F16, mode=sc.RESCALE_NONE, ws=None, **kw):
+    """(dq, dk, dv), amax_out, the forward's out and lse, the workspace."""
+    out, lse = run_fwd(case, q, k, v)
+    arrays = [lr.scaled(t, f, e) for t, f, e in ((do, fdo, -6), (q, case["fq"], case["eq"]), (k, case["fk"], case["ek"]),
+                                                 (v, case["fv"], case["ev"]))]
+    grads = [lr.empty(*t.shape, fg) for t in (q, k, v)]
+    amax = torch.full((3,), -1.0, device=DEV)
+    o = sc.attention_opts(arrays[1], **_opts(case))
+    if ws is None:
+        ws = sc.workspace(sc.scalify_attention_bwd_workspace_size(case["Tq"], case["Tk"], o, mode), DEV)
+        ws.fill_(0xFF)
+    sc.scalify_attention_bwd(*arrays, out, lse, *grads, rescale=mode, amax_out=amax, ws=ws, **_opts(case), **kw)
+    torch.cuda.synchronize()
+    return grads, amax.cpu(), out, lse, ws
+
+
+def _reference(case, q, k, v, do, out, lse):
+    alpha = case["alpha"] * 2.0 ** (case["eq"] + case["ek"])
+    return lr.attention_grads(do.to(lr.F64), q.to(lr.F64), k.to(lr.F64), v.to(lr.F64), lr.data(out), lse.cpu(), case["H"],
+                              case["Hkv"], (alpha, case["alpha"]), 0, _seqs(case), case["causal"])
+
+
+def _rows_of(case):
+    """Rows of q, and of k and v, that belong to a sequence (padding included)."""
+    B, ks = case["B"], case.get("k_start")
+    rk = torch.zeros(case["Tk"], dtype=torch.bool)
+    rk[ks[0] if ks else 0:ks[-1] if ks else case["Tk"]] = True
+    return covered(case), rk
+
+
+def check_bwd(case, q, k, v, do, res, fg=F16):
+    grads, amax, out, lse, _ = res
+    want, err = _reference(case, q, k, v, do, out, lse)
+    rq, rk = _rows_of(case)
+    base = [-6 + case["ev"] + case["ek"], -6 + case["ev"] + case["eq"], -6]
+    rel, sub = lr.HALF[fg]
+    for i, (x, rows) in enumerate(zip(grads, (rq, rk, rk))):
+        shift = lr.log2_of(x) - base[i]
+        got = lr.data(x) * 2.0 ** shift
+        tol = err[i] + (want[i].abs() + err[i]) * rel + sub * 2.0 ** shift
+        if fg == F16 and shift == 0:
+            assert (want[i].abs().max() if want[i].numel() else 0) < 60000
+        bad = ((got - want[i]).abs() > tol) & rows[:, None]
+        assert not bad.any(), (case["name"], "q k v".split()[i], int(bad.sum()),
+                               float(((got - want[i]).abs() / tol)[rows].max()))
+        left = lr.codes(x)[~rows.numpy()]
+        assert (left == (0x5A5A if fg == F16 else 0x5A)).all()
+    return want, err
+
+
+@pytest.mark.parametrize("case", BWD, ids=lambda c: c["name"])
+def test_backward(case):
+    say(f"attention bwd {case['name']}")
+    q, k, v, do = _bwd_inputs(case)
+    res = run_bwd(case, q, k, v, do)
+    check_bwd(case, q, k, v, do, res)
+    again = run_bwd(case, q, k, v, do)
+    for a, b in zip(res[0], again[0]):
+        assert np.array_equal(lr.codes(a), lr.codes(b)) and a.scale.item() == b.scale.item()
+
+
+@pytest.mark.parametrize("name", ["odd", "shared", "packed_max", "cache_chunk", "no_keys"])
+@pytest.mark.parametrize("fg,target", [(E5M2, 0), (F16, 3), (E4M3, 7)])
+def test_backward_dynamic_rescale(name, fg, target):
+    """The rescale's statistic, exponent and cast, exactly, on the kernels' own
+    fp32 gradients (kept in the workspace), and the values within the bounds."""
+    case = next(c for c in BWD if c["name"] == name)
+    q, k, v, do = _bwd_inputs(case, E5M2, heavy=True)
+    res = run_bwd(case, q, k, v, do, fdo=E5M2, fg=fg, mode=sc.RESCALE_AMAX, target_log2=target)
+    check_bwd(case, q, k, v, do, res, fg)
+    grads, amax, out, lse, ws = res
+    nq, nk = case["Tq"] * case["H"], case["Tk"] * case["Hkv"]
+    at = 256 + (2 * nq + nk + 3) // 4 * 16
+    base = [-6 + case["ev"] + case["ek"], -6 + case["ev"] + case["eq"], -6]
+    rq, rk = _rows_of(case)
+    for i, (x, rows) in enumerate(zip(grads, (rq, rk, rk))):
+        n = x.data.numel()
+        f = ws[at:at + 4 * n].cpu().numpy().view(np.float32).reshape(x.data.shape)[rows.numpy()]
+        at += 4 * n
+        a = np.abs(f).max() if f.size else 0.0
+        assert float(amax[i]) == a
+        e = (lr.floor_log2(a) or 0) - target if a > 0 else 0
+        assert lr.log2_of(x) == base[i] + e
+        assert np.array_equal(lr.codes(x)[rows.numpy()], lr.cast(f, fg, e))
+
+
+def test_backward_differences():
+    """The gradients against central differences of the 64-bit forward."""
+    case = _case("differences", Lq=7, Lk=9, H=2, Hkv=1, D=16, causal=True)
+    q, k, v, do = _bwd_inputs(case)
+    grads = run_bwd(case, q, k, v, do)[0]
+    t = [x.to(lr.F64) for x in (q, k, v)]
+    alpha = case["alpha"] * 2.0 ** (case["eq"] + case["ek"])
+
+    def loss(ts):
+        o = lr.attention(*ts, 2, 1, alpha, _seqs(case), True, F16)[0]
+        return float((o * do.to(lr.F64)).sum())
+    # dq, dk are with respect to true values: one unit of data is 2^e of them
+    unit = [2.0 ** (case["eq"] + case["ek"]), 2.0 ** (case["eq"] + case["ek"]), 1.0]
+    r = np.random.RandomState(3)
+    for i in range(3):
+        got = lr.data(grads[i])
+        for _ in range(12):
+            a, b = r.randint(t[i].shape[0]), r.randint(t[i].shape[1])
+            h = 1e-4
+            d = []
+            for sign in (1, -1):
+                ts = [x.clone() for x in t]
+                ts[i][a, b] += sign * h
+                d.append(loss(ts))
+            num = (d[0] - d[1]) / (2 * h) / unit[i]
+            # (the stored output that delta is taken from is rounded to F16: 2^-11 of |dO| |O|)
+            assert abs(float(got[a, b]) - num) <= 4e-3 * (1 + abs(num)), (i, a, b, float(got[a, b]), num)
+
+
+def test_backward_large_data():
+    """Data at the top of its formats: dP is far beyond F16, its power of two is not."""
+    case = _case("large", Lq=60, Lk=60, D=128, fq=E4M3, fk=E4M3, fv=E4M3, eq=-9, ek=-9)
+    q, k, _ = _inputs(case)
+    v = lr.values(60, 256, E4M3, 5, 200.0).clone()
+    do = lr.values(60, 256, E5M2, 6, 20000.0)
+    v, do = v.float().clamp(-448, 448).to(torch.float8_e4m3fn), do.float().clamp(-57344, 57344).to(torch.float8_e5m2)
+    res = run_bwd(case, q, k, v, do, fdo=E5M2, fg=E5M2, mode=sc.RESCALE_AMAX)
+    check_bwd(case, q, k, v, do, res, E5M2)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_backward_values_that_a_mask_hides(D):
+    """What is not finite reaches the gradients of pairs that see it, and no others."""
+    T, lk = 150, 140
+    case = _case("hidden", H=2, Hkv=1, D=D, Lq=T, Lk=T + 20, k_len=[lk])
+    q, k, v, do = _bwd_inputs(case)
+    clean = [lr.codes(x) for x in run_bwd(case, q, k, v, do)[0]]
+    k2, v2 = k.clone(), v.clone()
+    k2[lk:], v2[lk:] = float("nan"), float("inf")
+    got = run_bwd(case, q, k2, v2, do)[0]
+    assert all(np.array_equal(lr.codes(a), b) for a, b in zip(got, clean))
+    assert (got[1].data[lk:] == 0).all() and (got[2].data[lk:] == 0).all()
+    # dO of query 30 (it sees the keys up to 30 + lk - T = 20)
+    sees = 30 + lk - T
+    d2 = do.clone()
+    d2[30, 5], d2[30, 6] = float("inf"), float("nan")
+    got = run_bwd(case, q, k, v, d2)[0]
+    dq, dk, dv = (lr.codes(x) for x in got)
+    assert np.array_equal(np.delete(dq, 30, 0)[:, D:], np.delete(clean[0], 30, 0)[:, D:])
+    assert np.array_equal(dk[sees + 1:], clean[1][sees + 1:]) and np.array_equal(dv[sees + 1:], clean[2][sees + 1:])
+    v5, v6 = lr.data(got[2])[:sees + 1, 5], lr.data(got[2])[:sees + 1, 6]
+    assert (v5 == 65504).all() and v6.isnan().all()
+    # a NaN query, and a NaN key that the last query alone sees
+    q2 = q.clone()
+    q2[40] = float("nan")
+    dq, dk, dv = (lr.codes(x) for x in run_bwd(case, q2, k, v, do)[0])
+    sees = 40 + lk - T
+    assert np.array_equal(dk[sees + 1:], clean[1][sees + 1:]) and np.array_equal(dv[sees + 1:], clean[2][sees + 1:])
+    assert np.array_equal(np.delete(dq, 40, 0), np.delete(clean[0], 40, 0))
+    k3 = k.clone()
+    k3[lk - 1] = float("nan")
+    dq = lr.codes(run_bwd(case, q, k3, v, do)[0][0])
+    assert np.array_equal(dq[:T - 1], clean[0][:T - 1])
+
+
+def test_backward_capture():
+    """Both modes captured, replayed with the workspace dirtied between, and two
+    graphs on one workspace."""
+    case = next(c for c in BWD if c["name"] == "shared")
+    q, k, v, do = _bwd_inputs(case)
+    for mode, fg in ((sc.RESCALE_NONE, F16), (sc.RESCALE_AMAX, E5M2)):
+        want, _, out, lse, ws = run_bwd(case, q, k, v, do, fg=fg, mode=mode)
+        a = [lr.scaled(t, F16, e) for t, e in ((do, -6), (q, 1), (k, -2), (v, 3))]
+        sets = [[lr.empty(*t.shape, fg) for t in (q, k, v)] for _ in range(2)]
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        graphs = []
+        for grads in sets:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                sc.scalify_attention_bwd(*a, out, lse, *grads, rescale=mode, ws=ws, **_opts(case))
+            graphs.append(g)
+        for _ in range(3):
+            ws.fill_(0xFF)
+            for g in graphs:
+                g.replay()
+            torch.cuda.synchronize()
+            for grads in sets:
+                for x, y in zip(grads, want):
+                    assert np.array_equal(lr.codes(x), lr.codes(y)) and x.scale.item() == y.scale.item()
+            run_bwd(case, q, k, v, do, fg=fg, mode=mode, ws=ws)
