@@ -500,8 +500,9 @@ size_t scalify_attention_fwd_workspace_size(int64_t rows_q, int64_t rows_k,
  * gives zeros and lse = -Inf. What a mask or k_len hides has no effect, whatever
  * it holds (Inf, NaN); an admitted NaN gives NaN.
  * Scores, statistics and sums are fp32. The probabilities that multiply v are
- * rounded to F16 as 2^14 P relative to the row's running maximum (half a step:
- * 2^-11 of each; exact products with any v, and no loss down to P = 2^-28).
+ * rounded to F16 as 2^10 exp(S - m), m a running maximum of the row that a
+ * later score may pass by up to 5 log 2 (half a step: 2^-11 of each; normal
+ * numbers down to 2^-24 of the largest).
  * q, k, v: E4M3, E5M2 or F16, any mix of q with k and v, k and v any mix; out:
  * E4M3, E5M2 or F16. q and out: [rows of q][heads * head_dim], k and v: [rows of
  * k][kv_heads * head_dim]; trans = 0; data 16-byte aligned, every ld a multiple
@@ -536,7 +537,7 @@ size_t scalify_attention_bwd_workspace_size(int64_t rows_q, int64_t rows_k,
  *   AMAX: e_r = floor(log2 amax of its data) - target_log2 (0 for amax 0 / Inf / all
  *   NaN), NONE: e_r = 0; e_out = clamp(propagated + e_r, -127, 127).
  * amax_out: optional device fp32 [3], the statistics of dq, dk and dv.
- * Rows of k past k_len get zeros. P is rounded to F16 as above, dS to F16 times a
+ * Rows of k past k_len get zeros. P is rounded to F16 as 2^14 P, dS to F16 times a
  * power of two that a bound of its largest magnitude in the sequence and head,
  * 2 max |dO_i| max |v_j|, gives.
  * dout, q, k, v: E4M3, E5M2 or F16; out: F16 (delta needs more than 8-bit codes

@@ -46,11 +46,10 @@ struct AttnParams {
 
 constexpr int kAttnMaxD = 128;
 // Splits of a sequence's keys for the forward, 1 where the grid fills the
-// device without, and whether a workgroup's four waves share 32 query columns
-// (few queries) or hold 128.
+// device without, and a workgroup's query columns: 32 that its four waves share
+// (few queries), or 128.
 struct AttnPlan {
-  int splits;
-  bool narrow;
+  int splits, cols;
 };
 AttnPlan attention_plan(int64_t batch, int Hkv, int G, int64_t max_q, int64_t max_k);
 hipError_t launch_attention_fwd(const AttnParams& p, const AttnPlan& plan, hipStream_t s);

@@ -71,9 +71,13 @@ __device__ __forceinline__ int ds_exponent(float nd2, float nv2) {
 // Largest finite value of n floats, over the workgroup (256 threads).
 __device__ __forceinline__ float block_max(const float* x, int64_t n, float (&red)[4]) {
   float a = 0.0f;
-  for (int64_t i = threadIdx.x; i < n; i += 256) {
-    const float v = x[i];
-    if (v < 3.0e38f) a = fmaxf(a, v);
+  for (int64_t i = threadIdx.x; i < n; i += 256 * 8) {  // (eight loads in flight)
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = i + 256 * k < n ? x[i + 256 * k] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (v[k] < 3.0e38f) a = fmaxf(a, v[k]);
   }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) a = fmaxf(a, __shfl_xor(a, off, 64));
@@ -120,19 +124,60 @@ __device__ __forceinline__ void grad_exponents(const AttnParams& p, int (&e)[3])
   e[2] = eo;
 }
 
+// Values of dO that are not finite, in a tile that the mask cuts, added to dV pair by
+// pair (an admitted P is positive) for n queries from t on. Those of q need no more
+// than to be taken out: their scores, and so dS, are NaN where they are admitted.
+template <int DP, int DB>
+__device__ __forceinline__ void add_odd_queries(const uint8_t* dt, int n, int t, int first, int lq, int h, f16v (&acc)[DB]) {
+#pragma unroll 1
+  for (int j = 0; j < n; ++j) {
+    if (t + j < first || t + j >= lq) continue;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const u2 w = *(const u2*)(dt + tile_off<DP>(j, 4 * d + g) + 8 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[d][4 * g + i] += odd_part((w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
+      }
+  }
+}
+
+// 16 numbers of rows in a result's order, as a sum's start.
+__device__ __forceinline__ f16v row_start(const float* rows, int h) {
+  f16v r;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const float4 v = *(const float4*)(rows + 8 * g + 4 * h);
+    r[4 * g] = v.x;
+    r[4 * g + 1] = v.y;
+    r[4 * g + 2] = v.z;
+    r[4 * g + 3] = v.w;
+  }
+  return r;
+}
+
 // dK and dV of 128 keys, 32 a wave: scores and dP are formed with a key a lane
 // (rows: queries), which makes them the operands of the second products as they
-// stand. K and v rows stay in registers, tiles of 64 queries (q, dO) go through
-// two LDS buffers.
-template <int DP>
+// stand. K and v rows stay in registers; tiles of 64 queries (q, dO), two blocks of
+// 32, go through three LDS buffers. As in the forward, scores and dP of block b + 1
+// and the second products of block b - 1 are formed while P and dS of block b are,
+// in slices of four matrix instructions. The sums of a score and of dP start at
+// -(lse - 14) / factor and -delta of their row, which LDS holds, so that P = exp2(score
+// * factor) and dS = P dP need no row number in a register.
+// One wave a SIMD (its results, and the rows, take most of the 512 registers), so
+// what bounds it is the rate at which one wave issues, four clocks an instruction of
+// any kind: 32 products of 32 clocks leave 224 others.
+// Q16, O16: whether q and dO are F16 (and go straight into LDS) or have 8 bits.
+template <int DP, bool Q16, bool O16>
 __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tiles) {
-  constexpr int TQ = 64, KS = DP / 16, DB = DP / 32, BUF = TQ * DP * 2;
-  __shared__ __align__(16) uint8_t lds[4 * BUF];
-  __shared__ __align__(16) float row_l[2][TQ], row_d[2][TQ];
-  __shared__ int odd[2];
+  constexpr int TQ = 64, KS = DP / 16, DB = DP / 32, BUF = TQ * DP * 2, AHEAD = 2;
+  __shared__ __align__(16) uint8_t lds[6 * BUF];
+  __shared__ __align__(16) float row_l[3][TQ], row_d[3][TQ];
+  __shared__ int odd;
   __shared__ float red[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
-  const Place at = attn_place(p);
+  const Place at = attn_place(p, tiles);
   const int tile = (int)at.rest;  // (the first keys are seen by the most queries)
   const Seq sq = load_seq(p, at.b);
   const int kext = (int)min((int64_t)sq.kext, p.max_k);
@@ -149,136 +194,187 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
     kf[ks] = row_chunk(p.k_fmt, p.k, krow * p.ldk + (int64_t)at.hk * p.D, ks, h, p.D, have);
     vf[ks] = row_chunk(p.v_fmt, p.v, krow * p.ldv + (int64_t)at.hk * p.D, ks, h, p.D, have);
   }
-  // queries that see any of the keys, in whole tiles
+  // queries that see any of the keys, in whole tiles, head after head
   const int q_lo = p.causal ? max(0, j0 - behind) / TQ * TQ : 0;
   const int nt = j0 < sq.lk && q_lo < sq.lq ? (sq.lq - q_lo + TQ - 1) / TQ : 0;
-  const int steps = nt * p.G;
+  const int steps = nt * p.G, q_end = q_lo + nt * TQ;
+  // (a tile that every key of the workgroup sees whole has no masked pairs)
+  auto cut = [&](int t) { return t + TQ > sq.lq || j0 + 128 > sq.lk || (p.causal && t + behind < j0 + 127); };
 
-  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+  if (threadIdx.x == 0) odd = -1;
   float nd2 = 0.0f;
   for (int g = 0; g < p.G; ++g)
     nd2 = fmaxf(nd2, block_max(p.nd2 + (int64_t)(at.hk * p.G + g) * p.rows_q + sq.q0 + q_lo, max(0, sq.lq - q_lo), red));
   const float nv2 = block_max(p.nv2 + (int64_t)at.hk * p.rows_k + sq.k0 + j0, max(0, min(128, sq.lk - j0)), red);
   const int E = ds_exponent(nd2, nv2);
-  const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2);
+  const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2), inv_c1 = 1.0f / c1;
 
   f16v ak[DB], av[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) ak[d] = av[d] = f16v{};
-  TileLoader<TQ, DP, 256> lq, ld;
+  Tile<Q16, TQ, DP> lq;
+  Tile<O16, TQ, DP> ld;
+  lq.init(p.q, sq.q0 * p.ldq + (int64_t)at.hk * p.G * p.D, p.ldq, p.D, p.q_fmt);
+  ld.init(p.dout, sq.q0 * p.lddo + (int64_t)at.hk * p.G * p.D, p.lddo, p.D, p.do_fmt);
   float l_next = 0.0f, d_next = 0.0f;
-  auto fetch = [&](int step) {
-    const int g = step / nt, t = q_lo + (step - g * nt) * TQ, head = at.hk * p.G + g;
-    lq.init(p.q, sq.q0 * p.ldq + (int64_t)head * p.D, p.ldq, p.D, p.q_fmt);
-    ld.init(p.dout, sq.q0 * p.lddo + (int64_t)head * p.D, p.lddo, p.D, p.do_fmt);
-    lq.load(t, sq.lq);
-    ld.load(t, sq.lq);
-    if (threadIdx.x < TQ) {
-      // a row without keys, or past the end: exp2(score - Inf) = 0
-      const int i = t + (int)threadIdx.x;
-      const float l = i < sq.lq ? p.lse[(int64_t)head * p.rows_q + sq.q0 + i] : neg_inf();
-      l_next = l == neg_inf() ? __builtin_inff() : fmaf(l, kLog2e, -kProbLog2);
-      d_next = i < sq.lq ? p.delta[(int64_t)head * p.rows_q + sq.q0 + i] * c2 : 0.0f;
+  // The next tile to fetch: of head g from query t on; rows of zeros that see no key
+  // once the heads are done. Its row numbers: 16 rows a wave.
+  int g_next = 0, t_next = q_lo;
+  const int mine = 16 * wave + lane;
+  auto begin = [&](uint8_t* buf) {
+    const int t = g_next >= p.G ? sq.lq : t_next, g = min(g_next, p.G - 1);
+    lq.begin(t, sq.lq, buf, wave, (int64_t)g * p.D);
+    ld.begin(t, sq.lq, buf + BUF, wave, (int64_t)g * p.D);
+    l_next = neg_inf();
+    d_next = 0.0f;
+    if (lane < 16 && t + mine < sq.lq) {
+      const int64_t row = (int64_t)(at.hk * p.G + g) * p.rows_q + sq.q0 + t + mine;
+      l_next = p.lse[row];
+      d_next = p.delta[row];
+    }
+    t_next += TQ;
+    if (t_next >= q_end) {
+      t_next = q_lo;
+      ++g_next;
     }
   };
-  auto put = [&](int step) {
-    uint8_t* b = lds + (step & 1) * 2 * BUF;
-    lq.store(b);
-    ld.store(b + BUF);
-    if (threadIdx.x < TQ) {
-      row_l[step & 1][threadIdx.x] = l_next;
-      row_d[step & 1][threadIdx.x] = d_next;
-    }
-    const int t = q_lo + (step % nt) * TQ;
-    // (a tile that every key of the workgroup sees whole has no masked pairs)
-    if (t + TQ > sq.lq || j0 + 128 > sq.lk || (p.causal && t + behind < j0 + 127)) {
-      mark_not_finite(lq, &odd[step & 1], step);
-      mark_not_finite(ld, &odd[step & 1], step);
-    }
+  auto issue = [&](int i) {
+    if (i < KS / 2) lq.issue(i);
+    else ld.issue(i - KS / 2);
   };
-  if (steps > 0) {
-    fetch(0);
-    __syncthreads();  // (odd is cleared)
-    put(0);
-    if (steps > 1) fetch(1);
-  }
-  __syncthreads();
-#pragma unroll 1
-  for (int step = 0; step < steps; ++step) {
-    uint8_t* const qt = lds + (step & 1) * 2 * BUF;
-    uint8_t* const dt = qt + BUF;
-    const int t = q_lo + (step % nt) * TQ;
-    const bool is_odd = __builtin_amdgcn_readfirstlane(odd[step & 1]) == step;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int i0 = t + 32 * b;
-      if (!is_odd && !__any(i0 + 31 >= first)) continue;  // (no key of this wave is seen)
-      f16v s = {}, dp = {};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        s = mfma(row_operand<DP>(qt, 32 * b, ks, lane), kf[ks], s);
-        dp = mfma(row_operand<DP>(dt, 32 * b, ks, lane), vf[ks], dp);
-      }
-      float pr[16], ds[16];
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const float4 L = *(const float4*)&row_l[step & 1][32 * b + 8 * r4 + 4 * h];
-        const float4 Dl = *(const float4*)&row_d[step & 1][32 * b + 8 * r4 + 4 * h];
-        const float lv[4] = {L.x, L.y, L.z, L.w}, dv[4] = {Dl.x, Dl.y, Dl.z, Dl.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 4 * r4 + i;
-          pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c1, -lv[i]));
-          ds[r] = pr[r] * fmaf(dp[r], c2, -dv[i]);
-        }
-      }
-      if (__any(i0 < first) || i0 + 32 > sq.lq) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int i = i0 + result_row(r, h);
-          if (i < first || i >= sq.lq) pr[r] = ds[r] = 0.0f;
-        }
-      }
-      if (is_odd) {
-        // dO's values that are not finite: added pair by pair (an admitted P is
-        // positive). Those of q need no more than to be taken out: their scores, and
-        // so dS, are NaN where they are admitted.
-#pragma unroll 1
-        for (int j = 0; j < 32; ++j) {
-          if (i0 + j < first || i0 + j >= sq.lq) continue;
-#pragma unroll
-          for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const u2 w = *(const u2*)(dt + tile_off<DP>(32 * b + j, 4 * d + g) + 8 * h);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) av[d][4 * g + i] += odd_part((w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
-            }
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < 32 * DP / 8; i += 256) {
-          h8* a = (h8*)(qt + 32 * b * DP * 2) + i;
-          h8* c = (h8*)(dt + 32 * b * DP * 2) + i;
-          *a = finite_part(*a);
-          *c = finite_part(*c);
-        }
-        __syncthreads();
-      }
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const h8 pf = to_operand(pr, g), sf = to_operand(ds, g);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          av[d] = mfma(col_operand<DP>(dt, 32 * b + 16 * g, d, lane), pf, av[d]);
-          ak[d] = mfma(col_operand<DP>(qt, 32 * b + 16 * g, d, lane), sf, ak[d]);
-        }
-      }
-    }
-    if (step + 1 < steps) {
-      put(step + 1);
-      if (step + 2 < steps) fetch(step + 2);
+  auto arrive = [&](int n) {
+    lq.arrive(lds + n * 2 * BUF);
+    ld.arrive(lds + n * 2 * BUF + BUF);
+    if (lane < 16) {
+      // (here, not where they are fetched: their first use waits for the tile as well)
+      row_l[n][mine] = l_next == neg_inf() ? neg_inf() : -fmaf(l_next, kLog2e, -kProbLog2) * inv_c1;
+      row_d[n][mine] = -d_next;
     }
     __syncthreads();
+  };
+  // scores and dP of the last two blocks, P and dS of the last two
+  f16v sa = {}, da = {}, sb = {}, db = {};
+  h8 pa[2] = {}, ea[2] = {}, pb[2] = {}, eb[2] = {};
+  if (steps > 0) {
+    begin(lds);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) issue(i);
+    for (int i = threadIdx.x; i < 2 * TQ * DP / 8; i += 256) ((u4*)(lds + 4 * BUF))[i] = u4{0u, 0u, 0u, 0u};  // (the block before the first)
+    arrive(0);
+    sa = row_start(row_l[0], h);
+    da = row_start(row_d[0], h);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      sa = mfma(row_operand<DP>(lds, 0, ks, lane), kf[ks], sa);
+      da = mfma(row_operand<DP>(lds + BUF, 0, ks, lane), vf[ks], da);
+    }
+    begin(lds + 2 * BUF);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) issue(i);
+  }
+  settle_loads();
+
+  // One block of 32 queries from i0 on, with scores s and dP dp: its P and dS to pn
+  // and en; the next block's (rows at qn, on in LDS) scores and dP to sn and dn; the
+  // last block's P and dS times its dO and q (rows at ql, ol).
+  auto block = [&](int i0, f16v& s, f16v& dp, h8 (&pn)[2], h8 (&en)[2], f16v& sn, f16v& dn, const uint8_t* qn, const uint8_t* on,
+                   const float* ln, const float* rn, const h8 (&pl)[2], const h8 (&el)[2], const uint8_t* ql, const uint8_t* ol, auto&& also) {
+    if (__any(i0 < first) || i0 + 32 > sq.lq) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = i0 + result_row(r, h);
+        if (i < first || i >= sq.lq) {
+          s[r] = neg_inf();
+          dp[r] = 0.0f;
+        }
+      }
+    }
+    // Slices of four products: first the next block's scores and dP (two steps of
+    // their sums each), then the last block's dV and dK.
+    h8 fa[AHEAD + 1][2], fb[AHEAD + 1][2];
+    auto read = [&](int x) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        h8 &a = fa[x % (AHEAD + 1)][y], &b = fb[x % (AHEAD + 1)][y];
+        if (x < KS / 2) {
+          a = row_operand<DP>(qn, 0, 2 * x + y, lane);
+          b = row_operand<DP>(on, 0, 2 * x + y, lane);
+        } else {
+          const int z = 2 * (x - KS / 2) + y;
+          a = col_operand<DP>(ol, 16 * (z / DB), z % DB, lane);
+          b = col_operand<DP>(ql, 16 * (z / DB), z % DB, lane);
+        }
+      }
+    };
+    sn = row_start(ln, h);
+    dn = row_start(rn, h);
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) read(x);
+    slice_end();
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      if (i + AHEAD < KS) read(i + AHEAD);
+      also(i);
+      const int a = i % (AHEAD + 1);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        if (i < KS / 2) {
+          sn = mfma(fa[a][y], kf[2 * i + y], sn);
+          dn = mfma(fb[a][y], vf[2 * i + y], dn);
+        } else {
+          const int z = 2 * (i - KS / 2) + y;
+          av[z % DB] = mfma(fa[a][y], pl[z / DB], av[z % DB]);
+          ak[z % DB] = mfma(fb[a][y], el[z / DB], ak[z % DB]);
+        }
+      }
+#pragma unroll
+      for (int e = 16 / KS * i; e < 16 / KS * (i + 1); ++e) {
+        float x = __builtin_amdgcn_exp2f(s[e] * c1), y = x * (dp[e] * c2);
+        held(x);
+        held(y);
+        pn[e >> 3][e & 7] = (_Float16)x;
+        en[e >> 3][e & 7] = (_Float16)y;
+      }
+      slice_end();
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      held(pn[g]);
+      held(en[g]);
+    }
+  };
+  int n = 0;  // the buffer of this step
+#pragma unroll 1
+  for (int step = 0, t = q_lo; step < steps; ++step, t = t + TQ < q_end ? t + TQ : q_lo) {
+    const int n1 = n == 2 ? 0 : n + 1, n2 = n == 0 ? 2 : n - 1;
+    uint8_t* const cur = lds + n * 2 * BUF;
+    uint8_t* const nxt = lds + n1 * 2 * BUF;
+    uint8_t* const prv = lds + n2 * 2 * BUF;
+    block(t, sa, da, pa, ea, sb, db, cur + BUF / 2, cur + BUF + BUF / 2, row_l[n] + 32, row_d[n] + 32, pb, eb, prv + BUF / 2,
+          prv + BUF + BUF / 2, [](int) {});
+    arrive(n1);
+    if (cut(t)) {
+      mark_not_finite<2 * TQ, DP>(cur, &odd, step);
+      __syncthreads();
+      if (__builtin_amdgcn_readfirstlane(odd) == step) {
+        add_odd_queries<DP>(cur + BUF, TQ, t, first, sq.lq, h, av);
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * TQ * DP / 8; i += 256) ((h8*)cur)[i] = finite_part(((const h8*)cur)[i]);
+        __syncthreads();
+      }
+    }
+    begin(prv);
+    block(t + 32, sb, db, pb, eb, sa, da, nxt, nxt + BUF, row_l[n1], row_d[n1], pa, ea, cur, cur + BUF, issue);
+    n = n1;
+  }
+  if (steps > 0) {  // the last block's products
+    const uint8_t* const ql = lds + (n == 0 ? 2 : n - 1) * 2 * BUF + BUF / 2;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      av[i % DB] = mfma(col_operand<DP>(ql + BUF, 16 * (i / DB), i % DB, lane), pb[i / DB], av[i % DB]);
+      ak[i % DB] = mfma(col_operand<DP>(ql, 16 * (i / DB), i % DB, lane), eb[i / DB], ak[i % DB]);
+    }
+    wait_loads();  // (none may reach LDS after the workgroup has ended)
   }
   int e[3];
   grad_exponents(p, e);
@@ -307,7 +403,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles
   __shared__ int odd;
   __shared__ float red[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
-  const Place at = attn_place(p);
+  const Place at = attn_place(p, tiles);
   const int tile = tiles - 1 - (int)at.rest;
   const Seq sq = load_seq(p, at.b);
   const int64_t ncols = (int64_t)sq.lq * p.G, col0 = (int64_t)tile * 128;
@@ -349,22 +445,22 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles
   for (int d = 0; d < DB; ++d) acc[d] = f16v{};
   uint8_t* const kt = lds;
   uint8_t* const vt = lds + BUF;
-  TileLoader<TK, DP, 256> lk, lv;
+  StagedTile<TK, DP, 256> lk, lv;
   lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
   lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
   if (end > 0) {
-    lk.load(0, end);
-    lv.load(0, end);
+    lk.fetch(0, end, nullptr, 0);
+    lv.fetch(0, end, nullptr, 0);
   }
 #pragma unroll 1
   for (int t = 0; t < end; t += TK) {
-    lk.store(kt);
-    lv.store(vt);
+    lk.arrive(kt);
+    lv.arrive(vt);
     if (t + TK - 1 > last0) mark_not_finite(lk, &odd, t);
     __syncthreads();
     if (t + TK < end) {
-      lk.load(t + TK, end);
-      lv.load(t + TK, end);
+      lk.fetch(t + TK, end, nullptr, 0);
+      lv.fetch(t + TK, end, nullptr, 0);
     }
     const bool is_odd = __builtin_amdgcn_readfirstlane(odd) == t;
 #pragma unroll
@@ -466,11 +562,20 @@ __global__ __launch_bounds__(256) void attn_grads_kernel(AttnParams p, int64_t t
 }
 
 template <int DP>
+static void launch_dkv(const AttnParams& p, dim3 g, int tiles, hipStream_t s) {
+  const bool q16 = p.q_fmt == kF16, o16 = p.do_fmt == kF16;
+  if (q16 && o16) hipLaunchKernelGGL((attn_dkv_kernel<DP, true, true>), g, dim3(256), 0, s, p, tiles);
+  else if (q16) hipLaunchKernelGGL((attn_dkv_kernel<DP, true, false>), g, dim3(256), 0, s, p, tiles);
+  else if (o16) hipLaunchKernelGGL((attn_dkv_kernel<DP, false, true>), g, dim3(256), 0, s, p, tiles);
+  else hipLaunchKernelGGL((attn_dkv_kernel<DP, false, false>), g, dim3(256), 0, s, p, tiles);
+}
+
+template <int DP>
 static void launch(const AttnParams& p, hipStream_t s) {
   const int64_t heads = p.batch * p.Hkv;
   const int kt = (int)((p.max_k + 127) / 128), qt = (int)((p.max_q * p.G + 127) / 128);
   if (p.rows_k > 0 && kt > 0)
-    hipLaunchKernelGGL((attn_dkv_kernel<DP>), dim3((unsigned)(heads * kt)), dim3(256), 0, s, p, kt);
+    launch_dkv<DP>(p, dim3((unsigned)(heads * kt)), kt, s);
   if (p.rows_q > 0 && qt > 0)
     hipLaunchKernelGGL((attn_dq_kernel<DP>), dim3((unsigned)(heads * qt)), dim3(256), 0, s, p, qt);
 }

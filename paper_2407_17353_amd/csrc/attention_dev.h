@@ -114,13 +114,14 @@ __device__ __forceinline__ u4 load_f16x8(int fmt, const void* base, int64_t e) {
   return to_f16x8(fmt, u4{v[0], v[1], 0u, 0u});
 }
 
-// Rows of a matrix on their way into an LDS tile of ROWS x DP: loaded ahead
-// into registers, eight columns a chunk. The buffer's range check makes rows
-// past the end, and the columns past D, read as zeros.
-template <int ROWS, int DP, int THREADS>
-struct TileLoader {
+// 8-bit or (the format decides) any rows of a matrix on their way into an LDS tile of
+// ROWS x DP: fetched into registers, eight columns a chunk, and decoded and stored by
+// arrive(). The buffer's range check makes rows past the end, and the columns past
+// D, read as zeros.
+template <int ROWS, int DP, int THREADS, bool EIGHT = false>
+struct StagedTile {
   static constexpr int CH = DP / 8, N = ROWS * CH / THREADS;
-  u4 r[N];
+  typename std::conditional<EIGHT, u2, u4>::type r[N];
   int voff0, step;  // chunk i of a thread: voff0 + i step
   const uint8_t* base;
   int64_t pitch;
@@ -128,7 +129,7 @@ struct TileLoader {
 
   // first: element of row 0 (of the sequence) and column 0 (of the head)
   __device__ __forceinline__ void init(const void* data, int64_t first, int64_t ld, int D, int format) {
-    const int es = fmt_bytes(format);
+    const int es = EIGHT ? 1 : fmt_bytes(format);
     fmt = format;
     base = (const uint8_t*)data + first * es;
     pitch = ld * es;
@@ -138,12 +139,16 @@ struct TileLoader {
     // (past the end of any buffer: a tile's rows span less than 2^31 bytes)
     voff0 = ch * 8 < D ? row * (int)pitch + ch * 8 * es : (int)0x80000000;
   }
-  // rows row0 .. row0 + ROWS - 1, those from `end` on zero
-  __device__ __forceinline__ void load(int64_t row0, int64_t end) {
+  // rows row0 .. row0 + ROWS - 1 (of a matrix `skip` elements on), those from `end` on zero
+  __device__ __forceinline__ void fetch(int64_t row0, int64_t end, uint8_t*, int, int64_t skip = 0) {
     const int64_t n = end - row0 < ROWS ? end - row0 : ROWS;
     const uint32_t bytes = n > 0 ? (uint32_t)((n - 1) * pitch) + (uint32_t)bytes_d : 0u;
-    const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(base + row0 * pitch), 0, (int)bytes, 0x00027000);
-    if (fmt == kF16) {
+    const uint8_t* at = base + row0 * pitch + skip * (EIGHT ? 1 : fmt_bytes(fmt));
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, (int)bytes, 0x00027000);
+    if constexpr (EIGHT) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b64(rs, voff0 + i * step, 0, 0);
+    } else if (fmt == kF16) {
 #pragma unroll
       for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, voff0 + i * step, 0, 0);
     } else {
@@ -154,14 +159,96 @@ struct TileLoader {
       }
     }
   }
-  __device__ __forceinline__ void store(uint8_t* lds) const {
+  __device__ __forceinline__ void begin(int64_t row0, int64_t end, uint8_t* lds, int wave, int64_t skip = 0) {
+    fetch(row0, end, lds, wave, skip);
+  }
+  __device__ __forceinline__ void issue(int) const {}
+  __device__ __forceinline__ void arrive(uint8_t* lds) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = (int)threadIdx.x + i * THREADS;
-      *(u4*)(lds + tile_off<DP>(c / CH, c % CH)) = to_f16x8(fmt, r[i]);
+      *(u4*)(lds + tile_off<DP>(c / CH, c % CH)) = value(i);
     }
   }
+  // chunk i as F16
+  __device__ __forceinline__ u4 value(int i) const {
+    if constexpr (EIGHT) return fmt == kE4M3 ? to_f16x8(kE4M3, u4{r[i][0], r[i][1], 0u, 0u}) : to_f16x8(kE5M2, u4{r[i][0], r[i][1], 0u, 0u});
+    else return to_f16x8(fmt, r[i]);
+  }
 };
+
+// One buffer_load_dwordx4 ... lds: lane i's 16 bytes land at M0 + 16 i. (M0 has no
+// other user in these kernels; a scalar write of it and a buffer load need a wait
+// state between them.)
+typedef int v4i __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void load_to_lds16(v4i rsrc, uint32_t voff, const uint8_t* lds) {
+  const uint32_t at = (uint32_t)(uintptr_t)(ATTN_LDS const void*)lds;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+      "buffer_load_dwordx4 %1, %2, 0 offen lds"
+      :
+      : "s"(at), "v"(voff), "s"(rsrc)
+      : "memory", "m0");
+#pragma clang diagnostic pop
+}
+// A value that is there at this point (the compiler would else form what a branch
+// may replace only behind the branch, away from the products that it hides under).
+template <typename T>
+__device__ __forceinline__ void held(T& x) { asm volatile("" : "+v"(x)); }
+// Nothing is scheduled across.
+__device__ __forceinline__ void slice_end() { __builtin_amdgcn_sched_barrier(0); }
+// All loads so far are done, also for the compiler's own count of them (else it
+// waits for these inside the loop that uses them, and with them for that loop's).
+__device__ __forceinline__ void settle_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// F16 rows of a matrix loaded straight into an LDS tile of ROWS x DP: no
+// registers, and the chunks' permutation is applied to the address they are read
+// from. A wave's load fills 1 KiB, the workgroup's four 4 KiB.
+template <int ROWS, int DP>
+struct DirectTile {
+  static constexpr int CH = DP / 8, N = ROWS * CH / 256;
+  uint32_t voff0, step;
+  const uint8_t* base;
+  int64_t pitch;
+  int bytes_d;
+  v4i rs;       // of the tile under way
+  uint8_t* to;
+
+  __device__ __forceinline__ void init(const void* data, int64_t first, int64_t ld, int D, int) {
+    base = (const uint8_t*)data + first * 2;
+    pitch = ld * 2;
+    bytes_d = D * 2;
+    const int row = (int)threadIdx.x / CH, slot = (int)threadIdx.x % CH;
+    const int ch = (tile_off<DP>(row, slot) - row * DP * 2) >> 4;
+    step = 256 / CH * (uint32_t)pitch;
+    voff0 = ch * 8 < D ? (uint32_t)row * (uint32_t)pitch + ch * 16 : 0x80000000u;
+  }
+  // rows row0 ... (of a matrix `skip` elements on) into the tile at lds, those from
+  // `end` on zero: begin(), then issue(0) ... issue(N - 1). (A burst of them stops the
+  // wave for 700 clocks until the memory pipe has taken it; one in each slice of a
+  // block of products is hidden.)
+  __device__ __forceinline__ void begin(int64_t row0, int64_t end, uint8_t* lds, int wave, int64_t skip = 0) {
+    const int64_t n = end - row0 < ROWS ? end - row0 : ROWS;
+    const uint32_t bytes = n > 0 ? (uint32_t)((n - 1) * pitch) + (uint32_t)bytes_d : 0u;
+    const uint64_t at = (uint64_t)(uintptr_t)(base + row0 * pitch + 2 * skip);
+    rs = v4i{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)bytes, 0x00027000};
+    to = lds + wave * 1024;
+  }
+  __device__ __forceinline__ void issue(int i) const { load_to_lds16(rs, voff0 + i * step, to + i * 4096); }
+  __device__ __forceinline__ void fetch(int64_t row0, int64_t end, uint8_t* lds, int wave, int64_t skip = 0) {
+    begin(row0, end, lds, wave, skip);
+#pragma unroll
+    for (int i = 0; i < N; ++i) issue(i);
+  }
+  __device__ __forceinline__ void arrive(uint8_t*) const { wait_loads(); }
+};
+// A tile whose matrix is F16, or has 8 bits.
+template <bool F16, int ROWS, int DP>
+using Tile = typename std::conditional<F16, DirectTile<ROWS, DP>, StagedTile<ROWS, DP, 256, true>>::type;
 
 // Operand with one row of the tile a lane (rows row0 + (lane & 31)), k = columns
 // 16 ks + 8 h ...
@@ -199,7 +286,8 @@ __device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) {
 }
 
 // Registers 8 g ... 8 g + 7 of a result as an operand (round to nearest even).
-__device__ __forceinline__ h8 to_operand(const float (&x)[16], int g) {
+template <typename Values>
+__device__ __forceinline__ h8 to_operand(const Values& x, int g) {
   h8 r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = (_Float16)x[8 * g + i];
@@ -243,11 +331,19 @@ __device__ __forceinline__ h8 finite_part(h8 v) {
 // tile of those that holds an infinity or NaN is marked while it is stored
 // (`flag`: the tile's number, so it needs no clearing); its finite part is then
 // multiplied as usual, and the rest added pair by pair.
-template <int ROWS, int DP, int THREADS>
-__device__ __forceinline__ void mark_not_finite(const TileLoader<ROWS, DP, THREADS>& t, int* flag, int number) {
+template <int ROWS, int DP, int THREADS, bool EIGHT>
+__device__ __forceinline__ void mark_not_finite(const StagedTile<ROWS, DP, THREADS, EIGHT>& t, int* flag, int number) {
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < t.N; ++i) bad |= not_finite(__builtin_bit_cast(h8, to_f16x8(t.fmt, t.r[i])));
+  for (int i = 0; i < t.N; ++i) bad |= not_finite(__builtin_bit_cast(h8, t.value(i)));
+  if (bad) *flag = number;
+}
+
+// The same for a tile in LDS (256 threads, whose barrier the caller owes).
+template <int ROWS, int DP>
+__device__ __forceinline__ void mark_not_finite(const uint8_t* tile, int* flag, int number) {
+  bool bad = false;
+  for (int i = threadIdx.x; i < ROWS * DP / 8; i += 256) bad |= not_finite(((const h8*)tile)[i]);
   if (bad) *flag = number;
 }
 
@@ -287,21 +383,32 @@ __device__ __forceinline__ float score_factor(const AttnParams& p) {
   return __builtin_ldexpf(p.alpha * kLog2e, pow2_exponent(p.s_q) + pow2_exponent(p.s_k));
 }
 
-// Position in the grid: (sequence, key head) runs fastest, so that a head's
-// workgroups meet on one XCD (workgroups go to the eight XCDs in turn) where
-// batch * key heads is a multiple of 8, and its keys stay in that XCD's L2.
+// Position in the grid of `per_head` workgroups for each (sequence, key head). A
+// head's workgroups read the same rows (keys, or the queries of the backward) while
+// they run side by side, so they go to one XCD, whose L2 then serves them:
+// workgroups are dealt to the eight XCDs in turn, and where the heads are a
+// multiple of 8, XCD x takes heads x, x + 8, ... one after the other. (With heads
+// dealt out first, the rows of 16 heads at once missed L2: attention of 4 x 4096
+// tokens, 32 heads of 128, took PLACE_BEFORE.) Else the head runs fastest.
 struct Place {
   int64_t b;
   int hk;
   int64_t rest;
 };
-__device__ __forceinline__ Place attn_place(const AttnParams& p) {
+__device__ __forceinline__ Place attn_place(const AttnParams& p, int64_t per_head) {
   const int64_t heads = p.batch * p.Hkv, id = blockIdx.x;
+  int64_t bh;
   Place w;
-  const int64_t bh = id % heads;
-  w.rest = id / heads;
+  if ((heads & 7) == 0) {
+    const int64_t s = id >> 3, group = s / per_head;
+    w.rest = s - group * per_head;
+    bh = 8 * group + (id & 7);
+  } else {
+    w.rest = id / heads;
+    bh = id - w.rest * heads;
+  }
   w.b = bh / p.Hkv;
-  w.hk = (int)(bh % p.Hkv);
+  w.hk = (int)(bh - w.b * p.Hkv);
   return w;
 }
 

@@ -18,44 +18,156 @@
 
 namespace scalify {
 
-template <int DP, bool NARROW>
+// The forward keeps 2^10 p relative to the running maximum, which a score may pass
+// by kSlack before it is moved (moving it multiplies every result, and with 32
+// queries a wave some query would move it in most tiles): at most 2^15, and
+// normal F16 numbers down to p = 2^-24.
+constexpr float kRunLog2 = 10.0f, kSlack = 5.0f;
+
+// A query a lane: where it is, and what it sees.
+struct Query {
+  int64_t row;
+  int head, last;  // the last key it sees; a lane without a query sees every key (its result goes nowhere)
+  bool live;
+};
+__device__ __forceinline__ Query query_at(const AttnParams& p, const Seq& sq, int hk, int64_t col, int64_t ncols) {
+  Query q;
+  q.live = col < ncols;
+  const int pos = (int)(col / p.G);
+  q.head = hk * p.G + (int)(col - (int64_t)pos * p.G);
+  q.row = sq.q0 + pos;
+  q.last = !q.live ? 0x7FFFFFFF : (p.causal ? min(pos + sq.lk - sq.lq, sq.lk - 1) : sq.lk - 1);
+  return q;
+}
+
+// The keys of a workgroup: those that its last column sees, a split's share of
+// them in whole tiles.
+__device__ __forceinline__ void key_range(const AttnParams& p, const Seq& sq, int64_t last_col, int split, int tile, int& begin,
+                                          int& end) {
+  const int seen = p.causal ? max(0, min(sq.lk, (int)(last_col / p.G) + sq.lk - sq.lq + 1)) : sq.lk;
+  const int share = ((seen + p.splits - 1) / p.splits + tile - 1) / tile * tile;
+  begin = (int)min((int64_t)split * share, (int64_t)seen);
+  end = min(seen, begin + share);
+}
+
+// Block d (32 columns) of a query's result: of every four registers the columns
+// are consecutive.
+__device__ __forceinline__ void store_result(const AttnParams& p, const f16v& o, const Query& q, int d, int h, float l, int split) {
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int n = 32 * d + 8 * g + 4 * h;
+    if (n >= p.D) continue;
+    if (p.splits > 1) {
+      *(float4*)(p.part_o + ((split * p.rows_q + q.row) * p.H + q.head) * (int64_t)p.D + n) =
+          make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+    } else {
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = l == 0.0f ? 0.0f : o[4 * g + i] * inv;
+      store4_any(p.out_fmt, p.out, q.row * p.ldo + (int64_t)q.head * p.D + n, y, 0, p.sat != 0);
+    }
+  }
+}
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.0f ? neg_inf() : (m - kRunLog2 + __builtin_amdgcn_logf(l)) * kLn2;
+}
+__device__ __forceinline__ void store_row(const AttnParams& p, const Query& q, float m, float l, int split) {
+  if (p.splits > 1) p.part_ml[(split * p.rows_q + q.row) * p.H + q.head] = make_float2(m, l);
+  else if (p.lse) p.lse[(int64_t)q.head * p.rows_q + q.row] = log_sum(m, l);
+}
+
+// Scores (key0 + row, query) that the mask does not admit.
+__device__ __forceinline__ void mask_scores(f16v& s, int key0, int h, int last) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (key0 + result_row(r, h) > last) s[r] = neg_inf();
+}
+
+// The running maximum, in powers of two, with scores up to `top` (of this lane's
+// half, before their factor), and what the sum and the results have to be
+// multiplied with. The maximum is moved only when a score is past it by more than
+// kSlack: probabilities relative to it may then reach 2^kSlack, which F16 holds.
+template <int DB>
+__device__ __forceinline__ void run_max(float top, float c1, int h, float& m, float& l, f16v (&acc)[DB]) {
+  top = fmaxf(top, other_half(top, h)) * c1;
+  if (__any(top > m + kSlack)) {
+    const float now = fmaxf(m, top);
+    const float f = m == neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(m - now);  // (so far nothing but infinities may have been added)
+    m = now;
+    l *= f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] *= f;
+  }
+}
+__device__ __forceinline__ float block_top(const f16v& s) {
+  float top = s[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);  // (fmaxf skips NaN)
+  return top;
+}
+
+// Values of v that are not finite, in a tile that the mask cuts, are added pair by
+// pair (an admitted probability is positive, so its product with an infinity is
+// that infinity) and then taken out of the tile. n rows from row0 on, keys key0 ...
+template <int DP, int DB>
+__device__ __forceinline__ void add_odd(const uint8_t* vt, int row0, int n, int key0, int last, int h, f16v (&acc)[DB]) {
+#pragma unroll 1
+  for (int j = 0; j < n; ++j) {
+    if (key0 + j > last) continue;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const u2 w = *(const u2*)(vt + tile_off<DP>(row0 + j, 4 * d + g) + 8 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[d][4 * g + i] += odd_part((w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
+      }
+  }
+}
+template <int TK, int DP>
+__device__ __forceinline__ void remove_odd(uint8_t* vt) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < TK * DP / 8; i += 256) ((h8*)vt)[i] = finite_part(((const h8*)vt)[i]);
+  __syncthreads();
+}
+
+// Many queries: 128 columns, 32 a wave; tiles of 64 keys, two blocks of 32, that the
+// waves share. While the exponentials of key block b are taken, the scores of block
+// b + 1 are formed and the probabilities of block b - 1 multiplied with v: a block's
+// work is laid out in slices of two matrix instructions with the vector ones that
+// fit under them, operands read AHEAD slices before. (A SIMD does not run one wave's
+// exponentials under another's products by itself: in a probe the two took the sum
+// of their times, 692 ns for 245 and 466, while 16 products with an exponential and
+// three multiply-adds each, in one wave, took the products' 237.) k and v have two
+// LDS buffers each, with one barrier a tile, in its middle: the first block is the
+// last to use the older buffers.
+// K16, V16: whether k and v are F16 (and go straight into LDS) or have 8 bits.
+template <int DP, bool K16, bool V16>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tiles) {
-  constexpr int TK = NARROW ? 128 : 64, NB = NARROW ? 1 : 2, KS = DP / 16, DB = DP / 32;
-  constexpr int COLS = NARROW ? 32 : 128;
-  __shared__ __align__(16) uint8_t lds[2 * TK * DP * 2];
+  constexpr int TK = 64, KS = DP / 16, DB = DP / 32, BUF = TK * DP * 2;
+  constexpr int AHEAD = K16 && V16 ? 2 : 1;  // (the registers of staged tiles leave room for one)
+  __shared__ __align__(16) uint8_t lds[4 * BUF];
   __shared__ int odd;
-  uint8_t* const kt = lds;
-  uint8_t* const vt = lds + TK * DP * 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
-  const Place at = attn_place(p);
+  const Place at = attn_place(p, (int64_t)tiles * p.splits);
   const int split = (int)(at.rest % p.splits);
   // (the last columns see the most keys where the mask is causal: they go first)
   const int tile = tiles - 1 - (int)(at.rest / p.splits);
   const Seq sq = load_seq(p, at.b);
-  const int64_t ncols = (int64_t)sq.lq * p.G;
-  const int64_t col0 = (int64_t)tile * COLS;
+  const int64_t ncols = (int64_t)sq.lq * p.G, col0 = (int64_t)tile * 128;
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
   if (col0 >= ncols) return;
-
-  // This lane's query.
-  const int64_t col = col0 + (NARROW ? 0 : 32 * wave) + (lane & 31);
-  const bool live = col < ncols;
-  const int pos = (int)(col / p.G), head = at.hk * p.G + (int)(col - (int64_t)pos * p.G);
-  const int64_t qrow = sq.q0 + pos;
-  const int behind = sq.lk - sq.lq;  // causal: query i sees keys up to i + behind
-  // (a lane without a query sees every key: its result goes nowhere)
-  const int last = !live ? 0x7FFFFFFF : (p.causal ? min(pos + behind, sq.lk - 1) : sq.lk - 1);
-  const int last0 = p.causal ? min((int)(col0 / p.G) + behind, sq.lk - 1) : sq.lk - 1;  // of the first column
+  const int last0 = p.causal ? min((int)(col0 / p.G) + sq.lk - sq.lq, sq.lk - 1) : sq.lk - 1;  // of the first column
+  const Query q = query_at(p, sq, at.hk, col0 + 32 * wave + (lane & 31), ncols);
   h8 qf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks)
-    qf[ks] = row_chunk(p.q_fmt, p.q, qrow * p.ldq + (int64_t)head * p.D, ks, h, p.D, live);
-  // Keys of this workgroup: those that its last column sees, this split's share
-  // in whole tiles.
-  const int64_t last_col = col0 + COLS < ncols ? col0 + COLS - 1 : ncols - 1;
-  const int seen = p.causal ? max(0, min(sq.lk, (int)(last_col / p.G) + behind + 1)) : sq.lk;
-  const int share = ((seen + p.splits - 1) / p.splits + TK - 1) / TK * TK;
-  const int begin = (int)min((int64_t)split * share, (int64_t)seen), end = min(seen, begin + share);
+    qf[ks] = row_chunk(p.q_fmt, p.q, q.row * p.ldq + (int64_t)q.head * p.D, ks, h, p.D, q.live);
+  int begin, end;
+  key_range(p, sq, min(col0 + 127, ncols - 1), split, TK, begin, end);
 
   const float c1 = score_factor(p);
   float m = neg_inf(), l = 0.0f;
@@ -63,180 +175,247 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = f16v{};
 
-  TileLoader<TK, DP, 256> lk, lv;
+  uint8_t* const kb = lds;
+  uint8_t* const vb = lds + 2 * BUF;
+  Tile<K16, TK, DP> lk;
+  Tile<V16, TK, DP> lv;
   lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
   lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
+  auto arrive = [&](uint8_t* kt, uint8_t* vt) {
+    lk.arrive(kt);
+    lv.arrive(vt);
+    __syncthreads();
+  };
+  if (threadIdx.x == 0) odd = -1;
+  f16v sa = {}, sb = {};
+  h8 pa[2] = {}, pb[2] = {};  // probabilities of the last even and odd block
+  if (begin < end) {
+    lk.fetch(begin, end, kb, wave);
+    lv.fetch(end, end, vb + BUF, wave);  // (the block before the first: v of zeros)
+    arrive(kb, vb + BUF);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) sa = mfma(row_operand<DP>(kb, 0, ks, lane), qf[ks], sa);
+    lk.fetch(begin + TK, end, kb + BUF, wave);
+    lv.fetch(begin, end, vb, wave);
+  }
+  settle_loads();
 
-  auto compute = [&](int key0) {
-    float s[NB][16];
+  // One block: its keys key0 ... with scores s, whose probabilities go to pn; the
+  // next block's scores (rows kn of k) to sn, and the last block's probabilities pl
+  // times its v (rows vl).
+  auto block = [&](int key0, f16v& s, h8 (&pn)[2], f16v& sn, const uint8_t* kn, const h8 (&pl)[2], const uint8_t* vl, auto&& also) {
+    if (key0 + 31 > last0) mask_scores(s, key0, h, q.last);
+    const float off = kRunLog2 - (m == neg_inf() ? 0.0f : m);
+    float lb = 0.0f, top = s[0];
+    h8 kf[AHEAD + 1], vf[AHEAD + 1];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      f16v c = {};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        c = mfma(row_operand<DP>(kt, NARROW ? 32 * wave : 32 * b, ks, lane), qf[ks], c);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[b][r] = c[r];
+    for (int i = 0; i < AHEAD; ++i) {
+      kf[i] = row_operand<DP>(kn, 0, i, lane);
+      vf[i] = col_operand<DP>(vl, 16 * (i / DB), i % DB, lane);
     }
-    if (__any(key0 + 32 * NB - 1 > last)) {
+    f16v sc = {};
+    slice_end();
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+    for (int i = 0; i < KS; ++i) {
+      if (i + AHEAD < KS) {
+        const int x = i + AHEAD;
+        kf[x % (AHEAD + 1)] = row_operand<DP>(kn, 0, x, lane);
+        vf[x % (AHEAD + 1)] = col_operand<DP>(vl, 16 * (x / DB), x % DB, lane);
+      }
+      also(i);
+      sc = mfma(kf[i % (AHEAD + 1)], qf[i], sc);
+      acc[i % DB] = mfma(vf[i % (AHEAD + 1)], pl[i / DB], acc[i % DB]);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key0 + 32 * b + result_row(r, h) > last) s[b][r] = neg_inf();
+      for (int e = 16 / KS * i; e < 16 / KS * (i + 1); ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[e], c1, off));
+        top = fmaxf(top, s[e]);  // (fmaxf skips NaN)
+        lb += x;
+        pn[e >> 3][e & 7] = (_Float16)x;
+      }
+      held(lb);
+      slice_end();
     }
-    float top = s[0][0];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);  // (fmaxf skips NaN)
+    // The running maximum is moved only when a score is past it by more than
+    // kSlack: with what had been added relative to the old one the block's
+    // probabilities are then taken again.
+    held(pn[0]);
+    held(pn[1]);
+    sn = sc;
     top = fmaxf(top, other_half(top, h)) * c1;
-    if (__any(top > m)) {
+    if (__any(top > m + kSlack)) {
       const float now = fmaxf(m, top);
-      const float f = now == neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+      const float f = m == neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(m - now);  // (so far nothing but infinities may have been added)
       m = now;
       l *= f;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[d][r] *= f;
-    }
-    const float off = kProbLog2 - (m == neg_inf() ? 0.0f : m);
+      const float o = kRunLog2 - (m == neg_inf() ? 0.0f : m);
+      lb = 0.0f;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c1, off));
-        l += s[b][r];
-      }
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const h8 pf = to_operand(s[b], g);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const h8 vf = col_operand<DP>(vt, (NARROW ? 32 * wave : 32 * b) + 16 * g, d, lane);
-          acc[d] = mfma(vf, pf, acc[d]);
-        }
+      for (int e = 0; e < 16; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[e], c1, o));
+        lb += x;
+        pn[e >> 3][e & 7] = (_Float16)x;
       }
     }
+    l += lb;
   };
-  // Values that are not finite, in a tile that the mask cuts: added pair by pair
-  // (an admitted probability is positive, so its product with an infinity is that
-  // infinity), and taken out of the tile.
-  auto odd_values = [&](int key0) {
+  int n = 0;  // the buffers of tile t
 #pragma unroll 1
-    for (int j = 0; j < 32 * NB; ++j) {
-      if (key0 + j > last) continue;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const u2 w = *(const u2*)(vt + tile_off<DP>((NARROW ? 32 * wave : 0) + j, 4 * d + g) + 8 * h);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[d][4 * g + i] += odd_part((w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
-        }
+  for (int t = begin; t < end; t += TK, n ^= 1) {
+    uint8_t* const kt = kb + n * BUF;
+    uint8_t* const ko = kb + (n ^ 1) * BUF;
+    uint8_t* const vt = vb + n * BUF;
+    uint8_t* const vo = vb + (n ^ 1) * BUF;
+    block(t, sa, pa, sb, kt + BUF / 2, pb, vo + BUF / 2, [](int) {});
+    arrive(ko, vt);
+    if (t + TK - 1 > last0) {  // some pair of the workgroup is masked
+      mark_not_finite<TK, DP>(vt, &odd, t);
+      __syncthreads();
+      if (__builtin_amdgcn_readfirstlane(odd) == t) {
+        add_odd<DP>(vt, 0, TK, t, q.last, h, acc);
+        remove_odd<TK, DP>(vt);
+      }
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < TK * DP / 8; i += 256)
-      ((h8*)vt)[i] = finite_part(((const h8*)vt)[i]);
-    __syncthreads();
-  };
+    lk.begin(t + 2 * TK, end, kt, wave);
+    lv.begin(t + TK, end, vo, wave);
+    block(t + 32, sb, pb, sa, ko, pa, vt, [&](int i) {
+      if (i < KS / 2) lk.issue(i);
+      else lv.issue(i - KS / 2);
+    });
+  }
+  if (begin < end) {  // the last block's product
+    const uint8_t* const vl = vb + (n ^ 1) * BUF + BUF / 2;
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+      acc[i % DB] = mfma(col_operand<DP>(vl, 16 * (i / DB), i % DB, lane), pb[i / DB], acc[i % DB]);
+    wait_loads();  // (none may reach LDS after the workgroup has ended)
+  }
+  l += other_half(l, h);
+  if (q.live) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) store_result(p, acc[d], q, d, h, l, split);
+    if (h == 0) store_row(p, q, m, l, split);
+  }
+}
 
+// Few queries: 32 columns, and the waves take a quarter each of a tile of 128 keys.
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnParams p, int tiles) {
+  constexpr int TK = 128, KS = DP / 16, DB = DP / 32;
+  __shared__ __align__(16) uint8_t lds[2 * TK * DP * 2];
+  __shared__ int odd;
+  uint8_t* const kt = lds;
+  uint8_t* const vt = lds + TK * DP * 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const Place at = attn_place(p, (int64_t)tiles * p.splits);
+  const int split = (int)(at.rest % p.splits);
+  const int tile = tiles - 1 - (int)(at.rest / p.splits);
+  const Seq sq = load_seq(p, at.b);
+  const int64_t ncols = (int64_t)sq.lq * p.G, col0 = (int64_t)tile * 32;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
+  if (col0 >= ncols) return;
+  const Query q = query_at(p, sq, at.hk, col0 + (lane & 31), ncols);
+  const int last0 = p.causal ? min((int)(col0 / p.G) + sq.lk - sq.lq, sq.lk - 1) : sq.lk - 1;
+  h8 qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = row_chunk(p.q_fmt, p.q, q.row * p.ldq + (int64_t)q.head * p.D, ks, h, p.D, q.live);
+  int begin, end;
+  key_range(p, sq, min(col0 + 31, ncols - 1), split, TK, begin, end);
+
+  const float c1 = score_factor(p);
+  float m = neg_inf(), l = 0.0f;
+  f16v acc[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) acc[d] = f16v{};
+
+  StagedTile<TK, DP, 256> lk, lv;
+  lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
+  lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
   if (threadIdx.x == 0) odd = -1;
   __syncthreads();
   if (begin < end) {
-    lk.load(begin, end);
-    lv.load(begin, end);
+    lk.fetch(begin, end, kt, wave);
+    lv.fetch(begin, end, vt, wave);
   }
 #pragma unroll 1
   for (int t = begin; t < end; t += TK) {
-    lk.store(kt);
-    lv.store(vt);
+    lk.arrive(kt);
+    lv.arrive(vt);
     if (t + TK - 1 > last0) mark_not_finite(lv, &odd, t);
     __syncthreads();
     if (t + TK < end) {
-      lk.load(t + TK, end);
-      lv.load(t + TK, end);
+      lk.fetch(t + TK, end, kt, wave);
+      lv.fetch(t + TK, end, vt, wave);
     }
-    const int key0 = t + (NARROW ? 32 * wave : 0);
-    if (__builtin_amdgcn_readfirstlane(odd) == t) odd_values(key0);
-    compute(key0);
+    const int key0 = t + 32 * wave;
+    if (__builtin_amdgcn_readfirstlane(odd) == t) {
+      add_odd<DP>(vt, 32 * wave, 32, key0, q.last, h, acc);
+      remove_odd<TK, DP>(vt);
+    }
+    f16v s[1] = {f16v{}};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s[0] = mfma(row_operand<DP>(kt, 32 * wave, ks, lane), qf[ks], s[0]);
+    if (__any(key0 + 31 > q.last)) mask_scores(s[0], key0, h, q.last);
+    run_max(block_top(s[0]), c1, h, m, l, acc);
+    const float off = kRunLog2 - (m == neg_inf() ? 0.0f : m);
+    float pr[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      pr[r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c1, off));
+      l += pr[r];
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const h8 pf = to_operand(pr, g);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) acc[d] = mfma(col_operand<DP>(vt, 32 * wave + 16 * g, d, lane), pf, acc[d]);
+    }
     __syncthreads();
   }
   l += other_half(l, h);
 
-  auto finish = [&](int d, const f16v& o, float m1, float l1, int64_t c, int hd, int64_t row) {
-    // Block d (32 columns) of a query's result: registers 4 g ... are consecutive columns.
-    const float inv = l1 == 0.0f ? 0.0f : 1.0f / l1;
+  // Join the four waves: maxima and sums first, then the scaled results, of which
+  // wave w adds block w.
+  float2* ml = (float2*)lds;
+  if (h == 0) ml[wave * 32 + lane] = make_float2(m, l);
+  __syncthreads();
+  float top = neg_inf(), sum = 0.0f;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int n = 32 * d + 8 * g + 4 * h;
-      if (n < p.D) {
-        float y[4];
-        if (p.splits > 1) {
-          *(float4*)(p.part_o + ((split * p.rows_q + row) * p.H + hd) * (int64_t)p.D + n) =
-              make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
-        } else {
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * 32 + (lane & 31)].x);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = l1 == 0.0f ? 0.0f : o[4 * g + i] * inv;
-          store4_any(p.out_fmt, p.out, row * p.ldo + (int64_t)hd * p.D + n, y, 0, p.sat != 0);
-        }
-      }
+  for (int w = 0; w < 4; ++w) {
+    const float2 v = ml[w * 32 + (lane & 31)];
+    sum += v.x == neg_inf() ? v.y : v.y * __builtin_amdgcn_exp2f(v.x - top);
+  }
+  const float f = m == neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+  __syncthreads();
+  float* part = (float*)lds;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) part[((wave * DB + d) * 16 + r) * 64 + lane] = acc[d][r] * f;
+  __syncthreads();
+  if (wave < DB && q.live) {
+    f16v o;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float a = part[(wave * 16 + r) * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) a += part[((w * DB + wave) * 16 + r) * 64 + lane];
+      o[r] = a;
     }
-  };
-  auto finish_row = [&](float m1, float l1, int hd, int64_t row) {
-    if (p.splits > 1) p.part_ml[(split * p.rows_q + row) * p.H + hd] = make_float2(m1, l1);
-    else if (p.lse)
-      p.lse[(int64_t)hd * p.rows_q + row] = l1 == 0.0f ? neg_inf() : (m1 - kProbLog2 + __builtin_amdgcn_logf(l1)) * kLn2;
-  };
-
-  if constexpr (!NARROW) {
-    if (live) {
-#pragma unroll
-      for (int d = 0; d < DB; ++d) finish(d, acc[d], m, l, col, head, qrow);
-      if (h == 0) finish_row(m, l, head, qrow);
-    }
-  } else {
-    // Join the four waves: maxima and sums first, then the scaled results, of
-    // which wave w adds block w.
-    float2* ml = (float2*)lds;
-    if (h == 0) ml[wave * 32 + lane] = make_float2(m, l);
-    __syncthreads();
-    float top = neg_inf(), sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * 32 + (lane & 31)].x);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float2 v = ml[w * 32 + (lane & 31)];
-      sum += v.x == neg_inf() ? v.y : v.y * __builtin_amdgcn_exp2f(v.x - top);
-    }
-    const float f = m == neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-    __syncthreads();
-    float* part = (float*)lds;
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) part[((wave * DB + d) * 16 + r) * 64 + lane] = acc[d][r] * f;
-    __syncthreads();
-    if (wave < DB && live) {
-      f16v o;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float a = part[(wave * 16 + r) * 64 + lane];
-#pragma unroll
-        for (int w = 1; w < 4; ++w) a += part[((w * DB + wave) * 16 + r) * 64 + lane];
-        o[r] = a;
-      }
-      finish(wave, o, top, sum, col, head, qrow);
-      if (wave == 0 && h == 0) finish_row(top, sum, head, qrow);
-    }
+    store_result(p, o, q, wave, h, sum, split);
+    if (wave == 0 && h == 0) store_row(p, q, top, sum, split);
   }
 }
 
 // Joins the splits of a query: 32 lanes, four columns each.
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
   const int lane = threadIdx.x & 31;
-  const Place at = attn_place(p);
+  const Place at = attn_place(p, gridDim.x / (p.batch * p.Hkv));
   const Seq sq = load_seq(p, at.b);
   const int64_t col = at.rest * 8 + (threadIdx.x >> 5);
   if (col >= (int64_t)sq.lq * p.G) return;
@@ -265,8 +444,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
     for (int i = 0; i < 4; ++i) y[i] = l == 0.0f ? 0.0f : y[i] * inv;
     store4_any(p.out_fmt, p.out, row * p.ldo + (int64_t)head * p.D + 4 * lane, y, 0, p.sat != 0);
   }
-  if (p.lse && lane == 0)
-    p.lse[(int64_t)head * p.rows_q + row] = l == 0.0f ? neg_inf() : (m - kProbLog2 + __builtin_amdgcn_logf(l)) * kLn2;
+  if (p.lse && lane == 0) p.lse[(int64_t)head * p.rows_q + row] = log_sum(m, l);
 }
 
 __global__ void attn_scale_kernel(AttnParams p) { *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v))); }
@@ -276,8 +454,8 @@ __global__ void attn_scale_kernel(AttnParams p) { *p.out_scale = pow2_float(clam
 AttnPlan attention_plan(int64_t batch, int Hkv, int G, int64_t max_q, int64_t max_k) {
   AttnPlan r;
   const int64_t cols = max_q * G;
-  r.narrow = cols <= 32;
-  const int64_t groups = batch * Hkv * ((cols + (r.narrow ? 31 : 127)) / (r.narrow ? 32 : 128));
+  r.cols = cols <= 32 ? 32 : 128;
+  const int64_t groups = batch * Hkv * ((cols + r.cols - 1) / r.cols);
   int64_t s = groups > 0 ? 512 / groups : 1;
   if (s > max_k / 256) s = max_k / 256;
   if (s > 64) s = 64;
@@ -288,10 +466,13 @@ AttnPlan attention_plan(int64_t batch, int Hkv, int G, int64_t max_q, int64_t ma
 template <int DP>
 static void launch(const AttnParams& p, const AttnPlan& plan, hipStream_t s) {
   const int64_t cols = p.max_q * p.G;
-  const int tiles = (int)((cols + (plan.narrow ? 31 : 127)) / (plan.narrow ? 32 : 128));
+  const int tiles = (int)((cols + plan.cols - 1) / plan.cols);
   const dim3 g((unsigned)(p.batch * p.Hkv * tiles * plan.splits)), b(256);
-  if (plan.narrow) hipLaunchKernelGGL((attn_fwd_kernel<DP, true>), g, b, 0, s, p, tiles);
-  else hipLaunchKernelGGL((attn_fwd_kernel<DP, false>), g, b, 0, s, p, tiles);
+  if (plan.cols == 32) hipLaunchKernelGGL((attn_few_kernel<DP>), g, b, 0, s, p, tiles);
+  else if (p.k_fmt == kF16 && p.v_fmt == kF16) hipLaunchKernelGGL((attn_fwd_kernel<DP, true, true>), g, b, 0, s, p, tiles);
+  else if (p.k_fmt == kF16) hipLaunchKernelGGL((attn_fwd_kernel<DP, true, false>), g, b, 0, s, p, tiles);
+  else if (p.v_fmt == kF16) hipLaunchKernelGGL((attn_fwd_kernel<DP, false, true>), g, b, 0, s, p, tiles);
+  else hipLaunchKernelGGL((attn_fwd_kernel<DP, false, false>), g, b, 0, s, p, tiles);
 }
 
 hipError_t launch_attention_fwd(const AttnParams& p, const AttnPlan& plan, hipStream_t s) {

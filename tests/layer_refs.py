@@ -111,7 +111,9 @@ def attention(q, k, v, H, Hkv, alpha, seqs, causal, out_fmt):
             n = b / 16 + 80  # (additions of a result)
             at, cols = slice(q0, q0 + a), slice(h * D, (h + 1) * D)
             o[at, cols] = p @ z
-            err = av * (2 * es + 2.0 ** -11 + 2 * n * U) + 2.0 ** -38 * see.to(F64) @ z.abs()
+            # P in F16 as 2^10 P relative to a score's exponential: half a step is 2^-11 of
+            # it, and 2^-25 / 2^10 below the normal range (the row's sum is at least 1)
+            err = av * (2 * es + 2.0 ** -11 + 2 * n * U) + 2.0 ** -35 * see.to(F64) @ z.abs()
             eo[at, cols] = err + (o[at, cols].abs() + err) * rel + sub
             lse[h, at] = torch.logsumexp(s, 1)
             el[h, at] = (2 * es[:, 0] + 2 * n * U + 8 * U * (lse[h, at].abs().nan_to_num(posinf=0.0) + s.abs().nan_to_num(posinf=0.0).amax(1) + 30))
