@@ -189,11 +189,8 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   const int first = !have ? 0x7FFFFFFF : (p.causal ? key - behind : 0);  // first query that sees this key
   const int64_t krow = sq.k0 + key;
   h8 kf[KS], vf[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    kf[ks] = row_chunk(p.k_fmt, p.k, krow * p.ldk + (int64_t)at.hk * p.D, ks, h, p.D, have);
-    vf[ks] = row_chunk(p.v_fmt, p.v, krow * p.ldv + (int64_t)at.hk * p.D, ks, h, p.D, have);
-  }
+  load_row_operands(p.k_fmt, p.k, krow * p.ldk + (int64_t)at.hk * p.D, h, p.D, have, kf);
+  load_row_operands(p.v_fmt, p.v, krow * p.ldv + (int64_t)at.hk * p.D, h, p.D, have, vf);
   // queries that see any of the keys, in whole tiles, head after head
   const int q_lo = p.causal ? max(0, j0 - behind) / TQ * TQ : 0;
   const int nt = j0 < sq.lk && q_lo < sq.lq ? (sq.lq - q_lo + TQ - 1) / TQ : 0;
@@ -217,25 +214,36 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   lq.init(p.q, sq.q0 * p.ldq + (int64_t)at.hk * p.G * p.D, p.ldq, p.D, p.q_fmt);
   ld.init(p.dout, sq.q0 * p.lddo + (int64_t)at.hk * p.G * p.D, p.lddo, p.D, p.do_fmt);
   float l_next = 0.0f, d_next = 0.0f;
-  // The next tile to fetch: of head g from query t on; rows of zeros that see no key
-  // once the heads are done. Its row numbers: 16 rows a wave.
-  int g_next = 0, t_next = q_lo;
-  const int mine = 16 * wave + lane;
+  // The next tile to fetch: `left` queries of head g_next, 16 rows' numbers a wave;
+  // once the heads are done, rows of zeros that see no key. (Every address moves on
+  // by a constant: kernel arguments read again for each tile cost 700 clocks of it.)
+  const int mine = 16 * wave + lane, rows = nt * TQ;
+  int g_next = 0, left = sq.lq - q_lo;
+  const float* l_at = p.lse + (int64_t)at.hk * p.G * p.rows_q + sq.q0 + q_lo + mine;
+  const float* d_at = p.delta + (int64_t)at.hk * p.G * p.rows_q + sq.q0 + q_lo + mine;
+  const int64_t to_head = p.rows_q - rows;
+  lq.seek(q_lo);
+  ld.seek(q_lo);
   auto begin = [&](uint8_t* buf) {
-    const int t = g_next >= p.G ? sq.lq : t_next, g = min(g_next, p.G - 1);
-    lq.begin(t, sq.lq, buf, wave, (int64_t)g * p.D);
-    ld.begin(t, sq.lq, buf + BUF, wave, (int64_t)g * p.D);
+    const int there = g_next < p.G ? left : 0;
+    lq.begin(there, buf, wave);
+    ld.begin(there, buf + BUF, wave);
     l_next = neg_inf();
     d_next = 0.0f;
-    if (lane < 16 && t + mine < sq.lq) {
-      const int64_t row = (int64_t)(at.hk * p.G + g) * p.rows_q + sq.q0 + t + mine;
-      l_next = p.lse[row];
-      d_next = p.delta[row];
+    if (lane < 16 && mine < there) {
+      l_next = *l_at;
+      d_next = *d_at;
     }
-    t_next += TQ;
-    if (t_next >= q_end) {
-      t_next = q_lo;
+    l_at += TQ;
+    d_at += TQ;
+    left -= TQ;
+    if (left <= 0) {
+      left = sq.lq - q_lo;
       ++g_next;
+      lq.seek(q_lo, (int64_t)g_next * p.D);
+      ld.seek(q_lo, (int64_t)g_next * p.D);
+      l_at += to_head;
+      d_at += to_head;
     }
   };
   auto issue = [&](int i) {
@@ -289,53 +297,52 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
         }
       }
     }
-    // Slices of four products: first the next block's scores and dP (two steps of
-    // their sums each), then the last block's dV and dK.
+    // First the next block's scores and dP (a step of each in turn), then the last
+    // block's dV and dK: a slice is one product and what fits under it, either the
+    // operands of a later one or the probabilities of 16 / KS / 2 elements.
     h8 fa[AHEAD + 1][2], fb[AHEAD + 1][2];
-    auto read = [&](int x) {
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        h8 &a = fa[x % (AHEAD + 1)][y], &b = fb[x % (AHEAD + 1)][y];
-        if (x < KS / 2) {
-          a = row_operand<DP>(qn, 0, 2 * x + y, lane);
-          b = row_operand<DP>(on, 0, 2 * x + y, lane);
-        } else {
-          const int z = 2 * (x - KS / 2) + y;
-          a = col_operand<DP>(ol, 16 * (z / DB), z % DB, lane);
-          b = col_operand<DP>(ql, 16 * (z / DB), z % DB, lane);
-        }
+    auto read = [&](int x, int y) {
+      h8 &a = fa[x % (AHEAD + 1)][y], &b = fb[x % (AHEAD + 1)][y];
+      if (x < KS / 2) {
+        a = row_operand<DP>(qn, 0, 2 * x + y, lane);
+        b = row_operand<DP>(on, 0, 2 * x + y, lane);
+      } else {
+        const int z = 2 * (x - KS / 2) + y;
+        a = col_operand<DP>(ol, 16 * (z / DB), z % DB, lane);
+        b = col_operand<DP>(ql, 16 * (z / DB), z % DB, lane);
       }
     };
     sn = row_start(ln, h);
     dn = row_start(rn, h);
 #pragma unroll
-    for (int x = 0; x < AHEAD; ++x) read(x);
+    for (int x = 0; x < AHEAD; ++x) {
+      read(x, 0);
+      read(x, 1);
+    }
     slice_end();
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
-      if (i + AHEAD < KS) read(i + AHEAD);
-      also(i);
       const int a = i % (AHEAD + 1);
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        if (i < KS / 2) {
-          sn = mfma(fa[a][y], kf[2 * i + y], sn);
-          dn = mfma(fb[a][y], vf[2 * i + y], dn);
-        } else {
-          const int z = 2 * (i - KS / 2) + y;
-          av[z % DB] = mfma(fa[a][y], pl[z / DB], av[z % DB]);
-          ak[z % DB] = mfma(fb[a][y], el[z / DB], ak[z % DB]);
-        }
-      }
+        const int z = 2 * (i - KS / 2) + y;
+        if (i < KS / 2) sn = mfma(fa[a][y], kf[2 * i + y], sn);
+        else av[z % DB] = mfma(fa[a][y], pl[z / DB], av[z % DB]);
+        if (i + AHEAD < KS) read(i + AHEAD, y);
+        if (y == 0) also(i);
+        slice_end();
+        if (i < KS / 2) dn = mfma(fb[a][y], vf[2 * i + y], dn);
+        else ak[z % DB] = mfma(fb[a][y], el[z / DB], ak[z % DB]);
 #pragma unroll
-      for (int e = 16 / KS * i; e < 16 / KS * (i + 1); ++e) {
-        float x = __builtin_amdgcn_exp2f(s[e] * c1), y = x * (dp[e] * c2);
-        held(x);
-        held(y);
-        pn[e >> 3][e & 7] = (_Float16)x;
-        en[e >> 3][e & 7] = (_Float16)y;
+        for (int e = 8 / KS * (2 * i + y); e < 8 / KS * (2 * i + y + 1); ++e) {
+          float x = __builtin_amdgcn_exp2f(s[e] * c1), w = x * (dp[e] * c2);
+          held(x);
+          held(w);
+          pn[e >> 3][e & 7] = (_Float16)x;
+          en[e >> 3][e & 7] = (_Float16)w;
+        }
+        slice_end();
       }
-      slice_end();
     }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -416,11 +423,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles
   const int last = !live ? 0x7FFFFFFF : (p.causal ? min(pos + behind, sq.lk - 1) : sq.lk - 1);
   const int last0 = p.causal ? min((int)(col0 / p.G) + behind, sq.lk - 1) : sq.lk - 1;
   h8 qf[KS], df[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    qf[ks] = row_chunk(p.q_fmt, p.q, qrow * p.ldq + (int64_t)head * p.D, ks, h, p.D, live);
-    df[ks] = row_chunk(p.do_fmt, p.dout, qrow * p.lddo + (int64_t)head * p.D, ks, h, p.D, live);
-  }
+  load_row_operands(p.q_fmt, p.q, qrow * p.ldq + (int64_t)head * p.D, h, p.D, live, qf);
+  load_row_operands(p.do_fmt, p.dout, qrow * p.lddo + (int64_t)head * p.D, h, p.D, live, df);
   const int64_t last_col = col0 + 128 < ncols ? col0 + 127 : ncols - 1;
   const int end = p.causal ? max(0, min(sq.lk, (int)(last_col / p.G) + behind + 1)) : sq.lk;
 
@@ -445,12 +449,14 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles
   for (int d = 0; d < DB; ++d) acc[d] = f16v{};
   uint8_t* const kt = lds;
   uint8_t* const vt = lds + BUF;
-  StagedTile<TK, DP, 256> lk, lv;
+  StagedTile<TK, DP, 256, false> lk, lv;
   lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
   lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
   if (end > 0) {
-    lk.fetch(0, end, nullptr, 0);
-    lv.fetch(0, end, nullptr, 0);
+    lk.seek(0);
+    lv.seek(0);
+    lk.begin(end, nullptr, 0);
+    lv.begin(end, nullptr, 0);
   }
 #pragma unroll 1
   for (int t = 0; t < end; t += TK) {
@@ -459,8 +465,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles
     if (t + TK - 1 > last0) mark_not_finite(lk, &odd, t);
     __syncthreads();
     if (t + TK < end) {
-      lk.fetch(t + TK, end, nullptr, 0);
-      lv.fetch(t + TK, end, nullptr, 0);
+      lk.begin(end - t - TK, nullptr, 0);
+      lv.begin(end - t - TK, nullptr, 0);
     }
     const bool is_odd = __builtin_amdgcn_readfirstlane(odd) == t;
 #pragma unroll

@@ -114,37 +114,42 @@ __device__ __forceinline__ u4 load_f16x8(int fmt, const void* base, int64_t e) {
   return to_f16x8(fmt, u4{v[0], v[1], 0u, 0u});
 }
 
-// 8-bit or (the format decides) any rows of a matrix on their way into an LDS tile of
-// ROWS x DP: fetched into registers, eight columns a chunk, and decoded and stored by
-// arrive(). The buffer's range check makes rows past the end, and the columns past
-// D, read as zeros.
-template <int ROWS, int DP, int THREADS, bool EIGHT = false>
+// Rows of a matrix, of 8 bits (EIGHT) or of a format known at run time, on their way
+// into an LDS tile of ROWS x DP: fetched into the registers of a workgroup, or a
+// wave (THREADS 64), eight columns a chunk, and decoded and stored by arrive(). The
+// buffer's range check makes rows past the end, and the columns past D, read as
+// zeros.
+template <int ROWS, int DP, int THREADS, bool EIGHT>
 struct StagedTile {
   static constexpr int CH = DP / 8, N = ROWS * CH / THREADS;
   typename std::conditional<EIGHT, u2, u4>::type r[N];
   int voff0, step;  // chunk i of a thread: voff0 + i step
-  const uint8_t* base;
-  int64_t pitch;
+  const uint8_t *base, *at;
+  uint32_t pitch;
   int bytes_d, fmt;
 
   // first: element of row 0 (of the sequence) and column 0 (of the head)
   __device__ __forceinline__ void init(const void* data, int64_t first, int64_t ld, int D, int format) {
     const int es = EIGHT ? 1 : fmt_bytes(format);
     fmt = format;
-    base = (const uint8_t*)data + first * es;
-    pitch = ld * es;
+    at = base = (const uint8_t*)data + first * es;
+    pitch = (uint32_t)(ld * es);
     bytes_d = D * es;
-    const int row = (int)threadIdx.x / CH, ch = (int)threadIdx.x % CH;
+    const int me = (int)threadIdx.x % THREADS, row = me / CH, ch = me % CH;
     step = THREADS / CH * (int)pitch;
     // (past the end of any buffer: a tile's rows span less than 2^31 bytes)
     voff0 = ch * 8 < D ? row * (int)pitch + ch * 8 * es : (int)0x80000000;
   }
-  // rows row0 .. row0 + ROWS - 1 (of a matrix `skip` elements on), those from `end` on zero
-  __device__ __forceinline__ void fetch(int64_t row0, int64_t end, uint8_t*, int, int64_t skip = 0) {
-    const int64_t n = end - row0 < ROWS ? end - row0 : ROWS;
-    const uint32_t bytes = n > 0 ? (uint32_t)((n - 1) * pitch) + (uint32_t)bytes_d : 0u;
-    const uint8_t* at = base + row0 * pitch + skip * (EIGHT ? 1 : fmt_bytes(fmt));
+  // The next tile starts at row0 (of a matrix `skip` elements on).
+  __device__ __forceinline__ void seek(int64_t row0, int64_t skip = 0) {
+    at = base + row0 * pitch + skip * (EIGHT ? 1 : fmt_bytes(fmt));
+  }
+  __device__ __forceinline__ void skip(int64_t rows) { at += rows * pitch; }
+  // Loads the next tile, of which `left` rows are there, and moves on by a tile.
+  __device__ __forceinline__ void begin(int left, uint8_t*, int) {
+    const uint32_t bytes = left > 0 ? (uint32_t)(min(left, ROWS) - 1) * pitch + (uint32_t)bytes_d : 0u;
     const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, (int)bytes, 0x00027000);
+    at += (uint64_t)pitch * ROWS;
     if constexpr (EIGHT) {
 #pragma unroll
       for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b64(rs, voff0 + i * step, 0, 0);
@@ -159,14 +164,11 @@ struct StagedTile {
       }
     }
   }
-  __device__ __forceinline__ void begin(int64_t row0, int64_t end, uint8_t* lds, int wave, int64_t skip = 0) {
-    fetch(row0, end, lds, wave, skip);
-  }
   __device__ __forceinline__ void issue(int) const {}
   __device__ __forceinline__ void arrive(uint8_t* lds) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (int)threadIdx.x + i * THREADS;
+      const int c = (int)threadIdx.x % THREADS + i * THREADS;
       *(u4*)(lds + tile_off<DP>(c / CH, c % CH)) = value(i);
     }
   }
@@ -197,6 +199,13 @@ __device__ __forceinline__ void load_to_lds16(v4i rsrc, uint32_t voff, const uin
 // may replace only behind the branch, away from the products that it hides under).
 template <typename T>
 __device__ __forceinline__ void held(T& x) { asm volatile("" : "+v"(x)); }
+// What a wave's lanes wrote to LDS before is there for its other lanes after (a wave's
+// LDS instructions are done in order; this keeps the compiler to that order).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 // Nothing is scheduled across.
 __device__ __forceinline__ void slice_end() { __builtin_amdgcn_sched_barrier(0); }
 // All loads so far are done, also for the compiler's own count of them (else it
@@ -211,38 +220,61 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)"
 template <int ROWS, int DP>
 struct DirectTile {
   static constexpr int CH = DP / 8, N = ROWS * CH / 256;
-  uint32_t voff0, step;
-  const uint8_t* base;
-  int64_t pitch;
+  uint32_t voff0, step, pitch;
+  const uint8_t *base, *at;
   int bytes_d;
   v4i rs;       // of the tile under way
   uint8_t* to;
 
   __device__ __forceinline__ void init(const void* data, int64_t first, int64_t ld, int D, int) {
     base = (const uint8_t*)data + first * 2;
-    pitch = ld * 2;
+    pitch = (uint32_t)(ld * 2);
     bytes_d = D * 2;
     const int row = (int)threadIdx.x / CH, slot = (int)threadIdx.x % CH;
     const int ch = (tile_off<DP>(row, slot) - row * DP * 2) >> 4;
-    step = 256 / CH * (uint32_t)pitch;
-    voff0 = ch * 8 < D ? (uint32_t)row * (uint32_t)pitch + ch * 16 : 0x80000000u;
+    step = 256 / CH * pitch;
+    voff0 = ch * 8 < D ? row * pitch + ch * 16 : 0x80000000u;
   }
-  // rows row0 ... (of a matrix `skip` elements on) into the tile at lds, those from
-  // `end` on zero: begin(), then issue(0) ... issue(N - 1). (A burst of them stops the
-  // wave for 700 clocks until the memory pipe has taken it; one in each slice of a
-  // block of products is hidden.)
-  __device__ __forceinline__ void begin(int64_t row0, int64_t end, uint8_t* lds, int wave, int64_t skip = 0) {
-    const int64_t n = end - row0 < ROWS ? end - row0 : ROWS;
-    const uint32_t bytes = n > 0 ? (uint32_t)((n - 1) * pitch) + (uint32_t)bytes_d : 0u;
-    const uint64_t at = (uint64_t)(uintptr_t)(base + row0 * pitch + 2 * skip);
-    rs = v4i{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)bytes, 0x00027000};
+  __device__ __forceinline__ void seek(int64_t row0, int64_t skip = 0) { at = base + row0 * pitch + 2 * skip; }
+  // The next tile, of which `left` rows are there: begin(), then issue(0) ... issue(N -
+  // 1). (A burst of them stops the wave until the memory pipe has taken it; one in
+  // each slice of a block of products is hidden.)
+  __device__ __forceinline__ void begin(int left, uint8_t* lds, int wave) {
+    const uint32_t bytes = left > 0 ? (uint32_t)(min(left, ROWS) - 1) * pitch + (uint32_t)bytes_d : 0u;
+    rs = v4i{(int)(uint32_t)(uintptr_t)at, (int)(uint32_t)((uint64_t)(uintptr_t)at >> 32), (int)bytes, 0x00027000};
     to = lds + wave * 1024;
+    at += (uint64_t)pitch * ROWS;
   }
   __device__ __forceinline__ void issue(int i) const { load_to_lds16(rs, voff0 + i * step, to + i * 4096); }
-  __device__ __forceinline__ void fetch(int64_t row0, int64_t end, uint8_t* lds, int wave, int64_t skip = 0) {
-    begin(row0, end, lds, wave, skip);
+  __device__ __forceinline__ void arrive(uint8_t*) const { wait_loads(); }
+};
+// The same for a wave's own tile of 32 rows: a load covers so few rows that the
+// chunks' permutation differs from one to the next, with a period of four.
+template <int DP>
+struct WaveTile {
+  static constexpr int CH = DP / 8, PER = 64 / CH, N = 32 / PER;
+  uint32_t voff[4], pitch;
+  const uint8_t* at;
+  int bytes_d;
+
+  __device__ __forceinline__ void init(const void* data, int64_t first, int64_t ld, int D, int) {
+    at = (const uint8_t*)data + first * 2;
+    pitch = (uint32_t)(ld * 2);
+    bytes_d = D * 2;
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < N; ++i) issue(i);
+    for (int k = 0; k < 4; ++k) {
+      const int row = k * PER + lane / CH, ch = (tile_off<DP>(row, lane % CH) - row * DP * 2) >> 4;
+      voff[k] = ch * 8 < D ? row * pitch + ch * 16 : 0x80000000u;
+    }
+  }
+  __device__ __forceinline__ void skip(int64_t rows) { at += rows * pitch; }
+  __device__ __forceinline__ void begin(int left, uint8_t* lds, int) {
+    const uint32_t bytes = left > 0 ? (uint32_t)(min(left, 32) - 1) * pitch + (uint32_t)bytes_d : 0u;
+    const v4i rs = {(int)(uint32_t)(uintptr_t)at, (int)(uint32_t)((uint64_t)(uintptr_t)at >> 32), (int)bytes, 0x00027000};
+#pragma unroll
+    for (int i = 0; i < N; ++i) load_to_lds16(rs, voff[i & 3] + (i >> 2) * 4 * PER * pitch, lds + i * 1024);
+    at += (uint64_t)pitch * 32;
   }
   __device__ __forceinline__ void arrive(uint8_t*) const { wait_loads(); }
 };
@@ -272,13 +304,29 @@ __device__ __forceinline__ h8 col_operand(const uint8_t* lds, int row0, int db, 
   return __builtin_bit_cast(h8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// The same from global memory, a row a lane held in registers for the whole
-// kernel: chunk ks of a row that starts at element e (columns from D on zero).
-__device__ __forceinline__ h8 row_chunk(int fmt, const void* base, int64_t e, int ks, int h, int D, bool ok) {
-  u4 v = {0u, 0u, 0u, 0u};
-  const int col = 16 * ks + 8 * h;
-  if (ok && col < D) v = load_f16x8(fmt, base, e + col);
-  return __builtin_bit_cast(h8, v);
+// The same from global memory, for the whole kernel: the row that starts at element
+// e (columns from D on, and rows that are not there, zero).
+template <int KS>
+__device__ __forceinline__ void load_row_operands(int fmt, const void* base, int64_t e, int h, int D, bool ok, h8 (&v)[KS]) {
+  u4 w[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) w[ks] = u4{0u, 0u, 0u, 0u};
+  if (fmt == kF16) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      if (ok && 16 * ks + 8 * h < D) w[ks] = *(const u4*)((const uint16_t*)base + e + 16 * ks + 8 * h);
+  } else {
+    u2 b[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      b[ks] = u2{0u, 0u};
+      if (ok && 16 * ks + 8 * h < D) b[ks] = *(const u2*)((const uint8_t*)base + e + 16 * ks + 8 * h);
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) w[ks] = to_f16x8(fmt, u4{b[ks][0], b[ks][1], 0u, 0u});
+  }
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) v[ks] = __builtin_bit_cast(h8, w[ks]);
 }
 
 __device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) {
@@ -332,11 +380,15 @@ __device__ __forceinline__ h8 finite_part(h8 v) {
 // (`flag`: the tile's number, so it needs no clearing); its finite part is then
 // multiplied as usual, and the rest added pair by pair.
 template <int ROWS, int DP, int THREADS, bool EIGHT>
-__device__ __forceinline__ void mark_not_finite(const StagedTile<ROWS, DP, THREADS, EIGHT>& t, int* flag, int number) {
+__device__ __forceinline__ bool any_not_finite(const StagedTile<ROWS, DP, THREADS, EIGHT>& t) {
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < t.N; ++i) bad |= not_finite(__builtin_bit_cast(h8, t.value(i)));
-  if (bad) *flag = number;
+  return bad;
+}
+template <int ROWS, int DP, int THREADS, bool EIGHT>
+__device__ __forceinline__ void mark_not_finite(const StagedTile<ROWS, DP, THREADS, EIGHT>& t, int* flag, int number) {
+  if (any_not_finite(t)) *flag = number;
 }
 
 // The same for a tile in LDS (256 threads, whose barrier the caller owes).

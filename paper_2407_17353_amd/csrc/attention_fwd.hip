@@ -163,9 +163,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
   const int last0 = p.causal ? min((int)(col0 / p.G) + sq.lk - sq.lq, sq.lk - 1) : sq.lk - 1;  // of the first column
   const Query q = query_at(p, sq, at.hk, col0 + 32 * wave + (lane & 31), ncols);
   h8 qf[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
-    qf[ks] = row_chunk(p.q_fmt, p.q, q.row * p.ldq + (int64_t)q.head * p.D, ks, h, p.D, q.live);
+  load_row_operands(p.q_fmt, p.q, q.row * p.ldq + (int64_t)q.head * p.D, h, p.D, q.live, qf);
   int begin, end;
   key_range(p, sq, min(col0 + 127, ncols - 1), split, TK, begin, end);
 
@@ -190,13 +188,23 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
   f16v sa = {}, sb = {};
   h8 pa[2] = {}, pb[2] = {};  // probabilities of the last even and odd block
   if (begin < end) {
-    lk.fetch(begin, end, kb, wave);
-    lv.fetch(end, end, vb + BUF, wave);  // (the block before the first: v of zeros)
-    arrive(kb, vb + BUF);
+    lk.seek(begin);
+    lv.seek(begin);
+    lk.begin(end - begin, kb, wave);
+#pragma unroll
+    for (int i = 0; i < KS / 2; ++i) lk.issue(i);
+    for (int i = threadIdx.x; i < BUF / 16; i += 256) ((u4*)(vb + BUF))[i] = u4{0u, 0u, 0u, 0u};  // (the block before the first)
+    lk.arrive(kb);
+    __syncthreads();
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) sa = mfma(row_operand<DP>(kb, 0, ks, lane), qf[ks], sa);
-    lk.fetch(begin + TK, end, kb + BUF, wave);
-    lv.fetch(begin, end, vb, wave);
+    lk.begin(end - begin - TK, kb + BUF, wave);
+    lv.begin(end - begin, vb, wave);
+#pragma unroll
+    for (int i = 0; i < KS / 2; ++i) {
+      lk.issue(i);
+      lv.issue(i);
+    }
   }
   settle_loads();
 
@@ -223,17 +231,20 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
         vf[x % (AHEAD + 1)] = col_operand<DP>(vl, 16 * (x / DB), x % DB, lane);
       }
       also(i);
-      sc = mfma(kf[i % (AHEAD + 1)], qf[i], sc);
-      acc[i % DB] = mfma(vf[i % (AHEAD + 1)], pl[i / DB], acc[i % DB]);
 #pragma unroll
-      for (int e = 16 / KS * i; e < 16 / KS * (i + 1); ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[e], c1, off));
-        top = fmaxf(top, s[e]);  // (fmaxf skips NaN)
-        lb += x;
-        pn[e >> 3][e & 7] = (_Float16)x;
+      for (int y = 0; y < 2; ++y) {
+        if (y == 0) sc = mfma(kf[i % (AHEAD + 1)], qf[i], sc);
+        else acc[i % DB] = mfma(vf[i % (AHEAD + 1)], pl[i / DB], acc[i % DB]);
+#pragma unroll
+        for (int e = 8 / KS * (2 * i + y); e < 8 / KS * (2 * i + y + 1); ++e) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[e], c1, off));
+          top = fmaxf(top, s[e]);  // (fmaxf skips NaN)
+          lb += x;
+          pn[e >> 3][e & 7] = (_Float16)x;
+        }
+        held(lb);
+        slice_end();
       }
-      held(lb);
-      slice_end();
     }
     // The running maximum is moved only when a score is past it by more than
     // kSlack: with what had been added relative to the old one the block's
@@ -279,8 +290,8 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
         remove_odd<TK, DP>(vt);
       }
     }
-    lk.begin(t + 2 * TK, end, kt, wave);
-    lv.begin(t + TK, end, vo, wave);
+    lk.begin(end - t - 2 * TK, kt, wave);
+    lv.begin(end - t - TK, vo, wave);
     block(t + 32, sb, pb, sa, ko, pa, vt, [&](int i) {
       if (i < KS / 2) lk.issue(i);
       else lv.issue(i - KS / 2);
@@ -301,15 +312,20 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
   }
 }
 
-// Few queries: 32 columns, and the waves take a quarter each of a tile of 128 keys.
-template <int DP>
+// Few queries: 32 columns, which each wave holds; every fourth block of 32 keys is a
+// wave's, in an LDS tile of its own, so that no wave waits for another before the
+// end, where the four are joined. (With tiles that the workgroup loaded together the
+// barriers left memory idle: FEW_BEFORE.)
+// K16, V16: whether k and v are F16 or have 8 bits.
+template <int DP, bool K16, bool V16>
 __global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnParams p, int tiles) {
-  constexpr int TK = 128, KS = DP / 16, DB = DP / 32;
-  __shared__ __align__(16) uint8_t lds[2 * TK * DP * 2];
-  __shared__ int odd;
-  uint8_t* const kt = lds;
-  uint8_t* const vt = lds + TK * DP * 2;
+  // (F16 tiles go straight into LDS and have two buffers, 8-bit ones one: the next
+  // tile's codes wait in registers)
+  constexpr int TK = 128, KS = DP / 16, DB = DP / 32, BUF = 32 * DP * 2, NK = K16 ? 2 : 1, NV = V16 ? 2 : 1;
+  __shared__ __align__(16) uint8_t lds[4 * (NK + NV) * BUF];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  uint8_t* const kb = lds + wave * (NK + NV) * BUF;
+  uint8_t* const vb = kb + NK * BUF;
   const Place at = attn_place(p, (int64_t)tiles * p.splits);
   const int split = (int)(at.rest % p.splits);
   const int tile = tiles - 1 - (int)(at.rest / p.splits);
@@ -318,63 +334,69 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnParams p, int tile
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
   if (col0 >= ncols) return;
   const Query q = query_at(p, sq, at.hk, col0 + (lane & 31), ncols);
-  const int last0 = p.causal ? min((int)(col0 / p.G) + sq.lk - sq.lq, sq.lk - 1) : sq.lk - 1;
-  h8 qf[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) qf[ks] = row_chunk(p.q_fmt, p.q, q.row * p.ldq + (int64_t)q.head * p.D, ks, h, p.D, q.live);
   int begin, end;
   key_range(p, sq, min(col0 + 31, ncols - 1), split, TK, begin, end);
-
+  typename std::conditional<K16, WaveTile<DP>, StagedTile<32, DP, 64, true>>::type lk;
+  typename std::conditional<V16, WaveTile<DP>, StagedTile<32, DP, 64, true>>::type lv;
+  lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
+  lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
+  const int key0 = begin + 32 * wave;
+  lk.skip(key0);
+  lv.skip(key0);
+  lk.begin(end - key0, kb, 0);
+  lv.begin(end - key0, vb, 0);
+  h8 qf[KS];
+  load_row_operands(p.q_fmt, p.q, q.row * p.ldq + (int64_t)q.head * p.D, h, p.D, q.live, qf);
   const float c1 = score_factor(p);
   float m = neg_inf(), l = 0.0f;
   f16v acc[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = f16v{};
 
-  StagedTile<TK, DP, 256> lk, lv;
-  lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
-  lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
-  if (threadIdx.x == 0) odd = -1;
-  __syncthreads();
-  if (begin < end) {
-    lk.fetch(begin, end, kt, wave);
-    lv.fetch(begin, end, vt, wave);
-  }
 #pragma unroll 1
-  for (int t = begin; t < end; t += TK) {
+  for (int t = key0, n = 0; t < end; t += TK, n ^= 1) {
+    uint8_t* const kt = kb + (K16 ? n * BUF : 0);
+    uint8_t* const vt = vb + (V16 ? n * BUF : 0);
+    wave_sync();  // (the block before has been read)
     lk.arrive(kt);
     lv.arrive(vt);
-    if (t + TK - 1 > last0) mark_not_finite(lv, &odd, t);
-    __syncthreads();
-    if (t + TK < end) {
-      lk.fetch(t + TK, end, kt, wave);
-      lv.fetch(t + TK, end, vt, wave);
+    wave_sync();
+    lk.skip(3 * 32);
+    lv.skip(3 * 32);
+    lk.begin(end - t - TK, kb + (K16 ? (n ^ 1) * BUF : 0), 0);
+    lv.begin(end - t - TK, vb + (V16 ? (n ^ 1) * BUF : 0), 0);
+    const bool masked = __any(t + 31 > q.last);
+    if (masked) {
+      bool odd = false;
+      for (int i = lane; i < 32 * DP / 8; i += 64) odd |= not_finite(((const h8*)vt)[i]);
+      if (__any(odd)) {
+        add_odd<DP>(vt, 0, 32, t, q.last, h, acc);
+        wave_sync();
+        for (int i = lane; i < 32 * DP / 8; i += 64) ((h8*)vt)[i] = finite_part(((const h8*)vt)[i]);
+        wave_sync();
+      }
     }
-    const int key0 = t + 32 * wave;
-    if (__builtin_amdgcn_readfirstlane(odd) == t) {
-      add_odd<DP>(vt, 32 * wave, 32, key0, q.last, h, acc);
-      remove_odd<TK, DP>(vt);
-    }
-    f16v s[1] = {f16v{}};
+    f16v s = {};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[0] = mfma(row_operand<DP>(kt, 32 * wave, ks, lane), qf[ks], s[0]);
-    if (__any(key0 + 31 > q.last)) mask_scores(s[0], key0, h, q.last);
-    run_max(block_top(s[0]), c1, h, m, l, acc);
+    for (int ks = 0; ks < KS; ++ks) s = mfma(row_operand<DP>(kt, 0, ks, lane), qf[ks], s);
+    if (masked) mask_scores(s, t, h, q.last);
+    run_max(block_top(s), c1, h, m, l, acc);
     const float off = kRunLog2 - (m == neg_inf() ? 0.0f : m);
     float pr[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      pr[r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c1, off));
+      pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c1, off));
       l += pr[r];
     }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const h8 pf = to_operand(pr, g);
 #pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] = mfma(col_operand<DP>(vt, 32 * wave + 16 * g, d, lane), pf, acc[d]);
+      for (int d = 0; d < DB; ++d) acc[d] = mfma(col_operand<DP>(vt, 16 * g, d, lane), pf, acc[d]);
     }
-    __syncthreads();
   }
+  wait_loads();
+  __syncthreads();
   l += other_half(l, h);
 
   // Join the four waves: maxima and sums first, then the scaled results, of which
@@ -412,31 +434,48 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnParams p, int tile
   }
 }
 
-// Joins the splits of a query: 32 lanes, four columns each.
+// Joins the splits of a query, a query a workgroup: eight groups of 32 lanes take
+// every eighth split each, four columns a lane, and are added in order.
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
-  const int lane = threadIdx.x & 31;
+  __shared__ float4 part[8][32];
+  __shared__ float sums[8];
+  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
   const Place at = attn_place(p, gridDim.x / (p.batch * p.Hkv));
   const Seq sq = load_seq(p, at.b);
-  const int64_t col = at.rest * 8 + (threadIdx.x >> 5);
+  const int64_t col = at.rest;
   if (col >= (int64_t)sq.lq * p.G) return;
   const int pos = (int)(col / p.G), head = at.hk * p.G + (int)(col - (int64_t)pos * p.G);
-  const int64_t row = sq.q0 + pos;
+  const int64_t row = sq.q0 + pos, first = row * p.H + head, step = p.rows_q * p.H;
   float m = neg_inf();
-  for (int s = 0; s < p.splits; ++s) m = fmaxf(m, p.part_ml[(s * p.rows_q + row) * p.H + head].x);
+  for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, p.part_ml[first + s * step].x);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 32));
   float l = 0.0f, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < p.splits; ++s) {
-    const int64_t i = (s * p.rows_q + row) * p.H + head;
-    const float2 ml = p.part_ml[i];
+  for (int s = group; s < p.splits; s += 8) {
+    const float2 ml = p.part_ml[first + s * step];
     if (ml.y == 0.0f) continue;  // (nothing admitted)
     const float f = ml.x == neg_inf() ? 1.0f : __builtin_amdgcn_exp2f(ml.x - m);
     l += ml.y * f;
     if (4 * lane < p.D) {
-      const float4 o = *(const float4*)(p.part_o + i * p.D + 4 * lane);
+      const float4 o = *(const float4*)(p.part_o + (first + s * step) * p.D + 4 * lane);
       y[0] += o.x * f;
       y[1] += o.y * f;
       y[2] += o.z * f;
       y[3] += o.w * f;
     }
+  }
+  part[group][lane] = make_float4(y[0], y[1], y[2], y[3]);
+  if (lane == 0) sums[group] = l;
+  __syncthreads();
+  if (group != 0) return;
+#pragma unroll
+  for (int g = 1; g < 8; ++g) {
+    const float4 o = part[g][lane];
+    y[0] += o.x;
+    y[1] += o.y;
+    y[2] += o.z;
+    y[3] += o.w;
+    l += sums[g];
   }
   if (4 * lane < p.D) {
     const float inv = 1.0f / l;
@@ -468,10 +507,15 @@ static void launch(const AttnParams& p, const AttnPlan& plan, hipStream_t s) {
   const int64_t cols = p.max_q * p.G;
   const int tiles = (int)((cols + plan.cols - 1) / plan.cols);
   const dim3 g((unsigned)(p.batch * p.Hkv * tiles * plan.splits)), b(256);
-  if (plan.cols == 32) hipLaunchKernelGGL((attn_few_kernel<DP>), g, b, 0, s, p, tiles);
-  else if (p.k_fmt == kF16 && p.v_fmt == kF16) hipLaunchKernelGGL((attn_fwd_kernel<DP, true, true>), g, b, 0, s, p, tiles);
-  else if (p.k_fmt == kF16) hipLaunchKernelGGL((attn_fwd_kernel<DP, true, false>), g, b, 0, s, p, tiles);
-  else if (p.v_fmt == kF16) hipLaunchKernelGGL((attn_fwd_kernel<DP, false, true>), g, b, 0, s, p, tiles);
+  const bool k16 = p.k_fmt == kF16, v16 = p.v_fmt == kF16;
+  if (plan.cols == 32) {
+    if (k16 && v16) hipLaunchKernelGGL((attn_few_kernel<DP, true, true>), g, b, 0, s, p, tiles);
+    else if (k16) hipLaunchKernelGGL((attn_few_kernel<DP, true, false>), g, b, 0, s, p, tiles);
+    else if (v16) hipLaunchKernelGGL((attn_few_kernel<DP, false, true>), g, b, 0, s, p, tiles);
+    else hipLaunchKernelGGL((attn_few_kernel<DP, false, false>), g, b, 0, s, p, tiles);
+  } else if (k16 && v16) hipLaunchKernelGGL((attn_fwd_kernel<DP, true, true>), g, b, 0, s, p, tiles);
+  else if (k16) hipLaunchKernelGGL((attn_fwd_kernel<DP, true, false>), g, b, 0, s, p, tiles);
+  else if (v16) hipLaunchKernelGGL((attn_fwd_kernel<DP, false, true>), g, b, 0, s, p, tiles);
   else hipLaunchKernelGGL((attn_fwd_kernel<DP, false, false>), g, b, 0, s, p, tiles);
 }
 
@@ -484,7 +528,7 @@ hipError_t launch_attention_fwd(const AttnParams& p, const AttnPlan& plan, hipSt
   else launch<128>(p, plan, s);
   if (plan.splits > 1) {
     const int64_t cols = p.max_q * p.G;
-    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)(p.batch * p.Hkv * ((cols + 7) / 8))), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)(p.batch * p.Hkv * cols)), dim3(256), 0, s, p);
   }
   return hipGetLastError();
 }

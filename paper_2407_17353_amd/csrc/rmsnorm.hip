@@ -59,9 +59,11 @@ int rms_grid(int64_t R, int wpr, int waves) {
   return (int)(need < 1 ? 1 : (need < g ? need : g));
 }
 
-// Within the workspace's partial rows.
+// Within the workspace's partial rows. (512 workgroups: with 1024 the partial rows of
+// dgamma cost more than the further loads in flight bring, 134 us for 123 at 16384 x
+// 4096, with 256 too few loads are in flight, 195 us.)
 int rms_bwd_grid(const RmsParams& p) {
-  const int g = rms_grid(p.R, rms_wpr(p.D), 4);
+  const int g = rms_grid(p.R, rms_wpr(p.D), 2);
   const int64_t most = rmsnorm_groups(p.R, p.D);
   return g < most ? g : (int)most;
 }

@@ -27,7 +27,7 @@ static void bwd(const RmsParams& p, hipStream_t s) {
   if (p.D == 1024 * WPR) hipLaunchKernelGGL((rms_bwd_rows_kernel<kF32, DYF, WPR, true>), g, b, 0, s, p);
   else hipLaunchKernelGGL((rms_bwd_rows_kernel<kF32, DYF, WPR, false>), g, b, 0, s, p);
   if (p.mode == 1) {
-    const dim3 t((p.D + LN_TILE_COLS - 1) / LN_TILE_COLS, (unsigned)layernorm_row_tiles(p.R));
+    const dim3 t((p.D + LN_TILE_COLS - 1) / LN_TILE_COLS, (unsigned)((p.R + RMS_TILE_ROWS - 1) / RMS_TILE_ROWS));
     hipLaunchKernelGGL((rms_bwd_apply_kernel<kF32, DYF>), t, dim3(LN_TILE_THREADS), 0, s, p);
   }
 }
