@@ -39,6 +39,9 @@ struct AttnParams {
   int dq_fmt, dk_fmt, dv_fmt;
   float *dq_scale, *dk_scale, *dv_scale;
   float *dq32, *dk32, *dv32; // dynamic rescale: fp32 gradients [rows][heads * D], else NULL
+  int parts;                 // workgroups that share the queries of 128 keys
+  float* part;               // parts > 1: their dk and dv, [parts][2][rows_k][Hkv * D], the first in
+                             // place of dk32 and dv32
   uint32_t* amax;            // the three statistics
   float* amax_out;           // optional [3]
   int mode, target;
@@ -53,6 +56,8 @@ struct AttnPlan {
 };
 AttnPlan attention_plan(int64_t batch, int Hkv, int G, int64_t max_q, int64_t max_k);
 hipError_t launch_attention_fwd(const AttnParams& p, const AttnPlan& plan, hipStream_t s);
+// The backward's `parts`, 1 where the grid fills the device without.
+int attention_bwd_parts(int64_t batch, int Hkv, int G, int64_t max_q, int64_t max_k);
 hipError_t launch_attention_bwd(const AttnParams& p, hipStream_t s);
 
 }  // namespace scalify

