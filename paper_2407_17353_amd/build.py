@@ -13,9 +13,9 @@ destination and C operand are the same a[n:n+3], a write of 0, a read into a
 VGPR) names one of them -- the compiler spilling into it or using it as the
 data of a load or an MFMA operand.
 
-No GEMM kernel may use scratch memory, but for the fused epilogue of the 8-wave
-kernel (gemm_*_fused), which holds accumulators, residual codes and channel
-exponents at once and keeps some of them there.
+No GEMM, attention or RMS norm kernel may use scratch memory, but for the fused
+epilogue of the 8-wave GEMM kernel (gemm_*_fused), which holds accumulators,
+residual codes and channel exponents at once and keeps some of them there.
 
 The loads of these kernels are inline asm too, so the compiler does not keep
 the distance their scalar operands need: the build fails if a vector memory
@@ -206,7 +206,7 @@ def build(verbose: bool = False) -> str:
                 raise RuntimeError(f"hipcc failed for {src}:\n{r.stderr}")
             if verbose and r.stderr.strip():
                 print(r.stderr)
-            if os.path.basename(src).startswith(("gemm_", "mid_", "wave_")):
+            if os.path.basename(src).startswith(("gemm_", "mid_", "wave_", "attention_", "rmsnorm")):
                 check_code(obj, tmp)
             return obj
 

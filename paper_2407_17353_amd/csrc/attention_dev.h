@@ -114,15 +114,14 @@ __device__ __forceinline__ u4 load_f16x8(int fmt, const void* base, int64_t e) {
   return to_f16x8(fmt, u4{v[0], v[1], 0u, 0u});
 }
 
-// Rows of a matrix, of 8 bits (EIGHT) or of a format known at run time, on their way
-// into an LDS tile of ROWS x DP: fetched into the registers of a workgroup, or a
-// wave (THREADS 64), eight columns a chunk, and decoded and stored by arrive(). The
-// buffer's range check makes rows past the end, and the columns past D, read as
-// zeros.
-template <int ROWS, int DP, int THREADS, bool EIGHT>
+// Rows of a matrix of 8 bits on their way into an LDS tile of ROWS x DP: fetched into
+// the registers of a workgroup, or a wave (THREADS 64), eight columns a chunk, and
+// decoded and stored by arrive(). The buffer's range check makes rows past the end,
+// and the columns past D, read as zeros.
+template <int ROWS, int DP, int THREADS>
 struct StagedTile {
   static constexpr int CH = DP / 8, N = ROWS * CH / THREADS;
-  typename std::conditional<EIGHT, u2, u4>::type r[N];
+  u2 r[N];
   int voff0, step;  // chunk i of a thread: voff0 + i step
   const uint8_t *base, *at;
   uint32_t pitch;
@@ -130,52 +129,34 @@ struct StagedTile {
 
   // first: element of row 0 (of the sequence) and column 0 (of the head)
   __device__ __forceinline__ void init(const void* data, int64_t first, int64_t ld, int D, int format) {
-    const int es = EIGHT ? 1 : fmt_bytes(format);
     fmt = format;
-    at = base = (const uint8_t*)data + first * es;
-    pitch = (uint32_t)(ld * es);
-    bytes_d = D * es;
+    at = base = (const uint8_t*)data + first;
+    pitch = (uint32_t)ld;
+    bytes_d = D;
     const int me = (int)threadIdx.x % THREADS, row = me / CH, ch = me % CH;
     step = THREADS / CH * (int)pitch;
     // (past the end of any buffer: a tile's rows span less than 2^31 bytes)
-    voff0 = ch * 8 < D ? row * (int)pitch + ch * 8 * es : (int)0x80000000;
+    voff0 = ch * 8 < D ? row * (int)pitch + ch * 8 : (int)0x80000000;
   }
   // The next tile starts at row0 (of a matrix `skip` elements on).
-  __device__ __forceinline__ void seek(int64_t row0, int64_t skip = 0) {
-    at = base + row0 * pitch + skip * (EIGHT ? 1 : fmt_bytes(fmt));
-  }
+  __device__ __forceinline__ void seek(int64_t row0, int64_t skip = 0) { at = base + row0 * pitch + skip; }
   __device__ __forceinline__ void skip(int64_t rows) { at += rows * pitch; }
   // Loads the next tile, of which `left` rows are there, and moves on by a tile.
   __device__ __forceinline__ void begin(int left, uint8_t*, int) {
     const uint32_t bytes = left > 0 ? (uint32_t)(min(left, ROWS) - 1) * pitch + (uint32_t)bytes_d : 0u;
     const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, (int)bytes, 0x00027000);
     at += (uint64_t)pitch * ROWS;
-    if constexpr (EIGHT) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b64(rs, voff0 + i * step, 0, 0);
-    } else if (fmt == kF16) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, voff0 + i * step, 0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const u2 v = __builtin_amdgcn_raw_buffer_load_b64(rs, voff0 + i * step, 0, 0);
-        r[i] = u4{v[0], v[1], 0u, 0u};
-      }
-    }
+    for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b64(rs, voff0 + i * step, 0, 0);
   }
   __device__ __forceinline__ void issue(int) const {}
   __device__ __forceinline__ void arrive(uint8_t* lds) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = (int)threadIdx.x % THREADS + i * THREADS;
-      *(u4*)(lds + tile_off<DP>(c / CH, c % CH)) = value(i);
+      const u4 codes = {r[i][0], r[i][1], 0u, 0u};
+      *(u4*)(lds + tile_off<DP>(c / CH, c % CH)) = fmt == kE4M3 ? to_f16x8(kE4M3, codes) : to_f16x8(kE5M2, codes);
     }
-  }
-  // chunk i as F16
-  __device__ __forceinline__ u4 value(int i) const {
-    if constexpr (EIGHT) return fmt == kE4M3 ? to_f16x8(kE4M3, u4{r[i][0], r[i][1], 0u, 0u}) : to_f16x8(kE5M2, u4{r[i][0], r[i][1], 0u, 0u});
-    else return to_f16x8(fmt, r[i]);
   }
 };
 
@@ -280,7 +261,7 @@ struct WaveTile {
 };
 // A tile whose matrix is F16, or has 8 bits.
 template <bool F16, int ROWS, int DP>
-using Tile = typename std::conditional<F16, DirectTile<ROWS, DP>, StagedTile<ROWS, DP, 256, true>>::type;
+using Tile = typename std::conditional<F16, DirectTile<ROWS, DP>, StagedTile<ROWS, DP, 256>>::type;
 
 // Operand with one row of the tile a lane (rows row0 + (lane & 31)), k = columns
 // 16 ks + 8 h ...
@@ -376,22 +357,9 @@ __device__ __forceinline__ h8 finite_part(h8 v) {
 
 // A pair that the mask does not admit has weight 0, and 0 * Inf must add
 // nothing. Only tiles that a mask cuts hold such pairs next to admitted ones. A
-// tile of those that holds an infinity or NaN is marked while it is stored
-// (`flag`: the tile's number, so it needs no clearing); its finite part is then
-// multiplied as usual, and the rest added pair by pair.
-template <int ROWS, int DP, int THREADS, bool EIGHT>
-__device__ __forceinline__ bool any_not_finite(const StagedTile<ROWS, DP, THREADS, EIGHT>& t) {
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < t.N; ++i) bad |= not_finite(__builtin_bit_cast(h8, t.value(i)));
-  return bad;
-}
-template <int ROWS, int DP, int THREADS, bool EIGHT>
-__device__ __forceinline__ void mark_not_finite(const StagedTile<ROWS, DP, THREADS, EIGHT>& t, int* flag, int number) {
-  if (any_not_finite(t)) *flag = number;
-}
-
-// The same for a tile in LDS (256 threads, whose barrier the caller owes).
+// tile of those that holds an infinity or NaN is marked (`flag`: the tile's number, so
+// it needs no clearing; 256 threads, whose barrier the caller owes); its finite part is
+// then multiplied as usual, and the rest added pair by pair.
 template <int ROWS, int DP>
 __device__ __forceinline__ void mark_not_finite(const uint8_t* tile, int* flag, int number) {
   bool bad = false;

@@ -337,8 +337,8 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnParams p, int tile
   const Query q = query_at(p, sq, at.hk, col0 + (lane & 31), ncols);
   int begin, end;
   key_range(p, sq, min(col0 + 31, ncols - 1), split, TK, begin, end);
-  typename std::conditional<K16, WaveTile<DP>, StagedTile<32, DP, 64, true>>::type lk;
-  typename std::conditional<V16, WaveTile<DP>, StagedTile<32, DP, 64, true>>::type lv;
+  typename std::conditional<K16, WaveTile<DP>, StagedTile<32, DP, 64>>::type lk;
+  typename std::conditional<V16, WaveTile<DP>, StagedTile<32, DP, 64>>::type lv;
   lk.init(p.k, sq.k0 * p.ldk + (int64_t)at.hk * p.D, p.ldk, p.D, p.k_fmt);
   lv.init(p.v, sq.k0 * p.ldv + (int64_t)at.hk * p.D, p.ldv, p.D, p.v_fmt);
   const int key0 = begin + 32 * wave;
