@@ -471,7 +471,9 @@ typedef struct {
     int32_t causal;      /* 1: query i of a sequence of L_q queries and L_k keys sees the keys
                             j <= i + L_k - L_q (the last query sees all of them) */
     int64_t batch;       /* sequences */
-    float softmax_scale; /* alpha > 0, finite: the scores are alpha * q . k of the true values */
+    float softmax_scale; /* alpha > 0, finite: the scores are alpha * q . k of the true values. Their
+                            factor alpha s_q s_k log2(e) is held to [2^-100, 2^80], past which every
+                            probability is that of equal scores, or of the largest alone */
     const int64_t* q_start; /* optional device [batch + 1], not decreasing: sequence b has the rows
                             q_start[b] ... q_start[b + 1] - 1 of q; NULL: rows / batch each.
                             Rows that belong to no sequence are left as they were */
@@ -522,8 +524,9 @@ scalify_status scalify_attention_fwd(const scalify_scaled_array* q, const scalif
                                      void* stream);
 
 /* Bytes of device workspace scalify_attention_bwd needs: a 256-byte header, 2
- * fp32 numbers per query row and head and 1 per key row and head, and with AMAX
- * the fp32 gradients. 0 for invalid arguments. */
+ * fp32 numbers per query row and head and 1 per key row and head, with AMAX the
+ * fp32 gradients, and where the keys are too few to occupy the device, up to 16 fp32
+ * copies of dk and dv that are then summed in order. 0 for invalid arguments. */
 size_t scalify_attention_bwd_workspace_size(int64_t rows_q, int64_t rows_k,
                                             const scalify_attention_opts* opts, int32_t rescale);
 
@@ -537,6 +540,8 @@ size_t scalify_attention_bwd_workspace_size(int64_t rows_q, int64_t rows_k,
  *   AMAX: e_r = floor(log2 amax of its data) - target_log2 (0 for amax 0 / Inf / all
  *   NaN), NONE: e_r = 0; e_out = clamp(propagated + e_r, -127, 127).
  * amax_out: optional device fp32 [3], the statistics of dq, dk and dv.
+ * lse is fp32, so a P is off by 2^-23 |lse_i| of itself: meant for |lse| up to 2^14
+ * or so, where that is F16's rounding.
  * Rows of k past k_len get zeros. P is rounded to F16 as 2^14 P, dS to F16 times a
  * power of two that a bound of its largest magnitude in the sequence and head,
  * 2 max |dO_i| max |v_j|, gives.

@@ -409,6 +409,28 @@ def _struct_or_none(x: Optional[ScaledArray]):
     return ctypes.byref(x.c_struct()) if x is not None else None
 
 
+def _check_operands(arrays, tensors, vectors=(), stream=None):
+    """The memory of a call: codes in their format's storage type, contiguous fp32
+    tensors of their sizes (`vectors`: pairs of a tensor or None and its size), all on
+    the device of the call's stream, whose address space the kernels run in."""
+    dev = torch.device("cuda", torch.cuda.current_device()) if stream is None else stream.device
+    for x in arrays:
+        if x is None:
+            continue
+        if x.data.dtype != STORAGE_DTYPE[x.fmt]:
+            raise ValueError(f"data: {STORAGE_DTYPE[x.fmt]} for format {x.fmt}")
+        if x.data.device != dev or (x.scale is not None and x.scale.device != dev):
+            raise ValueError(f"every array and its scale: on {dev}, the call's device")
+        if x.scale is not None and (x.scale.dtype != torch.float32 or x.scale.numel() != 1):
+            raise ValueError("scale: one fp32")
+    for t, n in vectors:
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n):
+            raise ValueError(f"contiguous fp32 of {n} elements")
+    for t in (*tensors, *(t for t, _ in vectors)):
+        if t is not None and t.device != dev:
+            raise ValueError(f"every tensor: on {dev}, the call's device")
+
+
 def scalify_rmsnorm_fwd(x: ScaledArray, out: ScaledArray, *, residual: ScaledArray = None,
                         sum_out: ScaledArray = None, gamma: torch.Tensor = None, eps: float = 1e-5,
                         row_scale: torch.Tensor = None, block_scale: torch.Tensor = None,
@@ -426,6 +448,7 @@ def scalify_rmsnorm_fwd(x: ScaledArray, out: ScaledArray, *, residual: ScaledArr
     if block_scale is not None and (block_scale.dtype != torch.uint8 or not block_scale.is_contiguous() or
                                     block_scale.numel() != scalify_mx_packed_bytes(R, D)):
         raise ValueError("block_scale: contiguous uint8 [scalify_mx_packed_bytes(R, D)]")
+    _check_operands((x, out, residual, sum_out), (block_scale, row_scale), ((gamma, D), (pre_out, R * D)), stream)
     st = load_library().scalify_rmsnorm_fwd(
         _struct_or_none(x), _struct_or_none(residual), _ptr_or_none(gamma), float(eps),
         _struct_or_none(sum_out), _struct_or_none(out), _ptr_or_none(row_scale),
@@ -448,6 +471,7 @@ def scalify_rmsnorm_bwd(dy: ScaledArray, x: ScaledArray, dx: ScaledArray, *, dsu
     in include/scalify.h."""
     lib = load_library()
     R, D = x.shape
+    _check_operands((dy, x, dx, dsum), (ws,), ((gamma, D), (dgamma, D), (amax_out, 1), (pre_out, R * D)), stream)
     if ws is None:
         ws = _call_workspace(max(scalify_rmsnorm_bwd_workspace_size(R, D), 1), x.data.device, stream)
     st = lib.scalify_rmsnorm_bwd(
@@ -474,19 +498,19 @@ def attention_opts(q: ScaledArray, heads: int, *, kv_heads: int = None, batch: i
                           int(max_q), int(max_k))
 
 
-def _check_lse(lse: Optional[torch.Tensor], rows: int, heads: int):
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() != rows * heads):
-        raise ValueError("lse: contiguous fp32 [heads, rows of q]")
+def _seq_tensors(opts):
+    return tuple(opts.get(k) for k in ("q_start", "k_start", "k_len"))
 
 
 def _call_workspace(nbytes: int, device, stream) -> Optional[torch.Tensor]:
-    """A workspace that lives until the call's work on `stream` is done."""
+    """A workspace of the memory that belongs to `stream`, whose work on it is done
+    before another allocation of that stream gets it."""
     if nbytes == 0:
         return None
-    ws = workspace(nbytes, device)
-    if stream is not None:
-        ws.record_stream(stream)
-    return ws
+    if stream is None:
+        return workspace(nbytes, device)
+    with torch.cuda.stream(stream):
+        return workspace(nbytes, device)
 
 
 def scalify_attention_fwd_workspace_size(rows_q: int, rows_k: int, opts: CAttentionOpts) -> int:
@@ -502,7 +526,7 @@ def scalify_attention_fwd(q: ScaledArray, k: ScaledArray, v: ScaledArray, out: S
     attention_opts."""
     lib = load_library()
     o = attention_opts(q, heads, **opts)
-    _check_lse(lse, q.shape[0], heads)
+    _check_operands((q, k, v, out), (ws, *_seq_tensors(opts)), ((lse, q.shape[0] * heads),), stream)
     if ws is None:
         ws = _call_workspace(scalify_attention_fwd_workspace_size(q.shape[0], k.shape[0], o), q.data.device, stream)
     st = lib.scalify_attention_fwd(_struct_or_none(q), _struct_or_none(k), _struct_or_none(v), _struct_or_none(out),
@@ -525,7 +549,7 @@ def scalify_attention_bwd(dout: ScaledArray, q: ScaledArray, k: ScaledArray, v: 
     optional fp32 [3] device tensor. Further arguments: those of attention_opts."""
     lib = load_library()
     o = attention_opts(q, heads, **opts)
-    _check_lse(lse, q.shape[0], heads)
+    _check_operands((dout, q, k, v, out, dq, dk, dv), (ws, *_seq_tensors(opts)), ((lse, q.shape[0] * heads), (amax_out, 3)), stream)
     if ws is None:
         ws = _call_workspace(scalify_attention_bwd_workspace_size(q.shape[0], k.shape[0], o, rescale),
                              q.data.device, stream)

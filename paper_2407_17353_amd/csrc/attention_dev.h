@@ -398,9 +398,12 @@ __device__ __forceinline__ void store4_any(int fmt, void* base, int64_t e, const
   }
 }
 
-// Factor of the scores in powers of two: alpha s_q s_k log2 e.
+// Factor of the scores in powers of two: alpha s_q s_k log2 e, held to where its
+// inverse and its product with any score are finite (a score of F16 data lies under
+// 2^39 and, where it is not 0, over 2^-48).
 __device__ __forceinline__ float score_factor(const AttnParams& p) {
-  return __builtin_ldexpf(p.alpha * kLog2e, pow2_exponent(p.s_q) + pow2_exponent(p.s_k));
+  const float f = __builtin_ldexpf(p.alpha, pow2_exponent(p.s_q) + pow2_exponent(p.s_k)) * kLog2e;
+  return fminf(fmaxf(f, 0x1p-100f), 0x1p80f);
 }
 
 // Position in the grid of `per_head` workgroups for each (sequence, key head). A

@@ -320,3 +320,27 @@ def test_capture():
         for o in outs:
             assert np.array_equal(lr.codes(o), lr.codes(want[0])) and o.scale.item() == want[0].scale.item()
         run_bwd(dy, E5M2, x, F16, None, ds, fo=E5M2, ws=ws)
+
+
+def test_offsets_past_32_bits():
+    """Rows of one matrix of 5 GB: the results of the same rows side by side."""
+    R, D, ld = 70000, 64, 37000 // 8 * 8
+    st = torch.empty((R, ld), dtype=torch.int16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    def pair(i, t=None):
+        near = sc.ScaledArray(t if t is not None else torch.zeros((R, D), dtype=torch.int16, device=DEV), F16, sc.scale_tensor(i, DEV))
+        far = sc.ScaledArray(st[:, 64 * i:64 * i + 64], F16, sc.scale_tensor(i, DEV))
+        far.data.copy_(near.data)
+        return near, far
+    x, r, d = (pair(i, torch.randn((R, D), generator=g, device=DEV).half().view(torch.int16)) for i in range(3))
+    s, y, dx = (pair(i) for i in range(3, 6))
+    ends = []
+    for i in range(2):
+        dg = torch.empty(D, device=DEV)
+        sc.scalify_rmsnorm_fwd(x[i], y[i], residual=r[i], sum_out=s[i])
+        sc.scalify_rmsnorm_bwd(d[i], s[i], dx[i], dsum=r[i], dgamma=dg)
+        ends.append(dg)
+    torch.cuda.synchronize()
+    for a, b in (s, y, dx):
+        assert torch.equal(a.data, b.data) and a.scale.item() == b.scale.item()
+    assert torch.equal(*ends)
