@@ -323,12 +323,13 @@ def test_capture():
 
 
 def test_offsets_past_32_bits():
-    """Rows of one matrix of 5 GB: the results of the same rows side by side."""
+    """Rows of matrices of 5 GB: the results of the same rows side by side."""
     R, D, ld = 70000, 64, 37000 // 8 * 8
-    st = torch.empty((R, ld), dtype=torch.int16, device=DEV)
+    inputs = torch.empty((R, ld), dtype=torch.int16, device=DEV)
     g = torch.Generator(device=DEV).manual_seed(1)
     def pair(i, t=None):
         near = sc.ScaledArray(t if t is not None else torch.zeros((R, D), dtype=torch.int16, device=DEV), F16, sc.scale_tensor(i, DEV))
+        st = inputs if t is not None else torch.empty_like(inputs)
         far = sc.ScaledArray(st[:, 64 * i:64 * i + 64], F16, sc.scale_tensor(i, DEV))
         far.data.copy_(near.data)
         return near, far
