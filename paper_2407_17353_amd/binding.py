@@ -168,18 +168,22 @@ class ScaledArray:
         d = self.data
         if d.dim() != 2:
             raise ValueError("ScaledArray data must be 2-D")
-        if d.shape[0] * d.shape[1] > 0 and d.stride(1) != 1:
-            raise ValueError("ScaledArray rows must be contiguous")
-        rows, cols = self.shape
-        ld = d.stride(0) if d.numel() else 0
-        return CScaledArray(d.data_ptr() if d.numel() else None,
-                            self.scale.data_ptr() if self.scale is not None else None,
+        rows, cols = d.shape
+        ptr, ld = None, 0
+        if rows * cols:
+            ld, one = d.stride()
+            if one != 1:
+                raise ValueError("ScaledArray rows must be contiguous")
+            ptr = d.data_ptr()
+        if self.trans:
+            rows, cols = cols, rows
+        return CScaledArray(ptr, self.scale.data_ptr() if self.scale is not None else None,
                             int(self.fmt), int(bool(self.trans)), rows, cols, ld)
 
 
 def _stream_handle(stream) -> Optional[int]:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:  # (the handle alone: a torch.cuda.Stream object takes 2.4 us more)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream
 
 
@@ -413,22 +417,26 @@ def _check_operands(arrays, tensors, vectors=(), stream=None):
     """The memory of a call: codes in their format's storage type, contiguous fp32
     tensors of their sizes (`vectors`: pairs of a tensor or None and its size), all on
     the device of the call's stream, whose address space the kernels run in."""
-    dev = torch.device("cuda", torch.cuda.current_device()) if stream is None else stream.device
+    dev = torch.cuda.current_device() if stream is None else stream.device_index
+    where = [t.get_device() for t in tensors if t is not None]
     for x in arrays:
         if x is None:
             continue
-        if x.data.dtype != STORAGE_DTYPE[x.fmt]:
+        if x.data.dtype is not STORAGE_DTYPE[x.fmt]:
             raise ValueError(f"data: {STORAGE_DTYPE[x.fmt]} for format {x.fmt}")
-        if x.data.device != dev or (x.scale is not None and x.scale.device != dev):
-            raise ValueError(f"every array and its scale: on {dev}, the call's device")
-        if x.scale is not None and (x.scale.dtype != torch.float32 or x.scale.numel() != 1):
-            raise ValueError("scale: one fp32")
+        where.append(x.data.get_device())
+        s = x.scale
+        if s is not None:
+            where.append(s.get_device())
+            if s.dtype is not torch.float32 or s.numel() != 1:
+                raise ValueError("scale: one fp32")
     for t, n in vectors:
-        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n):
-            raise ValueError(f"contiguous fp32 of {n} elements")
-    for t in (*tensors, *(t for t, _ in vectors)):
-        if t is not None and t.device != dev:
-            raise ValueError(f"every tensor: on {dev}, the call's device")
+        if t is not None:
+            where.append(t.get_device())
+            if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"contiguous fp32 of {n} elements")
+    if where.count(dev) != len(where):
+        raise ValueError(f"every tensor: on cuda:{dev}, the call's device")
 
 
 def scalify_rmsnorm_fwd(x: ScaledArray, out: ScaledArray, *, residual: ScaledArray = None,
