@@ -170,7 +170,9 @@ __device__ __forceinline__ f16v row_start(const float* rows, int h) {
 // * factor) and dS = P dP need no row number in a register.
 // One wave a SIMD (its results, and the rows, take most of the 512 registers), so
 // what bounds it is the rate at which one wave issues, four clocks an instruction of
-// any kind: 32 products of 32 clocks leave 224 others.
+// any kind: 32 products of 32 clocks leave 224 others. 4 x 4096 causal tokens, 32
+// heads of 128: 1.47 ms, the matrix cores busy for 32 % of it (of 2.3 GHz); of a block's
+// 3290 clocks 910 are waits and 1080 go to 250 vector and 60 LDS instructions.
 // Q16, O16: whether q and dO are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool Q16, bool O16>
 __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tiles) {
@@ -415,7 +417,9 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
 // of 64 keys, with q and dO rows in registers, laid out as dK and dV above: scores
 // and dP of key block b + 1 and the product of block b - 1 while dS of block b is
 // formed. k is read twice, by rows for the scores and by columns for the product a
-// block later, and has three LDS buffers, v two.
+// block later, and has three LDS buffers, v two. The same tokens: 1.06 ms, the matrix
+// cores busy for 34 % (one product after another, its tiles shared by barriers: 1.23).
+// Buffers known at compile time save 15 of a block's 220 instructions and no time (1.10).
 // K16, V16: whether k and v are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool K16, bool V16>
 __global__ __launch_bounds__(256, 1) void attn_dq_kernel(AttnParams p, int tiles) {

@@ -9,7 +9,7 @@
 //
 //   wide (128 columns, 32 a wave; tiles of 64 keys that the waves share):
 //     prompts and training; bound by the matrix cores and the exponentials;
-//   narrow (32 columns; the waves take a quarter each of a tile of 128 keys and
+//   few (32 columns, which each wave holds, with tiles of keys of its own; the waves
 //     are joined at the end): single tokens; bound by reading the cache.
 // Where that leaves the device idle the keys of a sequence are split over
 // workgroups, whose unnormalised results a second kernel joins.
@@ -144,6 +144,8 @@ __device__ __forceinline__ void remove_odd(uint8_t* vt) {
 // three multiply-adds each, in one wave, took the products' 237.) k and v have two
 // LDS buffers each, with one barrier a tile, in its middle: the first block is the
 // last to use the older buffers.
+// 4 x 4096 causal tokens, 32 heads of 128: 650 to 670 us, 825 TFLOP/s, where the card's
+// power lowers its clock to 1.75 GHz (all-zero inputs: 488); 64 queries a wave 820.
 // K16, V16: whether k and v are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool K16, bool V16>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tiles) {
@@ -436,7 +438,8 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnParams p, int tile
 }
 
 // Joins the splits of a query, a query a workgroup: eight groups of 32 lanes take
-// every eighth split each, four columns a lane, and are added in order.
+// every eighth split each, four columns a lane, and are added in order. (32 heads of 64
+// splits: 7 us; a thread a column that walks the splits took 42.)
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
   __shared__ float4 part[8][32];
   __shared__ float sums[8];
