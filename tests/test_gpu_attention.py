@@ -316,7 +316,25 @@ def test_backward(case):
 def test_backward_dynamic_rescale(name, fg, target):
     """The rescale's statistic, exponent and cast, exactly, on the kernels' own
     fp32 gradients (kept in the workspace), and the values within the bounds."""
-    case = next(c for c in BWD if c["name"] == name)
+    _check_rescale(next(c for c in BWD if c["name"] == name), fg, target)
+
+
+@pytest.mark.parametrize("D,causal", [(64, True), (128, False), (80, True)])
+@pytest.mark.parametrize("B,Lq,Lk,H", [(1, 1100, 70, 8), (2, 500, 200, 4), (1, 2500, 300, 1)])
+def test_backward_many_queries_of_few_keys(B, Lq, Lk, H, D, causal):
+    """Queries that several workgroups share: the sums of their parts in both modes."""
+    say(f"attention bwd parts {B} {Lq} {Lk} {H} {D}")
+    case = _case("parts", B=B, Lq=Lq, Lk=Lk, H=H, Hkv=1, D=D, causal=causal, k_len=[Lk - 3, Lk // 2][:B], fk=E4M3)
+    q, k, v, do = _bwd_inputs(case)
+    res = run_bwd(case, q, k, v, do)
+    check_bwd(case, q, k, v, do, res)
+    assert (res[0][1].data[Lk - 3:Lk] == 0).all() and (res[0][2].data[Lk - 3:Lk] == 0).all()
+    again = run_bwd(case, q, k, v, do)
+    assert all(np.array_equal(lr.codes(a), lr.codes(b)) for a, b in zip(res[0], again[0]))
+    _check_rescale(case, E5M2, 0)
+
+
+def _check_rescale(case, fg, target):
     q, k, v, do = _bwd_inputs(case, E5M2, heavy=True)
     res = run_bwd(case, q, k, v, do, fdo=E5M2, fg=fg, mode=sc.RESCALE_AMAX, target_log2=target)
     check_bwd(case, q, k, v, do, res, fg)
