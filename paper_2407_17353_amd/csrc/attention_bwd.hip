@@ -97,28 +97,6 @@ __device__ __forceinline__ void fold_amax(uint32_t* word, float a) {
     __hip_atomic_fetch_max(word, __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// One gradient row's block of 32 columns times f, to codes or fp32; returns the
-// largest magnitude.
-template <int DP>
-__device__ __forceinline__ float store_block(const f16v& acc, float f, int d, int h, int D, float* f32, void* codes, int fmt,
-                                             int64_t e32, int64_t e, int shift, bool sat) {
-  float a = 0.0f;
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const int n = 32 * d + 8 * g + 4 * h;
-    if (n >= D) continue;
-    float y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[i] = acc[4 * g + i] * f;
-      a = fmaxf(a, fabsf(y[i]));  // (fmaxf skips NaN)
-    }
-    if (f32) *(float4*)(f32 + e32 + n) = make_float4(y[0], y[1], y[2], y[3]);
-    else store4_any(fmt, codes, e + n, y, shift, sat);
-  }
-  return a;
-}
-
 // Exponents of the propagated scales of dq, dk, dv.
 __device__ __forceinline__ void grad_exponents(const AttnParams& p, int (&e)[3]) {
   const int eo = pow2_exponent(p.s_do), ev = pow2_exponent(p.s_v);
@@ -394,20 +372,23 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   }
   int e[3];
   grad_exponents(p, e);
-  float mk = 0.0f, mv = 0.0f;
-  if (key < kext) {
-    const float fk = __builtin_ldexpf(p.alpha, -E), fv = pow2_float(-(int)kProbLog2);
-    const int64_t c = (int64_t)at.hk * p.D, e32 = krow * p.Hkv * p.D + c, half = p.rows_k * p.Hkv * p.D;
-    float* const dk32 = p.parts > 1 ? p.part + 2 * part * half : p.dk32;
-    float* const dv32 = p.parts > 1 ? dk32 + half : p.dv32;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      mk = fmaxf(mk, store_block<DP>(ak[d], fk, d, h, p.D, dk32, p.dk, p.dk_fmt, e32, krow * p.lddk + c,
-                                     clamp_e8m0(e[1]) - e[1], p.sat != 0));
-      mv = fmaxf(mv, store_block<DP>(av[d], fv, d, h, p.D, dv32, p.dv, p.dv_fmt, e32, krow * p.lddv + c,
-                                     clamp_e8m0(e[2]) - e[2], p.sat != 0));
-    }
-  }
+  const float fk = __builtin_ldexpf(p.alpha, -E), fv = pow2_float(-(int)kProbLog2);
+  const int64_t c = (int64_t)at.hk * p.D, half = p.rows_k * p.Hkv * p.D, row0 = sq.k0 + j0 + 32 * wave;
+  float* const dk32 = p.parts > 1 ? p.part + 2 * part * half : p.dk32;
+  float* const dv32 = p.parts > 1 ? dk32 + half : p.dv32;
+  auto place = [&](int64_t ld) {
+    return [&, ld](int r, int64_t& e32, int64_t& x) {
+      e32 = (row0 + r) * p.Hkv * p.D + c;
+      x = (row0 + r) * ld + c;
+    };
+  };
+  const int rows_here = min(32, kext - j0 - 32 * wave);
+  uint8_t* const stage = lds + wave * (32 * DP * 4);
+  __syncthreads();  // (the tiles have been read)
+  const float mk = store_rows<DP>(stage, ak, fk, lane, rows_here, p.D, dk32, p.dk, p.dk_fmt, clamp_e8m0(e[1]) - e[1], p.sat != 0,
+                                  place(p.lddk));
+  const float mv = store_rows<DP>(stage, av, fv, lane, rows_here, p.D, dv32, p.dv, p.dv_fmt, clamp_e8m0(e[2]) - e[2], p.sat != 0,
+                                  place(p.lddv));
   if (p.parts > 1) return;  // (attn_parts_kernel forms the sums' magnitudes)
   fold_amax(p.amax + 1, mk);
   fold_amax(p.amax + 2, mv);
@@ -589,15 +570,15 @@ __global__ __launch_bounds__(256, 1) void attn_dq_kernel(AttnParams p, int tiles
   wait_loads();  // (none may reach LDS after the workgroup has ended)
   int e[3];
   grad_exponents(p, e);
-  float mq = 0.0f;
-  if (live) {
-    const float f = __builtin_ldexpf(p.alpha, -E);
-    const int64_t c = (int64_t)head * p.D;
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-      mq = fmaxf(mq, store_block<DP>(acc[d], f, d, h, p.D, p.dq32, p.dq, p.dq_fmt, qrow * p.H * p.D + c,
-                                     qrow * p.lddq + c, clamp_e8m0(e[0]) - e[0], p.sat != 0));
-  }
+  const int64_t wave0 = col0 + 32 * wave;
+  __syncthreads();  // (the tiles have been read)
+  const float mq = store_rows<DP>(lds + wave * (32 * DP * 4), acc, __builtin_ldexpf(p.alpha, -E), lane, (int)min((int64_t)32, ncols - wave0),
+                                  p.D, p.dq32, p.dq, p.dq_fmt, clamp_e8m0(e[0]) - e[0], p.sat != 0,
+                                  [&](int r, int64_t& e32, int64_t& x) {
+                                    const int i = (int)(wave0 + r) / p.G, hd = at.hk * p.G + (int)(wave0 + r) - i * p.G;
+                                    e32 = (sq.q0 + i) * p.H * p.D + (int64_t)hd * p.D;
+                                    x = (sq.q0 + i) * p.lddq + (int64_t)hd * p.D;
+                                  });
   fold_amax(p.amax, mq);
 }
 

@@ -355,6 +355,65 @@ __device__ __forceinline__ h8 finite_part(h8 v) {
   return __builtin_bit_cast(h8, w);
 }
 
+// A wave's result of 32 rows (a row a lane pair, columns over the registers) times f,
+// 0 where f is, through `lds` (32 rows of DP floats, the wave's own) so that whole rows
+// are stored: to fp32 where f32 is given, else to codes. place(row, e32, e): the element
+// of a row's first column in either. Returns the largest magnitude of the lane's row.
+// (Stored from the registers, 16 bytes of 32 rows at a time, dK and dV of 128 keys
+// took 26000 clocks, as much as the products of six tiles.)
+template <int DP, typename PlaceOf>
+__device__ __forceinline__ float store_rows(uint8_t* lds, const f16v (&acc)[DP / 32], float f, int lane, int rows, int D, float* f32,
+                                            void* codes, int fmt, int shift, bool sat, PlaceOf place) {
+  constexpr int CH = DP / 16, MASK = DP / 4 - 1;
+  const int h = lane >> 5, r = lane & 31;
+  float a = 0.0f;
+  wave_sync();
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[i] = f == 0.0f ? 0.0f : acc[d][4 * g + i] * f;
+        a = fmaxf(a, fabsf(y[i]));  // (fmaxf skips NaN)
+      }
+      *(float4*)(lds + r * DP * 4 + (((8 * d + 2 * g + h) ^ (r & MASK)) << 4)) = make_float4(y[0], y[1], y[2], y[3]);
+    }
+  wave_sync();
+  const bool fast = shift >= kFastShiftMinSub && shift <= kFastShiftMax;
+  const float scale = fast ? pow2_float(shift) : 1.0f;
+  const int c = lane % CH;
+#pragma unroll 1
+  for (int row = lane / CH; row < 32; row += 64 / CH) {
+    if (row >= rows || 16 * c >= D) continue;
+    int64_t e32, e;
+    place(row, e32, e);
+    uint32_t u[16], w[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const u4 x = *(const u4*)(lds + row * DP * 4 + (((4 * c + k) ^ (row & MASK)) << 4));
+      u[4 * k] = x[0];
+      u[4 * k + 1] = x[1];
+      u[4 * k + 2] = x[2];
+      u[4 * k + 3] = x[3];
+      if (f32) *(u4*)(f32 + e32 + 16 * c + 4 * k) = x;
+    }
+    if (f32) continue;
+    if (fmt == kF16) {
+      encode16<kF16>(u, shift, scale, fast, sat, w);
+      store_words16<kF16>(codes, e + 16 * c, w);
+    } else if (fmt == kE4M3) {
+      encode16<kE4M3>(u, shift, scale, fast, sat, w);
+      store_words16<kE4M3>(codes, e + 16 * c, w);
+    } else {
+      encode16<kE5M2>(u, shift, scale, fast, sat, w);
+      store_words16<kE5M2>(codes, e + 16 * c, w);
+    }
+  }
+  return r < rows ? a : 0.0f;
+}
+
 // A pair that the mask does not admit has weight 0, and 0 * Inf must add
 // nothing. Only tiles that a mask cuts hold such pairs next to admitted ones. A
 // tile of those that holds an infinity or NaN is marked (`flag`: the tile's number, so
@@ -410,10 +469,12 @@ __device__ __forceinline__ float score_factor(const AttnParams& p) {
 // head's workgroups read the same rows (keys, or the queries of the backward) while
 // they run side by side, so they go to one XCD, whose L2 then serves them:
 // workgroups are dealt to the eight XCDs in turn, and where the heads are a
-// multiple of 8, XCD x takes heads x, x + 8, ... one after the other. (With heads
-// dealt out first, the rows of 16 heads at once missed L2: attention of 4 x 4096
-// tokens, 32 heads of 128: backward 2993 us against 2884, forward 667 and 672.) Else
-// the head runs fastest.
+// multiple of 8, XCD x takes heads x, x + 8, ..., four at a time and of these the
+// longest workgroups first. (4 x 4096 causal tokens, 32 heads of 128: forward 672 us
+// with one head at a time, whose last workgroups find CUs busy with long ones, 664
+// with two, 641 with four, 644 with eight, 662 with all 16; dK and dV 1517, 1481, 1474
+// and 1486 us with one, two, four and eight.) Else the head runs fastest.
+constexpr int kHeadsAtOnce = 4;
 struct Place {
   int64_t b;
   int hk;
@@ -424,9 +485,10 @@ __device__ __forceinline__ Place attn_place(const AttnParams& p, int64_t per_hea
   int64_t bh;
   Place w;
   if ((heads & 7) == 0) {
-    const int64_t s = id >> 3, group = s / per_head;
-    w.rest = s - group * per_head;
-    bh = 8 * group + (id & 7);
+    const int64_t s = id >> 3, group = s / (per_head * kHeadsAtOnce);
+    const int64_t r = s - group * per_head * kHeadsAtOnce, n = min((int64_t)kHeadsAtOnce, heads / 8 - group * kHeadsAtOnce);
+    w.rest = r / n;
+    bh = 8 * (group * kHeadsAtOnce + r - w.rest * n) + (id & 7);
   } else {
     w.rest = id / heads;
     bh = id - w.rest * heads;

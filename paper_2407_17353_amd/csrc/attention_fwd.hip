@@ -307,11 +307,16 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
     wait_loads();  // (none may reach LDS after the workgroup has ended)
   }
   l += other_half(l, h);
-  if (q.live) {
-#pragma unroll
-    for (int d = 0; d < DB; ++d) store_result(p, acc[d], q, d, h, l, split);
-    if (h == 0) store_row(p, q, m, l, split);
-  }
+  if (q.live && h == 0) store_row(p, q, m, l, split);
+  const int64_t wave0 = col0 + 32 * wave;
+  const bool part = p.splits > 1;
+  __syncthreads();  // (the tiles have been read)
+  store_rows<DP>(lds + wave * (32 * DP * 4), acc, part ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l), lane, (int)min((int64_t)32, ncols - wave0),
+                 p.D, part ? p.part_o : nullptr, p.out, p.out_fmt, 0, p.sat != 0, [&](int r, int64_t& e32, int64_t& x) {
+                   const int i = (int)(wave0 + r) / p.G, hd = at.hk * p.G + (int)(wave0 + r) - i * p.G;
+                   e32 = ((split * p.rows_q + sq.q0 + i) * p.H + hd) * (int64_t)p.D;
+                   x = (sq.q0 + i) * p.ldo + (int64_t)hd * p.D;
+                 });
 }
 
 // Few queries: 32 columns, which each wave holds; every fourth block of 32 keys is a
