@@ -56,7 +56,7 @@ __device__ __forceinline__ Seq load_seq(const AttnParams& p, int64_t b) {
     s.q0 = clamp64(p.q_start[b], 0, p.rows_q);
     q1 = clamp64(p.q_start[b + 1], s.q0, p.rows_q);
   } else {
-    const int64_t n = p.rows_q / p.batch;
+    const int64_t n = (uint32_t)p.rows_q / (uint32_t)p.batch;  // (both at most 2^30)
     s.q0 = b * n;
     q1 = s.q0 + n;
   }
@@ -64,7 +64,7 @@ __device__ __forceinline__ Seq load_seq(const AttnParams& p, int64_t b) {
     s.k0 = clamp64(p.k_start[b], 0, p.rows_k);
     k1 = clamp64(p.k_start[b + 1], s.k0, p.rows_k);
   } else {
-    const int64_t n = p.rows_k / p.batch;
+    const int64_t n = (uint32_t)p.rows_k / (uint32_t)p.batch;
     s.k0 = b * n;
     k1 = s.k0 + n;
   }
@@ -480,21 +480,22 @@ struct Place {
   int hk;
   int64_t rest;
 };
-__device__ __forceinline__ Place attn_place(const AttnParams& p, int64_t per_head) {
-  const int64_t heads = p.batch * p.Hkv, id = blockIdx.x;
-  int64_t bh;
+__device__ __forceinline__ Place attn_place(const AttnParams& p, int64_t in_head) {
+  // (32 bits: the grid has less than 2^31 workgroups)
+  const uint32_t heads = (uint32_t)(p.batch * p.Hkv), per_head = (uint32_t)in_head, id = blockIdx.x;
+  uint32_t bh;
   Place w;
   if ((heads & 7) == 0) {
-    const int64_t s = id >> 3, group = s / (per_head * kHeadsAtOnce);
-    const int64_t r = s - group * per_head * kHeadsAtOnce, n = min((int64_t)kHeadsAtOnce, heads / 8 - group * kHeadsAtOnce);
+    const uint32_t s = id >> 3, group = s / (per_head * kHeadsAtOnce);
+    const uint32_t r = s - group * per_head * kHeadsAtOnce, n = min((uint32_t)kHeadsAtOnce, heads / 8 - group * kHeadsAtOnce);
     w.rest = r / n;
-    bh = 8 * (group * kHeadsAtOnce + r - w.rest * n) + (id & 7);
+    bh = 8 * (group * kHeadsAtOnce + r - (uint32_t)w.rest * n) + (id & 7);
   } else {
     w.rest = id / heads;
-    bh = id - w.rest * heads;
+    bh = id - (uint32_t)w.rest * heads;
   }
-  w.b = bh / p.Hkv;
-  w.hk = (int)(bh - w.b * p.Hkv);
+  w.b = bh / (uint32_t)p.Hkv;
+  w.hk = (int)(bh - (uint32_t)w.b * p.Hkv);
   return w;
 }
 
