@@ -172,8 +172,6 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   const int first = !have ? 0x7FFFFFFF : (p.causal ? key - behind : 0);  // first query that sees this key
   const int64_t krow = sq.k0 + key;
   h8 kf[KS], vf[KS];
-  load_row_operands(p.k_fmt, p.k, krow * p.ldk + (int64_t)at.hk * p.D, h, p.D, have, kf);
-  load_row_operands(p.v_fmt, p.v, krow * p.ldv + (int64_t)at.hk * p.D, h, p.D, have, vf);
   // queries that see any of the keys, in whole tiles, head after head
   const int q_lo = p.causal ? max(0, j0 - behind) / TQ * TQ : 0;
   const int nt = j0 < sq.lk && q_lo < sq.lq ? (sq.lq - q_lo + TQ - 1) / TQ : 0;
@@ -232,8 +230,22 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
     begin(lds);
 #pragma unroll
     for (int i = 0; i < KS; ++i) issue(i);
-    for (int i = threadIdx.x; i < 2 * TQ * DP / 8; i += 256) ((u4*)(lds + 4 * BUF))[i] = u4{0u, 0u, 0u, 0u};  // (the block before the first)
   }
+  // The keys' own rows: F16 through the two buffers that are still free, in whole rows.
+  // (Loaded as operands, 16 bytes of 32 rows at a time, they took 15000 clocks.)
+  const bool k16 = p.k_fmt == kF16, v16 = p.v_fmt == kF16;
+  auto fetch = [&](const void* x, int64_t ld, uint8_t* to) {
+    DirectTile<2 * TQ, DP> own;
+    own.init(x, sq.k0 * ld + (int64_t)at.hk * p.D, ld, p.D, kF16);
+    own.seek(j0);
+    own.begin(sq.lk - j0, to, wave);
+#pragma unroll
+    for (int i = 0; i < own.N; ++i) own.issue(i);
+  };
+  if (k16) fetch(p.k, p.ldk, lds + 2 * BUF);
+  else load_row_operands(p.k_fmt, p.k, krow * p.ldk + (int64_t)at.hk * p.D, h, p.D, have, kf);
+  if (v16) fetch(p.v, p.ldv, lds + 4 * BUF);
+  else load_row_operands(p.v_fmt, p.v, krow * p.ldv + (int64_t)at.hk * p.D, h, p.D, have, vf);
   if (threadIdx.x == 0) odd = -1;
   float nd2 = 0.0f;
   for (int g = g0; g < g_end; ++g)
@@ -241,6 +253,15 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   const float nv2 = block_max(p.nv2 + (int64_t)at.hk * p.rows_k + sq.k0 + j0, max(0, min(128, sq.lk - j0)), red);
   const int E = ds_exponent(nd2, nv2);
   const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2), inv_c1 = 1.0f / c1;
+  wait_loads();
+  __syncthreads();
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    if (k16) kf[ks] = row_operand<DP>(lds + 2 * BUF, 32 * wave, ks, lane);
+    if (v16) vf[ks] = row_operand<DP>(lds + 4 * BUF, 32 * wave, ks, lane);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * TQ * DP / 8; i += 256) ((u4*)(lds + 4 * BUF))[i] = u4{0u, 0u, 0u, 0u};  // (the block before the first)
   auto arrive = [&](int n) {
     lq.arrive(lds + n * 2 * BUF);
     ld.arrive(lds + n * 2 * BUF + BUF);
