@@ -149,8 +149,8 @@ __device__ __forceinline__ f16v row_start(const float* rows, int h) {
 // One wave a SIMD (its results, and the rows, take most of the 512 registers), so
 // what bounds it is the rate at which one wave issues, four clocks an instruction of
 // any kind: 32 products of 32 clocks leave 224 others. 4 x 4096 causal tokens, 32
-// heads of 128: 1.47 ms, the matrix cores busy for 32 % of it (of 2.3 GHz); of a block's
-// 3290 clocks 910 are waits and 1080 go to 250 vector and 60 LDS instructions.
+// heads of 128: 1.30 to 1.35 ms, the matrix cores busy for 36 % of it (at 2.3 GHz): a
+// tile takes 4360 clocks of the loop, 2048 of them its products.
 // Q16, O16: whether q and dO are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool Q16, bool O16>
 __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tiles) {
@@ -419,8 +419,8 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
 // of 64 keys, with q and dO rows in registers, laid out as dK and dV above: scores
 // and dP of key block b + 1 and the product of block b - 1 while dS of block b is
 // formed. k is read twice, by rows for the scores and by columns for the product a
-// block later, and has three LDS buffers, v two. The same tokens: 1.06 ms, the matrix
-// cores busy for 34 % (one product after another, its tiles shared by barriers: 1.23).
+// block later, and has three LDS buffers, v two. The same tokens: 1.00 to 1.04 ms, the
+// matrix cores busy for 35 % (one product after another, its tiles shared by barriers: 1.23).
 // Buffers known at compile time save 15 of a block's 220 instructions and no time (1.10).
 // K16, V16: whether k and v are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool K16, bool V16>
@@ -734,8 +734,8 @@ static void launch(const AttnParams& p, hipStream_t s) {
 // Where the workgroups of 128 keys leave CUs without one, the queries (tiles of 64, of
 // all the heads that share the keys) are split among several, four tiles or more each,
 // as far as there are 256. (1777 tokens of 3 sequences, 16 heads on 4 of keys: dK and dV
-// took 123 us unsplit, 55 in 3 parts and 19 for their sum; up to 512 workgroups 56
-// and 27, up to 1024 72 and 35.)
+// took 123 us unsplit, 55 in 3 parts; up to 512 workgroups 56, up to 1024 72, and the
+// sum of the parts 19, 27 and 35. Now 51 and 12.)
 int attention_bwd_parts(int64_t batch, int Hkv, int G, int64_t max_q, int64_t max_k) {
   const int64_t groups = batch * Hkv * ((max_k + 127) / 128), tiles = (max_q + 63) / 64 * G;
   int64_t s = groups > 0 ? 256 / groups : 1;

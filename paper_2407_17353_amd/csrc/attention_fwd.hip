@@ -144,8 +144,9 @@ __device__ __forceinline__ void remove_odd(uint8_t* vt) {
 // three multiply-adds each, in one wave, took the products' 237.) k and v have two
 // LDS buffers each, with one barrier a tile, in its middle: the first block is the
 // last to use the older buffers.
-// 4 x 4096 causal tokens, 32 heads of 128: 650 to 670 us, 825 TFLOP/s, where the card's
-// power lowers its clock to 1.75 GHz (all-zero inputs: 488); 64 queries a wave 820.
+// 4 x 4096 causal tokens, 32 heads of 128: 603 to 640 us, 860 to 910 TFLOP/s, where the
+// card's power lowers its clock (before results were stored by rows 650, all-zero
+// inputs 488 and 64 queries a wave 820).
 // K16, V16: whether k and v are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool K16, bool V16>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tiles) {
