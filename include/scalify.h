@@ -543,8 +543,8 @@ size_t scalify_attention_bwd_workspace_size(int64_t rows_q, int64_t rows_k,
  * lse is fp32, so a P is off by 2^-23 |lse_i| of itself: meant for |lse| up to 2^14
  * or so, where that is F16's rounding.
  * Rows of k past k_len get zeros. P is rounded to F16 as 2^14 P, dS to F16 times a
- * power of two that a bound of its largest magnitude in the sequence and head,
- * 2 max |dO_i| max |v_j|, gives.
+ * power of two that a bound of its largest magnitude among the queries and keys of a
+ * workgroup, 2 max(max |dO_i| max |v_j|, max |delta_i|), gives.
  * dout, q, k, v: E4M3, E5M2 or F16; out: F16 (delta needs more than 8-bit codes
  * keep); dq, dk, dv: E4M3, E5M2 or F16. Shapes, layouts and limits as in the
  * forward; sequences must not share rows. dq, dk and dv must not overlap an

@@ -11,9 +11,11 @@
 // fp32 gradient in memory unless a rescale needs one.
 //
 // F16 operands of the second products: P as 2^14 P, dS as 2^E dS with the power of
-// two that its bound allows, |dS| <= P (|dP| + |delta|) <= 2 max|dO_i| max|v_j|
-// (Cauchy-Schwarz; delta_i is a mean of dP_ij): 2^E dS <= 2^15, so 29 binades below
-// the bound are normal F16 numbers.
+// two that its bound allows, |dS_ij| <= P (|dP_ij| + |delta_i|) <= 2 max(max|dO_i|
+// max|v_j|, max|delta_i|) (Cauchy-Schwarz): 2^E dS <= 2^15, so 29 binades below the
+// bound are normal F16 numbers. delta_i is a mean of dP_ij over every key that the
+// query sees: where a workgroup holds some of these keys (dK and dV), |dO_i| |v_j|
+// of its own does not bound it, and it stands for itself; over all of them (dQ) it does.
 #include "attention_dev.h"
 #include "kernels.h"
 
@@ -61,11 +63,20 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(AttnParams p) {
   }
 }
 
-// E for the largest |dO_i|^2 and |v_j|^2.
-__device__ __forceinline__ int ds_exponent(float nd2, float nv2) {
-  const float n = nd2 * nv2;
+// E for the largest |dO_i|^2 |v_j|^2, or delta_i^2.
+__device__ __forceinline__ int ds_exponent(float n) {
   if (!(n > 0.0f) || !(n < 3.0e38f)) return 0;
   return 14 - ((floor_log2_bits(__float_as_uint(n)) + 2) >> 1);
+}
+
+// Largest value of 256 threads.
+__device__ __forceinline__ float group_max(float a, float (&red)[4]) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) a = fmaxf(a, __shfl_xor(a, off, 64));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
+  __syncthreads();
+  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
 }
 
 // Largest finite value of n floats, over the workgroup (256 threads).
@@ -79,12 +90,28 @@ __device__ __forceinline__ float block_max(const float* x, int64_t n, float (&re
     for (int k = 0; k < 8; ++k)
       if (v[k] < 3.0e38f) a = fmaxf(a, v[k]);
   }
+  return group_max(a, red);
+}
+
+// A thread's share of the largest finite x and |y| of n (at most 2^30) rows each.
+// (Sixteen loads in flight, at the last row's place past it: the backward of 4 x 4096
+// causal tokens, 32 heads of 128, takes 2.49 ms, as it did without y, and took 2.57 with
+// a loop of its own for y, each load behind a branch.)
+__device__ __forceinline__ void rows_max(const float* x, const float* y, int n, float& ax, float& ay) {
+  for (int i = threadIdx.x; i < n; i += 256 * 8) {
+    float v[8], w[8];
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) a = fmaxf(a, __shfl_xor(a, off, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
-  __syncthreads();
-  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    for (int k = 0; k < 8; ++k) {
+      const int at = min(i + 256 * k, n - 1);
+      v[k] = x[at];
+      w[k] = fabsf(y[at]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (v[k] < 3.0e38f) ax = fmaxf(ax, v[k]);
+      if (w[k] < 3.0e38f) ay = fmaxf(ay, w[k]);
+    }
+  }
 }
 
 __device__ __forceinline__ void fold_amax(uint32_t* word, float a) {
@@ -247,11 +274,15 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   if (v16) fetch(p.v, p.ldv, lds + 4 * BUF);
   else load_row_operands(p.v_fmt, p.v, krow * p.ldv + (int64_t)at.hk * p.D, h, p.D, have, vf);
   if (threadIdx.x == 0) odd = -1;
-  float nd2 = 0.0f;
-  for (int g = g0; g < g_end; ++g)
-    nd2 = fmaxf(nd2, block_max(p.nd2 + (int64_t)(at.hk * p.G + g) * p.rows_q + sq.q0 + q_lo, max(0, sq.lq - q_lo), red));
+  float nd2 = 0.0f, dl = 0.0f;
+  for (int g = g0; g < g_end; ++g) {
+    const int64_t rows0 = (int64_t)(at.hk * p.G + g) * p.rows_q + sq.q0 + q_lo;
+    rows_max(p.nd2 + rows0, p.delta + rows0, sq.lq - q_lo, nd2, dl);
+  }
+  nd2 = group_max(nd2, red);
+  dl = group_max(dl, red);
   const float nv2 = block_max(p.nv2 + (int64_t)at.hk * p.rows_k + sq.k0 + j0, max(0, min(128, sq.lk - j0)), red);
-  const int E = ds_exponent(nd2, nv2);
+  const int E = ds_exponent(fmaxf(nd2 * nv2, dl * dl));
   const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2), inv_c1 = 1.0f / c1;
   wait_loads();
   __syncthreads();
@@ -476,7 +507,7 @@ __global__ __launch_bounds__(256, 1) void attn_dq_kernel(AttnParams p, int tiles
   if (!(nd2 < 3.0e38f)) nd2 = 0.0f;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) nd2 = fmaxf(nd2, __shfl_xor(nd2, off, 64));
-  const int E = ds_exponent(nd2, nv2);  // (of this wave)
+  const int E = ds_exponent(nd2 * nv2);  // (of this wave)
   const float c1 = score_factor(p), c2 = pow2_float(E - (int)kProbLog2);
   Dl *= c2;
   f16v acc[DB];

@@ -1,0 +1,71 @@
+"""GPU parity of attention where its sizes, masks and magnitudes meet their
+edges, against the plain 64-bit forms and bounds of tests/layer_refs.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2407_17353_amd import binding as sc
+from tests import layer_refs as lr
+from tests import test_gpu_attention as attn
+from tests.helpers import say
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F16, E4M3, E5M2 = sc.F16, sc.E4M3, sc.E5M2
+
+
+# ---------------------------------------------------------------- magnitudes of v along a sequence
+
+def _lone_last_key(D, small, H=1, Lq=64, n=128, causal=False):
+    """n keys of equal scores and values along one direction, and a last key of about
+    half of every query's weight whose value is `small` of theirs: dS of the last
+    key, -P delta, is far beyond what its own value gives."""
+    case = attn._case("lone", H=H, Hkv=1, D=D, Lq=Lq, Lk=n + 1, causal=causal)
+    g = torch.Generator().manual_seed(D)
+    w = torch.randn(D, generator=g)
+    factor = case["alpha"] * 2.0 ** (case["eq"] + case["ek"])
+    q = 1.0 + 0.01 * torch.randn((Lq, H * D), generator=g)
+    k = 0.01 * torch.randn((n + 1, D), generator=g)
+    k[n] += math.log(n) / (factor * D)
+    v = w + 0.05 * torch.randn((n + 1, D), generator=g)
+    v[n] *= small
+    do = w.repeat(H) + 0.05 * torch.randn((Lq, H * D), generator=g)
+    return case, [t.half() for t in (q, k, v, do)]
+
+
+@pytest.mark.parametrize("small", [2.0 ** -6, 2.0 ** -8, 2.0 ** -12])
+@pytest.mark.parametrize("D,H", [(64, 1), (128, 1), (80, 4)])
+def test_backward_small_value_of_a_heavy_key(D, H, small):
+    say(f"attention bwd lone key {D} {H} {small}")
+    case, t = _lone_last_key(D, small, H)
+    res = attn.run_bwd(case, *t)
+    attn.check_bwd(case, *t, res)
+    assert all(lr.data(x).isfinite().all() for x in res[0])
+
+
+@pytest.mark.parametrize("causal,sq,e", [(False, 1.0, -13), (False, 4.0, -10), (True, 4.0, -13)])
+@pytest.mark.parametrize("D,H,Lq", [(64, 2, 160), (128, 2, 160), (64, 8, 1000)])
+def test_backward_small_values_of_the_last_keys(D, H, Lq, causal, sq, e):
+    """The last of 160 keys' values times 2^e (with 1000 queries of 8 heads a key head: in parts)."""
+    say(f"attention bwd small values {D} {H} {Lq} {causal} {e}")
+    case = attn._case("small", H=H, Hkv=1 if H == 8 else 2, D=D, Lq=Lq, Lk=160, sq=sq, causal=causal)
+    q, k, v, do = attn._bwd_inputs(case)
+    v[128:] *= 2.0 ** e
+    for mode in (sc.RESCALE_NONE, sc.RESCALE_AMAX):
+        attn.check_bwd(case, q, k, v, do, attn.run_bwd(case, q, k, v, do, mode=mode))
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -8, 2.0 ** -12])
+@pytest.mark.parametrize("D,causal", [(64, False), (128, True)])
+def test_backward_keys_without_values(D, causal, scale):
+    """Keys 128 ... 255 of 300 with zeros for values: their dS is -P delta."""
+    say(f"attention bwd no values {D} {scale}")
+    case = attn._case("zeros", H=2, Hkv=1, D=D, Lq=300, Lk=300, causal=causal)
+    q, k, v, do = attn._bwd_inputs(case)
+    v[128:256] = 0
+    do = (do.float() * scale).half()
+    res = attn.run_bwd(case, q, k, v, do, mode=sc.RESCALE_AMAX)
+    attn.check_bwd(case, q, k, v, do, res)
+    assert (res[0][1].data[128:256] != 0).any()
