@@ -500,9 +500,12 @@ __global__ __launch_bounds__(256, 1) void attn_dq_kernel(AttnParams p, int tiles
   if (live) {
     const int64_t row = (int64_t)head * p.rows_q + qrow;
     const float l = p.lse[row];
-    nd2 = p.nd2[row];
-    Dl = p.delta[row];
-    L = l == neg_inf() ? __builtin_inff() : fmaf(l, kLog2e, -kProbLog2);
+    // (a query that sees no key, whose P is 0 throughout, keeps neither norm nor delta: its dO may hold Inf or NaN)
+    if (l != neg_inf()) {
+      nd2 = p.nd2[row];
+      Dl = p.delta[row];
+      L = fmaf(l, kLog2e, -kProbLog2);
+    }
   }
   if (!(nd2 < 3.0e38f)) nd2 = 0.0f;
 #pragma unroll

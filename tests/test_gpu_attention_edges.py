@@ -69,3 +69,24 @@ def test_backward_keys_without_values(D, causal, scale):
     res = attn.run_bwd(case, q, k, v, do, mode=sc.RESCALE_AMAX)
     attn.check_bwd(case, q, k, v, do, res)
     assert (res[0][1].data[128:256] != 0).any()
+
+
+# ---------------------------------------------------------------- rows without keys
+
+@pytest.mark.parametrize("D,H", [(64, 2), (128, 2), (64, 1)])
+@pytest.mark.parametrize("mode", [sc.RESCALE_NONE, sc.RESCALE_AMAX])
+def test_backward_query_without_keys_of_any_value(D, H, mode):
+    """A query that sees no key has no gradient and gives none, whatever q, dO and
+    the rows beside it hold (rows 0 to 9 of 150 queries over 140 keys)."""
+    say(f"attention bwd no keys {D} {H} {mode}")
+    case = attn._case("empty_rows", H=H, Hkv=1, D=D, Lq=150, Lk=140)
+    q, k, v, do = attn._bwd_inputs(case)
+    clean = attn.run_bwd(case, q, k, v, do, mode=mode)
+    q2, d2 = q.clone(), do.clone()
+    q2[0], q2[5, 3], q2[9] = float("nan"), float("inf"), float("nan")
+    d2[1, 2], d2[2], d2[3, 4], d2[9] = float("inf"), float("nan"), float("-inf"), float("nan")
+    got = attn.run_bwd(case, q2, k, v, d2, mode=mode)
+    assert (got[0][0].data[:10] == 0).all()
+    for a, b in zip(got[0], clean[0]):
+        assert np.array_equal(lr.codes(a), lr.codes(b)) and a.scale.item() == b.scale.item()
+    assert torch.equal(got[1], clean[1])
