@@ -414,8 +414,9 @@ scalify_status scalify_layernorm_bwd(const scalify_scaled_array* dy, const scali
  * the very same matrix as x or residual (same data, element size and ld) but must
  * not otherwise overlap them or each other; with a residual an output's scale
  * must not be the memory of an input's scale or the other output's
- * (SCALIFY_ERR_LAYOUT). saturate applies to both casts. Squares of F32 inputs
- * of any magnitude stay in range (the row is divided by a power of two first).
+ * (SCALIFY_ERR_LAYOUT). saturate applies to both casts. Squares of F32 inputs, and
+ * of sums that are not stored, of any magnitude stay in range (the row is
+ * divided by a power of two first).
  * Sums are fp32 in a fixed order: reruns are bit-identical. */
 scalify_status scalify_rmsnorm_fwd(const scalify_scaled_array* x,
                                    const scalify_scaled_array* residual, const float* gamma,

@@ -82,11 +82,17 @@ __device__ __forceinline__ void rms_store_sum(void* sum, int64_t off, int valid,
   ln_decode16<F>(w, h);
 }
 
-// 1 / sqrt(ss / D + eps) of a row, 0 where that is 1 / 0. FP32 rows (RANGE) may
-// hold any magnitude: they are first divided by the power of two 2^k of their
+// Whether the rows of a forward call may hold any magnitude: FP32 ones, and the sum
+// of a residual that no 16- or 8-bit array takes up (its parts lie on scales that may be
+// far apart, and where the larger one's is 0 the other is what is normalised: 16384 x
+// 4096 with row scales 68 us, 65 without the division).
+inline bool rms_ranged(const RmsParams& p) { return p.x_fmt == kF32 || (p.has_res && !p.sum); }
+
+// 1 / sqrt(ss / D + eps) of a row, 0 where that is 1 / 0. Rows that may hold any
+// magnitude (RANGE) are first divided by the power of two 2^k of their
 // largest one, so that no square leaves the range, ss is that of the divided
 // row, and so is the result (rms(h) = 2^k rms(h / 2^k)); in 64 bits, since
-// eps / 2^2k may be any size. (Of 16- and 8-bit inputs, sums included, no
+// eps / 2^2k may be any size. (Of 16- and 8-bit data, stored sums among them, no
 // square or sum of squares leaves the fp32 range.)
 template <bool RANGE>
 __device__ __forceinline__ float rms_inv(float ss, int D, float eps, int k) {
@@ -141,11 +147,11 @@ __device__ __forceinline__ int64_t mx_byte(int64_t r, int b, int64_t groups) {
   return 4 * word + ((r >> 4) & 3);
 }
 
-template <int XF, int WPR, bool FULL>
+// RANGE: of rows of any magnitude (rms_ranged).
+template <int XF, int WPR, bool FULL, bool RANGE>
 __global__ __launch_bounds__(rms_threads(WPR)) void rms_fwd_rows_kernel(RmsParams p) {
 #pragma clang fp contract(off)
   constexpr int RPW = rms_rpw(WPR);
-  constexpr bool RANGE = XF == kF32;
   __shared__ float s1[2][RPW][WPR][1], sm[2][RPW][WPR], sr[2][RPW][WPR];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int slot = wave / WPR, part = wave % WPR;

@@ -3,22 +3,28 @@
 
 namespace scalify {
 
-template <int WPR>
+template <int WPR, bool RANGE>
 static void fwd(const RmsParams& p, hipStream_t s) {
   const int64_t rows = p.block_scale ? (p.R + 63) / 64 * 64 : p.R;
   const dim3 g(rms_grid(rows, WPR, 4)), b(rms_threads(WPR));
-  if (p.D == 1024 * WPR) hipLaunchKernelGGL((rms_fwd_rows_kernel<kF16, WPR, true>), g, b, 0, s, p);
-  else hipLaunchKernelGGL((rms_fwd_rows_kernel<kF16, WPR, false>), g, b, 0, s, p);
+  if (p.D == 1024 * WPR) hipLaunchKernelGGL((rms_fwd_rows_kernel<kF16, WPR, true, RANGE>), g, b, 0, s, p);
+  else hipLaunchKernelGGL((rms_fwd_rows_kernel<kF16, WPR, false, RANGE>), g, b, 0, s, p);
+}
+
+template <bool RANGE>
+static void fwd_rows(const RmsParams& p, hipStream_t s) {
+  switch (rms_wpr(p.D)) {
+    case 1: fwd<1, RANGE>(p, s); break;
+    case 2: fwd<2, RANGE>(p, s); break;
+    case 4: fwd<4, RANGE>(p, s); break;
+    default: fwd<8, RANGE>(p, s); break;
+  }
 }
 
 template <>
 void launch_rms_fwd_rows<kF16>(const RmsParams& p, hipStream_t s) {
-  switch (rms_wpr(p.D)) {
-    case 1: fwd<1>(p, s); break;
-    case 2: fwd<2>(p, s); break;
-    case 4: fwd<4>(p, s); break;
-    default: fwd<8>(p, s); break;
-  }
+  if (rms_ranged(p)) fwd_rows<true>(p, s);
+  else fwd_rows<false>(p, s);
 }
 
 template <int DYF, int WPR>

@@ -7,8 +7,8 @@ template <int WPR>
 static void fwd(const RmsParams& p, hipStream_t s) {
   const int64_t rows = p.block_scale ? (p.R + 63) / 64 * 64 : p.R;
   const dim3 g(rms_grid(rows, WPR, 4)), b(rms_threads(WPR));
-  if (p.D == 1024 * WPR) hipLaunchKernelGGL((rms_fwd_rows_kernel<kF32, WPR, true>), g, b, 0, s, p);
-  else hipLaunchKernelGGL((rms_fwd_rows_kernel<kF32, WPR, false>), g, b, 0, s, p);
+  if (p.D == 1024 * WPR) hipLaunchKernelGGL((rms_fwd_rows_kernel<kF32, WPR, true, true>), g, b, 0, s, p);
+  else hipLaunchKernelGGL((rms_fwd_rows_kernel<kF32, WPR, false, true>), g, b, 0, s, p);
 }
 
 template <>
