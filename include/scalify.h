@@ -482,7 +482,7 @@ typedef struct {
     const int64_t* k_len;   /* optional device [batch]: only the first k_len[b] of sequence b's
                             rows of k and v are keys (a cache that is not full) */
     int64_t max_q;       /* with q_start: no sequence has more queries (0: any number). Rows
-                            past it are left as they were */
+                            past it are left as they were, and count in L_q alone */
     int64_t max_k;       /* with k_start: no sequence has more rows of k (0: any number); the
                             backward leaves rows past it as they were. With k_len, the most
                             keys of a sequence, if that is known (0: it is not): a hint for how

@@ -193,7 +193,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
   const int kext = (int)min((int64_t)sq.kext, p.max_k);
   const int j0 = tile * 128;
   if (j0 >= kext) return;
-  const int behind = sq.lk - sq.lq;
+  const int behind = sq.behind;
   const int key = j0 + 32 * wave + (lane & 31);
   const bool have = key < sq.lk;
   const int first = !have ? 0x7FFFFFFF : (p.causal ? key - behind : 0);  // first query that sees this key
@@ -470,7 +470,7 @@ __global__ __launch_bounds__(256, 1) void attn_dq_kernel(AttnParams p, int tiles
   const bool live = col < ncols;
   const int pos = (int)(col / p.G), head = at.hk * p.G + (int)(col - (int64_t)pos * p.G);
   const int64_t qrow = sq.q0 + pos;
-  const int behind = sq.lk - sq.lq;
+  const int behind = sq.behind;
   const int last = !live ? 0x7FFFFFFF : (p.causal ? min(pos + behind, sq.lk - 1) : sq.lk - 1);
   const int last0 = p.causal ? min((int)(col0 / p.G) + behind, sq.lk - 1) : sq.lk - 1;
   const int64_t last_col = col0 + 128 < ncols ? col0 + 127 : ncols - 1;

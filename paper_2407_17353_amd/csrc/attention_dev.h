@@ -42,7 +42,8 @@ __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 // hold, the rows stay inside the matrices.
 struct Seq {
   int64_t q0, k0;
-  int lq, lk, kext;  // queries, keys, key rows of the sequence (keys past lk are padding)
+  int lq, lk, kext;  // queries (up to max_q), keys, key rows of the sequence (keys past lk are padding)
+  int behind;        // a causal mask lets query i see the keys up to i + behind: lk less all of the sequence's queries
 };
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
@@ -72,6 +73,7 @@ __device__ __forceinline__ Seq load_seq(const AttnParams& p, int64_t b) {
   s.lq = (int)(lq < p.max_q ? lq : p.max_q);
   s.kext = (int)(k1 - s.k0);
   s.lk = p.k_len ? (int)clamp64(p.k_len[b], 0, s.kext) : s.kext;
+  s.behind = s.lk - (int)lq;
   return s;
 }
 

@@ -36,7 +36,7 @@ __device__ __forceinline__ Query query_at(const AttnParams& p, const Seq& sq, in
   const int pos = (int)(col / p.G);
   q.head = hk * p.G + (int)(col - (int64_t)pos * p.G);
   q.row = sq.q0 + pos;
-  q.last = !q.live ? 0x7FFFFFFF : (p.causal ? min(pos + sq.lk - sq.lq, sq.lk - 1) : sq.lk - 1);
+  q.last = !q.live ? 0x7FFFFFFF : (p.causal ? min(pos + sq.behind, sq.lk - 1) : sq.lk - 1);
   return q;
 }
 
@@ -44,7 +44,7 @@ __device__ __forceinline__ Query query_at(const AttnParams& p, const Seq& sq, in
 // them in whole tiles.
 __device__ __forceinline__ void key_range(const AttnParams& p, const Seq& sq, int64_t last_col, int split, int tile, int& begin,
                                           int& end) {
-  const int seen = p.causal ? max(0, min(sq.lk, (int)(last_col / p.G) + sq.lk - sq.lq + 1)) : sq.lk;
+  const int seen = p.causal ? max(0, min(sq.lk, (int)(last_col / p.G) + sq.behind + 1)) : sq.lk;
   const int share = ((seen + p.splits - 1) / p.splits + tile - 1) / tile * tile;
   begin = (int)min((int64_t)split * share, (int64_t)seen);
   end = min(seen, begin + share);
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
   const int64_t ncols = (int64_t)sq.lq * p.G, col0 = (int64_t)tile * 128;
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
   if (col0 >= ncols) return;
-  const int last0 = p.causal ? min((int)(col0 / p.G) + sq.lk - sq.lq, sq.lk - 1) : sq.lk - 1;  // of the first column
+  const int last0 = p.causal ? min((int)(col0 / p.G) + sq.behind, sq.lk - 1) : sq.lk - 1;  // of the first column
   const Query q = query_at(p, sq, at.hk, col0 + 32 * wave + (lane & 31), ncols);
   h8 qf[KS];
   load_row_operands(p.q_fmt, p.q, q.row * p.ldq + (int64_t)q.head * p.D, h, p.D, q.live, qf);

@@ -90,3 +90,30 @@ def test_backward_query_without_keys_of_any_value(D, H, mode):
     for a, b in zip(got[0], clean[0]):
         assert np.array_equal(lr.codes(a), lr.codes(b)) and a.scale.item() == b.scale.item()
     assert torch.equal(got[1], clean[1])
+
+
+@pytest.mark.parametrize("Lq,max_q,Lk", [(100, 40, 130), (70, 8, 300), (90, 1, 60), (300, 140, 300)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_past_max_q(D, Lq, max_q, Lk):
+    """Rows of a sequence past max_q are left out; the others see the keys that
+    their place in the whole sequence gives them."""
+    say(f"attention past max_q {D} {Lq} {max_q} {Lk}")
+    case = attn._case("past", H=2, Hkv=1, D=D, B=2, Tq=2 * Lq, Tk=2 * Lk, q_start=[0, Lq, 2 * Lq], max_q=max_q)
+    q, k, v, do = attn._bwd_inputs(case)
+    res = attn.run_bwd(case, q, k, v, do)
+    out, lse = res[2], res[3]
+    live = torch.zeros(2 * Lq, dtype=torch.bool)
+    live[:max_q] = live[Lq:Lq + max_q] = True
+    o, eo, l, el = lr.attention(q.to(lr.F64), k.to(lr.F64), v.to(lr.F64), 2, 1, case["alpha"] * 2.0 ** (case["eq"] + case["ek"]),
+                                attn._seqs(case), True, F16)
+    assert ((lr.data(out) - o).abs() <= eo)[live].all() and (lr.codes(out)[~live.numpy()] == 0x5A5A).all()
+    m = lse.cpu().to(lr.F64)
+    assert torch.equal(m[:, live].isinf(), l[:, live].isinf()) and (m[:, ~live] == 7.0).all()
+    f = l.isfinite() & live
+    assert ((m - l).abs() <= el)[f].all()
+    do[~live] = 0  # (what a query that is left out gives)
+    want, err = attn._reference(case, q, k, v, do, out, lse)
+    rel, sub = lr.HALF[F16]
+    for x, w, e, rows in zip(res[0], want, err, (live, slice(None), slice(None))):
+        assert ((lr.data(x) - w).abs() <= e + (w.abs() + e) * rel + sub)[rows].all()
+    assert (lr.codes(res[0][0])[~live.numpy()] == 0x5A5A).all()
