@@ -512,7 +512,10 @@ size_t scalify_attention_fwd_workspace_size(int64_t rows_q, int64_t rows_k,
  * of 16 elements (8 for F16) with 128 rows below 2^31 bytes. out must not overlap q, k
  * or v (other columns of rows of the same pitch in bytes are no overlap);
  * out.scale may be v's but not q's or k's. At most 2^30 rows, 2^30 queries times
- * heads that share a key head per sequence, and 2^31 - 1 workgroups (SCALIFY_ERR_SHAPE).
+ * heads that share a key head per sequence, and 2^31 - 1 workgroups (SCALIFY_ERR_SHAPE):
+ * batch * kv_heads times one for each 32 queries and heads, and for each 128 keys, that a
+ * sequence may have. Where many sequences are packed and max_q and max_k are 0, most
+ * of these find no row of theirs; the two bounds spare them.
  * The values of q_start, k_start and k_len are not errors: they are clamped to
  * the matrices' rows. workspace: scalify_attention_fwd_workspace_size bytes (may be
  * NULL when that is 0), 256-byte aligned, not shared with a concurrent call.

@@ -17,6 +17,7 @@ struct AttnParams {
   float alpha;
   const int64_t *q_start, *k_start, *k_len;  // or NULL
   int64_t max_q, max_k;      // bounds of a sequence's rows
+  uint32_t group0;           // number of the launch's first workgroup (launch_groups)
   void* out;                 // forward: codes; backward: the stored output (F16)
   int64_t ldo;
   int out_fmt;
@@ -48,6 +49,23 @@ struct AttnParams {
 };
 
 constexpr int kAttnMaxD = 128;
+
+// A launch holds less than 2^32 threads in a dimension of its grid: `groups`
+// workgroups of 256 go out as launches of 2^23, which leaves a workgroup's XCD what it
+// is in one launch, each with the number of its first one. Stops at an error.
+constexpr int64_t kLaunchGroups = 1 << 23;
+template <typename Kernel, typename... Args>
+hipError_t launch_groups(Kernel kernel, int64_t groups, unsigned y, hipStream_t s, AttnParams p, Args... args) {
+  for (int64_t g = 0; g < groups; g += kLaunchGroups) {
+    const int64_t n = groups - g < kLaunchGroups ? groups - g : kLaunchGroups;
+    p.group0 = (uint32_t)g;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)n, y), dim3(256), 0, s, p, args...);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // Splits of a sequence's keys for the forward, 1 where the grid fills the
 // device without, and a workgroup's query columns: 32 that its four waves share
 // (few queries), or 128.

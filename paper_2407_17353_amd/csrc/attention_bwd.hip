@@ -23,10 +23,10 @@ namespace scalify {
 
 // delta, |dO_i|^2 and |v_j|^2: 16 lanes a row of a head, eight columns each.
 __global__ __launch_bounds__(256) void attn_rows_kernel(AttnParams p) {
-  const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+  const int64_t item = ((int64_t)(p.group0 + blockIdx.x) * 256 + threadIdx.x) >> 4;
   const int lane = threadIdx.x & 15;
   const int64_t nq = p.rows_q * p.H, nk = p.rows_k * p.Hkv;
-  if (blockIdx.x == 0 && threadIdx.x < 3) p.amax[threadIdx.x] = 0u;
+  if (p.group0 + blockIdx.x == 0 && threadIdx.x < 3) p.amax[threadIdx.x] = 0u;
   if (item >= nq + nk) return;
   const bool query = item < nq;
   const int heads = query ? p.H : p.Hkv;
@@ -700,12 +700,13 @@ __global__ __launch_bounds__(256) void attn_grads_kernel(AttnParams p, int64_t t
   const int base = e[which];
   const uint32_t amax = p.amax[which];
   const int e_out = clamp_e8m0(base + (p.mode == 1 ? rescale_exponent(amax, p.target) : 0));
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
+  const uint32_t id = p.group0 + blockIdx.x;
+  if (id == 0 && threadIdx.x == 0) {
     *(which == 0 ? p.dq_scale : which == 1 ? p.dk_scale : p.dv_scale) = pow2_float(e_out);
     if (p.amax_out) p.amax_out[which] = __uint_as_float(amax);
   }
   if (p.mode != 1) return;
-  const int64_t b = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+  const int64_t b = id / tiles, tile = id % tiles;
   const Seq sq = load_seq(p, b);
   const int64_t rows = which == 0 ? sq.lq : min((int64_t)sq.kext, p.max_k);
   const int64_t r0 = tile * ATTN_CAST_ROWS;
@@ -740,31 +741,31 @@ __global__ __launch_bounds__(256) void attn_grads_kernel(AttnParams p, int64_t t
 }
 
 template <int DP>
-static void launch_dkv(const AttnParams& p, dim3 g, int tiles, hipStream_t s) {
+static hipError_t launch_dkv(const AttnParams& p, hipStream_t s) {
   const bool q16 = p.q_fmt == kF16, o16 = p.do_fmt == kF16;
-  if (q16 && o16) hipLaunchKernelGGL((attn_dkv_kernel<DP, true, true>), g, dim3(256), 0, s, p, tiles);
-  else if (q16) hipLaunchKernelGGL((attn_dkv_kernel<DP, true, false>), g, dim3(256), 0, s, p, tiles);
-  else if (o16) hipLaunchKernelGGL((attn_dkv_kernel<DP, false, true>), g, dim3(256), 0, s, p, tiles);
-  else hipLaunchKernelGGL((attn_dkv_kernel<DP, false, false>), g, dim3(256), 0, s, p, tiles);
+  const int tiles = (int)((p.max_k + 127) / 128);
+  const int64_t g = p.rows_k > 0 ? p.batch * p.Hkv * tiles * p.parts : 0;
+  if (q16 && o16) return launch_groups(attn_dkv_kernel<DP, true, true>, g, 1, s, p, tiles);
+  if (q16) return launch_groups(attn_dkv_kernel<DP, true, false>, g, 1, s, p, tiles);
+  if (o16) return launch_groups(attn_dkv_kernel<DP, false, true>, g, 1, s, p, tiles);
+  return launch_groups(attn_dkv_kernel<DP, false, false>, g, 1, s, p, tiles);
 }
 
 template <int DP>
-static void launch_dq(const AttnParams& p, dim3 g, int tiles, hipStream_t s) {
+static hipError_t launch_dq(const AttnParams& p, hipStream_t s) {
   const bool k16 = p.k_fmt == kF16, v16 = p.v_fmt == kF16;
-  if (k16 && v16) hipLaunchKernelGGL((attn_dq_kernel<DP, true, true>), g, dim3(256), 0, s, p, tiles);
-  else if (k16) hipLaunchKernelGGL((attn_dq_kernel<DP, true, false>), g, dim3(256), 0, s, p, tiles);
-  else if (v16) hipLaunchKernelGGL((attn_dq_kernel<DP, false, true>), g, dim3(256), 0, s, p, tiles);
-  else hipLaunchKernelGGL((attn_dq_kernel<DP, false, false>), g, dim3(256), 0, s, p, tiles);
+  const int tiles = (int)((p.max_q * p.G + 127) / 128);
+  const int64_t g = p.rows_q > 0 ? p.batch * p.Hkv * tiles : 0;
+  if (k16 && v16) return launch_groups(attn_dq_kernel<DP, true, true>, g, 1, s, p, tiles);
+  if (k16) return launch_groups(attn_dq_kernel<DP, true, false>, g, 1, s, p, tiles);
+  if (v16) return launch_groups(attn_dq_kernel<DP, false, true>, g, 1, s, p, tiles);
+  return launch_groups(attn_dq_kernel<DP, false, false>, g, 1, s, p, tiles);
 }
 
 template <int DP>
-static void launch(const AttnParams& p, hipStream_t s) {
-  const int64_t heads = p.batch * p.Hkv;
-  const int kt = (int)((p.max_k + 127) / 128), qt = (int)((p.max_q * p.G + 127) / 128);
-  if (p.rows_k > 0 && kt > 0)
-    launch_dkv<DP>(p, dim3((unsigned)(heads * kt * p.parts)), kt, s);
-  if (p.rows_q > 0 && qt > 0)
-    launch_dq<DP>(p, dim3((unsigned)(heads * qt)), qt, s);
+static hipError_t launch(const AttnParams& p, hipStream_t s) {
+  const hipError_t e = launch_dkv<DP>(p, s);
+  return e == hipSuccess ? launch_dq<DP>(p, s) : e;
 }
 
 // Where the workgroups of 128 keys leave CUs without one, the queries (tiles of 64, of
@@ -782,18 +783,19 @@ int attention_bwd_parts(int64_t batch, int Hkv, int G, int64_t max_q, int64_t ma
 
 hipError_t launch_attention_bwd(const AttnParams& p, hipStream_t s) {
   const int64_t items = p.rows_q * p.H + p.rows_k * p.Hkv;
-  hipLaunchKernelGGL(attn_rows_kernel, dim3((unsigned)(items > 16 ? (items + 15) / 16 : 1)), dim3(256), 0, s, p);
-  if (p.D <= 64) launch<64>(p, s);
-  else launch<128>(p, s);
-  if (p.parts > 1) {
+  hipError_t e = launch_groups(attn_rows_kernel, items > 16 ? (items + 15) / 16 : 1, 1, s, p);
+  if (e == hipSuccess) e = p.D <= 64 ? launch<64>(p, s) : launch<128>(p, s);
+  if (e == hipSuccess && p.parts > 1) {
+    // (queries are shared among parts for at most 128 tiles of 128 keys)
     const int64_t tiles = (p.max_k + ATTN_PART_ROWS - 1) / ATTN_PART_ROWS;
     hipLaunchKernelGGL(attn_parts_kernel, dim3((unsigned)(p.batch * tiles), 2), dim3(256), 0, s, p, tiles);
+    e = hipGetLastError();
   }
+  if (e != hipSuccess) return e;
   const int64_t most = p.max_q > p.max_k ? p.max_q : p.max_k;
   int64_t tiles = p.mode == 1 ? (most + ATTN_CAST_ROWS - 1) / ATTN_CAST_ROWS : 0;
   if (tiles < 1) tiles = 1;
-  hipLaunchKernelGGL(attn_grads_kernel, dim3((unsigned)(p.mode == 1 ? p.batch * tiles : 1), 3), dim3(256), 0, s, p, tiles);
-  return hipGetLastError();
+  return launch_groups(attn_grads_kernel, p.mode == 1 ? p.batch * tiles : 1, 3, s, p, tiles);
 }
 
 }  // namespace scalify

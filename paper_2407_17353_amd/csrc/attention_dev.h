@@ -483,8 +483,8 @@ struct Place {
   int64_t rest;
 };
 __device__ __forceinline__ Place attn_place(const AttnParams& p, int64_t in_head) {
-  // (32 bits: the grid has less than 2^31 workgroups)
-  const uint32_t heads = (uint32_t)(p.batch * p.Hkv), per_head = (uint32_t)in_head, id = blockIdx.x;
+  // (32 bits: a call has less than 2^31 workgroups)
+  const uint32_t heads = (uint32_t)(p.batch * p.Hkv), per_head = (uint32_t)in_head, id = p.group0 + blockIdx.x;
   uint32_t bh;
   Place w;
   if ((heads & 7) == 0) {

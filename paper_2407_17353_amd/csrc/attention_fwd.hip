@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tile
   const int tile = tiles - 1 - (int)(at.rest / p.splits);
   const Seq sq = load_seq(p, at.b);
   const int64_t ncols = (int64_t)sq.lq * p.G, col0 = (int64_t)tile * 128;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
+  if (p.group0 + blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
   if (col0 >= ncols) return;
   const int last0 = p.causal ? min((int)(col0 / p.G) + sq.behind, sq.lk - 1) : sq.lk - 1;  // of the first column
   const Query q = query_at(p, sq, at.hk, col0 + 32 * wave + (lane & 31), ncols);
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(AttnParams p, int tile
   const int tile = tiles - 1 - (int)(at.rest / p.splits);
   const Seq sq = load_seq(p, at.b);
   const int64_t ncols = (int64_t)sq.lq * p.G, col0 = (int64_t)tile * 32;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
+  if (p.group0 + blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
   if (col0 >= ncols) return;
   const Query q = query_at(p, sq, at.hk, col0 + (lane & 31), ncols);
   int begin, end;
@@ -513,20 +513,21 @@ AttnPlan attention_plan(int64_t batch, int Hkv, int G, int64_t max_q, int64_t ma
 }
 
 template <int DP>
-static void launch(const AttnParams& p, const AttnPlan& plan, hipStream_t s) {
+static hipError_t launch(const AttnParams& p, const AttnPlan& plan, hipStream_t s) {
   const int64_t cols = p.max_q * p.G;
   const int tiles = (int)((cols + plan.cols - 1) / plan.cols);
-  const dim3 g((unsigned)(p.batch * p.Hkv * tiles * plan.splits)), b(256);
+  const int64_t g = p.batch * p.Hkv * tiles * plan.splits;
   const bool k16 = p.k_fmt == kF16, v16 = p.v_fmt == kF16;
   if (plan.cols == 32) {
-    if (k16 && v16) hipLaunchKernelGGL((attn_few_kernel<DP, true, true>), g, b, 0, s, p, tiles);
-    else if (k16) hipLaunchKernelGGL((attn_few_kernel<DP, true, false>), g, b, 0, s, p, tiles);
-    else if (v16) hipLaunchKernelGGL((attn_few_kernel<DP, false, true>), g, b, 0, s, p, tiles);
-    else hipLaunchKernelGGL((attn_few_kernel<DP, false, false>), g, b, 0, s, p, tiles);
-  } else if (k16 && v16) hipLaunchKernelGGL((attn_fwd_kernel<DP, true, true>), g, b, 0, s, p, tiles);
-  else if (k16) hipLaunchKernelGGL((attn_fwd_kernel<DP, true, false>), g, b, 0, s, p, tiles);
-  else if (v16) hipLaunchKernelGGL((attn_fwd_kernel<DP, false, true>), g, b, 0, s, p, tiles);
-  else hipLaunchKernelGGL((attn_fwd_kernel<DP, false, false>), g, b, 0, s, p, tiles);
+    if (k16 && v16) return launch_groups(attn_few_kernel<DP, true, true>, g, 1, s, p, tiles);
+    if (k16) return launch_groups(attn_few_kernel<DP, true, false>, g, 1, s, p, tiles);
+    if (v16) return launch_groups(attn_few_kernel<DP, false, true>, g, 1, s, p, tiles);
+    return launch_groups(attn_few_kernel<DP, false, false>, g, 1, s, p, tiles);
+  }
+  if (k16 && v16) return launch_groups(attn_fwd_kernel<DP, true, true>, g, 1, s, p, tiles);
+  if (k16) return launch_groups(attn_fwd_kernel<DP, true, false>, g, 1, s, p, tiles);
+  if (v16) return launch_groups(attn_fwd_kernel<DP, false, true>, g, 1, s, p, tiles);
+  return launch_groups(attn_fwd_kernel<DP, false, false>, g, 1, s, p, tiles);
 }
 
 hipError_t launch_attention_fwd(const AttnParams& p, const AttnPlan& plan, hipStream_t s) {
@@ -534,12 +535,10 @@ hipError_t launch_attention_fwd(const AttnParams& p, const AttnPlan& plan, hipSt
     hipLaunchKernelGGL(attn_scale_kernel, dim3(1), dim3(1), 0, s, p);
     return hipGetLastError();
   }
-  if (p.D <= 64) launch<64>(p, plan, s);
-  else launch<128>(p, plan, s);
-  if (plan.splits > 1) {
-    const int64_t cols = p.max_q * p.G;
-    hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)(p.batch * p.Hkv * cols)), dim3(256), 0, s, p);
-  }
+  const hipError_t e = p.D <= 64 ? launch<64>(p, plan, s) : launch<128>(p, plan, s);
+  if (e != hipSuccess || plan.splits < 2) return e;
+  // (keys are split for at most 256 tiles of at most 128 columns)
+  hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)(p.batch * p.Hkv * p.max_q * p.G)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -281,9 +281,10 @@ scalify_status attention_sizes(const scalify_attention_opts* o, int64_t rows_q, 
   if (z->max_q * z->G > kMaxDim) return SCALIFY_ERR_SHAPE;
   // (workgroups: 32 query columns or 128 keys each; 512 and a column each where keys are split)
   const int64_t heads = o->batch * o->kv_heads;
+  if (heads > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
   const int64_t wide = heads * ((z->max_q * z->G + 31) / 32);
   const int64_t tall = heads * ((z->max_k + 127) / 128);
-  if (heads > 0x7FFFFFFF || wide > 0x7FFFFFFF || tall > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
+  if (wide > 0x7FFFFFFF || tall > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
   return SCALIFY_OK;
 }
 

@@ -117,3 +117,69 @@ def test_queries_past_max_q(D, Lq, max_q, Lk):
     for x, w, e, rows in zip(res[0], want, err, (live, slice(None), slice(None))):
         assert ((lr.data(x) - w).abs() <= e + (w.abs() + e) * rel + sub)[rows].all()
     assert (lr.codes(res[0][0])[~live.numpy()] == 0x5A5A).all()
+
+
+# ---------------------------------------------------------------- grids
+
+MANY = dict(B=2048, H=32, Hkv=32, D=16, Tq=32768, Tk=32768)
+
+
+def _many(seed=1):
+    """2048 short sequences packed into 32768 rows of 32 heads, with the bounds that
+    the options give by default (any number of rows each)."""
+    case = attn._case("many", fk=F16, **MANY)
+    r = np.random.RandomState(seed)
+    at = np.sort(r.randint(0, case["Tq"] + 1, case["B"] - 1))
+    case["q_start"] = case["k_start"] = [0, *at.tolist(), case["Tq"]]
+    return case
+
+
+def _bounded(case):
+    n = int(np.diff(case["q_start"]).max())
+    return dict(case, max_q=n, max_k=n)
+
+
+@pytest.mark.parametrize("mode", [sc.RESCALE_NONE, sc.RESCALE_AMAX])
+def test_packed_sequences_without_bounds(mode):
+    """More than 2^24 workgroups: what a call with the bounds gives, to the bit."""
+    say(f"attention many workgroups {mode}")
+    case = _many()
+    q, k, v, do = attn._bwd_inputs(case)
+    want = attn.run_bwd(_bounded(case), q, k, v, do, mode=mode)
+    got = attn.run_bwd(case, q, k, v, do, mode=mode)
+    assert np.array_equal(lr.codes(got[2]), lr.codes(want[2])) and torch.equal(got[3], want[3])
+    for a, b in zip(got[0], want[0]):
+        assert np.array_equal(lr.codes(a), lr.codes(b)) and a.scale.item() == b.scale.item()
+    assert torch.equal(got[1], want[1])
+    assert lr.data(want[2]).isfinite().all() and (lr.data(want[2]) != 0).any()
+
+
+def test_more_rows_and_heads_than_threads_of_a_launch():
+    """The last 64 of 2^20 + 64 rows of 256 heads (25 GB in all): their numbers lie past
+    2^32 threads of the kernel that forms them. What the same rows give by themselves."""
+    say("attention bwd 2^28 rows and heads")
+    n, H, D, before = 64, 256, 16, 1 << 20
+    case = attn._case("rows", H=H, D=D, Lq=n, Lk=n, fq=E4M3, fk=E4M3)
+    q, k, v = attn._inputs(case)
+    do = lr.values(n, H * D, E4M3, 9)
+    want = attn.run_bwd(case, q, k, v, do, fdo=E4M3, fg=E4M3)
+    T = before + n
+
+    def tall(fmt, e, t=None):
+        x = torch.zeros((T, H * D), dtype=sc.STORAGE_DTYPE[fmt], device=DEV)
+        if t is not None:
+            x[before:] = t
+        return sc.ScaledArray(x, fmt, sc.scale_tensor(e, DEV))
+    K, V = lr.scaled(k, E4M3, case["ek"]), lr.scaled(v, E4M3, case["ev"])
+    Q, DO = (tall(E4M3, e, t.view(torch.uint8).to(DEV)) for t, e in ((q, case["eq"]), (do, -6)))
+    out, dq = tall(F16, 0), tall(E4M3, 0)
+    dk, dv = lr.empty(n, H * D, E4M3), lr.empty(n, H * D, E4M3)
+    lse = torch.zeros((H, T), device=DEV)
+    opts = dict(attn._opts(case), q_start=attn._i64([before, T]), max_q=n)
+    sc.scalify_attention_fwd(Q, K, V, out, lse=lse, **opts)
+    sc.scalify_attention_bwd(DO, Q, K, V, out, lse, dq, dk, dv, rescale=sc.RESCALE_NONE, **opts)
+    torch.cuda.synchronize()
+    assert torch.equal(out.data[before:], want[2].data) and torch.equal(lse[:, before:], want[3])
+    for x, y in ((sc.ScaledArray(dq.data[before:], E4M3, dq.scale), want[0][0]), (dk, want[0][1]), (dv, want[0][2])):
+        assert np.array_equal(lr.codes(x), lr.codes(y)) and x.scale.item() == y.scale.item()
+    assert (dq.data[:before] == 0).all() and (out.data[:before] == 0).all()
