@@ -183,3 +183,43 @@ def test_more_rows_and_heads_than_threads_of_a_launch():
     for x, y in ((sc.ScaledArray(dq.data[before:], E4M3, dq.scale), want[0][0]), (dk, want[0][1]), (dv, want[0][2])):
         assert np.array_equal(lr.codes(x), lr.codes(y)) and x.scale.item() == y.scale.item()
     assert (dq.data[:before] == 0).all() and (out.data[:before] == 0).all()
+
+
+# ---------------------------------------------------------------- placement over the XCDs
+
+@pytest.mark.parametrize("B,H,Hkv,D,L,causal", [(5, 16, 8, 64, 150, True), (10, 8, 8, 64, 140, True), (5, 8, 8, 128, 131, False),
+                                                (3, 16, 16, 64, 129, True), (7, 8, 8, 64, 65, True)])
+def test_heads_in_groups(B, H, Hkv, D, L, causal):
+    """Key heads a multiple of 8: 5, 6, 7 or 10 of them on an XCD, the last group of
+    one, two or three, with several tiles each."""
+    say(f"attention placement {B} {H} {Hkv} {D}")
+    case = attn._case("placed", B=B, H=H, Hkv=Hkv, D=D, Lq=L, Lk=L, causal=causal)
+    t = attn._bwd_inputs(case)
+    res = attn.run_bwd(case, *t)
+    attn.check_fwd(case, *t[:3], res[2], res[3])
+    attn.check_bwd(case, *t, res)
+
+
+@pytest.mark.parametrize("B,Hkv", [(5, 8), (10, 8), (1, 40), (2, 4)])
+@pytest.mark.parametrize("Lq,fk", [(1, F16), (1, E4M3), (9, F16)])
+def test_heads_in_groups_split_keys(B, Hkv, Lq, fk):
+    """The same for few queries, whose keys are split over workgroups and joined."""
+    say(f"attention placement split {B} {Hkv} {Lq}")
+    case = attn._case("placed_split", B=B, H=4 * Hkv, Hkv=Hkv, D=64, Lq=Lq, Lk=1100, fk=fk, k_len=[1100 - 37 * b for b in range(B)])
+    q, k, v = attn._inputs(case)
+    Q = lr.scaled(q, F16, case["eq"])
+    assert sc.scalify_attention_fwd_workspace_size(B * Lq, B * 1100, sc.attention_opts(Q, **attn._opts(case))) > 0
+    out, lse = attn.run_fwd(case, q, k, v)
+    attn.check_fwd(case, q, k, v, out, lse)
+
+
+@pytest.mark.parametrize("B,Hkv", [(5, 8), (3, 16)])
+def test_heads_in_groups_parts(B, Hkv):
+    """The same for the backward whose queries are shared by several workgroups."""
+    say(f"attention placement parts {B} {Hkv}")
+    case = attn._case("placed_parts", B=B, H=2 * Hkv, Hkv=Hkv, D=64, Lq=500, Lk=100)
+    t = attn._bwd_inputs(case)
+    Q = lr.scaled(t[0], F16, case["eq"])
+    n = sc.scalify_attention_bwd_workspace_size(500 * B, 100 * B, sc.attention_opts(Q, **attn._opts(case)), sc.RESCALE_NONE)
+    assert n > 256 + 4 * (2 * 500 * B * 2 * Hkv + 100 * B * Hkv) + 16
+    attn.check_bwd(case, *t, attn.run_bwd(case, *t))
