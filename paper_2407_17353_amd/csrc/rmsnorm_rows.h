@@ -124,13 +124,15 @@ __device__ __forceinline__ float row_max(float a, float (*slot)[WPR], int row, i
   return a;
 }
 
-// The row divided by the power of two of its largest magnitude; returns its exponent.
+// The row divided by the power of two of its largest magnitude; returns its exponent. Not
+// below 2^-100: the squares of the smallest numbers, 2^-149, then lie over 2^-98, and the
+// divided row's 1 / rms, which eps alone may give (2^-100 / sqrt(eps)), is a normal number.
 template <int WPR>
 __device__ __forceinline__ int rms_range(float (&h)[16], float (*slot)[WPR], int row, int part, int lane) {
   float a = 0.0f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) a = fmaxf(a, fabsf(h[i]));
-  const int k = rescale_exponent(__float_as_uint(row_max<WPR>(a, slot, row, part, lane)), 0);
+  const int k = max(rescale_exponent(__float_as_uint(row_max<WPR>(a, slot, row, part, lane)), 0), -100);
 #pragma unroll
   for (int i = 0; i < 16; ++i) h[i] = __builtin_ldexpf(h[i], -k);
   return k;

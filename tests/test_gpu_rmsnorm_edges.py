@@ -54,3 +54,28 @@ def test_residual_without_a_stored_sum(D, scales, fx, fr, eps, ex, er):
         assert torch.equal(blk, sc.scalify_mx_pack_block_scales(torch.from_numpy((ee + 127).astype(np.uint8)).to(DEV), D))
         sh += np.repeat(ee, 32, axis=1)[:, :D]
     assert np.array_equal(lr.codes(out), lr.cast(np.ldexp(p.astype(np.float64), -sh), E4M3))
+
+
+@pytest.mark.parametrize("eps", [1e-5, 3e-9, 1e-30])
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("D", [300, 2048, 5000])
+def test_backward_rows_of_subnormal_numbers(D, mode, eps):
+    """F32 rows whose largest number is 2^-126 to 2^-149: eps alone is their mean square."""
+    say(f"rmsnorm bwd subnormal {D} {mode} {eps}")
+    x = lr.values(9, D, F32, 4)
+    for i, e in enumerate([0, -126, -130, -134, -138, -142, -146, -149]):
+        x[i] = torch.ldexp(x[i].clamp(-1.9, 1.9), torch.tensor(e))
+    assert (x[7] != 0).any()
+    dy = lr.values(9, D, F16, 5)
+    got = rms.run_bwd(dy, F16, x, F32, None, None, fo=F16, mode=mode, eps=eps)
+    rms.check_bwd(dy, x, None, None, F16, mode, 0, got, eps=eps)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-5, 1e-30])
+def test_rows_of_subnormal_numbers(eps):
+    x = lr.values(9, 300, F32, 4)
+    for i, e in enumerate([0, -126, -130, -134, -138, -142, -146, -149]):
+        x[i] = torch.ldexp(x[i].clamp(-1.9, 1.9), torch.tensor(e))
+    for scales in ("row", "mx"):
+        got = rms.run_fwd(x, F32, None, None, scales=scales, target=7, eps=eps)
+        rms.check_fwd(x, F32, None, None, F16, F16, E4M3, scales, 7, eps, got)
