@@ -544,8 +544,8 @@ size_t scalify_attention_bwd_workspace_size(int64_t rows_q, int64_t rows_k,
  *   AMAX: e_r = floor(log2 amax of its data) - target_log2 (0 for amax 0 / Inf / all
  *   NaN), NONE: e_r = 0; e_out = clamp(propagated + e_r, -127, 127).
  * amax_out: optional device fp32 [3], the statistics of dq, dk and dv.
- * lse is fp32, so a P is off by 2^-23 |lse_i| of itself: meant for |lse| up to 2^14
- * or so, where that is F16's rounding.
+ * dK and dV take lse into the scores' fp32 sums, so a P is off by up to about 2^-20
+ * |lse_i| of itself: F16's rounding, 2^-11, where |lse| is 2^9.
  * Rows of k past k_len get zeros. P is rounded to F16 as 2^14 P, dS to F16 times a
  * power of two that a bound of its largest magnitude among the queries and keys of a
  * workgroup, 2 max(max |dO_i| max |v_j|, max |delta_i|), gives.

@@ -176,7 +176,7 @@ __device__ __forceinline__ f16v row_start(const float* rows, int h) {
 // One wave a SIMD (its results, and the rows, take most of the 512 registers), so
 // what bounds it is the rate at which one wave issues, four clocks an instruction of
 // any kind: 32 products of 32 clocks leave 224 others. 4 x 4096 causal tokens, 32
-// heads of 128: 1.30 to 1.35 ms, the matrix cores busy for 36 % of it (at 2.3 GHz): a
+// heads of 128: 1.30 to 1.37 ms, the matrix cores busy for 36 % of it (at 2.3 GHz): a
 // tile takes 4360 clocks of the loop, 2048 of them its products.
 // Q16, O16: whether q and dO are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool Q16, bool O16>
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnParams p, int tile
 // of 64 keys, with q and dO rows in registers, laid out as dK and dV above: scores
 // and dP of key block b + 1 and the product of block b - 1 while dS of block b is
 // formed. k is read twice, by rows for the scores and by columns for the product a
-// block later, and has three LDS buffers, v two. The same tokens: 1.00 to 1.04 ms, the
+// block later, and has three LDS buffers, v two. The same tokens: 1.00 to 1.06 ms, the
 // matrix cores busy for 35 % (one product after another, its tiles shared by barriers: 1.23).
 // Buffers known at compile time save 15 of a block's 220 instructions and no time (1.10).
 // K16, V16: whether k and v are F16 (and go straight into LDS) or have 8 bits.

@@ -144,9 +144,10 @@ __device__ __forceinline__ void remove_odd(uint8_t* vt) {
 // three multiply-adds each, in one wave, took the products' 237.) k and v have two
 // LDS buffers each, with one barrier a tile, in its middle: the first block is the
 // last to use the older buffers.
-// 4 x 4096 causal tokens, 32 heads of 128: 603 to 640 us, 860 to 910 TFLOP/s, where the
-// card's power lowers its clock (before results were stored by rows 650, all-zero
-// inputs 488 and 64 queries a wave 820).
+// 4 x 4096 causal tokens, 32 heads of 128: 603 to 663 us on several cards, 830 to 910
+// TFLOP/s, the matrix cores busy for 49 % of it. The card's power lowers its clock (one
+// card took 634 us, and 472 with zeros for inputs); before results were stored by rows
+// it was 650, and 820 with 64 queries a wave.
 // K16, V16: whether k and v are F16 (and go straight into LDS) or have 8 bits.
 template <int DP, bool K16, bool V16>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnParams p, int tiles) {
@@ -498,8 +499,15 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
 
 __global__ void attn_scale_kernel(AttnParams p) { *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v))); }
 
-// 512 workgroups (two on each of the 256 CUs) fill the device; a split is worth
-// its second kernel from 256 keys on.
+// 512 workgroups (two on each of the 256 CUs) fill the device. Both limits of the rule
+// lie where neither side is better throughout (us, a captured call's kernels).
+// Columns: the few-query kernel reads the keys once for each 32, the wide one has more
+// products in flight. Few against wide: 40 columns over 8192 F16 keys of 4 heads 15.4,
+// 17.6; 32 sequences of 40 over 4096 F16 keys of 8 heads 129, 124, over E4M3 keys 65, 93;
+// 64 columns over 8192 keys of 8 heads 31, 23; 64 prompts of 48 tokens 26, 15.
+// Keys of a split: without a split, from 256 keys on, from 128 on: 513 keys of 16 heads of
+// 64 9.3, 9.9, 9.4; 1024 keys 10.6, 9.4, 9.0; 32 heads on 8 of 128, 2048 keys 22.5, 13.7,
+// 12.7; 8192 keys 62.7, 17.2, 25.5.
 AttnPlan attention_plan(int64_t batch, int Hkv, int G, int64_t max_q, int64_t max_k) {
   AttnPlan r;
   const int64_t cols = max_q * G;
