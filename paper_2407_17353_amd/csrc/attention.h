@@ -52,16 +52,20 @@ constexpr int kAttnMaxD = 128;
 
 // A launch holds less than 2^32 threads in a dimension of its grid: `groups`
 // workgroups of 256 go out as launches of 2^23, which leaves a workgroup's XCD what it
-// is in one launch, each with the number of its first one. Stops at an error.
+// is in one launch, each with the number of its first one. Stops at a launch that is
+// refused, and goes by that launch's status alone, not by an error of an earlier call.
 constexpr int64_t kLaunchGroups = 1 << 23;
-template <typename Kernel, typename... Args>
-hipError_t launch_groups(Kernel kernel, int64_t groups, unsigned y, hipStream_t s, AttnParams p, Args... args) {
+template <typename... Args>
+hipError_t launch_groups(void (*kernel)(AttnParams, Args...), int64_t groups, unsigned y, hipStream_t s, AttnParams p, Args... args) {
   for (int64_t g = 0; g < groups; g += kLaunchGroups) {
     const int64_t n = groups - g < kLaunchGroups ? groups - g : kLaunchGroups;
     p.group0 = (uint32_t)g;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)n, y), dim3(256), 0, s, p, args...);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    void* a[] = {&p, (void*)&args...};
+    const hipError_t e = hipLaunchKernel((const void*)kernel, dim3((unsigned)n, y), dim3(256), a, 0, s);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      return e;
+    }
   }
   return hipSuccess;
 }

@@ -786,10 +786,9 @@ hipError_t launch_attention_bwd(const AttnParams& p, hipStream_t s) {
   hipError_t e = launch_groups(attn_rows_kernel, items > 16 ? (items + 15) / 16 : 1, 1, s, p);
   if (e == hipSuccess) e = p.D <= 64 ? launch<64>(p, s) : launch<128>(p, s);
   if (e == hipSuccess && p.parts > 1) {
-    // (queries are shared among parts for at most 128 tiles of 128 keys)
+    // (queries are shared among parts for at most 128 tiles of 128 keys: one launch)
     const int64_t tiles = (p.max_k + ATTN_PART_ROWS - 1) / ATTN_PART_ROWS;
-    hipLaunchKernelGGL(attn_parts_kernel, dim3((unsigned)(p.batch * tiles), 2), dim3(256), 0, s, p, tiles);
-    e = hipGetLastError();
+    e = launch_groups(attn_parts_kernel, p.batch * tiles, 2, s, p, tiles);
   }
   if (e != hipSuccess) return e;
   const int64_t most = p.max_q > p.max_k ? p.max_q : p.max_k;

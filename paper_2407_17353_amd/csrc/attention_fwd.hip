@@ -497,7 +497,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
   if (p.lse && lane == 0) p.lse[(int64_t)head * p.rows_q + row] = log_sum(m, l);
 }
 
-__global__ void attn_scale_kernel(AttnParams p) { *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v))); }
+__global__ void attn_scale_kernel(AttnParams p) {
+  if (threadIdx.x == 0) *p.out_scale = pow2_float(clamp_e8m0(pow2_exponent(p.s_v)));
+}
 
 // 512 workgroups (two on each of the 256 CUs) fill the device. Both limits of the rule
 // lie where neither side is better throughout (us, a captured call's kernels).
@@ -539,15 +541,11 @@ static hipError_t launch(const AttnParams& p, const AttnPlan& plan, hipStream_t 
 }
 
 hipError_t launch_attention_fwd(const AttnParams& p, const AttnPlan& plan, hipStream_t s) {
-  if (p.rows_q == 0 || p.batch == 0 || p.max_q == 0) {
-    hipLaunchKernelGGL(attn_scale_kernel, dim3(1), dim3(1), 0, s, p);
-    return hipGetLastError();
-  }
+  if (p.rows_q == 0 || p.batch == 0 || p.max_q == 0) return launch_groups(attn_scale_kernel, 1, 1, s, p);
   const hipError_t e = p.D <= 64 ? launch<64>(p, plan, s) : launch<128>(p, plan, s);
   if (e != hipSuccess || plan.splits < 2) return e;
-  // (keys are split for at most 256 tiles of at most 128 columns)
-  hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)(p.batch * p.Hkv * p.max_q * p.G)), dim3(256), 0, s, p);
-  return hipGetLastError();
+  // (keys are split for at most 256 tiles of at most 128 columns: one launch)
+  return launch_groups(attn_join_kernel, p.batch * p.Hkv * p.max_q * p.G, 1, s, p);
 }
 
 }  // namespace scalify

@@ -1,5 +1,6 @@
 """GPU parity of attention where its sizes, masks and magnitudes meet their
 edges, against the plain 64-bit forms and bounds of tests/layer_refs.py."""
+import ctypes
 import math
 
 import numpy as np
@@ -223,3 +224,27 @@ def test_heads_in_groups_parts(B, Hkv):
     n = sc.scalify_attention_bwd_workspace_size(500 * B, 100 * B, sc.attention_opts(Q, **attn._opts(case)), sc.RESCALE_NONE)
     assert n > 256 + 4 * (2 * 500 * B * 2 * Hkv + 100 * B * Hkv) + 16
     attn.check_bwd(case, *t, attn.run_bwd(case, *t))
+
+
+def test_an_error_of_an_earlier_call_stops_nothing():
+    """The HIP runtime keeps the last error of any call; a call's launches go by their own."""
+    case = attn._case("stale", Lq=70, Lk=90)
+    t = attn._bwd_inputs(case)
+    want = attn.run_bwd(case, *t)
+    with open("/proc/self/maps") as f:
+        path = next(line.split()[-1] for line in f if "libamdhip64" in line)
+    hip = ctypes.CDLL(path)
+    Q, K, V, DO = (lr.scaled(x, F16, e) for x, e in zip((*t[:3], t[3]), (case["eq"], case["ek"], case["ev"], -6)))
+    out, lse = lr.empty(70, 128, F16), torch.zeros((2, 70), device=DEV)
+    grads = [lr.empty(*x.shape, F16) for x in t[:3]]
+    o = attn._opts(case)
+    ws = sc.workspace(sc.scalify_attention_bwd_workspace_size(70, 90, sc.attention_opts(Q, **o), sc.RESCALE_NONE), DEV)
+    torch.cuda.synchronize()
+    assert hip.hipSetDevice(1 << 20) != 0
+    sc.scalify_attention_fwd(Q, K, V, out, lse=lse, **o)
+    hip.hipSetDevice(1 << 20)
+    sc.scalify_attention_bwd(DO, Q, K, V, out, lse, *grads, rescale=sc.RESCALE_NONE, ws=ws, **o)
+    hip.hipGetLastError()
+    torch.cuda.synchronize()
+    assert np.array_equal(lr.codes(out), lr.codes(want[2]))
+    assert all(np.array_equal(lr.codes(a), lr.codes(b)) for a, b in zip(grads, want[0]))
