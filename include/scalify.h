@@ -565,6 +565,105 @@ scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
                                      int32_t target_log2, int32_t saturate, float* amax_out,
                                      void* workspace, size_t workspace_bytes, void* stream);
 
+/* Losses behind the last layer, from the hidden states x (R x D) and the output
+ * matrix w (V x D, a row a token: the matrix that scalify_matmul takes as b with trans =
+ * 1); the R x V logits are not kept. In true values
+ *   z_ij = s_x s_w row_scale[i] sum_d x_id w_jd / T      (T = 1 for the cross entropy)
+ *   lse_i = log sum_j exp z_ij,  p_ij = exp(z_ij - lse_i)
+ *   cross entropy: loss_i = lse_i - z_i,labels[i]
+ *   distillation:  q_i = softmax_k(s_t t_ik / T) over the teacher's entries of the row,
+ *     loss_i = T^2 sum_k q_ik (log q_ik - z_i,index[i][k] + lse_i)
+ * A row counts if its label lies in [0, V), for distillation if one of its tokens does
+ * with a teacher's logit above -Inf. The others' loss, lse and logits are 0, and of them
+ * nothing else is read. Entries of the teacher whose token lies outside [0, V) are not
+ * there; those of one token add up.
+ * x, w: E4M3, E5M2 or F16, any mix; trans = 0, rows 16-byte aligned (ld a multiple of 16
+ * bytes), 1 <= D <= 2^20, rows of w below 2^23 bytes. row_scale (optional device fp32
+ * [R], powers of two, 4-byte aligned): the a_channel_scale of x, as scalify_rmsnorm_fwd
+ * gives it. The factor s_x s_w row_scale log2(e) / T is held to [2^-100, 2^64].
+ * labels: device int64 [R]. Sizes: R and V at most 2^30, and at most 2^30 tiles of 256
+ * x 256 (R x V and V x D; 2^24 of R x D) (SCALIFY_ERR_SHAPE).
+ * Products are F16 with fp32 sums (8-bit values are F16 values), statistics fp32.
+ * Deterministic on one device: every sum has a fixed order. No call synchronises;
+ * which rows count is found on the device, and work goes by their number. */
+
+/* Bytes of device workspace scalify_cross_entropy_fwd needs: a copy of x in F16, 8 bytes
+ * for each row and 128 columns of V, and up to 512 MiB of w in F16 where w has 8 bits or
+ * D is no multiple of 8. 0 for invalid arguments. */
+size_t scalify_cross_entropy_fwd_workspace_size(int64_t R, int64_t V, int64_t D, int32_t w_dtype);
+
+/* Softmax cross entropy of every row: loss, and lse (optional) for the backward; device
+ * fp32 [R]. workspace: 256-byte aligned, not shared with a concurrent call. */
+scalify_status scalify_cross_entropy_fwd(const scalify_scaled_array* x,
+                                         const scalify_scaled_array* w, const int64_t* labels,
+                                         const float* row_scale, float* loss, float* lse,
+                                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace scalify_cross_entropy_bwd needs: two copies of x in F16,
+ * up to 512 MiB each of the logits' gradient (of 256 tokens at least) and of w in F16,
+ * fp32 products of dx for each part of the vocabulary that the device works on at once,
+ * and with AMAX fp32 products of dw. 0 for invalid arguments. */
+size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D, int32_t w_dtype,
+                                                int32_t rescale);
+
+/* Gradients of scalify_cross_entropy_fwd from its stored lse, the logits computed
+ * again in pieces of the vocabulary. The upstream gradient of loss_i is g_i s_g, g =
+ * dloss (device fp32 [R]; NULL = 1), s_g = *dloss_scale (a power of two; NULL = 1):
+ *   dz_ij = g_i (p_ij - [j = labels[i]]),  dx_i = sum_j dz_ij w_j, scale s_g s_w,
+ *   dw_j = sum_i dz_ij row_scale[i] x_i, scale s_g s_x
+ * (of the true values of x and w), as ScaledArrays with their rescale as in
+ * scalify_layernorm_bwd (AMAX, or NONE: the propagated scales). A row that does not
+ * count, or whose g_i is 0, gives 0 and adds nothing, whatever it holds.
+ * dx (R x D), dw (V x D): E4M3, E5M2 or F16, layouts as x; either may be NULL, not both.
+ * They must not overlap x, w or each other, nor their scales those of x, w, dloss or each
+ * other (SCALIFY_ERR_LAYOUT). amax_out: optional device fp32 [2], the statistics of dx and
+ * dw. dz is rounded to F16 as 2^14 dz / 2^E, 2^E <= max |g| the power of two below it
+ * (normal numbers down to 2^-28 of 2^E); for dw, x times row_scale over the largest
+ * row_scale to F16 (exact where that is a normal number of F16). */
+scalify_status scalify_cross_entropy_bwd(const float* dloss, const float* dloss_scale,
+                                         const scalify_scaled_array* x,
+                                         const scalify_scaled_array* w, const int64_t* labels,
+                                         const float* row_scale, const float* lse,
+                                         scalify_scaled_array* dx, scalify_scaled_array* dw,
+                                         int32_t rescale, int32_t target_log2, int32_t saturate,
+                                         float* amax_out, void* workspace, size_t workspace_bytes,
+                                         void* stream);
+
+/* Workspace bytes of scalify_distillation_fwd: those of scalify_cross_entropy_fwd and 8
+ * for each row and entry of the teacher (`top` entries a row, rounded up to 16). */
+size_t scalify_distillation_fwd_workspace_size(int64_t R, int64_t V, int64_t D, int64_t top,
+                                               int32_t w_dtype);
+
+/* Distillation loss of every row (above) against a teacher's top logits: teacher [R][top]
+ * (any scalify_dtype, layout as x, 1 <= top <= 256) of the tokens index (device int64
+ * [R][top], contiguous), temperature T in [2^-20, 2^20] (SCALIFY_ERR_VALUE). loss: device
+ * fp32 [R]. lse (fp32 [R]) and picked (fp32 [R][top]: z of the teacher's tokens, 0 where a
+ * token or the row does not count) are optional; the backward reads both. */
+scalify_status scalify_distillation_fwd(const scalify_scaled_array* x,
+                                        const scalify_scaled_array* w,
+                                        const scalify_scaled_array* teacher, const int64_t* index,
+                                        float temperature, const float* row_scale, float* loss,
+                                        float* lse, float* picked, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of scalify_distillation_bwd: those of scalify_cross_entropy_bwd and 4
+ * for each row and entry. */
+size_t scalify_distillation_bwd_workspace_size(int64_t R, int64_t V, int64_t D, int64_t top,
+                                               int32_t w_dtype, int32_t rescale);
+
+/* Gradients of scalify_distillation_fwd with respect to x and w, from its stored lse and
+ * picked: dz_ij = g_i T (p_ij - q_ij), q_ij the sum over the row's entries of token j;
+ * everything else as in scalify_cross_entropy_bwd (2^E goes by max |g T|). */
+scalify_status scalify_distillation_bwd(const float* dloss, const float* dloss_scale,
+                                        const scalify_scaled_array* x,
+                                        const scalify_scaled_array* w,
+                                        const scalify_scaled_array* teacher, const int64_t* index,
+                                        float temperature, const float* row_scale, const float* lse,
+                                        const float* picked, scalify_scaled_array* dx,
+                                        scalify_scaled_array* dw, int32_t rescale,
+                                        int32_t target_log2, int32_t saturate, float* amax_out,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
 /* Human-readable name of a status code (static string). */
 const char* scalify_status_string(int32_t status);
 

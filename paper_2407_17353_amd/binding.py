@@ -69,7 +69,11 @@ EXPORTED = ("scalify_matmul_scale_log2", "scalify_matmul_workspace_size",
             "scalify_matmul_noalloc", "scalify_rmsnorm_fwd",
             "scalify_rmsnorm_bwd_workspace_size", "scalify_rmsnorm_bwd",
             "scalify_attention_fwd_workspace_size", "scalify_attention_fwd",
-            "scalify_attention_bwd_workspace_size", "scalify_attention_bwd")
+            "scalify_attention_bwd_workspace_size", "scalify_attention_bwd",
+            "scalify_cross_entropy_fwd_workspace_size", "scalify_cross_entropy_fwd",
+            "scalify_cross_entropy_bwd_workspace_size", "scalify_cross_entropy_bwd",
+            "scalify_distillation_fwd_workspace_size", "scalify_distillation_fwd",
+            "scalify_distillation_bwd_workspace_size", "scalify_distillation_bwd")
 
 _lib = None
 
@@ -137,6 +141,23 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.scalify_attention_bwd.argtypes = [A, A, A, A, A, vp, A, A, A, P(CAttentionOpts), i32, i32, i32, vp,
                                           vp, ctypes.c_size_t, vp]
     lib.scalify_attention_bwd.restype = ctypes.c_int
+    sz = ctypes.c_size_t
+    lib.scalify_cross_entropy_fwd_workspace_size.argtypes = [i64, i64, i64, i32]
+    lib.scalify_cross_entropy_fwd_workspace_size.restype = sz
+    lib.scalify_cross_entropy_fwd.argtypes = [A, A, vp, vp, vp, vp, vp, sz, vp]
+    lib.scalify_cross_entropy_fwd.restype = ctypes.c_int
+    lib.scalify_cross_entropy_bwd_workspace_size.argtypes = [i64, i64, i64, i32, i32]
+    lib.scalify_cross_entropy_bwd_workspace_size.restype = sz
+    lib.scalify_cross_entropy_bwd.argtypes = [vp, vp, A, A, vp, vp, vp, A, A, i32, i32, i32, vp, vp, sz, vp]
+    lib.scalify_cross_entropy_bwd.restype = ctypes.c_int
+    lib.scalify_distillation_fwd_workspace_size.argtypes = [i64, i64, i64, i64, i32]
+    lib.scalify_distillation_fwd_workspace_size.restype = sz
+    lib.scalify_distillation_fwd.argtypes = [A, A, A, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+    lib.scalify_distillation_fwd.restype = ctypes.c_int
+    lib.scalify_distillation_bwd_workspace_size.argtypes = [i64, i64, i64, i64, i32, i32]
+    lib.scalify_distillation_bwd_workspace_size.restype = sz
+    lib.scalify_distillation_bwd.argtypes = [vp, vp, A, A, A, vp, f32, vp, vp, vp, A, A, i32, i32, i32, vp, vp, sz, vp]
+    lib.scalify_distillation_bwd.restype = ctypes.c_int
     lib.scalify_status_string.argtypes = [i32]
     lib.scalify_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -567,6 +588,114 @@ def scalify_attention_bwd(dout: ScaledArray, q: ScaledArray, k: ScaledArray, v: 
                                    int(bool(saturate)), _ptr_or_none(amax_out), _ptr_or_none(ws),
                                    ws.numel() if ws is not None else 0, _stream_handle(stream))
     _check(st, "scalify_attention_bwd")
+
+
+def _check_index(t: torch.Tensor, n: int, name: str):
+    if t.dtype != torch.int64 or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{name}: contiguous int64 of {n} elements")
+
+
+def scalify_cross_entropy_fwd_workspace_size(R: int, V: int, D: int, w_fmt: int) -> int:
+    return int(load_library().scalify_cross_entropy_fwd_workspace_size(R, V, D, int(w_fmt)))
+
+
+def scalify_cross_entropy_fwd(x: ScaledArray, w: ScaledArray, labels: torch.Tensor, loss: torch.Tensor, *,
+                              lse: torch.Tensor = None, row_scale: torch.Tensor = None, ws: torch.Tensor = None,
+                              stream=None) -> None:
+    """Softmax cross entropy of the rows of x (R x D) against the output matrix w
+    (V x D); see scalify_cross_entropy_fwd in include/scalify.h. labels: contiguous
+    int64 [R]; loss, lse and row_scale: contiguous fp32 [R], the last two optional."""
+    R, D = x.shape
+    V = w.shape[0]
+    _check_index(labels, R, "labels")
+    _check_operands((x, w), (labels, ws), ((loss, R), (lse, R), (row_scale, R)), stream)
+    if ws is None:
+        ws = _call_workspace(scalify_cross_entropy_fwd_workspace_size(R, V, D, w.fmt), x.data.device, stream)
+    st = load_library().scalify_cross_entropy_fwd(
+        _struct_or_none(x), _struct_or_none(w), labels.data_ptr(), _ptr_or_none(row_scale), loss.data_ptr(),
+        _ptr_or_none(lse), _ptr_or_none(ws), ws.numel() if ws is not None else 0, _stream_handle(stream))
+    _check(st, "scalify_cross_entropy_fwd")
+
+
+def scalify_cross_entropy_bwd_workspace_size(R: int, V: int, D: int, w_fmt: int, rescale: int = RESCALE_AMAX) -> int:
+    return int(load_library().scalify_cross_entropy_bwd_workspace_size(R, V, D, int(w_fmt), int(rescale)))
+
+
+def scalify_cross_entropy_bwd(x: ScaledArray, w: ScaledArray, labels: torch.Tensor, lse: torch.Tensor, *,
+                              dx: ScaledArray = None, dw: ScaledArray = None, dloss: torch.Tensor = None,
+                              dloss_scale: torch.Tensor = None, row_scale: torch.Tensor = None,
+                              rescale: int = RESCALE_AMAX, target_log2: int = 0, saturate: bool = True,
+                              amax_out: torch.Tensor = None, ws: torch.Tensor = None, stream=None) -> None:
+    """Gradients of the cross entropy with their rescales; see
+    scalify_cross_entropy_bwd in include/scalify.h. lse: what the forward stored;
+    dloss: contiguous fp32 [R] or None (1), times dloss_scale; amax_out: fp32 [2]."""
+    R, D = x.shape
+    V = w.shape[0]
+    _check_index(labels, R, "labels")
+    _check_operands((x, w, dx, dw), (labels, ws),
+                    ((lse, R), (dloss, R), (dloss_scale, 1), (row_scale, R), (amax_out, 2)), stream)
+    if ws is None:
+        ws = _call_workspace(scalify_cross_entropy_bwd_workspace_size(R, V, D, w.fmt, rescale), x.data.device, stream)
+    st = load_library().scalify_cross_entropy_bwd(
+        _ptr_or_none(dloss), _ptr_or_none(dloss_scale), _struct_or_none(x), _struct_or_none(w), labels.data_ptr(),
+        _ptr_or_none(row_scale), lse.data_ptr(), _struct_or_none(dx), _struct_or_none(dw), int(rescale),
+        int(target_log2), int(bool(saturate)), _ptr_or_none(amax_out), _ptr_or_none(ws),
+        ws.numel() if ws is not None else 0, _stream_handle(stream))
+    _check(st, "scalify_cross_entropy_bwd")
+
+
+def scalify_distillation_fwd_workspace_size(R: int, V: int, D: int, top: int, w_fmt: int) -> int:
+    return int(load_library().scalify_distillation_fwd_workspace_size(R, V, D, top, int(w_fmt)))
+
+
+def scalify_distillation_fwd(x: ScaledArray, w: ScaledArray, teacher: ScaledArray, index: torch.Tensor,
+                             loss: torch.Tensor, *, temperature: float = 1.0, lse: torch.Tensor = None,
+                             picked: torch.Tensor = None, row_scale: torch.Tensor = None, ws: torch.Tensor = None,
+                             stream=None) -> None:
+    """Distillation loss of the rows of x against a teacher's top logits; see
+    scalify_distillation_fwd in include/scalify.h. teacher: [R, top]; index:
+    contiguous int64 [R, top]; loss, lse: contiguous fp32 [R]; picked: fp32 [R, top]."""
+    R, D = x.shape
+    V, top = w.shape[0], teacher.shape[1]
+    _check_index(index, R * top, "index")
+    _check_operands((x, w, teacher), (index, ws), ((loss, R), (lse, R), (picked, R * top), (row_scale, R)), stream)
+    if ws is None:
+        ws = _call_workspace(scalify_distillation_fwd_workspace_size(R, V, D, top, w.fmt), x.data.device, stream)
+    st = load_library().scalify_distillation_fwd(
+        _struct_or_none(x), _struct_or_none(w), _struct_or_none(teacher), index.data_ptr(), float(temperature),
+        _ptr_or_none(row_scale), loss.data_ptr(), _ptr_or_none(lse), _ptr_or_none(picked), _ptr_or_none(ws),
+        ws.numel() if ws is not None else 0, _stream_handle(stream))
+    _check(st, "scalify_distillation_fwd")
+
+
+def scalify_distillation_bwd_workspace_size(R: int, V: int, D: int, top: int, w_fmt: int,
+                                            rescale: int = RESCALE_AMAX) -> int:
+    return int(load_library().scalify_distillation_bwd_workspace_size(R, V, D, top, int(w_fmt), int(rescale)))
+
+
+def scalify_distillation_bwd(x: ScaledArray, w: ScaledArray, teacher: ScaledArray, index: torch.Tensor,
+                             lse: torch.Tensor, picked: torch.Tensor, *, temperature: float = 1.0,
+                             dx: ScaledArray = None, dw: ScaledArray = None, dloss: torch.Tensor = None,
+                             dloss_scale: torch.Tensor = None, row_scale: torch.Tensor = None,
+                             rescale: int = RESCALE_AMAX, target_log2: int = 0, saturate: bool = True,
+                             amax_out: torch.Tensor = None, ws: torch.Tensor = None, stream=None) -> None:
+    """Gradients of the distillation loss with their rescales; see
+    scalify_distillation_bwd in include/scalify.h. lse, picked: what the forward stored."""
+    R, D = x.shape
+    V, top = w.shape[0], teacher.shape[1]
+    _check_index(index, R * top, "index")
+    _check_operands((x, w, teacher, dx, dw), (index, ws),
+                    ((lse, R), (picked, R * top), (dloss, R), (dloss_scale, 1), (row_scale, R), (amax_out, 2)), stream)
+    if ws is None:
+        ws = _call_workspace(scalify_distillation_bwd_workspace_size(R, V, D, top, w.fmt, rescale), x.data.device,
+                             stream)
+    st = load_library().scalify_distillation_bwd(
+        _ptr_or_none(dloss), _ptr_or_none(dloss_scale), _struct_or_none(x), _struct_or_none(w),
+        _struct_or_none(teacher), index.data_ptr(), float(temperature), _ptr_or_none(row_scale), lse.data_ptr(),
+        picked.data_ptr(), _struct_or_none(dx), _struct_or_none(dw), int(rescale), int(target_log2),
+        int(bool(saturate)), _ptr_or_none(amax_out), _ptr_or_none(ws), ws.numel() if ws is not None else 0,
+        _stream_handle(stream))
+    _check(st, "scalify_distillation_bwd")
 
 
 def empty_scaled(rows: int, cols: int, fmt: int, device, ld: int = None) -> ScaledArray:

@@ -13,7 +13,7 @@ destination and C operand are the same a[n:n+3], a write of 0, a read into a
 VGPR) names one of them -- the compiler spilling into it or using it as the
 data of a load or an MFMA operand.
 
-No GEMM, attention or RMS norm kernel may use scratch memory, but for the fused
+No GEMM, attention, RMS norm or loss kernel may use scratch memory, but for the fused
 epilogue of the 8-wave GEMM kernel (gemm_*_fused), which holds accumulators,
 residual codes and channel exponents at once and keeps some of them there.
 
@@ -119,11 +119,11 @@ _MID_KERNEL = re.compile(r"mid_gemm_kernelILb[01]ELb[01]ELi\d+ELi\d+ELi(\d+)ELi\
 
 def pinned_kernel(src: str, name: str) -> bool:
     """Whether a kernel of this source that multiplies into AGPRs keeps its
-    accumulators in asm-named ones: every such kernel of the gemm_* sources,
+    accumulators in asm-named ones: every such kernel of the gemm_* and loss_* sources,
     and of the mid_* sources those with 256 columns (8 accumulator tiles per
     row of tiles); the others leave their accumulators to the compiler."""
     base = os.path.basename(src)
-    if base.startswith("gemm_"):
+    if base.startswith(("gemm_", "loss_")):
         return True
     if base.startswith("mid_"):
         m = _MID_KERNEL.search(name)
@@ -206,7 +206,7 @@ def build(verbose: bool = False) -> str:
                 raise RuntimeError(f"hipcc failed for {src}:\n{r.stderr}")
             if verbose and r.stderr.strip():
                 print(r.stderr)
-            if os.path.basename(src).startswith(("gemm_", "mid_", "wave_", "attention_", "rmsnorm")):
+            if os.path.basename(src).startswith(("gemm_", "mid_", "wave_", "attention_", "rmsnorm", "loss")):
                 check_code(obj, tmp)
             return obj
 

@@ -380,6 +380,11 @@ struct AccTile;
         asm volatile("v_mfma_f32_16x16x128_f8f6f4 a[" r "], %0, %1, a[" r "] cbsz:1 blgp:1"    \
                      :: "v"(b), "v"(a) : "a" r0, "a" r1, "a" r2, "a" r3);                      \
     }                                                                                          \
+    /* F16 operands, 32 k */                                                                   \
+    static __device__ __forceinline__ void mfma_f16(const v4i& b, const v4i& a) {              \
+      asm volatile("v_mfma_f32_16x16x32_f16 a[" r "], %0, %1, a[" r "]"                        \
+                   :: "v"(b), "v"(a) : "a" r0, "a" r1, "a" r2, "a" r3);                        \
+    }                                                                                          \
     static __device__ __forceinline__ void zero() {                                            \
       asm volatile("v_accvgpr_write_b32 a" r0 ", 0\n\tv_accvgpr_write_b32 a" r1 ", 0\n\t"       \
                    "v_accvgpr_write_b32 a" r2 ", 0\n\tv_accvgpr_write_b32 a" r3 ", 0"          \

@@ -1,0 +1,133 @@
+// Internal interface of the losses from hidden states and the output matrix:
+// softmax cross entropy and distillation from a teacher's top logits.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace scalify {
+
+// Words of the workspace header (kHeaderBytes):
+enum LossWord : int {
+  LOSS_COUNT = 0,   // rows that count
+  LOSS_CMAX = 1,    // largest finite |upstream gradient| of them, fp32 bits
+  LOSS_RMAX = 2,    // largest row scale of them, fp32 bits
+  LOSS_AMAX_DX = 3, // statistics of the gradients' data, in the products' units
+  LOSS_AMAX_DW = 4,
+};
+
+constexpr int kLossMaxTop = 256;  // teacher's entries of a row
+// The gradient of the logits is kept in F16 as 2^14 c (p - q) with c at most 1 in
+// magnitude (below 2^15): normal numbers down to |c (p - q)| = 2^-28.
+constexpr int kLossGradLog2 = 14;
+
+struct LossParams {
+  // the call's operands
+  const void *x, *w;
+  int64_t ldx, ldw;
+  int x_fmt, w_fmt;
+  const float *s_x, *s_w, *row_scale;
+  int R, V, D;
+  const int64_t* labels;  // cross entropy, else NULL
+  const int64_t* index;   // distillation: [R][top]
+  const void* teacher;
+  int64_t ldt;
+  int t_fmt, top;
+  const float* s_t;
+  float temp;
+  const float *dloss, *s_dloss;
+  float *loss, *lse, *picked;
+  void *dx, *dw;
+  int64_t lddx, lddw;
+  int dx_fmt, dw_fmt;
+  float *dx_scale, *dw_scale, *amax_out;
+  int mode, target, sat;
+  // workspace; rows that count stand in their order at 0 .. count - 1
+  uint32_t* hdr;
+  int *rows, *pos;     // [R] row of a place; place of a row, or -1
+  int* label;          // [R] of places
+  float *factor;       // [R] logits in base 2 are factor * (x . w)
+  float *lse2, *coef;  // [R] log-sum-exp in base 2; upstream gradient over 2^E, times 2^14
+  float* picked2;      // [R] label's logit in base 2
+  int* top32;          // [R][topp] teacher's tokens, -1 where absent
+  int topp;
+  void *xc, *xw;       // F16 rows of x; times their row scale over the largest
+  int64_t ldxc;
+  void* w16;           // F16 rows of a piece of w (8 bits, or columns no multiple of 8)
+  int64_t ldw16;
+  int piece;           // rows of w at a time
+  float2* stats;       // [2 tiles of V][R] maximum (base 2) and sum
+  void* dz;            // F16 [R][ldz]
+  int64_t ldz;
+  float* part;         // [splits][R][ldp] products of dx
+  float* dw32;         // [V][ldp] (dynamic rescale)
+  int64_t ldp;
+  int splits;
+};
+
+// Sizes that the host decides: pieces of w, splits of dx, and the bytes of a workspace.
+struct LossPlan {
+  int piece, splits, topp;
+  bool copy_w;
+  int64_t ldxc, ldw16, ldz, ldp;
+  size_t bytes;
+};
+// Also sets the workspace's pointers of p, where p is not NULL (base 256-byte aligned).
+LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool back, bool amax, LossParams* p, void* base);
+
+hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s);
+hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s);
+
+// One launch, by its own status alone (not by an error of an earlier call).
+template <typename... Args>
+hipError_t launch_one(void (*kernel)(Args...), int64_t groups, int threads, hipStream_t s, Args... args) {
+  void* a[] = {(void*)&args...};
+  const hipError_t e = hipLaunchKernel((const void*)kernel, dim3((unsigned)groups), dim3((unsigned)threads), a, 0, s);
+  if (e != hipSuccess) (void)hipGetLastError();
+  return e;
+}
+
+// ---- one F16 product C[M][N] = sum_k A B of the losses (loss_gemm.h)
+
+enum LossEpi : int {
+  LOSS_STATS = 0,  // logits: row statistics, the label's logit
+  LOSS_PICK = 1,   // logits: row statistics, the logits of the teacher's tokens
+  LOSS_DZ = 2,     // logits: their gradient, F16
+  LOSS_DX = 3,     // dz w: fp32, added to what earlier pieces left
+  LOSS_DW = 4,     // dz^T x: fp32, or codes
+};
+
+struct LossGemm {
+  const void *a, *b;
+  int64_t lda, ldb;       // bytes
+  int M, N, K;
+  int count_is;           // the dimension that is the number of rows that count: 0 M, 1 K
+  const uint32_t* hdr;
+  int splits, k_split;    // k of a split (a multiple of 128)
+  int v0;                 // first row of w
+  // logits
+  const float *factor, *lse2, *coef;
+  const int* label;
+  float* picked2;
+  const int* top32;
+  int topp, top;
+  const int* rows;
+  float* picked;
+  float2* stats;
+  int64_t R;
+  void* dz;
+  int64_t ldz;
+  // gradients
+  float* part;
+  int64_t ldp;
+  int accumulate;
+  void* out;
+  int64_t ldo;
+  int out_fmt, sat, mode;
+  uint32_t* amax;
+  const float *s0, *s1;   // factors of the propagated scale
+  int rowscaled;          // a factor of the largest row scale is due
+};
+hipError_t launch_loss_logits(const LossGemm& p, int epi, int grid, hipStream_t s);
+hipError_t launch_loss_grads(const LossGemm& p, int epi, int grid, hipStream_t s);
+
+}  // namespace scalify

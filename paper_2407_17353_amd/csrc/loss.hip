@@ -1,0 +1,638 @@
+// Losses from hidden states x and the output matrix w: softmax cross entropy and
+// distillation from a teacher's top logits, without the R x V logits.
+//
+//   z_ij = s_x s_w r_i (x_i . w_j) / T, lse_i = log sum_j exp z_ij
+//   cross entropy (T = 1): loss_i = lse_i - z_i,y_i, dz_ij = g_i (p_ij - [j = y_i])
+//   distillation: q_i the softmax of the teacher's t_i / T over its tokens,
+//     loss_i = T^2 sum_k q_k (log q_k - z_k + lse_i), dz_ij = g_i T (p_ij - q_ij)
+//   dx_i = s_w sum_j dz_ij w_j, dw_j = s_x sum_i dz_ij r_i x_i, p = exp(z - lse)
+//
+// Rows that do not count (no label or teacher, an upstream gradient of 0) need no
+// work: the others are gathered first, as F16, and every product runs over them
+// alone. The forward's product (loss_gemm.h) leaves a maximum and a sum for each 128
+// columns of a row, which a kernel here joins. The backward goes over w in pieces:
+// a piece's logits again, their gradient dz in F16 (rounded once, half a step: 2^-12),
+// dx += dz w and the piece's rows of dw = dz^T x. A piece is as large as 512 MiB of dz
+// allow: each one adds to dx, which costs 8 bytes an element and piece.
+#include "attention_dev.h"
+#include "kernels.h"
+#include "loss.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace scalify {
+
+// ---- which rows count
+
+// Distillation: pos[row] = 0 where the row has a token of the teacher with a logit
+// that is not -Inf, else -1. A wave a row.
+__global__ __launch_bounds__(256) void loss_flags_kernel(LossParams p);
+
+__device__ __forceinline__ float load_any(const void* base, int fmt, int64_t e) {
+  if (fmt == kF32) return ((const float*)base)[e];
+  if (fmt == kF16) return decode_hw<kF16>(((const uint16_t*)base)[e]);
+  const uint32_t c = ((const uint8_t*)base)[e];
+  return fmt == kE4M3 ? decode_hw<kE4M3>(c) : decode_hw<kE5M2>(c);
+}
+__device__ __forceinline__ float scale_of(const float* s) { return s ? *s : 1.0f; }
+__device__ __forceinline__ float wave_max(float v) {
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// A row's teacher in a wave: entry lane + 64 j in registers j; token -1 where there is none.
+constexpr int kTopRegs = kLossMaxTop / 64;
+struct TeacherRow {
+  int token[kTopRegs];
+  float t[kTopRegs];  // logit / T, -Inf where there is no token
+};
+__device__ __forceinline__ TeacherRow load_teacher(const LossParams& p, int64_t row, int lane) {
+  TeacherRow r;
+  const float f = scale_of(p.s_t) / p.temp;
+#pragma unroll
+  for (int j = 0; j < kTopRegs; ++j) {
+    const int e = lane + 64 * j;
+    r.token[j] = -1;
+    r.t[j] = -__builtin_inff();
+    if (e < p.top) {
+      const int64_t i = p.index[row * p.top + e];
+      if (i >= 0 && i < p.V) {
+        r.token[j] = (int)i;
+        r.t[j] = load_any(p.teacher, p.t_fmt, row * p.ldt + e) * f;
+      }
+    }
+  }
+  return r;
+}
+// The entries' probabilities, and the logarithms of these.
+__device__ __forceinline__ void teacher_softmax(const TeacherRow& r, float (&q)[kTopRegs], float (&logq)[kTopRegs]) {
+  float m = -__builtin_inff(), n = 0.f;
+#pragma unroll
+  for (int j = 0; j < kTopRegs; ++j) m = fmaxf(m, r.t[j]);
+  m = wave_max(m);
+  if (m == -__builtin_inff()) m = 0.f;
+#pragma unroll
+  for (int j = 0; j < kTopRegs; ++j) {
+    q[j] = expf(r.t[j] - m);
+    n += q[j];
+  }
+  n = wave_sum(n);
+  const float l = logf(n);
+#pragma unroll
+  for (int j = 0; j < kTopRegs; ++j) {
+    logq[j] = r.t[j] - m - l;
+    q[j] /= n;
+  }
+}
+
+__global__ __launch_bounds__(256) void loss_flags_kernel(LossParams p) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < p.R; row += (int64_t)gridDim.x * 4) {
+    const TeacherRow r = load_teacher(p, row, lane);
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < kTopRegs; ++j) any |= r.t[j] != -__builtin_inff();  // (a NaN counts)
+    const bool some = __ballot(any) != 0;
+    if (lane == 0) p.pos[row] = some ? 0 : -1;
+  }
+}
+
+// Rows that count, in order, their number, and the largest upstream gradient and row
+// scale among them. One workgroup: a thread has consecutive rows.
+__global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
+  __shared__ int sums[16];
+  __shared__ float cs[16], rs[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t per = (p.R + 1023) / 1024, lo = tid * per, hi = lo + per < p.R ? lo + per : p.R;
+  auto counts = [&](int64_t i) {
+    const bool has = p.labels ? p.labels[i] >= 0 && p.labels[i] < p.V : p.pos[i] >= 0;
+    return has && !(p.dloss && p.dloss[i] == 0.0f);
+  };
+  int n = 0;
+  float c = 0.f, r = 0.f;
+  for (int64_t i = lo; i < hi; ++i)
+    if (counts(i)) {
+      ++n;
+      const float g = fabsf(p.dloss ? p.dloss[i] * p.temp : p.temp);
+      if (g < __builtin_inff()) c = fmaxf(c, g);
+      if (p.row_scale) r = fmaxf(r, p.row_scale[i]);
+    }
+  int at = n;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(at, o, 64);
+    if (lane >= o) at += v;
+  }
+  c = wave_max(c), r = wave_max(r);
+  if (lane == 63) sums[wave] = at;
+  if (lane == 0) cs[wave] = c, rs[wave] = r;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) before += sums[w];
+    all += sums[w];
+  }
+  at += before - n;
+  for (int64_t i = lo; i < hi; ++i) {
+    const bool on = counts(i);
+    p.pos[i] = on ? at : -1;
+    if (on) p.rows[at++] = (int)i;
+  }
+  if (tid == 0) {
+    for (int w = 1; w < 16; ++w) c = fmaxf(c, cs[w]), r = fmaxf(r, rs[w]);
+    p.hdr[LOSS_COUNT] = (uint32_t)all;
+    p.hdr[LOSS_CMAX] = __float_as_uint(c);
+    p.hdr[LOSS_RMAX] = __float_as_uint(r);
+    p.hdr[LOSS_AMAX_DX] = p.hdr[LOSS_AMAX_DW] = 0u;
+  }
+}
+
+__device__ __forceinline__ int hdr_exponent(const uint32_t* hdr, int word) {
+  return hdr[word] == 0u ? 0 : floor_log2_bits(hdr[word]);
+}
+
+// Eight codes from element e of a row on, as F16, those past the row's D columns 0.
+__device__ __forceinline__ u4 load_tail8(int fmt, const void* base, int64_t e, int left) {
+  u4 v = load_f16x8(fmt, base, e);
+  if (left < 8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (2 * i >= left) v[i] = 0u;
+      else if (2 * i + 1 >= left) v[i] &= 0xFFFFu;
+    }
+  }
+  return v;
+}
+
+// The rows that count: x in F16 (D rounded up to 8 columns), and its numbers.
+__global__ __launch_bounds__(256) void loss_gather_kernel(LossParams p) {
+  const int count = (int)p.hdr[LOSS_COUNT], chunks = (p.D + 7) / 8;
+  const int ec = hdr_exponent(p.hdr, LOSS_CMAX), er = hdr_exponent(p.hdr, LOSS_RMAX);
+  for (int64_t i = blockIdx.x; i < count; i += gridDim.x) {
+    const int64_t row = p.rows[i];
+    const float r = p.row_scale ? p.row_scale[row] : 1.0f;
+    if (threadIdx.x == 0) {
+      // logits in base 2; a factor past [2^-100, 2^64] gives equal ones, or the largest alone
+      const int e = pow2_exponent(p.s_x) + pow2_exponent(p.s_w) + (p.row_scale ? pow2_exponent(p.row_scale + row) : 0);
+      const float f = ldexpf(kLog2e / p.temp, e < -200 ? -200 : (e > 200 ? 200 : e));
+      p.factor[i] = fminf(fmaxf(f, 0x1p-100f), 0x1p64f);
+      if (p.labels) p.label[i] = (int)p.labels[row];
+      if (p.lse2) {
+        p.lse2[i] = p.lse[row] * kLog2e;
+        p.coef[i] = ldexpf(p.dloss ? p.dloss[row] * p.temp : p.temp, kLossGradLog2 - ec);
+      }
+    }
+    if (p.top32)
+      for (int j = threadIdx.x; j < p.topp; j += 256) {
+        const int64_t t = j < p.top ? p.index[row * p.top + j] : -1;
+        p.top32[i * p.topp + j] = t >= 0 && t < p.V ? (int)t : -1;
+      }
+    const float rf = p.xw ? ldexpf(r, -er) : 1.0f;
+    for (int c = threadIdx.x; c < chunks; c += 256) {
+      const u4 v = load_tail8(p.x_fmt, p.x, row * p.ldx + 8 * c, p.D - 8 * c);
+      *(u4*)((uint16_t*)p.xc + i * p.ldxc + 8 * c) = v;
+      if (p.xw) {
+        h8 h = __builtin_bit_cast(h8, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) h[k] = (_Float16)((float)h[k] * rf);
+        *(h8*)((uint16_t*)p.xw + i * p.ldxc + 8 * c) = h;
+      }
+    }
+  }
+}
+
+// n rows of w from v0 on as F16, D rounded up to 8 columns.
+__global__ __launch_bounds__(256) void loss_copy_w_kernel(LossParams p, int v0, int n) {
+  const int chunks = (p.D + 15) / 16, cols = (p.D + 7) & ~7;
+  const int64_t all = (int64_t)n * chunks;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / chunks;
+    const int c = 16 * (int)(i - r * chunks);
+    uint16_t* o = (uint16_t*)p.w16 + r * p.ldw16 + c;
+    const int64_t e = (v0 + r) * p.ldw + c;
+    u4 lo, hi;
+    if (p.w_fmt == kF16) {
+      lo = load_tail8(kF16, p.w, e, p.D - c);
+      hi = c + 8 < cols ? load_tail8(kF16, p.w, e + 8, p.D - c - 8) : u4{0u, 0u, 0u, 0u};
+    } else {  // (rows of 8 bits hold whole groups of 16)
+      const u4 v = *(const u4*)((const uint8_t*)p.w + e);
+      lo = to_f16x8(p.w_fmt, u4{v[0], v[1], 0u, 0u});
+      hi = to_f16x8(p.w_fmt, u4{v[2], v[3], 0u, 0u});
+      if (c + 16 > p.D) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          lo[k] &= (c + 2 * k < p.D ? 0xFFFFu : 0u) | (c + 2 * k + 1 < p.D ? 0xFFFF0000u : 0u);
+          hi[k] &= (c + 8 + 2 * k < p.D ? 0xFFFFu : 0u) | (c + 9 + 2 * k < p.D ? 0xFFFF0000u : 0u);
+        }
+      }
+    }
+    *(u4*)o = lo;
+    if (c + 8 < cols) *(u4*)(o + 8) = hi;
+  }
+}
+
+// Joins the maxima and sums of a row's column groups: log-sum-exp, and the cross
+// entropy. 64 places a workgroup, the groups dealt to its four waves (a fixed order).
+// Rows that do not count get 0.
+__global__ __launch_bounds__(256) void loss_join_kernel(LossParams p, int groups) {
+  __shared__ float sm[4][64], ss[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int count = (int)p.hdr[LOSS_COUNT];
+  for (int64_t b = blockIdx.x; b * 64 < p.R; b += gridDim.x) {
+    const int64_t i = b * 64 + lane;
+    float m = -__builtin_inff(), n = 0.f;
+    if (i < count) {
+#pragma unroll 4
+      for (int g = wave; g < groups; g += 4) {
+        const float2 v = p.stats[(int64_t)g * p.R + i];
+        const float t = fmaxf(m, v.x);  // (a NaN is in the sums)
+        const float a = m == -__builtin_inff() ? 0.f : n * exp2f(m - t), c = v.x == -__builtin_inff() ? 0.f : v.y * exp2f(v.x - t);
+        n = a + c;
+        m = t;
+      }
+    }
+    sm[wave][lane] = m;
+    ss[wave][lane] = n;
+    __syncthreads();
+    if (wave == 0) {
+      if (i < count) {
+        for (int w = 1; w < 4; ++w) {
+          const float t = fmaxf(m, sm[w][lane]);
+          const float a = m == -__builtin_inff() ? 0.f : n * exp2f(m - t);
+          const float c = sm[w][lane] == -__builtin_inff() ? 0.f : ss[w][lane] * exp2f(sm[w][lane] - t);
+          n = a + c;
+          m = t;
+        }
+        const float l2 = m + log2f(n);
+        const int row = p.rows[i];
+        if (p.lse) p.lse[row] = kLn2 * l2;
+        if (p.labels) p.loss[row] = kLn2 * (l2 - p.picked2[i]);
+      }
+      if (i < p.R && p.pos[i] < 0) {
+        p.loss[i] = 0.f;
+        if (p.lse) p.lse[i] = 0.f;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Distillation's loss, and 0 for logits of tokens that are not there. A wave a row.
+__global__ __launch_bounds__(256) void loss_top_kernel(LossParams p) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < p.R; row += (int64_t)gridDim.x * 4) {
+    const bool on = p.pos[row] >= 0;
+    const TeacherRow r = load_teacher(p, row, lane);
+    float q[kTopRegs], logq[kTopRegs], sum = 0.f;
+    teacher_softmax(r, q, logq);
+    const float l = on ? p.lse[row] : 0.f;
+#pragma unroll
+    for (int j = 0; j < kTopRegs; ++j) {
+      const int e = lane + 64 * j;
+      if (e >= p.top) continue;
+      float* z = p.picked + row * p.top + e;
+      if (!on || r.token[j] < 0)
+        *z = 0.f;
+      else if (q[j] != 0.f)
+        sum += q[j] * (logq[j] - (*z - l));
+    }
+    sum = wave_sum(sum);
+    if (lane == 0 && on) p.loss[row] = p.temp * p.temp * sum;
+  }
+}
+
+// Distillation's backward: dz of the teacher's tokens in the piece of n rows of w from
+// v0 on, from their stored logits: c (p - q), q the sum over a token's entries. A wave
+// a place.
+__global__ __launch_bounds__(256) void loss_fix_kernel(LossParams p, int v0, int n) {
+  const int lane = threadIdx.x & 63;
+  const int count = (int)p.hdr[LOSS_COUNT];
+  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < count; i += (int64_t)gridDim.x * 4) {
+    const int64_t row = p.rows[i];
+    const TeacherRow r = load_teacher(p, row, lane);
+    float q[kTopRegs], logq[kTopRegs], want[kTopRegs];
+    teacher_softmax(r, q, logq);
+#pragma unroll
+    for (int j = 0; j < kTopRegs; ++j) want[j] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kTopRegs; ++k)
+      for (int o = 0; o < 64 && o + 64 * k < p.top; ++o) {
+        const int token = __shfl(r.token[k], o, 64);
+        const float add = __shfl(q[k], o, 64);
+#pragma unroll
+        for (int j = 0; j < kTopRegs; ++j)
+          if (r.token[j] == token) want[j] += add;
+      }
+    const float l2 = p.lse2[i], c = p.coef[i];
+#pragma unroll
+    for (int j = 0; j < kTopRegs; ++j) {
+      const int e = lane + 64 * j, d = r.token[j] - v0;
+      if (e < p.top && r.token[j] >= 0 && d >= 0 && d < n) {
+        const float prob = exp2f(p.picked[row * p.top + e] * kLog2e - l2);
+        ((_Float16*)p.dz)[i * p.ldz + d] = (_Float16)(c * (prob - want[j]));
+      }
+    }
+  }
+}
+
+// ---- the gradients' rescale and cast
+
+// Unit of the products: a gradient's data in its propagated scale is the product times
+// 2^unit.
+__device__ __forceinline__ int unit_of(const LossParams& p, bool dw) {
+  const int u = hdr_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2;
+  return dw && p.row_scale ? u + hdr_exponent(p.hdr, LOSS_RMAX) : u;
+}
+__device__ __forceinline__ int base_of(const LossParams& p, bool dw) { return pow2_exponent(p.s_dloss) + pow2_exponent(dw ? p.s_x : p.s_w); }
+__device__ __forceinline__ int out_exponent(const LossParams& p, bool dw, int base, int unit) {
+  const uint32_t a = p.hdr[dw ? LOSS_AMAX_DW : LOSS_AMAX_DX];
+  const bool plain = p.mode != 1 || a == 0u || a >= 0x7F800000u;
+  return clamp_e8m0(base + (plain ? 0 : floor_log2_bits(a) + unit - p.target));
+}
+
+// dx: the splits' sum into the first of them, and its statistic.
+__global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
+  const int count = (int)p.hdr[LOSS_COUNT], chunks = (p.D + 3) / 4;
+  const int64_t all = (int64_t)count * chunks;
+  float a = 0.f;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / chunks;
+    const int c = 4 * (int)(i - r * chunks);
+    float4* o = (float4*)(p.part + r * p.ldp + c);
+    float4 v = *o;
+    for (int s = 1; s < p.splits; ++s) {
+      const float4 w = *(const float4*)(p.part + ((int64_t)s * p.R + r) * p.ldp + c);
+      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    if (p.splits > 1) *o = v;
+    a = fmaxf(a, fabsf(v.x));
+    if (c + 1 < p.D) a = fmaxf(a, fabsf(v.y));
+    if (c + 2 < p.D) a = fmaxf(a, fabsf(v.z));
+    if (c + 3 < p.D) a = fmaxf(a, fabsf(v.w));
+  }
+  a = wave_max(a);
+  if ((threadIdx.x & 63) == 0 && a > 0.f) atomicMax(p.hdr + LOSS_AMAX_DX, __float_as_uint(a));
+}
+
+template <int F>
+__device__ __forceinline__ void store_codes(void* out, int64_t e, const uint32_t (&u)[16], int cols, int shift, bool sat) {
+  const bool fast = shift >= kFastShiftMinSub && shift <= kFastShiftMax;
+  uint32_t w[8];
+  encode16<F>(u, shift, fast ? pow2_float(shift) : 1.0f, fast, sat, w);
+  if (cols >= 16) {
+    store_words16<F>(out, e, w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 15; ++i)
+      if (i < cols) store1<F>(out, e + i, word_code<F>(w, i));
+  }
+}
+
+// Rows of fp32 products cast to codes; dx: rows that do not count are 0.
+__global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw) {
+  const bool dw = is_dw != 0;
+  const int unit = unit_of(p, dw), base = base_of(p, dw), e_out = out_exponent(p, dw, base, unit);
+  const int shift = e_out - base - unit, chunks = (p.D + 15) / 16;
+  const int64_t all = (int64_t)(dw ? p.V : p.R) * chunks;
+  const float* src = dw ? p.dw32 : p.part;
+  void* out = dw ? p.dw : p.dx;
+  const int fmt = dw ? p.dw_fmt : p.dx_fmt;
+  const int64_t ldo = dw ? p.lddw : p.lddx;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / chunks;
+    const int c = 16 * (int)(i - r * chunks), cols = p.D - c;
+    const int64_t from = dw ? r : p.pos[r];
+    uint32_t u[16];
+    if (from >= 0) {
+      load16<kF32>(src, from * p.ldp + c, u);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) u[k] = 0u;
+    }
+    const int64_t e = r * ldo + c;
+    if (fmt == kF16) store_codes<kF16>(out, e, u, cols, shift, p.sat);
+    else if (fmt == kE4M3) store_codes<kE4M3>(out, e, u, cols, shift, p.sat);
+    else store_codes<kE5M2>(out, e, u, cols, shift, p.sat);
+  }
+}
+
+// The gradients' scales and statistics (threads 0 and 1: dx, dw).
+__global__ void loss_scales_kernel(LossParams p) {
+  const bool dw = threadIdx.x == 1;
+  if (!(dw ? p.dw : p.dx)) return;
+  const int unit = unit_of(p, dw), base = base_of(p, dw);
+  *(dw ? p.dw_scale : p.dx_scale) = pow2_float(out_exponent(p, dw, base, unit));
+  if (p.amax_out) p.amax_out[dw ? 1 : 0] = ldexpf(__uint_as_float(p.hdr[dw ? LOSS_AMAX_DW : LOSS_AMAX_DX]), unit);
+}
+
+// ---- host
+
+static int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool back, bool amax, LossParams* p, void* base) {
+  LossPlan z = {};
+  z.copy_w = w_fmt != kF16 || D % 8 != 0;
+  z.topp = (int)up(top, 16);
+  // (a pitch of an odd number of 128 bytes: rows of a power of two would share memory channels)
+  auto pitch = [](int64_t cols) { return up(cols, 64) + (up(cols, 64) / 64 % 2 == 0 ? 64 : 0); };
+  z.ldxc = z.ldw16 = pitch(D);
+  z.ldp = up(D, 16);
+  // rows of w at a time: 512 MiB of dz, 512 MiB of decoded w
+  int64_t most = (int64_t)1 << 20;
+  if (back && R > 0) most = std::min(most, std::max<int64_t>(256, ((int64_t)1 << 28) / R / 256 * 256));
+  if (z.copy_w) most = std::min(most, std::max<int64_t>(256, ((int64_t)1 << 28) / z.ldw16 / 256 * 256));
+  const int64_t pieces = (V + most - 1) / most;
+  z.piece = (int)up((V + pieces - 1) / pieces, 256);
+  z.ldz = pitch(z.piece);
+  z.splits = 1;
+  if (back) {
+    // dx has few tiles: its k is split where that fills the device's rounds of tiles (4.9e12
+    // operations a second and CU) for more than the sums' bytes cost (4e12 a second)
+    const int64_t cus = gemm4_grid(1 << 30), tiles = ((R + 255) / 256) * ((D + 255) / 256);
+    double best = 1e300;
+    for (int s = 1; s <= 64 && (s == 1 || z.piece / s >= 256); ++s) {
+      const double t = (double)((tiles * s + cus - 1) / cus) / s * 2.0 * 65536.0 * z.piece / 4.9e12 +
+                       8.0 * s * (double)R * (double)D / 4e12;
+      if (t < best * 0.98) best = t, z.splits = s;
+    }
+  }
+  size_t at = kHeaderBytes;
+  auto take = [&](auto** to, size_t bytes) {
+    if (p) *to = (std::remove_reference_t<decltype(**to)>*)((uint8_t*)base + at);
+    at += (bytes + 255) / 256 * 256;
+  };
+  LossParams none;
+  LossParams& q = p ? *p : none;
+  if (p) p->hdr = (uint32_t*)base;
+  const size_t r = (size_t)R;
+  take(&q.rows, 4 * r);
+  take(&q.pos, 4 * r);
+  take(&q.factor, 4 * r);
+  take(&q.label, 4 * r);
+  if (top) take(&q.top32, 4 * r * (size_t)z.topp);
+  auto bytes_of = [](int64_t rows, int64_t ld, int64_t size) { return (size_t)rows * (size_t)ld * (size_t)size; };
+  uint16_t *xc = nullptr, *xw = nullptr, *w16 = nullptr, *dz = nullptr;
+  take(&xc, bytes_of(R, z.ldxc, 2));
+  if (z.copy_w) take(&w16, bytes_of(std::min<int64_t>(z.piece, V), z.ldw16, 2));
+  if (back) {
+    take(&q.lse2, 4 * r);
+    take(&q.coef, 4 * r);
+    take(&xw, bytes_of(R, z.ldxc, 2));
+    take(&dz, bytes_of(R, z.ldz, 2));
+    take(&q.part, bytes_of(R, z.ldp, 4 * (int64_t)z.splits));
+    if (amax) take(&q.dw32, bytes_of(V, z.ldp, 4));
+  } else {
+    if (top) {
+      float *lse = nullptr, *picked = nullptr;
+      take(&lse, 4 * r);
+      take(&picked, 4 * r * (size_t)top);
+      if (p && !p->lse) p->lse = lse;
+      if (p && !p->picked) p->picked = picked;
+    }
+    take(&q.picked2, 4 * r);
+    take(&q.stats, 8 * r * (size_t)(2 * ((V + 255) / 256)));
+  }
+  if (p) {
+    p->xc = xc;
+    p->xw = back && p->row_scale ? xw : nullptr;
+    p->w16 = w16;
+    p->dz = dz;
+    p->topp = z.topp;
+    p->ldxc = z.ldxc;
+    p->ldw16 = z.ldw16;
+    p->ldz = z.ldz;
+    p->ldp = z.ldp;
+    p->piece = z.piece;
+    p->splits = z.splits;
+  }
+  z.bytes = at;
+  return z;
+}
+
+static int64_t groups_for(int64_t n, int64_t each, int64_t most) {
+  const int64_t g = (n + each - 1) / each;
+  return g < 1 ? 1 : (g < most ? g : most);
+}
+
+// A workgroup a CU, one at least (no rows: it leaves at once).
+static int grid_for(int64_t tiles) { return std::max(1, gemm4_grid((int)tiles)); }
+
+#define TRY(call)                        \
+  do {                                   \
+    const hipError_t e_ = (call);        \
+    if (e_ != hipSuccess) return e_;     \
+  } while (0)
+
+// Rows that count and their x.
+static hipError_t begin_loss(const LossParams& p, hipStream_t s) {
+  if (!p.labels) TRY(launch_one(loss_flags_kernel, groups_for(p.R, 4, 8192), 256, s, p));
+  TRY(launch_one(loss_scan_kernel, 1, 1024, s, p));
+  return launch_one(loss_gather_kernel, groups_for(p.R, 1, 16384), 256, s, p);
+}
+
+// The product of a piece's logits.
+static hipError_t piece_logits(const LossParams& p, int v0, int n, int epi, LossGemm* g, hipStream_t s) {
+  *g = LossGemm{};
+  if (p.w16) TRY(launch_one(loss_copy_w_kernel, groups_for((int64_t)n * ((p.D + 15) / 16), 1024, 16384), 256, s, p, v0, n));
+  g->a = p.xc;
+  g->lda = 2 * p.ldxc;
+  g->b = p.w16 ? p.w16 : (const void*)((const uint16_t*)p.w + (int64_t)v0 * p.ldw);
+  g->ldb = 2 * (p.w16 ? p.ldw16 : p.ldw);
+  g->M = p.R;
+  g->N = n;
+  g->K = p.D;
+  g->hdr = p.hdr;
+  g->splits = 1;
+  g->v0 = v0;
+  g->factor = p.factor;
+  g->lse2 = p.lse2;
+  g->coef = p.coef;
+  g->label = p.labels ? p.label : nullptr;
+  g->picked2 = p.picked2;
+  g->top32 = p.top32;
+  g->topp = p.topp;
+  g->top = p.top;
+  g->rows = p.rows;
+  g->picked = p.picked;
+  g->stats = p.stats;
+  g->R = p.R;
+  g->dz = p.dz;
+  g->ldz = p.ldz;
+  const int64_t tiles = (int64_t)((p.R + 255) / 256) * ((n + 255) / 256);
+  return launch_loss_logits(*g, epi, grid_for(tiles), s);
+}
+
+hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s) {
+  TRY(begin_loss(p, s));
+  LossGemm g;
+  for (int v0 = 0; v0 < p.V; v0 += p.piece)
+    TRY(piece_logits(p, v0, std::min(p.piece, p.V - v0), p.labels ? LOSS_STATS : LOSS_PICK, &g, s));
+  TRY(launch_one(loss_join_kernel, groups_for(p.R, 64, 16384), 256, s, p, 2 * ((p.V + 255) / 256)));
+  if (!p.labels) TRY(launch_one(loss_top_kernel, groups_for(p.R, 4, 8192), 256, s, p));
+  return hipSuccess;
+}
+
+hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
+  TRY(begin_loss(p, s));
+  for (int v0 = 0; v0 < p.V; v0 += p.piece) {
+    const int n = std::min(p.piece, p.V - v0);
+    LossGemm g;
+    TRY(piece_logits(p, v0, n, LOSS_DZ, &g, s));
+    if (!p.labels) TRY(launch_one(loss_fix_kernel, groups_for(p.R, 4, 8192), 256, s, p, v0, n));
+    const void* w = g.b;
+    const int64_t ldw = g.ldb;
+    if (p.dx) {
+      g.a = p.dz;
+      g.lda = 2 * p.ldz;
+      g.b = w;
+      g.ldb = ldw;
+      g.M = p.R;
+      g.N = p.D;
+      g.K = n;
+      g.splits = p.splits;
+      g.k_split = (int)up((n + p.splits - 1) / p.splits, 128);
+      g.part = p.part;
+      g.ldp = p.ldp;
+      g.accumulate = v0 > 0;
+      const int64_t tiles = (int64_t)((p.R + 255) / 256) * ((p.D + 255) / 256) * p.splits;
+      TRY(launch_loss_grads(g, LOSS_DX, grid_for(tiles), s));
+    }
+    if (p.dw) {
+      g.a = p.dz;
+      g.lda = 2 * p.ldz;
+      g.b = p.xw ? p.xw : p.xc;
+      g.ldb = 2 * p.ldxc;
+      g.M = n;
+      g.N = p.D;
+      g.K = 0;
+      g.count_is = 1;
+      g.splits = 1;
+      g.part = p.dw32;
+      g.ldp = p.ldp;
+      g.out = p.dw;
+      g.ldo = p.lddw;
+      g.out_fmt = p.dw_fmt;
+      g.sat = p.sat;
+      g.mode = p.mode;
+      g.amax = p.hdr + LOSS_AMAX_DW;
+      g.s0 = p.s_dloss;
+      g.s1 = p.s_x;
+      g.rowscaled = p.row_scale != nullptr;
+      const int64_t tiles = (int64_t)((n + 255) / 256) * ((p.D + 255) / 256);
+      TRY(launch_loss_grads(g, LOSS_DW, grid_for(tiles), s));
+    }
+  }
+  if (p.dx) {
+    TRY(launch_one(loss_sum_kernel, groups_for((int64_t)p.R * ((p.D + 3) / 4), 1024, 4096), 256, s, p));
+    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0));
+  }
+  if (p.dw && p.mode == 1)
+    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1));
+  return launch_one(loss_scales_kernel, 1, 2, s, p);
+}
+
+}  // namespace scalify

@@ -1,0 +1,498 @@
+// F16 matrix product of the losses for gfx950, its epilogues fused: the logits
+// z = x w^T with their row statistics (forward) or their gradient (backward), and
+// the products dx = dz w and dw = dz^T x. 8-bit operands are F16 values and come
+// decoded; all sums are fp32.
+//
+// Bound: the matrix instructions (2 M N K operations; a workgroup reads 64 KiB for
+// 8.4e6 of them). The arrangement is that of gemm4_kernel.h, whose tiles have the
+// same bytes (64 k of F16 instead of 128 of FP8): one workgroup of four waves a CU
+// walks its tiles of 256 x 256, a wave holds 128 x 128 of them in AGPRs, loads go
+// straight to LDS two steps ahead, over the end of a tile into the next one.
+// Operands whose k is contiguous ("KC", 128-byte rows) are read with ds_read_b128,
+// the others ("MC", 64 k-rows of 512 bytes) with the transposing ds_read_b64_tr_b16.
+#pragma once
+#include "gemm4_kernel.h"
+#include "loss.h"
+
+namespace scalify {
+
+constexpr int LK = 64;  // k of a step
+typedef _Float16 lh2 __attribute__((ext_vector_type(2)));
+typedef short ls4 __attribute__((ext_vector_type(4)));
+
+// MC tiles: 16-byte chunks of a k-row are permuted in pairs, so that the four rows
+// of a transposing read of 16 lanes, and those of its neighbour, meet distinct banks.
+__device__ __forceinline__ int swz_mc16(int k) { return 2 * ((k & 3) | (((k >> 4) & 1) << 2)); }
+
+// A wave's operands in LDS. Part S (32 k of a step) of the operand of 16 rows or
+// columns 16 i .. of the wave's tile: lane l serves row or column l & 15, k = 16
+// (l >> 4) + 8 S .. + 7 (any order does that both operands share). A lane's address
+// of part 0, i = 0 (wave_first: the wave's first row or column in the tile):
+template <bool MC>
+__device__ __forceinline__ uint32_t operand_addr(int wave_first, int lane) {
+  const int t = lane & 15, g = lane >> 4;
+  if constexpr (MC) {
+    const int k = 16 * g + (t >> 2);
+    return (uint32_t)(k * 512 + 2 * wave_first + swz_mc16(k) * 16 + ((t & 3) >> 1) * 16 + (t & 1) * 8);
+  } else {
+    return (uint32_t)((wave_first + t) * 128 + (((2 * g) ^ swz_kc(t)) * 16));
+  }
+}
+// Read Q of an operand (both parts; KC 2 reads, MC 4). The permutations are of the
+// lane alone, so i and the part only move the address, or flip bits of it.
+template <bool MC, int I, int Q>
+__device__ __forceinline__ void read_part(v4i (&f)[2], const uint8_t* lds, uint32_t addr) {
+  if constexpr (MC) {
+    constexpr int S = Q / 2, H = Q % 2;
+    const ls4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS ls4*)(lds + (addr ^ (32 * I)) + 4096 * S + 2048 * H));
+    const v2i w = __builtin_bit_cast(v2i, v);
+    f[S][2 * H] = w.x;
+    f[S][2 * H + 1] = w.y;
+  } else {
+    f[Q] = *(const v4i*)(lds + (addr ^ (16 * Q)) + 2048 * I);
+  }
+}
+
+// Sum or maximum over the four lanes that hold a row.
+__device__ __forceinline__ float row4_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float row4_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// Exponent of the largest |upstream gradient| (0 where there is none).
+__device__ __forceinline__ int loss_exponent(const uint32_t* hdr, int word) {
+  const uint32_t u = hdr[word];
+  return u == 0u ? 0 : floor_log2_bits(u);
+}
+
+// A value that the compiler forms anew from here on (the flipped addresses would
+// else each stay in a register over the whole loop).
+__device__ __forceinline__ void held(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
+template <bool A_MC, bool B_MC, int EPI>
+__global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
+  using C = WaveCfg<4>;
+  constexpr int WTM = C::WTM, WTN = C::WTN, MI = C::MI, NI = C::NI, BPW = C::BPW;
+  constexpr int STAGE = EPI == LOSS_PICK ? 8192 : (EPI == LOSS_DZ ? 4096 : 0);
+  // [A of even steps | A of odd steps | B | B | the waves' staging]
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TILE_BYTES + 4 * STAGE];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = gridDim.x;
+  const int count = (int)p.hdr[LOSS_COUNT];
+  const int M = p.count_is == 0 ? count : p.M, N = p.N, K = p.count_is == 1 ? count : p.K;
+  const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+  const int T1 = tiles_m * tiles_n, T = T1 * p.splits;
+  const int ntiles = (T - (int)blockIdx.x + G - 1) / G;
+  if (ntiles <= 0) return;
+  const int k_span = p.splits > 1 ? p.k_split : K;
+  const int KT = (k_span + LK - 1) / LK;
+  const int KTe = KT < 2 ? 2 : KT + (KT & 1);  // steps a tile, even
+  const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb;
+
+  uint32_t qa[BPW], qb[BPW];
+  int kc[2];
+#pragma unroll
+  for (int q = 0; q < BPW; ++q) {
+    const uint32_t blk = (uint32_t)(wave * BPW + q);
+    // KC: 8 rows of 128 bytes a block; MC: two k-rows of 512 bytes
+    const int c = (lane & 7) ^ (lane >> 3) ^ (q & 1);
+    const int kr = (int)(2 * blk) + (lane >> 5);
+    const uint32_t cm = (uint32_t)((lane & 31) ^ swz_mc16(kr));
+    qa[q] = A_MC ? (uint32_t)kr * lda + 16u * cm : (blk * 8u + (uint32_t)(lane >> 3)) * lda + 16u * (uint32_t)c;
+    qb[q] = B_MC ? (uint32_t)kr * ldb + 16u * cm : (blk * 8u + (uint32_t)(lane >> 3)) * ldb + 16u * (uint32_t)c;
+    if (q < 2) kc[q] = 8 * c;
+  }
+
+  // Tile r of this workgroup: split and origin.
+  auto origin = [&](int r, int& m0, int& n0, int& split) {
+    const int t = (int)blockIdx.x + r * G;
+    split = p.splits > 1 ? t / T1 : 0;
+    tile_origin(t - split * T1, tiles_m, tiles_n, m0, n0);
+  };
+  // Load cursor: the (tile, step) whose loads go out next; k l_k up to l_end. A KC
+  // operand's buffer starts at the tile's first row, an MC operand's at the step's
+  // first k-row; both end with the matrix, and loads past that, or past l_end, read
+  // zeros.
+  int l_r = 0, l_kt = 0, l_k, l_end;
+  v4i ra, rb;
+  const uint8_t *la, *lb;  // MC: the step's first row
+  uint32_t wa, wb;         // MC: bytes of a row that are left (rows hold whole groups of 8)
+  auto rows_buffer = [&](const void* base, int64_t ld, int row0, int rows) {
+    const int n = min(rows - row0, 256);
+    return make_rsrc((const uint8_t*)base + (int64_t)row0 * ld, (uint32_t)((int64_t)(n - 1) * ld) + 2u * (uint32_t)((K + 7) & ~7));
+  };
+  auto k_buffer = [&](const uint8_t* base, uint32_t ld, uint32_t width) {
+    const int n = min(l_end - l_k, LK);
+    return make_rsrc(base, n > 0 ? (uint32_t)(n - 1) * ld + width : 0u);
+  };
+  auto load_tile = [&]() {
+    int m0, n0, split;
+    origin(l_r, m0, n0, split);
+    l_k = split * k_span;
+    l_end = min(K, l_k + k_span);
+    if constexpr (A_MC) {
+      la = (const uint8_t*)p.a + (int64_t)l_k * p.lda + 2 * (int64_t)m0;
+      wa = 2u * (uint32_t)(((M + 7) & ~7) - m0);
+      ra = k_buffer(la, lda, wa);
+    } else {
+      ra = rows_buffer(p.a, p.lda, m0, M);
+    }
+    if constexpr (B_MC) {
+      lb = (const uint8_t*)p.b + (int64_t)l_k * p.ldb + 2 * (int64_t)n0;
+      wb = 2u * (uint32_t)(((N + 7) & ~7) - n0);
+      rb = k_buffer(lb, ldb, wb);
+    } else {
+      rb = rows_buffer(p.b, p.ldb, n0, N);
+    }
+  };
+  load_tile();
+  auto advance = [&]() {
+    l_k += LK;
+    if (++l_kt == KTe) {
+      l_kt = 0;
+      if (++l_r < ntiles) {
+        load_tile();
+        return;
+      }
+      l_k = l_end;  // (and on from there: nothing is left)
+    }
+    if constexpr (A_MC) {
+      la += (uint64_t)lda * LK;
+      ra = k_buffer(la, lda, wa);
+    }
+    if constexpr (B_MC) {
+      lb += (uint64_t)ldb * LK;
+      rb = k_buffer(lb, ldb, wb);
+    }
+  };
+  // Load j of a step into its stage P: j < BPW are A blocks, the rest B blocks.
+  auto issue_one = [&](int j, int P) {
+    const bool is_a = j < BPW;
+    const int q = is_a ? j : j - BPW;
+    uint32_t off = is_a ? qa[q] : qb[q];
+    if (!(is_a ? A_MC : B_MC)) {
+      off += 2u * (uint32_t)l_k;
+      if (l_k + kc[q & 1] >= l_end) off = 0x80000000u;
+    }
+    load_lds16(is_a ? ra : rb, off, smem + (is_a ? P : 2 + P) * TILE_BYTES + (wave * BPW + q) * 1024);
+  };
+
+  const int wm = (wave / C::WAVES_N) * WTM;
+  const int wn = (wave % C::WAVES_N) * WTN;
+  constexpr int DSA = A_MC ? 4 : 2, DSB = B_MC ? 4 : 2;
+  constexpr int H = 6;
+  constexpr int TS = (NI - H) * MI, AS = (H - 1) * MI, BP = 2 * DSB;
+  constexpr int RX = MI < (NI - 2) * DSB ? MI : (NI - 2) * DSB;
+  static_assert((NI - 2) * DSB <= H * MI, "head too short for its reads");
+  v4i af[2][MI][2];
+  v4i bf[NI][2];
+  uint32_t aa = operand_addr<A_MC>(wm, lane), ab = operand_addr<B_MC>(wn, lane);
+
+  // Schedule of a step: that of gemm4_kernel, with a pair of products in the place of
+  // each of its products (the two k parts of 32).
+  auto head = [&](auto par_tag) {
+    constexpr int P = decltype(par_tag)::value;
+    const uint8_t* cB = smem + (2 + P) * TILE_BYTES;
+    held(ab);
+    static_for<0, H * MI>([&](auto I) {
+      constexpr int i = decltype(I)::value;
+      constexpr int ni = i / MI, u = 2 * (i % MI), ks = u / MI, mi = u % MI;
+      AccTile<mi * NI + ni>::mfma_f16(bf[ni][ks], af[P][mi][ks]);
+      AccTile<(mi + 1) * NI + ni>::mfma_f16(bf[ni][ks], af[P][mi + 1][ks]);
+      if constexpr (i < (NI - 2) * DSB) {
+        constexpr int g = 2 + i / DSB;
+        read_part<B_MC, g, i % DSB>(bf[g], cB, ab);
+      }
+      if constexpr (i == MI - 1) {
+        wait_lgkmcnt<RX>();
+        __builtin_amdgcn_s_barrier();
+      }
+      if constexpr (i >= MI) {
+        constexpr int j = i - MI;
+        static_for<j * BPW / AS, (j + 1) * BPW / AS>([&](auto J) { issue_one(decltype(J)::value, P); });
+      }
+    });
+    wait_vmcnt<BPW>();
+    wait_lgkmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+  };
+  auto tail = [&](auto par_tag) {
+    constexpr int P = decltype(par_tag)::value;
+    const uint8_t* nA = smem + (P ^ 1) * TILE_BYTES;
+    const uint8_t* nB = smem + (2 + (P ^ 1)) * TILE_BYTES;
+    held(aa);
+    held(ab);
+    static_assert(NI - H == 2, "a slot of the tail is a k part of a row of tiles");
+    static_for<0, TS>([&](auto I) {
+      constexpr int i = decltype(I)::value;
+      constexpr int ks = i % 4 / 2, mi = 2 * (i / 4) + i % 2;
+      AccTile<mi * NI + H>::mfma_f16(bf[H][ks], af[P][mi][ks]);
+      AccTile<mi * NI + H + 1>::mfma_f16(bf[H + 1][ks], af[P][mi][ks]);
+      static_for<i * BPW / TS, (i + 1) * BPW / TS>([&](auto J) { issue_one(BPW + decltype(J)::value, P); });
+      static_for<i * BP / TS, (i + 1) * BP / TS>([&](auto Q) {
+        constexpr int q = decltype(Q)::value;
+        read_part<B_MC, q / DSB, q % DSB>(bf[q / DSB], nB, ab);
+      });
+      static_for<i * (MI * DSA) / TS, (i + 1) * (MI * DSA) / TS>([&](auto Q) {
+        constexpr int q = decltype(Q)::value;
+        read_part<A_MC, q / DSA, q % DSA>(af[P ^ 1][q / DSA], nA, aa);
+      });
+    });
+    advance();
+  };
+
+  // ---- epilogues: a lane holds C[m][n .. n + 3] of tile (mi, ni) at m = m0 + wm +
+  // 16 mi + (lane & 15), n = n0 + wn + 16 ni + 4 (lane >> 4)
+  uint8_t* const st = smem + 4 * TILE_BYTES + wave * STAGE;
+  const int lr = lane & 15, lq = lane >> 4;
+  float lmax = 0.f;
+  int d_shift = 0, e_out = 0;
+  bool d_fast = false;
+  float d_scale = 1.0f, d_inv = 1.0f;
+  if constexpr (EPI == LOSS_DW) {
+    if (p.mode != 1) {  // the scale is known: codes at once
+      const int unit = loss_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2 + (p.rowscaled ? loss_exponent(p.hdr, LOSS_RMAX) : 0);
+      const int base = pow2_exponent(p.s0) + pow2_exponent(p.s1);
+      e_out = clamp_e8m0(base);
+      d_shift = e_out - base - unit;
+      d_fast = d_shift >= kFastShiftMinSub && d_shift <= kFastShiftMax;
+      if (d_fast) d_scale = pow2_float(d_shift), d_inv = pow2_float(-d_shift);
+    }
+  }
+  // The 32 values of a lane's row (mi) of the wave's tile, and the accumulators back to 0.
+  auto take = [&](auto mi_tag, float (&x)[4 * NI]) {
+    constexpr int mi = decltype(mi_tag)::value;
+    static_for<0, NI>([&](auto J) {
+      constexpr int ni = decltype(J)::value;
+      const v4f v = AccTile<mi * NI + ni>::read();
+      AccTile<mi * NI + ni>::zero();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * ni + i] = v[i];
+    });
+  };
+  auto store_tile = [&](int m0, int n0, int split) {
+    // (the call's other operands are read here, by the scalar unit, not held over the loop)
+    typedef const __attribute__((address_space(4))) LossGemm* Args;
+    Args args = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(args));
+    const auto& p = *args;
+    uint32_t first_n = (uint32_t)(n0 + wn + 4 * lq);
+    const bool all_n = n0 + wn + WTN <= N;
+    static_for<0, MI>([&](auto J) {
+      constexpr int mi = decltype(J)::value;
+      const int m = m0 + wm + 16 * mi + lr;
+      const bool in = m < M;
+      float x[4 * NI];
+      take(J, x);
+      held(first_n);  // (the masks of its columns would else be kept from row to row)
+      const int nb = (int)first_n;
+      if constexpr (EPI == LOSS_STATS || EPI == LOSS_PICK) {
+        const float f = in ? p.factor[m] : 0.f;
+        if (!all_n) {
+#pragma unroll
+          for (int i = 0; i < 4 * NI; ++i)
+            if (nb + 16 * (i >> 2) + (i & 3) >= N) x[i] = -__builtin_inff();
+        }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < 4 * NI; ++i) top = fmaxf(top, x[i]);
+        // (a factor is positive; a row of -Inf alone has the sum 0, one of NaN alone NaN)
+        top = row4_max(top);
+        const float m2 = top == -__builtin_inff() || top != top ? 0.f : top * f;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * NI; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -m2));
+        sum = row4_sum(sum);
+        if (lq == 0 && in) p.stats[(int64_t)((p.v0 + n0 + wn) / WTN) * p.R + m] = float2{top == -__builtin_inff() ? top : m2, sum};
+        if constexpr (EPI == LOSS_STATS) {
+          const int d = in ? p.label[m] - (p.v0 + nb) : -1;
+          // (the lane that has the label's column: d = 16 ni + i)
+          const bool mine = d >= 0 && d < WTN && (d & 15) < 4;
+          if (__ballot(mine)) {
+            float z = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4 * NI; ++i)
+              if (d == 16 * (i >> 2) + (i & 3)) z = x[i];
+            if (mine) p.picked2[m] = z * f;
+          }
+        } else {
+          // the row's logits through LDS: the lanes of a row go through its tokens
+          static_for<0, NI>([&](auto Q) {
+            constexpr int ni = decltype(Q)::value;
+            *(v4f*)(st + lr * 512 + (((4 * ni + lq) ^ lr) * 16)) = v4f{x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
+          });
+          wait_lgkmcnt<0>();
+          if (in) {
+            const int64_t to = (int64_t)p.rows[m] * p.top;
+            const float fn = f * 0.69314718055994530942f;
+            for (int j = 4 * lq; j < p.topp; j += 16) {
+              const v4i t = *(const v4i*)(p.top32 + (int64_t)m * p.topp + j);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int d = t[i] - (p.v0 + n0 + wn);
+                if (t[i] >= 0 && d >= 0 && d < WTN)
+                  p.picked[to + j + i] = fn * *(const float*)(st + lr * 512 + (((d >> 2) ^ lr) * 16) + 4 * (d & 3));
+              }
+            }
+          }
+          wait_lgkmcnt<0>();
+        }
+      } else if constexpr (EPI == LOSS_DZ) {
+        const float f = in ? p.factor[m] : 0.f, l = in ? p.lse2[m] : 0.f, c = in ? p.coef[m] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * NI; ++i) x[i] = c * __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -l));
+        if (p.label) {
+          const int d = in ? p.label[m] - (p.v0 + nb) : -1;
+          const bool mine = d >= 0 && d < WTN && (d & 15) < 4;
+          if (__ballot(mine)) {
+#pragma unroll
+            for (int i = 0; i < 4 * NI; ++i)
+              if (d == 16 * (i >> 2) + (i & 3)) x[i] -= c;
+          }
+        }
+        if (!all_n) {
+#pragma unroll
+          for (int i = 0; i < 4 * NI; ++i)
+            if (nb + 16 * (i >> 2) + (i & 3) >= N) x[i] = 0.f;
+        }
+        // whole rows through LDS (the chunks of a row permuted by the row)
+        static_for<0, NI>([&](auto Q) {
+          constexpr int ni = decltype(Q)::value;
+          const lh2 a = {(_Float16)x[4 * ni], (_Float16)x[4 * ni + 1]}, b = {(_Float16)x[4 * ni + 2], (_Float16)x[4 * ni + 3]};
+          *(v2i*)(st + lr * 256 + (((2 * ni + (lq >> 1)) ^ lr) * 16) + 8 * (lq & 1)) =
+              v2i{__builtin_bit_cast(int, a), __builtin_bit_cast(int, b)};
+        });
+        wait_lgkmcnt<0>();
+        u4 d[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = 4 * j + (lane >> 4);
+          d[j] = *(const u4*)(st + r * 256 + (((lane & 15) ^ r) * 16));
+        }
+        wait_lgkmcnt<0>();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int row = m0 + wm + 16 * mi + 4 * j + (lane >> 4), col = n0 + wn + 8 * (lane & 15);
+          // (ldz is a multiple of 64: a row holds every column of the tiles it reaches)
+          if (row < M && col < p.ldz) *(u4*)((uint16_t*)p.dz + (int64_t)row * p.ldz + col) = d[j];
+        }
+      } else if constexpr (EPI == LOSS_DX) {
+        if (in) {
+          float* o = p.part + ((int64_t)split * p.R + m) * p.ldp + nb;
+          static_for<0, NI>([&](auto Q) {
+            constexpr int ni = decltype(Q)::value;
+            if (nb + 16 * ni < p.ldp) {
+              v4f v = {x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
+              if (p.accumulate) v += *(const v4f*)(o + 16 * ni);
+              *(v4f*)(o + 16 * ni) = v;
+            }
+          });
+        }
+      } else {
+        if (!all_n) {
+#pragma unroll
+          for (int i = 0; i < 4 * NI; ++i)
+            if (nb + 16 * (i >> 2) + (i & 3) >= N) x[i] = 0.f;
+        }
+        if (in) {
+          if (p.mode == 1) {
+            float* o = p.part + (int64_t)(p.v0 + m) * p.ldp + nb;
+            static_for<0, NI>([&](auto Q) {
+              constexpr int ni = decltype(Q)::value;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) lmax = fmaxf(lmax, fabsf(x[4 * ni + i]));
+              if (nb + 16 * ni < p.ldp) *(v4f*)(o + 16 * ni) = v4f{x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
+            });
+          } else {
+            static_for<0, NI>([&](auto Q) {
+              constexpr int ni = decltype(Q)::value;
+              const v4f v = {x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) lmax = fmaxf(lmax, fabsf(v[i]));
+              const int cols = N - (nb + 16 * ni);
+              const int64_t e = (int64_t)(p.v0 + m) * p.ldo + nb + 16 * ni;
+              uint32_t code[4];
+              if (p.out_fmt == kF16) {
+                const v2i w = cast4_f16_any(v, d_fast, d_inv, d_shift, p.sat);
+                code[0] = (uint32_t)w.x & 0xFFFFu, code[1] = (uint32_t)w.x >> 16;
+                code[2] = (uint32_t)w.y & 0xFFFFu, code[3] = (uint32_t)w.y >> 16;
+                if (cols >= 4) *(v2i*)((uint16_t*)p.out + e) = w;
+              } else {
+                const uint32_t w = p.out_fmt == kE4M3 ? cast4_fp8_any<kE4M3>(v, d_fast, d_scale, d_shift, p.sat)
+                                                      : cast4_fp8_any<kE5M2>(v, d_fast, d_scale, d_shift, p.sat);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) code[i] = (w >> (8 * i)) & 0xFFu;
+                if (cols >= 4) *(uint32_t*)((uint8_t*)p.out + e) = w;
+              }
+              if (cols < 4) {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                  if (i < cols) {
+                    if (p.out_fmt == kF16)
+                      ((uint16_t*)p.out)[e + i] = (uint16_t)code[i];
+                    else
+                      ((uint8_t*)p.out)[e + i] = (uint8_t)code[i];
+                  }
+              }
+            });
+          }
+        }
+      }
+    });
+  };
+
+  // ---- the first two steps of the first tile
+#pragma unroll
+  for (int j = 0; j < 2 * BPW; ++j) issue_one(j, 0);
+  advance();
+#pragma unroll
+  for (int j = 0; j < 2 * BPW; ++j) issue_one(j, 1);
+  advance();
+  static_for<0, MI * NI>([&](auto I) { AccTile<decltype(I)::value>::zero(); });
+  wait_vmcnt<2 * BPW>();
+  __syncthreads();
+  static_for<0, MI * DSA>([&](auto Q) {
+    constexpr int q = decltype(Q)::value;
+    read_part<A_MC, q / DSA, q % DSA>(af[0][q / DSA], smem, aa);
+  });
+  static_for<0, BP>([&](auto Q) {
+    constexpr int q = decltype(Q)::value;
+    read_part<B_MC, q / DSB, q % DSB>(bf[q / DSB], smem + 2 * TILE_BYTES, ab);
+  });
+  mfma_drain();
+
+  using P0 = std::integral_constant<int, 0>;
+  using P1 = std::integral_constant<int, 1>;
+  int c_r = 0, c_m0, c_n0, c_split;
+  origin(0, c_m0, c_n0, c_split);
+  head(P0{});
+  for (int kt = 0;;) {
+    tail(P0{});
+    head(P1{});
+    tail(P1{});
+    kt += 2;
+    if (kt == KTe) {
+      kt = 0;
+      mfma_drain();
+      store_tile(c_m0, c_n0, c_split);
+      if (++c_r == ntiles) break;
+      origin(c_r, c_m0, c_n0, c_split);
+      mfma_drain();  // the zeroing writes before the next products read them
+    }
+    head(P0{});
+  }
+  wait_vmcnt<0>();  // the out-of-range loads past the last tile
+  if constexpr (EPI == LOSS_DW) {
+    for (int off = 32; off > 0; off >>= 1) lmax = fmaxf(lmax, __shfl_xor(lmax, off, 64));
+    if (lane == 0 && lmax > 0.f) atomicMax(p.amax, __float_as_uint(lmax));
+  }
+}
+
+}  // namespace scalify

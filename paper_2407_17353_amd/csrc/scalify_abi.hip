@@ -16,6 +16,7 @@
 #include "gemm_choice.h"
 #include "kernels.h"
 #include "layernorm.h"
+#include "loss.h"
 #include "mid_gemm.h"
 #include "rmsnorm.h"
 #include "wave_gemm.h"
@@ -235,6 +236,13 @@ size_t rmsnorm_bwd_ws(int64_t R, int64_t D) {
   return kHeaderBytes + (size_t)rmsnorm_ws_floats(R, D) * sizeof(float);
 }
 
+// Sizes that the losses take: places and tiles are counted in 32 bits.
+bool loss_sizes_ok(int64_t R, int64_t V, int64_t D) {
+  return R >= 0 && R <= kMaxDim && V >= 1 && V <= kMaxDim && D >= 1 && D <= ((int64_t)1 << 20) &&
+         ((R + 255) / 256) * ((V + 255) / 256) <= kMaxDim && ((R + 255) / 256) * ((D + 255) / 256) <= ((int64_t)1 << 24) &&
+         ((V + 255) / 256) * ((D + 255) / 256) <= kMaxDim;
+}
+
 // Two outputs of one call (different formats allowed) must not overlap at all.
 bool rows_overlap(const scalify_scaled_array* a, const scalify_scaled_array* b, int64_t R, int64_t D) {
   if (R == 0 || D == 0) return false;
@@ -332,6 +340,109 @@ bool tokens_overlap(const scalify_scaled_array* a, const scalify_scaled_array* b
   if (ap != bp) return true;
   const uint64_t d = b0 >= a0 ? (b0 - a0) % ap : (ap - (a0 - b0) % ap) % ap;  // b's first column after a's
   return !(d >= aw && d + bw <= ap);
+}
+
+// ---- losses
+
+// x [R][D], w [V][D] and the optional row scales of x; the numbers of either loss.
+scalify_status check_loss(const scalify_scaled_array* x, const scalify_scaled_array* w, const float* row_scale) {
+  if (!is_out(x->dtype) || !is_out(w->dtype)) return SCALIFY_ERR_DTYPE;
+  const int64_t R = x->rows, V = w->rows, D = x->cols;
+  if (!loss_sizes_ok(R, V, D)) return SCALIFY_ERR_SHAPE;
+  scalify_status st;
+  if ((st = check_tokens(x, R, D)) != SCALIFY_OK) return st;
+  if ((st = check_tokens(w, V, D)) != SCALIFY_OK) return st;
+  if (w->ld * elem_bytes(w->dtype) >= ((int64_t)1 << 23)) return SCALIFY_ERR_SHAPE;  // (256 rows below 2^31 bytes)
+  if ((uintptr_t)row_scale & 3u) return SCALIFY_ERR_ALIGN;
+  return SCALIFY_OK;
+}
+
+// The teacher's logits and tokens of a distillation.
+scalify_status check_teacher(const scalify_scaled_array* t, const int64_t* index, int64_t R, float temperature) {
+  if (!is_any(t->dtype)) return SCALIFY_ERR_DTYPE;
+  if (t->cols < 1 || t->cols > kLossMaxTop) return SCALIFY_ERR_SHAPE;
+  const scalify_status st = check_tokens(t, R, t->cols);
+  if (st != SCALIFY_OK) return st;
+  if (!index && R > 0) return SCALIFY_ERR_NULL;
+  if ((uintptr_t)index & 7u) return SCALIFY_ERR_ALIGN;
+  if (!(temperature >= 0x1p-20f) || !(temperature <= 0x1p20f)) return SCALIFY_ERR_VALUE;
+  return SCALIFY_OK;
+}
+
+void loss_operands(LossParams* p, const scalify_scaled_array* x, const scalify_scaled_array* w, const float* row_scale) {
+  p->x = x->data;
+  p->ldx = x->ld;
+  p->x_fmt = x->dtype;
+  p->s_x = x->scale;
+  p->w = w->data;
+  p->ldw = w->ld;
+  p->w_fmt = w->dtype;
+  p->s_w = w->scale;
+  p->row_scale = row_scale;
+  p->R = (int)x->rows;
+  p->V = (int)w->rows;
+  p->D = (int)x->cols;
+  p->temp = 1.0f;
+}
+
+void loss_teacher(LossParams* p, const scalify_scaled_array* t, const int64_t* index, float temperature) {
+  p->teacher = t->data;
+  p->ldt = t->ld;
+  p->t_fmt = t->dtype;
+  p->s_t = t->scale;
+  p->top = (int)t->cols;
+  p->index = index;
+  p->temp = temperature;
+}
+
+scalify_status loss_forward(LossParams* p, void* workspace, size_t workspace_bytes, void* stream) {
+  if (p->R == 0) return SCALIFY_OK;
+  const size_t need = loss_plan(p->R, p->V, p->D, p->w_fmt, p->top, false, false, nullptr, nullptr).bytes;
+  if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)) return SCALIFY_ERR_WORKSPACE;
+  loss_plan(p->R, p->V, p->D, p->w_fmt, p->top, false, false, p, workspace);
+  return launch_loss_fwd(*p, (hipStream_t)stream) == hipSuccess ? SCALIFY_OK : SCALIFY_ERR_HIP;
+}
+
+// The backward's outputs, and the rest of its call.
+scalify_status loss_backward(LossParams* p, const scalify_scaled_array* x, const scalify_scaled_array* w,
+                             scalify_scaled_array* dx, scalify_scaled_array* dw, int32_t rescale, int32_t target_log2,
+                             int32_t saturate, float* amax_out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dx && !dw) return SCALIFY_ERR_NULL;
+  if ((dx && !dx->scale) || (dw && !dw->scale)) return SCALIFY_ERR_NULL;
+  if ((dx && !is_out(dx->dtype)) || (dw && !is_out(dw->dtype))) return SCALIFY_ERR_DTYPE;
+  if (rescale != SCALIFY_RESCALE_NONE && rescale != SCALIFY_RESCALE_AMAX) return SCALIFY_ERR_VALUE;
+  if (target_log2 < -1000 || target_log2 > 1000) return SCALIFY_ERR_VALUE;
+  scalify_status st;
+  if (dx && (st = check_tokens(dx, p->R, p->D)) != SCALIFY_OK) return st;
+  if (dw && (st = check_tokens(dw, p->V, p->D)) != SCALIFY_OK) return st;
+  if (((uintptr_t)p->dloss | (uintptr_t)p->lse | (uintptr_t)p->picked | (uintptr_t)amax_out) & 3u) return SCALIFY_ERR_ALIGN;
+  for (scalify_scaled_array* y : {dx, dw}) {
+    if (!y) continue;
+    if (tokens_overlap(y, x) || tokens_overlap(y, w)) return SCALIFY_ERR_LAYOUT;
+    if (y->scale == x->scale || y->scale == w->scale || y->scale == p->s_dloss) return SCALIFY_ERR_LAYOUT;
+  }
+  if (dx && dw && (tokens_overlap(dx, dw) || dx->scale == dw->scale)) return SCALIFY_ERR_LAYOUT;
+  const bool amax = rescale == SCALIFY_RESCALE_AMAX;
+  const size_t need = loss_plan(p->R, p->V, p->D, p->w_fmt, p->top, true, amax, nullptr, nullptr).bytes;
+  if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)) return SCALIFY_ERR_WORKSPACE;
+  if (dx) {
+    p->dx = dx->data;
+    p->lddx = dx->ld;
+    p->dx_fmt = dx->dtype;
+    p->dx_scale = dx->scale;
+  }
+  if (dw) {
+    p->dw = dw->data;
+    p->lddw = dw->ld;
+    p->dw_fmt = dw->dtype;
+    p->dw_scale = dw->scale;
+  }
+  p->amax_out = amax_out;
+  p->mode = amax ? 1 : 0;
+  p->target = target_log2;
+  p->sat = saturate != 0;
+  loss_plan(p->R, p->V, p->D, p->w_fmt, p->top, true, amax, p, workspace);
+  return launch_loss_bwd(*p, (hipStream_t)stream) == hipSuccess ? SCALIFY_OK : SCALIFY_ERR_HIP;
 }
 
 void attention_params(AttnParams* p, const scalify_scaled_array* q, const scalify_scaled_array* k,
@@ -1056,6 +1167,106 @@ scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
   p.mode = rescale == SCALIFY_RESCALE_AMAX ? 1 : 0;
   p.target = target_log2;
   return launch_attention_bwd(p, (hipStream_t)stream) == hipSuccess ? SCALIFY_OK : SCALIFY_ERR_HIP;
+}
+
+size_t scalify_cross_entropy_fwd_workspace_size(int64_t R, int64_t V, int64_t D, int32_t w_dtype) {
+  if (!loss_sizes_ok(R, V, D) || !is_out(w_dtype)) return 0;
+  return loss_plan(R, V, D, w_dtype, 0, false, false, nullptr, nullptr).bytes;
+}
+
+scalify_status scalify_cross_entropy_fwd(const scalify_scaled_array* x, const scalify_scaled_array* w,
+                                         const int64_t* labels, const float* row_scale, float* loss,
+                                         float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !w) return SCALIFY_ERR_NULL;
+  const scalify_status st = check_loss(x, w, row_scale);
+  if (st != SCALIFY_OK) return st;
+  if (x->rows > 0 && (!labels || !loss)) return SCALIFY_ERR_NULL;
+  if (((uintptr_t)labels & 7u) || (((uintptr_t)loss | (uintptr_t)lse) & 3u)) return SCALIFY_ERR_ALIGN;
+  LossParams p = {};
+  loss_operands(&p, x, w, row_scale);
+  p.labels = labels;
+  p.loss = loss;
+  p.lse = lse;
+  return loss_forward(&p, workspace, workspace_bytes, stream);
+}
+
+size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D, int32_t w_dtype, int32_t rescale) {
+  if (!loss_sizes_ok(R, V, D) || !is_out(w_dtype)) return 0;
+  if (rescale != SCALIFY_RESCALE_NONE && rescale != SCALIFY_RESCALE_AMAX) return 0;
+  return loss_plan(R, V, D, w_dtype, 0, true, rescale == SCALIFY_RESCALE_AMAX, nullptr, nullptr).bytes;
+}
+
+scalify_status scalify_cross_entropy_bwd(const float* dloss, const float* dloss_scale,
+                                         const scalify_scaled_array* x, const scalify_scaled_array* w,
+                                         const int64_t* labels, const float* row_scale, const float* lse,
+                                         scalify_scaled_array* dx, scalify_scaled_array* dw, int32_t rescale,
+                                         int32_t target_log2, int32_t saturate, float* amax_out,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !w) return SCALIFY_ERR_NULL;
+  const scalify_status st = check_loss(x, w, row_scale);
+  if (st != SCALIFY_OK) return st;
+  if (x->rows > 0 && (!labels || !lse)) return SCALIFY_ERR_NULL;
+  if ((uintptr_t)labels & 7u) return SCALIFY_ERR_ALIGN;
+  LossParams p = {};
+  loss_operands(&p, x, w, row_scale);
+  p.dloss = dloss;
+  p.s_dloss = dloss_scale;
+  p.labels = labels;
+  p.lse = (float*)lse;
+  return loss_backward(&p, x, w, dx, dw, rescale, target_log2, saturate, amax_out, workspace, workspace_bytes, stream);
+}
+
+size_t scalify_distillation_fwd_workspace_size(int64_t R, int64_t V, int64_t D, int64_t top, int32_t w_dtype) {
+  if (!loss_sizes_ok(R, V, D) || !is_out(w_dtype) || top < 1 || top > kLossMaxTop) return 0;
+  return loss_plan(R, V, D, w_dtype, (int)top, false, false, nullptr, nullptr).bytes;
+}
+
+scalify_status scalify_distillation_fwd(const scalify_scaled_array* x, const scalify_scaled_array* w,
+                                        const scalify_scaled_array* teacher, const int64_t* index,
+                                        float temperature, const float* row_scale, float* loss, float* lse,
+                                        float* picked, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !w || !teacher) return SCALIFY_ERR_NULL;
+  scalify_status st = check_loss(x, w, row_scale);
+  if (st != SCALIFY_OK) return st;
+  if ((st = check_teacher(teacher, index, x->rows, temperature)) != SCALIFY_OK) return st;
+  if (x->rows > 0 && !loss) return SCALIFY_ERR_NULL;
+  if (((uintptr_t)loss | (uintptr_t)lse | (uintptr_t)picked) & 3u) return SCALIFY_ERR_ALIGN;
+  LossParams p = {};
+  loss_operands(&p, x, w, row_scale);
+  loss_teacher(&p, teacher, index, temperature);
+  p.loss = loss;
+  p.lse = lse;
+  p.picked = picked;
+  return loss_forward(&p, workspace, workspace_bytes, stream);
+}
+
+size_t scalify_distillation_bwd_workspace_size(int64_t R, int64_t V, int64_t D, int64_t top, int32_t w_dtype,
+                                               int32_t rescale) {
+  if (!loss_sizes_ok(R, V, D) || !is_out(w_dtype) || top < 1 || top > kLossMaxTop) return 0;
+  if (rescale != SCALIFY_RESCALE_NONE && rescale != SCALIFY_RESCALE_AMAX) return 0;
+  return loss_plan(R, V, D, w_dtype, (int)top, true, rescale == SCALIFY_RESCALE_AMAX, nullptr, nullptr).bytes;
+}
+
+scalify_status scalify_distillation_bwd(const float* dloss, const float* dloss_scale,
+                                        const scalify_scaled_array* x, const scalify_scaled_array* w,
+                                        const scalify_scaled_array* teacher, const int64_t* index,
+                                        float temperature, const float* row_scale, const float* lse,
+                                        const float* picked, scalify_scaled_array* dx, scalify_scaled_array* dw,
+                                        int32_t rescale, int32_t target_log2, int32_t saturate, float* amax_out,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !w || !teacher) return SCALIFY_ERR_NULL;
+  scalify_status st = check_loss(x, w, row_scale);
+  if (st != SCALIFY_OK) return st;
+  if ((st = check_teacher(teacher, index, x->rows, temperature)) != SCALIFY_OK) return st;
+  if (x->rows > 0 && (!lse || !picked)) return SCALIFY_ERR_NULL;
+  LossParams p = {};
+  loss_operands(&p, x, w, row_scale);
+  loss_teacher(&p, teacher, index, temperature);
+  p.dloss = dloss;
+  p.s_dloss = dloss_scale;
+  p.lse = (float*)lse;
+  p.picked = (float*)picked;
+  return loss_backward(&p, x, w, dx, dw, rescale, target_log2, saturate, amax_out, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,448 @@
+"""GPU parity of the losses from hidden states and the output matrix: softmax cross
+entropy and distillation, forward and backward, against their plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+from paper_2407_17353_amd import binding as sc
+from tests import layer_refs as lr
+from tests import loss_refs as ref
+from tests.helpers import say
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F16, E4M3, E5M2 = sc.F16, sc.E4M3, sc.E5M2
+NAMES = {F16: "f16", E4M3: "e4m3", E5M2: "e5m2"}
+
+
+class Case:
+    """Inputs of a call: rows whose logits spread, some of which do not count."""
+
+    def __init__(self, R, V, D, fx=F16, fw=F16, rows=False, top=0, T=1.0, seed=1, skip=3, ldx=None, ldw=None):
+        g = torch.Generator().manual_seed(seed)
+        self.R, self.V, self.D, self.top, self.T = R, V, D, top, T
+        e = -max(0, round(math.log2(D) / 2) - 1)
+        self.ew, self.ex = e, -1
+        self.w = lr.scaled(lr.values(V, D, fw, seed + 10), fw, e, ld=ldw)
+        self.x = lr.scaled(lr.values(R, D, fx, seed + 20), fx, self.ex, ld=ldx)
+        self.row = torch.exp2(torch.randint(-2, 2, (R,), generator=g).float()).to(DEV) if rows else None
+        labels = torch.randint(0, V, (R,), generator=g)
+        if R > 1 and skip:
+            labels[1::skip] = torch.tensor([-100, V, -1, 1 << 40])[torch.arange(len(labels[1::skip])) % 4]
+        self.labels = self.teacher = self.index = None
+        if top:
+            index = torch.randint(0, V, (R, top), generator=g)          # (tokens may come twice)
+            index[:, top // 2::3] = torch.where(torch.rand((R, len(range(top // 2, top, 3))), generator=g) < 0.3,
+                                                torch.tensor(-1), index[:, top // 2::3])
+            index[labels < 0] = -1
+            index[labels >= V] = V + 5
+            t = lr.values(R, top, F16, seed + 30, 2.0)
+            if R > 4:
+                t[4] = -math.inf                                        # a row of a teacher that says nothing
+            if top > 2:
+                t[::2, 2] = -math.inf
+            self.teacher, self.index = lr.scaled(t, F16, 1), index.to(DEV)
+        else:
+            self.labels = labels.to(DEV)
+        self.loss, self.lse = (torch.full((R,), 7.0, device=DEV) for _ in range(2))
+        self.picked = torch.full((R, top), 7.0, device=DEV) if top else None
+        self.g = (torch.randn(R, generator=g) * torch.exp2(-6 * torch.rand(R, generator=g))).to(DEV)
+        self.g[2::5] = 0.0
+
+    def reference(self):
+        return ref.Loss(self.x, self.w, self.row, self.labels, self.teacher, self.index, self.T)
+
+    def forward(self, **kw):
+        if self.top:
+            sc.scalify_distillation_fwd(self.x, self.w, self.teacher, self.index, self.loss, temperature=self.T, lse=self.lse,
+                                        picked=self.picked, row_scale=self.row, **kw)
+        else:
+            sc.scalify_cross_entropy_fwd(self.x, self.w, self.labels, self.loss, lse=self.lse, row_scale=self.row, **kw)
+
+    def backward(self, dx, dw, eg=-3, g=True, **kw):
+        kw = dict(dx=dx, dw=dw, dloss=self.g if g else None, dloss_scale=sc.scale_tensor(eg, DEV), row_scale=self.row, **kw)
+        if self.top:
+            sc.scalify_distillation_bwd(self.x, self.w, self.teacher, self.index, self.lse, self.picked, temperature=self.T, **kw)
+        else:
+            sc.scalify_cross_entropy_bwd(self.x, self.w, self.labels, self.lse, **kw)
+
+    def check(self, fg=F16, mode=sc.RESCALE_NONE, target=0, g=True, eg=-3):
+        self.forward()
+        torch.cuda.synchronize()
+        r = self.reference()
+        r.check_forward(self.loss, self.lse, self.picked)
+        dx, dw = lr.empty(self.R, self.D, fg), lr.empty(self.V, self.D, fg)
+        amax = torch.full((2,), -1.0, device=DEV)
+        self.backward(dx, dw, rescale=mode, target_log2=target, amax_out=amax, g=g, eg=eg)
+        torch.cuda.synchronize()
+        up = (self.g if g else torch.ones_like(self.g)).double() * 2.0 ** eg
+        want = r.gradients(up, self.lse)
+        ref.check_gradient(dx, want[0], want[2], eg + self.ew, mode, target, amax[0])
+        ref.check_gradient(dw, want[1], want[3], eg + self.ex, mode, target, amax[1])
+        for a in (dx, dw):  # what lies behind the columns is left as it was
+            st = a.data
+            full = torch.as_strided(st, (st.shape[0], st.stride(0)), (st.stride(0), 1))[:, st.shape[1]:]
+            assert (full.contiguous().view(torch.uint8) == 0x5A).all()
+        return dx, dw
+
+
+SIZES = [(1, 1, 1), (1, 2, 8), (3, 130, 7), (2, 1000, 64), (17, 255, 65), (64, 256, 128), (65, 257, 100), (255, 513, 72),
+         (256, 384, 192), (257, 129, 1000), (600, 2000, 40), (40, 5003, 321)]
+
+
+@pytest.mark.parametrize("R,V,D", SIZES)
+@pytest.mark.parametrize("fx,fw,rows", [(F16, F16, False), (E4M3, E4M3, True), (F16, E5M2, False), (E5M2, F16, True)])
+def test_cross_entropy(R, V, D, fx, fw, rows):
+    say(f"cross entropy {R} {V} {D} {NAMES[fx]} {NAMES[fw]} {rows}")
+    Case(R, V, D, fx, fw, rows).check()
+
+
+@pytest.mark.parametrize("R,V,D,top,T", [(1, 1, 1, 1, 1.0), (1, 3, 8, 2, 4.0), (5, 130, 7, 16, 1.0), (17, 255, 65, 3, 2.0), (65, 257, 100, 64, 1.5),
+                                         (257, 1000, 72, 20, 1.0), (300, 384, 64, 256, 3.0), (40, 5003, 321, 129, 0.5)])
+@pytest.mark.parametrize("fx,fw,rows", [(F16, F16, False), (E4M3, E4M3, True), (E5M2, E4M3, False)])
+def test_distillation(R, V, D, top, T, fx, fw, rows):
+    say(f"distillation {R} {V} {D} {top} {T} {NAMES[fx]} {NAMES[fw]} {rows}")
+    Case(R, V, D, fx, fw, rows, top, T).check()
+
+
+@pytest.mark.parametrize("top", [0, 9])
+@pytest.mark.parametrize("fg,mode,target", [(F16, 1, 0), (E5M2, 1, 14), (E4M3, 1, 7), (E5M2, 0, 0), (E4M3, 0, 0)])
+@pytest.mark.parametrize("R,V,D", [(70, 600, 130), (300, 257, 33), (7, 300, 512)])
+def test_gradient_formats(R, V, D, fg, mode, target, top):
+    say(f"loss gradients {R} {V} {D} {NAMES[fg]} {mode} {target} {top}")
+    Case(R, V, D, E4M3, F16, True, top).check(fg, mode, target, eg=2)
+
+
+@pytest.mark.parametrize("top", [0, 5])
+def test_no_upstream_gradient_is_one(top):
+    Case(50, 300, 64, top=top).check(g=False, eg=0)
+
+
+@pytest.mark.parametrize("top", [0, 6])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_rows_that_do_not_count_hold_anything(top, bad):
+    """Not-a-numbers and infinities in rows without a label (a teacher), or with an
+    upstream gradient of 0, reach nothing: not dw either."""
+    say(f"loss rows {top} {bad}")
+    c = Case(90, 400, 72, top=top)
+    c.forward()
+    dx, dw = lr.empty(90, 72, F16), lr.empty(400, 72, F16)
+    c.backward(dx, dw)
+    on = c.reference().on
+    off = torch.nonzero(~on | (c.g == 0))[:, 0]
+    kept, lse0, loss0 = c.x.data.clone(), c.lse.clone(), c.loss.clone()
+    c.x.data.view(torch.float16)[off] = bad
+    if top:
+        c.teacher.data.view(torch.float16)[~on] = -math.inf
+    dx2, dw2 = lr.empty(90, 72, F16), lr.empty(400, 72, F16)
+    c.backward(dx2, dw2)
+    torch.cuda.synchronize()
+    assert torch.equal(dw.data, dw2.data) and torch.equal(dx.data, dx2.data)
+    assert (dx2.data[off] == 0).all()
+    c.x.data.copy_(kept)
+    c.x.data.view(torch.float16)[~on] = bad
+    c.forward()
+    torch.cuda.synchronize()
+    assert torch.equal(c.lse, lse0) and torch.equal(c.loss, loss0)
+
+
+@pytest.mark.parametrize("top", [0, 4])
+def test_counted_nan(top):
+    """A NaN in a row that counts makes that row's results NaN, and no other's."""
+    c = Case(40, 300, 64, top=top, skip=0)
+    c.forward()
+    loss = c.loss.clone()
+    i = 8
+    c.x.data.view(torch.float16)[i, 5] = float("nan")
+    c.forward()
+    torch.cuda.synchronize()
+    others = torch.arange(40, device=DEV) != i
+    assert torch.isnan(c.loss[i]) and torch.isnan(c.lse[i]) and torch.equal(c.loss[others], loss[others])
+
+
+@pytest.mark.parametrize("top", [0, 3])
+def test_no_row_counts(top):
+    """Gradients of nothing are 0 on the propagated scales."""
+    c = Case(33, 200, 40, top=top)
+    (c.index if top else c.labels).fill_(-1)
+    dx, dw = c.check(mode=sc.RESCALE_AMAX)
+    assert (dx.data == 0).all() and (dw.data == 0).all()
+
+
+def test_no_rows():
+    c = Case(1, 50, 24)
+    x = sc.ScaledArray(c.x.data[:0], F16, c.x.scale)
+    e = torch.empty(0, device=DEV)
+    lab = torch.empty(0, dtype=torch.int64, device=DEV)
+    sc.scalify_cross_entropy_fwd(x, c.w, lab, e)
+    dw = lr.empty(50, 24, F16)
+    sc.scalify_cross_entropy_bwd(x, c.w, lab, e, dw=dw)
+    torch.cuda.synchronize()
+    assert (dw.data == 0).all() and lr.log2_of(dw) == c.ex
+
+
+@pytest.mark.parametrize("top", [0, 7])
+def test_either_gradient_alone(top):
+    c = Case(130, 500, 96, E4M3, E4M3, True, top)
+    dx, dw = c.check(mode=sc.RESCALE_AMAX)
+    a, b = lr.empty(130, 96, F16), lr.empty(500, 96, F16)
+    c.backward(a, None)
+    c.backward(None, b)
+    torch.cuda.synchronize()
+    for x, y in ((a, dx), (b, dw)):
+        assert torch.equal(x.data, y.data) and torch.equal(x.scale, y.scale)
+
+
+def test_column_ranges():
+    """x, w and the gradients as columns of wider matrices (pitches of their own), w
+    read where it stands (F16, columns a multiple of 8)."""
+    say("loss columns")
+    c = Case(70, 300, 64, ldx=200, ldw=344)
+    c.check()
+    wide = torch.full((70, 160), 0x5A5A, dtype=torch.int16, device=DEV)
+    dx = sc.ScaledArray(wide[:, 32:96], F16, torch.ones(1, device=DEV))
+    ref_dx, dw = lr.empty(70, 64, F16), lr.empty(300, 64, F16)
+    c.backward(ref_dx, dw)
+    c.backward(dx, None)
+    torch.cuda.synchronize()
+    assert torch.equal(dx.data, ref_dx.data)
+    assert (wide[:, :32] == 0x5A5A).all() and (wide[:, 96:] == 0x5A5A).all()
+
+
+@pytest.mark.parametrize("top", [0, 6])
+def test_pieces_of_the_vocabulary(top):
+    """More logits than one piece of their gradient holds: dx adds up over the pieces."""
+    say(f"loss pieces {top}")
+    Case(2100, 131101, 24, E4M3, E4M3, False, top, seed=3).check(mode=sc.RESCALE_AMAX)
+
+
+def test_pieces_of_the_output_matrix():
+    """An 8-bit output matrix larger than its decoded piece."""
+    say("loss pieces of w")
+    Case(5, 40001, 7200, F16, E4M3, seed=4).check()
+
+
+@pytest.mark.parametrize("top", [0, 30])
+def test_reruns_and_workspaces(top):
+    """Any content of the workspace, a workspace of the stated size and no byte more, and
+    reruns: the same bits."""
+    c = Case(300, 700, 200, E4M3, E5M2, True, top)
+    R, V, D = 300, 700, 200
+    sizes = (sc.scalify_distillation_fwd_workspace_size(R, V, D, top, E5M2), sc.scalify_distillation_bwd_workspace_size(R, V, D, top, E5M2)) \
+        if top else (sc.scalify_cross_entropy_fwd_workspace_size(R, V, D, E5M2), sc.scalify_cross_entropy_bwd_workspace_size(R, V, D, E5M2))
+    seen = []
+    for fill in (0x00, 0xFF, 0x7B):
+        guards = [torch.full((n + 4096,), fill, dtype=torch.uint8, device=DEV) for n in sizes]
+        c.forward(ws=guards[0][:sizes[0]])
+        dx, dw = lr.empty(R, D, E5M2), lr.empty(V, D, E5M2)
+        c.backward(dx, dw, ws=guards[1][:sizes[1]])
+        torch.cuda.synchronize()
+        for gd, n in zip(guards, sizes):
+            assert (gd[n:] == fill).all()
+        seen.append([t.clone() for t in (c.loss, c.lse, dx.data, dw.data, dx.scale, dw.scale)] + ([c.picked.clone()] if top else []))
+    for other in seen[1:]:
+        for a, b in zip(seen[0], other):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("top", [0, 12])
+def test_capture(top):
+    """Forward and backward captured, two graphs on one workspace, replayed with eager
+    calls between and other labels: equal to the eager results."""
+    say(f"loss capture {top}")
+    c = Case(200, 900, 136, E4M3, E4M3, True, top)
+    n = max(sc.scalify_distillation_bwd_workspace_size(200, 900, 136, max(top, 1), E4M3),
+            sc.scalify_distillation_fwd_workspace_size(200, 900, 136, max(top, 1), E4M3))
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    c.forward(ws=ws)
+    outs = [[lr.empty(200, 136, F16), lr.empty(900, 136, F16)] for _ in range(2)]
+    for o in outs:
+        c.backward(*o, ws=ws)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    for o, mode in zip(outs, (sc.RESCALE_AMAX, sc.RESCALE_NONE)):
+        g = torch.cuda.CUDAGraph()
+        scale = sc.scale_tensor(-3, DEV)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=s):
+            c.forward(ws=ws)
+            kw = dict(dx=o[0], dw=o[1], dloss=c.g, dloss_scale=scale, row_scale=c.row, rescale=mode, ws=ws)
+            if top:
+                sc.scalify_distillation_bwd(c.x, c.w, c.teacher, c.index, c.lse, c.picked, temperature=c.T, **kw)
+            else:
+                sc.scalify_cross_entropy_bwd(c.x, c.w, c.labels, c.lse, **kw)
+        graphs.append((g, scale))
+    what = c.index if top else c.labels
+    for k in range(3):
+        what.copy_(torch.roll(what, 1, 0))
+        eager = [[lr.empty(200, 136, F16), lr.empty(900, 136, F16)] for _ in range(2)]
+        c.forward()
+        want = [c.loss.clone(), c.lse.clone()]
+        for e, mode in zip(eager, (sc.RESCALE_AMAX, sc.RESCALE_NONE)):
+            c.backward(*e, rescale=mode)
+        torch.cuda.synchronize()
+        ws.fill_(0xFF)
+        c.loss.fill_(9.0)
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.loss, want[0]) and torch.equal(c.lse, want[1])
+        for o, e in zip(outs, eager):
+            for a, b in zip(o, e):
+                assert torch.equal(a.data, b.data) and torch.equal(a.scale, b.scale)
+
+
+def test_two_streams():
+    """Two calls at once, each on its own stream and workspace."""
+    a, b = Case(300, 2000, 256, seed=5), Case(500, 1500, 128, E4M3, E4M3, True, 10, 2.0, seed=6)
+    want = []
+    for c in (a, b):
+        c.forward()
+        dx, dw = lr.empty(c.R, c.D, F16), lr.empty(c.V, c.D, F16)
+        c.backward(dx, dw)
+        want.append([t.clone() for t in (c.loss, c.lse, dx.data, dw.data)])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[lr.empty(c.R, c.D, F16), lr.empty(c.V, c.D, F16)] for c in (a, b)]
+    scale = sc.scale_tensor(-3, DEV)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, s, g in zip((a, b), streams, got):
+            c.forward(stream=s)
+            kw = dict(dx=g[0], dw=g[1], dloss=c.g, dloss_scale=scale, row_scale=c.row, stream=s)
+            if c.top:
+                sc.scalify_distillation_bwd(c.x, c.w, c.teacher, c.index, c.lse, c.picked, temperature=c.T, **kw)
+            else:
+                sc.scalify_cross_entropy_bwd(c.x, c.w, c.labels, c.lse, **kw)
+    torch.cuda.synchronize()
+    for c, g, w in zip((a, b), got, want):
+        for x, y in zip((c.loss, c.lse, g[0].data, g[1].data), w):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("ex,ew", [(-127, -120), (-60, -70), (70, 60), (100, 27)])
+def test_scales_of_any_size(ex, ew):
+    """Logits whose factor leaves fp32, either way: equal probabilities, or the largest alone."""
+    say(f"loss scales {ex} {ew}")
+    R, V, D = 20, 150, 32
+    g = torch.Generator().manual_seed(8)
+    x = torch.randint(-2, 3, (R, D), generator=g).to(torch.float16)
+    w = torch.randint(-2, 3, (V, D), generator=g).to(torch.float16)
+    X, W = lr.scaled(x, F16, ex), lr.scaled(w, F16, ew)
+    labels = torch.randint(0, V, (R,), generator=g).to(DEV)
+    loss, lse = torch.empty(R, device=DEV), torch.empty(R, device=DEV)
+    sc.scalify_cross_entropy_fwd(X, W, labels, loss, lse=lse)
+    dx, dw = lr.empty(R, D, F16), lr.empty(V, D, F16)
+    if ex + ew < 0:
+        sc.scalify_cross_entropy_bwd(X, W, labels, lse, dx=dx, dw=dw, rescale=sc.RESCALE_NONE)
+    torch.cuda.synchronize()
+    z = (x.double() @ w.double().t()).to(DEV)
+    if ex + ew < 0:
+        assert ((loss.double() - math.log(V)).abs() < 1e-5).all()
+        dz = torch.full((R, V), 1.0 / V, dtype=torch.float64, device=DEV)
+        dz[torch.arange(R, device=DEV), labels] -= 1.0
+        got = lr.data(dx).to(DEV)
+        # dz: 2^-11 of a value; sums of V; the output's rounding
+        bound = (2.0 ** -10 + V * 2.0 ** -22) * (dz.abs() @ w.double().abs().to(DEV)) + 2.0 ** -11 * got.abs() + 2.0 ** -24
+        assert ((got - dz @ w.double().to(DEV)).abs() <= bound).all()
+    else:
+        # the factor is held to 2^64: a row's largest logits share the probability
+        top = z.amax(1)
+        hit = z[torch.arange(R, device=DEV), labels] == top
+        assert torch.isfinite(lse).all() and torch.isfinite(loss).all()
+        assert (loss[~hit] >= 2.0 ** 60).all() and (loss[hit] >= 0).all()
+
+
+def test_against_differences():
+    """Gradients against central differences of the forward's losses."""
+    say("loss differences")
+    R, V, D, h = 6, 40, 16, 2.0 ** -4
+    for top in (0, 5):
+        c = Case(R, V, D, top=top, T=1.5 if top else 1.0, skip=0, seed=9)
+        c.g.fill_(1.0)
+        c.forward()
+        dx, dw = lr.empty(R, D, F16), lr.empty(V, D, F16)
+        c.backward(dx, dw, eg=0)
+        torch.cuda.synchronize()
+        gx, gw = ref.true(dx), ref.true(dw)
+        r0 = c.reference()
+        want = r0.gradients(torch.ones(R, device=DEV), c.lse)
+
+        def total(mat, i, j, step):
+            t = mat.data.view(torch.float16)
+            old = t[i, j].clone()
+            t[i, j] = old + step
+            moved = (t[i, j].double() - old.double()).item()
+            c.forward()
+            torch.cuda.synchronize()
+            v = c.loss.double().sum().item()
+            t[i, j] = old
+            return v, moved
+
+        for mat, grad, err, e, (n, m) in ((c.x, gx, want[2], c.ex, (R, D)), (c.w, gw, want[3], c.ew, (V, D))):
+            for i, j in ((0, 0), (n - 1, m - 1), (3, 7), (5, 2)):
+                if mat is c.x and not r0.on[i]:
+                    continue
+                (a, sa), (b, sb) = total(mat, i, j, h), total(mat, i, j, -h)
+                slope = (a - b) / ((sa - sb) * 2.0 ** e)
+                # third derivatives of log-sum-exp are at most 1 times the logits' slope cubed (the other factor's
+                # largest value), a step's second order where the two differ, the losses' own errors
+                other = (r0.W if mat is c.x else r0.X).abs().max().item() / c.T
+                s = max(abs(sa), abs(sb)) * 2.0 ** e
+                rows = 1 if mat is c.x else R
+                tol = rows * c.T ** 2 * (other ** 3 * s * s / 6 + abs(sa + sb) * 2.0 ** e * other ** 2) + \
+                    2 * r0.lse_error().max().item() * R * c.T ** 2 / s * 3 + err[i, j].item() + 2.0 ** -11 * abs(slope) + 2.0 ** -20
+                assert abs(grad[i, j].item() - slope) <= tol, (top, i, j, grad[i, j].item(), slope, tol)
+
+
+def test_a_training_step():
+    """A step's end as it is run: the norm's 8-bit rows with their scales into the loss, its
+    gradients, and the norm's own backward; captured, and checked stage by stage."""
+    say("loss training step")
+    R, V, D = 160, 777, 192
+    x, r = lr.values(R, D, F16, 1), lr.values(R, D, F16, 2)
+    X, S = lr.scaled(x, F16, 0), lr.scaled(r, F16, 1)
+    W = lr.scaled(lr.values(V, D, E4M3, 3), E4M3, -4)
+    h, n = lr.empty(R, D, F16), lr.empty(R, D, E4M3)
+    row = torch.empty(R, device=DEV)
+    gen = torch.Generator().manual_seed(4)
+    labels = torch.randint(0, V, (R,), generator=gen)
+    labels[:50] = -100
+    labels = labels.to(DEV)
+    loss, lse = torch.empty(R, device=DEV), torch.empty(R, device=DEV)
+    dn, dw, dh = lr.empty(R, D, F16), lr.empty(V, D, E5M2), lr.empty(R, D, E5M2)
+    mean = torch.full((R,), 1.0 / 110, device=DEV)
+    scale = sc.scale_tensor(10, DEV)  # (a loss scale)
+
+    def step():
+        sc.scalify_rmsnorm_fwd(X, n, residual=S, sum_out=h, row_scale=row, target_log2=7)
+        sc.scalify_cross_entropy_fwd(n, W, labels, loss, lse=lse, row_scale=row)
+        sc.scalify_cross_entropy_bwd(n, W, labels, lse, dx=dn, dw=dw, dloss=mean, dloss_scale=scale, row_scale=row)
+        sc.scalify_rmsnorm_bwd(dn, h, dh)
+
+    step()
+    torch.cuda.synchronize()
+    rl = ref.Loss(n, W, row, labels)
+    rl.check_forward(loss, lse)
+    want = rl.gradients(mean.double() * 2.0 ** 10, lse)
+    ref.check_gradient(dn, want[0], want[2], 10 - 4, sc.RESCALE_AMAX)
+    ref.check_gradient(dw, want[1], want[3], 10, sc.RESCALE_AMAX)
+    # the rows that do not count get no gradient through the norm either
+    assert (lr.data(dh)[:50] == 0).all() and torch.isfinite(lr.data(dh)).all() and (lr.data(dh)[50:] != 0).any()
+    outs = [loss, lse, dn.data, dn.scale, dw.data, dw.scale, dh.data, dh.scale]
+    eager = [t.clone() for t in outs]
+    g = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=s):
+        step()
+    for _ in range(3):
+        for t in outs:
+            t.fill_(3)
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert torch.equal(a, b)
