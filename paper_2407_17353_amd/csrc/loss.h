@@ -123,7 +123,7 @@ struct LossGemm {
   void* out;
   int64_t ldo;
   int out_fmt, sat, mode;
-  uint32_t* amax;
+  uint32_t* amax;         // statistic of the products, or NULL
   const float *s0, *s1;   // factors of the propagated scale
   int rowscaled;          // a factor of the largest row scale is due
 };

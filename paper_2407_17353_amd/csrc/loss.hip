@@ -103,44 +103,48 @@ __global__ __launch_bounds__(256) void loss_flags_kernel(LossParams p) {
 }
 
 // Rows that count, in order, their number, and the largest upstream gradient and row
-// scale among them. One workgroup: a thread has consecutive rows.
+// scale among them. One workgroup of 16 waves, each with consecutive rows, 64 at a time:
+// a first pass counts, a second one places them.
 __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
   __shared__ int sums[16];
   __shared__ float cs[16], rs[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t per = (p.R + 1023) / 1024, lo = tid * per, hi = lo + per < p.R ? lo + per : p.R;
+  const int64_t per = (p.R + 1023) / 1024 * 64, lo = wave * per, hi = lo + per < p.R ? lo + per : p.R;
   auto counts = [&](int64_t i) {
+    if (i >= hi) return false;
     const bool has = p.labels ? p.labels[i] >= 0 && p.labels[i] < p.V : p.pos[i] >= 0;
     return has && !(p.dloss && p.dloss[i] == 0.0f);
   };
   int n = 0;
   float c = 0.f, r = 0.f;
-  for (int64_t i = lo; i < hi; ++i)
-    if (counts(i)) {
-      ++n;
+#pragma unroll 4
+  for (int64_t at = lo; at < hi; at += 64) {
+    const int64_t i = at + lane;
+    const bool on = counts(i);
+    n += (int)__popcll(__ballot(on));
+    if (on) {
       const float g = fabsf(p.dloss ? p.dloss[i] * p.temp : p.temp);
       if (g < __builtin_inff()) c = fmaxf(c, g);
       if (p.row_scale) r = fmaxf(r, p.row_scale[i]);
     }
-  int at = n;
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(at, o, 64);
-    if (lane >= o) at += v;
   }
   c = wave_max(c), r = wave_max(r);
-  if (lane == 63) sums[wave] = at;
-  if (lane == 0) cs[wave] = c, rs[wave] = r;
+  if (lane == 0) sums[wave] = n, cs[wave] = c, rs[wave] = r;
   __syncthreads();
-  int before = 0, all = 0;
+  int place = 0, all = 0;
   for (int w = 0; w < 16; ++w) {
-    if (w < wave) before += sums[w];
+    if (w < wave) place += sums[w];
     all += sums[w];
   }
-  at += before - n;
-  for (int64_t i = lo; i < hi; ++i) {
+#pragma unroll 4
+  for (int64_t at = lo; at < hi; at += 64) {
+    const int64_t i = at + lane;
     const bool on = counts(i);
-    p.pos[i] = on ? at : -1;
-    if (on) p.rows[at++] = (int)i;
+    const uint64_t mask = __ballot(on);
+    const int to = place + (int)__popcll(mask & (((uint64_t)1 << lane) - 1));
+    if (i < hi) p.pos[i] = on ? to : -1;
+    if (on) p.rows[to] = (int)i;
+    place += (int)__popcll(mask);
   }
   if (tid == 0) {
     for (int w = 1; w < 16; ++w) c = fmaxf(c, cs[w]), r = fmaxf(r, rs[w]);
@@ -236,10 +240,10 @@ __global__ __launch_bounds__(256) void loss_copy_w_kernel(LossParams p, int v0, 
 }
 
 // Joins the maxima and sums of a row's column groups: log-sum-exp, and the cross
-// entropy. 64 places a workgroup, the groups dealt to its four waves (a fixed order).
+// entropy. 64 places a workgroup, the groups dealt to its 16 waves (a fixed order).
 // Rows that do not count get 0.
-__global__ __launch_bounds__(256) void loss_join_kernel(LossParams p, int groups) {
-  __shared__ float sm[4][64], ss[4][64];
+__global__ __launch_bounds__(1024) void loss_join_kernel(LossParams p, int groups) {
+  __shared__ float sm[16][64], ss[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int count = (int)p.hdr[LOSS_COUNT];
   for (int64_t b = blockIdx.x; b * 64 < p.R; b += gridDim.x) {
@@ -247,7 +251,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossParams p, int groups
     float m = -__builtin_inff(), n = 0.f;
     if (i < count) {
 #pragma unroll 4
-      for (int g = wave; g < groups; g += 4) {
+      for (int g = wave; g < groups; g += 16) {
         const float2 v = p.stats[(int64_t)g * p.R + i];
         const float t = fmaxf(m, v.x);  // (a NaN is in the sums)
         const float a = m == -__builtin_inff() ? 0.f : n * exp2f(m - t), c = v.x == -__builtin_inff() ? 0.f : v.y * exp2f(v.x - t);
@@ -260,7 +264,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossParams p, int groups
     __syncthreads();
     if (wave == 0) {
       if (i < count) {
-        for (int w = 1; w < 4; ++w) {
+        for (int w = 1; w < 16; ++w) {
           const float t = fmaxf(m, sm[w][lane]);
           const float a = m == -__builtin_inff() ? 0.f : n * exp2f(m - t);
           const float c = sm[w][lane] == -__builtin_inff() ? 0.f : ss[w][lane] * exp2f(sm[w][lane] - t);
@@ -354,28 +358,32 @@ __device__ __forceinline__ int out_exponent(const LossParams& p, bool dw, int ba
   return clamp_e8m0(base + (plain ? 0 : floor_log2_bits(a) + unit - p.target));
 }
 
-// dx: the splits' sum into the first of them, and its statistic.
+// dx: the splits' sum into the first of them, and its statistic (one split's is the
+// product's own). A workgroup a row at a time.
 __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
-  const int count = (int)p.hdr[LOSS_COUNT], chunks = (p.D + 3) / 4;
-  const int64_t all = (int64_t)count * chunks;
+  const int count = (int)p.hdr[LOSS_COUNT];
   float a = 0.f;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / chunks;
-    const int c = 4 * (int)(i - r * chunks);
-    float4* o = (float4*)(p.part + r * p.ldp + c);
-    float4 v = *o;
-    for (int s = 1; s < p.splits; ++s) {
-      const float4 w = *(const float4*)(p.part + ((int64_t)s * p.R + r) * p.ldp + c);
-      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+  for (int64_t r = blockIdx.x; r < count; r += gridDim.x)
+    for (int c = 4 * (int)threadIdx.x; c < p.D; c += 1024) {
+      float* o = p.part + r * p.ldp + c;
+      float4 v = *(const float4*)o;
+#pragma unroll 4
+      for (int s = 1; s < p.splits; ++s) {
+        const float4 w = *(const float4*)(o + (int64_t)s * p.R * p.ldp);
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+      }
+      *(float4*)o = v;
+      a = fmaxf(a, fabsf(v.x));
+      if (c + 1 < p.D) a = fmaxf(a, fabsf(v.y));
+      if (c + 2 < p.D) a = fmaxf(a, fabsf(v.z));
+      if (c + 3 < p.D) a = fmaxf(a, fabsf(v.w));
     }
-    if (p.splits > 1) *o = v;
-    a = fmaxf(a, fabsf(v.x));
-    if (c + 1 < p.D) a = fmaxf(a, fabsf(v.y));
-    if (c + 2 < p.D) a = fmaxf(a, fabsf(v.z));
-    if (c + 3 < p.D) a = fmaxf(a, fabsf(v.w));
-  }
+  __shared__ float red[4];
   a = wave_max(a);
-  if ((threadIdx.x & 63) == 0 && a > 0.f) atomicMax(p.hdr + LOSS_AMAX_DX, __float_as_uint(a));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
+  __syncthreads();
+  a = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  if (threadIdx.x == 0 && a > 0.f) atomicMax(p.hdr + LOSS_AMAX_DX, __float_as_uint(a));
 }
 
 template <int F>
@@ -407,7 +415,11 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw)
     const int c = 16 * (int)(i - r * chunks), cols = p.D - c;
     const int64_t from = dw ? r : p.pos[r];
     uint32_t u[16];
-    if (from >= 0) {
+    if (dw && fmt != kF16) {
+      load16<kF16>(src, from * p.ldp + c, u);  // (16 bits of each fp32, sticky16)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) u[k] <<= 16;
+    } else if (from >= 0) {
       load16<kF32>(src, from * p.ldp + c, u);
     } else {
 #pragma unroll
@@ -571,7 +583,7 @@ hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s) {
   LossGemm g;
   for (int v0 = 0; v0 < p.V; v0 += p.piece)
     TRY(piece_logits(p, v0, std::min(p.piece, p.V - v0), p.labels ? LOSS_STATS : LOSS_PICK, &g, s));
-  TRY(launch_one(loss_join_kernel, groups_for(p.R, 64, 16384), 256, s, p, 2 * ((p.V + 255) / 256)));
+  TRY(launch_one(loss_join_kernel, groups_for(p.R, 64, 16384), 1024, s, p, 2 * ((p.V + 255) / 256)));
   if (!p.labels) TRY(launch_one(loss_top_kernel, groups_for(p.R, 4, 8192), 256, s, p));
   return hipSuccess;
 }
@@ -598,6 +610,7 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
       g.part = p.part;
       g.ldp = p.ldp;
       g.accumulate = v0 > 0;
+      g.amax = p.splits == 1 && v0 + n == p.V ? p.hdr + LOSS_AMAX_DX : nullptr;
       const int64_t tiles = (int64_t)((p.R + 255) / 256) * ((p.D + 255) / 256) * p.splits;
       TRY(launch_loss_grads(g, LOSS_DX, grid_for(tiles), s));
     }
@@ -627,7 +640,7 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
     }
   }
   if (p.dx) {
-    TRY(launch_one(loss_sum_kernel, groups_for((int64_t)p.R * ((p.D + 3) / 4), 1024, 4096), 256, s, p));
+    if (p.splits > 1) TRY(launch_one(loss_sum_kernel, groups_for(p.R, 2, 8192), 256, s, p));
     TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0));
   }
   if (p.dw && p.mode == 1)

@@ -53,14 +53,19 @@ __device__ __forceinline__ void read_part(v4i (&f)[2], const uint8_t* lds, uint3
   }
 }
 
-// Sum or maximum over the four lanes that hold a row.
+// Sum or maximum over the four lanes that hold a row (lane ^ 16, lane ^ 32).
+template <typename F>
+__device__ __forceinline__ float row4(float v, F f) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 __device__ __forceinline__ float row4_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+  return row4(v, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float row4_sum(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
+  return row4(v, [](float a, float b) { return a + b; });
 }
 
 // Exponent of the largest |upstream gradient| (0 where there is none).
@@ -73,11 +78,19 @@ __device__ __forceinline__ int loss_exponent(const uint32_t* hdr, int word) {
 // else each stay in a register over the whole loop).
 __device__ __forceinline__ void held(uint32_t& x) { asm volatile("" : "+v"(x)); }
 
-template <bool A_MC, bool B_MC, int EPI>
+// OF (LOSS_DW): what is stored: codes of a format, fp32, or the 16-bit form of fp32 that
+// keeps an 8-bit rounding (sticky16).
+enum LossForm : int { FORM_F32 = 8, FORM_STICKY = 9 };
+
+template <bool A_MC, bool B_MC, int EPI, int OF>
 __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   using C = WaveCfg<4>;
   constexpr int WTM = C::WTM, WTN = C::WTN, MI = C::MI, NI = C::NI, BPW = C::BPW;
-  constexpr int STAGE = EPI == LOSS_PICK ? 8192 : (EPI == LOSS_DZ ? 4096 : 0);
+  // bytes of an element that goes through LDS, and of a wave's 16 rows
+  constexpr int ESZ = EPI == LOSS_DZ ? 2 : (EPI != LOSS_DW ? 4 : (OF == FORM_F32 ? 4 : (OF == kF16 || OF == FORM_STICKY ? 2 : 1)));
+  constexpr int STAGE = EPI == LOSS_STATS || EPI == LOSS_DX ? 0 : 2048 * ESZ;
+  // stores of an epilogue whose tile lies inside the matrix, at least
+  constexpr int STORES = EPI == LOSS_DZ ? 32 : (EPI == LOSS_DW ? 16 * ESZ : 0);
   // [A of even steps | A of odd steps | B | B | the waves' staging]
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TILE_BYTES + 4 * STAGE];
 
@@ -195,6 +208,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   v4i bf[NI][2];
   uint32_t aa = operand_addr<A_MC>(wm, lane), ab = operand_addr<B_MC>(wn, lane);
 
+  bool stored = false;  // the last thing done is an epilogue with all its stores
   // Schedule of a step: that of gemm4_kernel, with a pair of products in the place of
   // each of its products (the two k parts of 32).
   auto head = [&](auto par_tag) {
@@ -219,7 +233,13 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
         static_for<j * BPW / AS, (j + 1) * BPW / AS>([&](auto J) { issue_one(decltype(J)::value, P); });
       }
     });
-    wait_vmcnt<BPW>();
+    // (vector memory is done in order: behind an epilogue's stores, the loads of the next
+    // step are older than they are)
+    if (STORES > 0 && P == 0 && stored)
+      wait_vmcnt<(BPW + STORES < 63 ? BPW + STORES : 63)>();
+    else
+      wait_vmcnt<BPW>();
+    stored = false;
     wait_lgkmcnt<0>();
     __builtin_amdgcn_s_barrier();
   };
@@ -257,7 +277,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   bool d_fast = false;
   float d_scale = 1.0f, d_inv = 1.0f;
   if constexpr (EPI == LOSS_DW) {
-    if (p.mode != 1) {  // the scale is known: codes at once
+    if constexpr (OF != FORM_F32 && OF != FORM_STICKY) {  // the scale is known: codes at once
       const int unit = loss_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2 + (p.rowscaled ? loss_exponent(p.hdr, LOSS_RMAX) : 0);
       const int base = pow2_exponent(p.s0) + pow2_exponent(p.s1);
       e_out = clamp_e8m0(base);
@@ -266,6 +286,23 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       if (d_fast) d_scale = pow2_float(d_shift), d_inv = pow2_float(-d_shift);
     }
   }
+  // A tile's numbers of a lane's rows, loaded while its last steps run.
+  float r_f[MI], r_l[MI], r_c[MI];
+  int r_i[MI];  // label; LOSS_PICK: row
+  auto load_rows = [&](int m0) {
+    if constexpr (EPI == LOSS_STATS || EPI == LOSS_PICK || EPI == LOSS_DZ) {
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) {
+        const int m = min(m0 + wm + 16 * mi + lr, M - 1);
+        r_f[mi] = p.factor[m];
+        if constexpr (EPI == LOSS_DZ) r_l[mi] = p.lse2[m], r_c[mi] = p.coef[m];
+        if constexpr (EPI == LOSS_PICK)
+          r_i[mi] = p.rows[m];
+        else
+          r_i[mi] = p.label ? p.label[m] : -1;
+      }
+    }
+  };
   // The 32 values of a lane's row (mi) of the wave's tile, and the accumulators back to 0.
   auto take = [&](auto mi_tag, float (&x)[4 * NI]) {
     constexpr int mi = decltype(mi_tag)::value;
@@ -277,7 +314,51 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       for (int i = 0; i < 4; ++i) x[4 * ni + i] = v[i];
     });
   };
+  // 16 rows of a wave's 128 columns through its LDS (the 16-byte chunks of a row permuted
+  // by the row), so that whole rows are stored: group(ni) gives a lane's four elements.
+  constexpr int CPR = 8 * ESZ;  // chunks of a row
+  auto stage_rows = [&](auto group) {
+    static_for<0, NI>([&](auto Q) {
+      constexpr int ni = decltype(Q)::value;
+      const int chunk = ESZ == 4 ? 4 * ni + lq : (ESZ == 2 ? 2 * ni + (lq >> 1) : ni);
+      const int off = ESZ == 4 ? 0 : (ESZ == 2 ? 8 * (lq & 1) : 4 * lq);
+      const auto w = group(Q);
+      *(std::remove_const_t<decltype(w)>*)(st + lr * 16 * CPR + ((chunk ^ (lr & (CPR - 1))) * 16) + off) = w;
+    });
+    wait_lgkmcnt<0>();
+  };
+  // They go to rows m0 .. and columns n0 .. (below cols) of a matrix of pitch ld.
+  auto store_rows = [&](void* base, int64_t ld, int m0, int n0, int cols) {
+    constexpr int ROWS = 64 / CPR, PER = 16 / ESZ;
+    u4 o[16 / ROWS];
+#pragma unroll
+    for (int j = 0; j < 16 / ROWS; ++j) {
+      const int r = ROWS * j + lane / CPR, c = lane % CPR;
+      o[j] = *(const u4*)(st + r * 16 * CPR + ((c ^ (r & (CPR - 1))) * 16));
+    }
+    wait_lgkmcnt<0>();
+#pragma unroll
+    for (int j = 0; j < 16 / ROWS; ++j) {
+      const int row = m0 + ROWS * j + lane / CPR, col = n0 + PER * (lane % CPR);
+      uint8_t* to = (uint8_t*)base + ((int64_t)row * ld + col) * ESZ;
+      if (row < M && col < cols) {
+        if (EPI != LOSS_DW || OF == FORM_F32 || OF == FORM_STICKY || col + PER <= cols) {  // (pitches of whole chunks)
+          *(u4*)to = o[j];
+        } else {
+#pragma unroll
+          for (int i = 0; i < PER - 1; ++i)
+            if (col + i < cols) {
+              if constexpr (ESZ == 2)
+                ((uint16_t*)to)[i] = (uint16_t)(o[j][i / 2] >> (16 * (i % 2)));
+              else if constexpr (ESZ == 1)
+                to[i] = (uint8_t)(o[j][i / 4] >> (8 * (i % 4)));
+            }
+        }
+      }
+    }
+  };
   auto store_tile = [&](int m0, int n0, int split) {
+    stored = m0 + wm + WTM <= M && n0 + wn + WTN <= N;
     // (the call's other operands are read here, by the scalar unit, not held over the loop)
     typedef const __attribute__((address_space(4))) LossGemm* Args;
     Args args = (Args)__builtin_amdgcn_kernarg_segment_ptr();
@@ -294,7 +375,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       held(first_n);  // (the masks of its columns would else be kept from row to row)
       const int nb = (int)first_n;
       if constexpr (EPI == LOSS_STATS || EPI == LOSS_PICK) {
-        const float f = in ? p.factor[m] : 0.f;
+        const float f = r_f[mi];
         if (!all_n) {
 #pragma unroll
           for (int i = 0; i < 4 * NI; ++i)
@@ -312,7 +393,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
         sum = row4_sum(sum);
         if (lq == 0 && in) p.stats[(int64_t)((p.v0 + n0 + wn) / WTN) * p.R + m] = float2{top == -__builtin_inff() ? top : m2, sum};
         if constexpr (EPI == LOSS_STATS) {
-          const int d = in ? p.label[m] - (p.v0 + nb) : -1;
+          const int d = in ? r_i[mi] - (p.v0 + nb) : -1;
           // (the lane that has the label's column: d = 16 ni + i)
           const bool mine = d >= 0 && d < WTN && (d & 15) < 4;
           if (__ballot(mine)) {
@@ -330,7 +411,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
           });
           wait_lgkmcnt<0>();
           if (in) {
-            const int64_t to = (int64_t)p.rows[m] * p.top;
+            const int64_t to = (int64_t)r_i[mi] * p.top;
             const float fn = f * 0.69314718055994530942f;
             for (int j = 4 * lq; j < p.topp; j += 16) {
               const v4i t = *(const v4i*)(p.top32 + (int64_t)m * p.topp + j);
@@ -345,44 +426,27 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
           wait_lgkmcnt<0>();
         }
       } else if constexpr (EPI == LOSS_DZ) {
-        const float f = in ? p.factor[m] : 0.f, l = in ? p.lse2[m] : 0.f, c = in ? p.coef[m] : 0.f;
+        const float f = r_f[mi], l = r_l[mi], c = r_c[mi];
 #pragma unroll
         for (int i = 0; i < 4 * NI; ++i) x[i] = c * __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -l));
-        if (p.label) {
-          const int d = in ? p.label[m] - (p.v0 + nb) : -1;
-          const bool mine = d >= 0 && d < WTN && (d & 15) < 4;
-          if (__ballot(mine)) {
+        const int d = r_i[mi] - (p.v0 + nb);  // (no label: below 0)
+        if (__ballot(d >= 0 && d < WTN && (d & 15) < 4)) {
 #pragma unroll
-            for (int i = 0; i < 4 * NI; ++i)
-              if (d == 16 * (i >> 2) + (i & 3)) x[i] -= c;
-          }
+          for (int i = 0; i < 4 * NI; ++i)
+            if (d == 16 * (i >> 2) + (i & 3)) x[i] -= c;
         }
         if (!all_n) {
 #pragma unroll
           for (int i = 0; i < 4 * NI; ++i)
             if (nb + 16 * (i >> 2) + (i & 3) >= N) x[i] = 0.f;
         }
-        // whole rows through LDS (the chunks of a row permuted by the row)
-        static_for<0, NI>([&](auto Q) {
+        stage_rows([&](auto Q) {
           constexpr int ni = decltype(Q)::value;
           const lh2 a = {(_Float16)x[4 * ni], (_Float16)x[4 * ni + 1]}, b = {(_Float16)x[4 * ni + 2], (_Float16)x[4 * ni + 3]};
-          *(v2i*)(st + lr * 256 + (((2 * ni + (lq >> 1)) ^ lr) * 16) + 8 * (lq & 1)) =
-              v2i{__builtin_bit_cast(int, a), __builtin_bit_cast(int, b)};
+          return v2i{__builtin_bit_cast(int, a), __builtin_bit_cast(int, b)};
         });
-        wait_lgkmcnt<0>();
-        u4 d[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = 4 * j + (lane >> 4);
-          d[j] = *(const u4*)(st + r * 256 + (((lane & 15) ^ r) * 16));
-        }
-        wait_lgkmcnt<0>();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int row = m0 + wm + 16 * mi + 4 * j + (lane >> 4), col = n0 + wn + 8 * (lane & 15);
-          // (ldz is a multiple of 64: a row holds every column of the tiles it reaches)
-          if (row < M && col < p.ldz) *(u4*)((uint16_t*)p.dz + (int64_t)row * p.ldz + col) = d[j];
-        }
+        // (ldz is a multiple of 64: a row holds every column of the tiles it reaches)
+        store_rows(p.dz, p.ldz, m0 + wm + 16 * mi, n0 + wn, (int)p.ldz);
       } else if constexpr (EPI == LOSS_DX) {
         if (in) {
           float* o = p.part + ((int64_t)split * p.R + m) * p.ldp + nb;
@@ -392,6 +456,9 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
               v4f v = {x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
               if (p.accumulate) v += *(const v4f*)(o + 16 * ni);
               *(v4f*)(o + 16 * ni) = v;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (nb + 16 * ni + i < N) lmax = fmaxf(lmax, fabsf(v[i]));
             }
           });
         }
@@ -402,47 +469,72 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
             if (nb + 16 * (i >> 2) + (i & 3) >= N) x[i] = 0.f;
         }
         if (in) {
-          if (p.mode == 1) {
-            float* o = p.part + (int64_t)(p.v0 + m) * p.ldp + nb;
-            static_for<0, NI>([&](auto Q) {
-              constexpr int ni = decltype(Q)::value;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) lmax = fmaxf(lmax, fabsf(x[4 * ni + i]));
-              if (nb + 16 * ni < p.ldp) *(v4f*)(o + 16 * ni) = v4f{x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
-            });
-          } else {
-            static_for<0, NI>([&](auto Q) {
-              constexpr int ni = decltype(Q)::value;
-              const v4f v = {x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
+          for (int i = 0; i < 4 * NI; ++i) lmax = fmaxf(lmax, fabsf(x[i]));
+        }
+        if constexpr (OF == FORM_F32) {
+          stage_rows([&](auto Q) {
+            constexpr int ni = decltype(Q)::value;
+            return v4f{x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
+          });
+          store_rows(p.part + (int64_t)p.v0 * p.ldp, p.ldp, m0 + wm + 16 * mi, n0 + wn, (int)p.ldp);
+        } else if constexpr (OF == FORM_STICKY) {
+          stage_rows([&](auto Q) {
+            constexpr int ni = decltype(Q)::value;
+            uint32_t u[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) lmax = fmaxf(lmax, fabsf(v[i]));
-              const int cols = N - (nb + 16 * ni);
-              const int64_t e = (int64_t)(p.v0 + m) * p.ldo + nb + 16 * ni;
-              uint32_t code[4];
-              if (p.out_fmt == kF16) {
-                const v2i w = cast4_f16_any(v, d_fast, d_inv, d_shift, p.sat);
-                code[0] = (uint32_t)w.x & 0xFFFFu, code[1] = (uint32_t)w.x >> 16;
-                code[2] = (uint32_t)w.y & 0xFFFFu, code[3] = (uint32_t)w.y >> 16;
-                if (cols >= 4) *(v2i*)((uint16_t*)p.out + e) = w;
-              } else {
-                const uint32_t w = p.out_fmt == kE4M3 ? cast4_fp8_any<kE4M3>(v, d_fast, d_scale, d_shift, p.sat)
-                                                      : cast4_fp8_any<kE5M2>(v, d_fast, d_scale, d_shift, p.sat);
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t b = __float_as_uint(x[4 * ni + i]);
+              u[i] = b | ((b & 0xFFFFu) + 0xFFFFu);  // (bit 16 is set if a lower one is)
+            }
+            return v2i{(int)__builtin_amdgcn_perm(u[1], u[0], 0x07060302u), (int)__builtin_amdgcn_perm(u[3], u[2], 0x07060302u)};
+          });
+          store_rows((uint16_t*)p.part + (int64_t)p.v0 * p.ldp, p.ldp, m0 + wm + 16 * mi, n0 + wn, (int)p.ldp);
+        } else {
+          // a shift outside the conversions' window: exact wherever the result is normal
+          // (below, zero either way)
+          if (!d_fast) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) code[i] = (w >> (8 * i)) & 0xFFu;
-                if (cols >= 4) *(uint32_t*)((uint8_t*)p.out + e) = w;
-              }
-              if (cols < 4) {
-#pragma unroll
-                for (int i = 0; i < 3; ++i)
-                  if (i < cols) {
-                    if (p.out_fmt == kF16)
-                      ((uint16_t*)p.out)[e + i] = (uint16_t)code[i];
-                    else
-                      ((uint8_t*)p.out)[e + i] = (uint8_t)code[i];
-                  }
-              }
-            });
+            for (int i = 0; i < 4 * NI; ++i) x[i] = __builtin_amdgcn_ldexpf(x[i], -d_shift);
           }
+          float any = 0.f;  // (NaN if there is one, or two infinities)
+#pragma unroll
+          for (int i = 0; i < 4 * NI; ++i) any += x[i];
+          const bool nan = __ballot(any != any) != 0;
+          auto emit = [&](auto nan_tag) {
+            stage_rows([&](auto Q) {
+              constexpr int ni = decltype(Q)::value;
+              const float* y = x + 4 * ni;
+              if constexpr (OF == kF16) {
+                v2i w = p.sat ? cvt4_f16_fast<true>(y[0], y[1], y[2], y[3], d_inv) : cvt4_f16_fast<false>(y[0], y[1], y[2], y[3], d_inv);
+                if constexpr (decltype(nan_tag)::value) {
+                  uint32_t h[4] = {(uint32_t)w.x & 0xFFFFu, (uint32_t)w.x >> 16, (uint32_t)w.y & 0xFFFFu, (uint32_t)w.y >> 16};
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    if (y[i] != y[i]) h[i] = FmtTraits<kF16>::NANC | ((__float_as_uint(y[i]) >> 16) & 0x8000u);
+                  w = v2i{(int)(h[0] | (h[1] << 16)), (int)(h[2] | (h[3] << 16))};
+                }
+                return w;
+              } else {
+                uint32_t w = cast4_fp8_hw<OF>(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]),
+                                              __float_as_uint(y[3]), d_scale, p.sat);
+                if constexpr (decltype(nan_tag)::value) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    if (y[i] != y[i]) {
+                      const uint32_t c = FmtTraits<OF>::NANC | ((__float_as_uint(y[i]) >> 24) & 0x80u);
+                      w = (w & ~(0xFFu << (8 * i))) | (c << (8 * i));
+                    }
+                }
+                return w;
+              }
+            });
+          };
+          if (__builtin_expect(nan, 0))
+            emit(std::true_type{});
+          else
+            emit(std::false_type{});
+          store_rows((uint8_t*)p.out + (int64_t)p.v0 * p.ldo * ESZ, p.ldo, m0 + wm + 16 * mi, n0 + wn, N);
         }
       }
     });
@@ -474,10 +566,11 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   origin(0, c_m0, c_n0, c_split);
   head(P0{});
   for (int kt = 0;;) {
+    kt += 2;
+    if (kt == KTe) load_rows(c_m0);
     tail(P0{});
     head(P1{});
     tail(P1{});
-    kt += 2;
     if (kt == KTe) {
       kt = 0;
       mfma_drain();
@@ -489,7 +582,8 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
     head(P0{});
   }
   wait_vmcnt<0>();  // the out-of-range loads past the last tile
-  if constexpr (EPI == LOSS_DW) {
+  if constexpr (EPI == LOSS_DW || EPI == LOSS_DX) {
+    if (!p.amax) return;
     for (int off = 32; off > 0; off >>= 1) lmax = fmaxf(lmax, __shfl_xor(lmax, off, 64));
     if (lane == 0 && lmax > 0.f) atomicMax(p.amax, __float_as_uint(lmax));
   }

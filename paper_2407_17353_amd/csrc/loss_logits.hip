@@ -4,9 +4,9 @@
 namespace scalify {
 
 hipError_t launch_loss_logits(const LossGemm& p, int epi, int grid, hipStream_t s) {
-  if (epi == LOSS_STATS) return launch_one(loss_gemm_kernel<false, false, LOSS_STATS>, grid, 256, s, p);
-  if (epi == LOSS_PICK) return launch_one(loss_gemm_kernel<false, false, LOSS_PICK>, grid, 256, s, p);
-  return launch_one(loss_gemm_kernel<false, false, LOSS_DZ>, grid, 256, s, p);
+  if (epi == LOSS_STATS) return launch_one(loss_gemm_kernel<false, false, LOSS_STATS, 0>, grid, 256, s, p);
+  if (epi == LOSS_PICK) return launch_one(loss_gemm_kernel<false, false, LOSS_PICK, 0>, grid, 256, s, p);
+  return launch_one(loss_gemm_kernel<false, false, LOSS_DZ, 0>, grid, 256, s, p);
 }
 
 }  // namespace scalify
