@@ -119,11 +119,12 @@ _MID_KERNEL = re.compile(r"mid_gemm_kernelILb[01]ELb[01]ELi\d+ELi\d+ELi(\d+)ELi\
 
 def pinned_kernel(src: str, name: str) -> bool:
     """Whether a kernel of this source that multiplies into AGPRs keeps its
-    accumulators in asm-named ones: every such kernel of the gemm_* and loss_* sources,
+    accumulators in asm-named ones: every such kernel of the gemm_*, loss_logits
+    and loss_grads sources,
     and of the mid_* sources those with 256 columns (8 accumulator tiles per
     row of tiles); the others leave their accumulators to the compiler."""
     base = os.path.basename(src)
-    if base.startswith(("gemm_", "loss_")):
+    if base.startswith(("gemm_", "loss_logits", "loss_grads")):
         return True
     if base.startswith("mid_"):
         m = _MID_KERNEL.search(name)

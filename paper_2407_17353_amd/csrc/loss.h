@@ -6,6 +6,10 @@
 
 namespace scalify {
 
+// How dw is stored, beside a format's codes: fp32, or the 16-bit form of fp32 that keeps an
+// 8-bit rounding (sticky16).
+enum LossForm : int { FORM_F32 = 8, FORM_STICKY = 9 };
+
 // Words of the workspace header (kHeaderBytes):
 enum LossWord : int {
   LOSS_COUNT = 0,   // rows that count
@@ -74,6 +78,13 @@ struct LossPlan {
 // Also sets the workspace's pointers of p, where p is not NULL (base 256-byte aligned).
 LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool back, bool amax, LossParams* p, void* base);
 
+// Rows up to which a call goes by the bytes of w (loss_few.hip); the backward's dz is then
+// one piece.
+constexpr int kLossFewRows = 128;
+inline bool loss_few_bwd(int64_t R, int64_t V) { return R <= kLossFewRows && R * V <= ((int64_t)1 << 28); }
+hipError_t launch_loss_few_dz(const LossParams& p, hipStream_t s);
+hipError_t launch_loss_few_grads(const LossParams& p, hipStream_t s);
+hipError_t launch_loss_few(const LossParams& p, hipStream_t s);
 hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s);
 hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s);
 

@@ -16,7 +16,7 @@
 // allow: each one adds to dx, which costs 8 bytes an element and piece.
 #include "attention_dev.h"
 #include "kernels.h"
-#include "loss.h"
+#include "loss_dev.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -36,10 +36,6 @@ __device__ __forceinline__ float load_any(const void* base, int fmt, int64_t e) 
   return fmt == kE4M3 ? decode_hw<kE4M3>(c) : decode_hw<kE5M2>(c);
 }
 __device__ __forceinline__ float scale_of(const float* s) { return s ? *s : 1.0f; }
-__device__ __forceinline__ float wave_max(float v) {
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
-}
 __device__ __forceinline__ float wave_sum(float v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
@@ -69,6 +65,13 @@ __device__ __forceinline__ TeacherRow load_teacher(const LossParams& p, int64_t 
   }
   return r;
 }
+// Whether a token of the row has a logit above -Inf (a NaN is one).
+__device__ __forceinline__ bool teaches(const TeacherRow& r) {
+  bool any = false;
+#pragma unroll
+  for (int j = 0; j < kTopRegs; ++j) any |= r.t[j] != -__builtin_inff();
+  return __ballot(any) != 0;
+}
 // The entries' probabilities, and the logarithms of these.
 __device__ __forceinline__ void teacher_softmax(const TeacherRow& r, float (&q)[kTopRegs], float (&logq)[kTopRegs]) {
   float m = -__builtin_inff(), n = 0.f;
@@ -94,10 +97,7 @@ __global__ __launch_bounds__(256) void loss_flags_kernel(LossParams p) {
   const int lane = threadIdx.x & 63;
   for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < p.R; row += (int64_t)gridDim.x * 4) {
     const TeacherRow r = load_teacher(p, row, lane);
-    bool any = false;
-#pragma unroll
-    for (int j = 0; j < kTopRegs; ++j) any |= r.t[j] != -__builtin_inff();  // (a NaN counts)
-    const bool some = __ballot(any) != 0;
+    const bool some = teaches(r);
     if (lane == 0) p.pos[row] = some ? 0 : -1;
   }
 }
@@ -155,10 +155,6 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
   }
 }
 
-__device__ __forceinline__ int hdr_exponent(const uint32_t* hdr, int word) {
-  return hdr[word] == 0u ? 0 : floor_log2_bits(hdr[word]);
-}
-
 // Eight codes from element e of a row on, as F16, those past the row's D columns 0.
 __device__ __forceinline__ u4 load_tail8(int fmt, const void* base, int64_t e, int left) {
   u4 v = load_f16x8(fmt, base, e);
@@ -180,10 +176,7 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(LossParams p) {
     const int64_t row = p.rows[i];
     const float r = p.row_scale ? p.row_scale[row] : 1.0f;
     if (threadIdx.x == 0) {
-      // logits in base 2; a factor past [2^-100, 2^64] gives equal ones, or the largest alone
-      const int e = pow2_exponent(p.s_x) + pow2_exponent(p.s_w) + (p.row_scale ? pow2_exponent(p.row_scale + row) : 0);
-      const float f = ldexpf(kLog2e / p.temp, e < -200 ? -200 : (e > 200 ? 200 : e));
-      p.factor[i] = fminf(fmaxf(f, 0x1p-100f), 0x1p64f);
+      p.factor[i] = logit_factor(p, row);
       if (p.labels) p.label[i] = (int)p.labels[row];
       if (p.lse2) {
         p.lse2[i] = p.lse[row] * kLog2e;
@@ -253,10 +246,7 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossParams p, int group
 #pragma unroll 4
       for (int g = wave; g < groups; g += 16) {
         const float2 v = p.stats[(int64_t)g * p.R + i];
-        const float t = fmaxf(m, v.x);  // (a NaN is in the sums)
-        const float a = m == -__builtin_inff() ? 0.f : n * exp2f(m - t), c = v.x == -__builtin_inff() ? 0.f : v.y * exp2f(v.x - t);
-        n = a + c;
-        m = t;
+        join_sums(m, n, v.x, v.y);
       }
     }
     sm[wave][lane] = m;
@@ -264,19 +254,13 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossParams p, int group
     __syncthreads();
     if (wave == 0) {
       if (i < count) {
-        for (int w = 1; w < 16; ++w) {
-          const float t = fmaxf(m, sm[w][lane]);
-          const float a = m == -__builtin_inff() ? 0.f : n * exp2f(m - t);
-          const float c = sm[w][lane] == -__builtin_inff() ? 0.f : ss[w][lane] * exp2f(sm[w][lane] - t);
-          n = a + c;
-          m = t;
-        }
+        for (int w = 1; w < 16; ++w) join_sums(m, n, sm[w][lane], ss[w][lane]);
         const float l2 = m + log2f(n);
         const int row = p.rows[i];
         if (p.lse) p.lse[row] = kLn2 * l2;
         if (p.labels) p.loss[row] = kLn2 * (l2 - p.picked2[i]);
       }
-      if (i < p.R && p.pos[i] < 0) {
+      if (p.labels && i < p.R && p.pos[i] < 0) {
         p.loss[i] = 0.f;
         if (p.lse) p.lse[i] = 0.f;
       }
@@ -285,15 +269,16 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossParams p, int group
   }
 }
 
-// Distillation's loss, and 0 for logits of tokens that are not there. A wave a row.
+// Distillation's loss; rows that do not count, and logits of tokens that are not there,
+// get 0. A wave a row.
 __global__ __launch_bounds__(256) void loss_top_kernel(LossParams p) {
   const int lane = threadIdx.x & 63;
   for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < p.R; row += (int64_t)gridDim.x * 4) {
-    const bool on = p.pos[row] >= 0;
     const TeacherRow r = load_teacher(p, row, lane);
+    const bool on = teaches(r);
     float q[kTopRegs], logq[kTopRegs], sum = 0.f;
     teacher_softmax(r, q, logq);
-    const float l = on ? p.lse[row] : 0.f;
+    const float l = p.lse[row];
 #pragma unroll
     for (int j = 0; j < kTopRegs; ++j) {
       const int e = lane + 64 * j;
@@ -305,7 +290,10 @@ __global__ __launch_bounds__(256) void loss_top_kernel(LossParams p) {
         sum += q[j] * (logq[j] - (*z - l));
     }
     sum = wave_sum(sum);
-    if (lane == 0 && on) p.loss[row] = p.temp * p.temp * sum;
+    if (lane == 0) {
+      p.loss[row] = on ? p.temp * p.temp * sum : 0.f;
+      if (!on) p.lse[row] = 0.f;
+    }
   }
 }
 
@@ -345,26 +333,13 @@ __global__ __launch_bounds__(256) void loss_fix_kernel(LossParams p, int v0, int
 
 // ---- the gradients' rescale and cast
 
-// Unit of the products: a gradient's data in its propagated scale is the product times
-// 2^unit.
-__device__ __forceinline__ int unit_of(const LossParams& p, bool dw) {
-  const int u = hdr_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2;
-  return dw && p.row_scale ? u + hdr_exponent(p.hdr, LOSS_RMAX) : u;
-}
-__device__ __forceinline__ int base_of(const LossParams& p, bool dw) { return pow2_exponent(p.s_dloss) + pow2_exponent(dw ? p.s_x : p.s_w); }
-__device__ __forceinline__ int out_exponent(const LossParams& p, bool dw, int base, int unit) {
-  const uint32_t a = p.hdr[dw ? LOSS_AMAX_DW : LOSS_AMAX_DX];
-  const bool plain = p.mode != 1 || a == 0u || a >= 0x7F800000u;
-  return clamp_e8m0(base + (plain ? 0 : floor_log2_bits(a) + unit - p.target));
-}
-
 // dx: the splits' sum into the first of them, and its statistic (one split's is the
-// product's own). A workgroup a row at a time.
+// product's own). A workgroup a row at a time, or with few rows 1024 columns of it.
 __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
   const int count = (int)p.hdr[LOSS_COUNT];
   float a = 0.f;
   for (int64_t r = blockIdx.x; r < count; r += gridDim.x)
-    for (int c = 4 * (int)threadIdx.x; c < p.D; c += 1024) {
+    for (int c = 4 * (int)(blockIdx.y * 256 + threadIdx.x); c < p.D; c += 1024 * gridDim.y) {
       float* o = p.part + r * p.ldp + c;
       float4 v = *(const float4*)o;
 #pragma unroll 4
@@ -384,20 +359,6 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
   __syncthreads();
   a = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   if (threadIdx.x == 0 && a > 0.f) atomicMax(p.hdr + LOSS_AMAX_DX, __float_as_uint(a));
-}
-
-template <int F>
-__device__ __forceinline__ void store_codes(void* out, int64_t e, const uint32_t (&u)[16], int cols, int shift, bool sat) {
-  const bool fast = shift >= kFastShiftMinSub && shift <= kFastShiftMax;
-  uint32_t w[8];
-  encode16<F>(u, shift, fast ? pow2_float(shift) : 1.0f, fast, sat, w);
-  if (cols >= 16) {
-    store_words16<F>(out, e, w);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 15; ++i)
-      if (i < cols) store1<F>(out, e + i, word_code<F>(w, i));
-  }
 }
 
 // Rows of fp32 products cast to codes; dx: rows that do not count are 0.
@@ -457,6 +418,7 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
   int64_t most = (int64_t)1 << 20;
   if (back && R > 0) most = std::min(most, std::max<int64_t>(256, ((int64_t)1 << 28) / R / 256 * 256));
   if (z.copy_w) most = std::min(most, std::max<int64_t>(256, ((int64_t)1 << 28) / z.ldw16 / 256 * 256));
+  if (back && loss_few_bwd(R, V)) most = V;
   const int64_t pieces = (V + most - 1) / most;
   z.piece = (int)up((V + pieces - 1) / pieces, 256);
   z.ldz = pitch(z.piece);
@@ -472,6 +434,13 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
       if (t < best * 0.98) best = t, z.splits = s;
     }
   }
+  const bool few = back ? loss_few_bwd(R, V) : R <= kLossFewRows;
+  if (back && few) {
+    // a workgroup 128 columns of dx and a part of the vocabulary: 4 for each CU, 2 where the
+    // parts' sums are more bytes
+    const int64_t tiles = (D + 127) / 128, most = (V + 63) / 64, per_cu = R <= 32 ? 4 : 2;
+    z.splits = (int)std::min(std::min<int64_t>(256, most), std::max<int64_t>(1, per_cu * gemm4_grid(1 << 30) / tiles));
+  }
   size_t at = kHeaderBytes;
   auto take = [&](auto** to, size_t bytes) {
     if (p) *to = (std::remove_reference_t<decltype(**to)>*)((uint8_t*)base + at);
@@ -485,11 +454,11 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
   take(&q.pos, 4 * r);
   take(&q.factor, 4 * r);
   take(&q.label, 4 * r);
-  if (top) take(&q.top32, 4 * r * (size_t)z.topp);
+  if (top && (back || !few)) take(&q.top32, 4 * r * (size_t)z.topp);
   auto bytes_of = [](int64_t rows, int64_t ld, int64_t size) { return (size_t)rows * (size_t)ld * (size_t)size; };
   uint16_t *xc = nullptr, *xw = nullptr, *w16 = nullptr, *dz = nullptr;
-  take(&xc, bytes_of(R, z.ldxc, 2));
-  if (z.copy_w) take(&w16, bytes_of(std::min<int64_t>(z.piece, V), z.ldw16, 2));
+  if (back || !few) take(&xc, bytes_of(R, z.ldxc, 2));
+  if (z.copy_w && !few) take(&w16, bytes_of(std::min<int64_t>(z.piece, V), z.ldw16, 2));
   if (back) {
     take(&q.lse2, 4 * r);
     take(&q.coef, 4 * r);
@@ -506,12 +475,12 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
       if (p && !p->picked) p->picked = picked;
     }
     take(&q.picked2, 4 * r);
-    take(&q.stats, 8 * r * (size_t)(2 * ((V + 255) / 256)));
+    take(&q.stats, 8 * r * (size_t)(few ? (V + 63) / 64 : 2 * ((V + 255) / 256)));
   }
   if (p) {
     p->xc = xc;
     p->xw = back && p->row_scale ? xw : nullptr;
-    p->w16 = w16;
+    p->w16 = few ? nullptr : w16;
     p->dz = dz;
     p->topp = z.topp;
     p->ldxc = z.ldxc;
@@ -579,6 +548,10 @@ static hipError_t piece_logits(const LossParams& p, int v0, int n, int epi, Loss
 }
 
 hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s) {
+  if (p.R <= kLossFewRows) {
+    TRY(launch_loss_few(p, s));
+    return p.labels ? hipSuccess : launch_one(loss_top_kernel, groups_for(p.R, 4, 8192), 256, s, p);
+  }
   TRY(begin_loss(p, s));
   LossGemm g;
   for (int v0 = 0; v0 < p.V; v0 += p.piece)
@@ -590,7 +563,13 @@ hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s) {
 
 hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
   TRY(begin_loss(p, s));
-  for (int v0 = 0; v0 < p.V; v0 += p.piece) {
+  const bool few = loss_few_bwd(p.R, p.V);
+  if (few) {
+    TRY(launch_loss_few_dz(p, s));
+    if (!p.labels) TRY(launch_one(loss_fix_kernel, groups_for(p.R, 4, 8192), 256, s, p, 0, p.V));
+    TRY(launch_loss_few_grads(p, s));
+  }
+  for (int v0 = few ? p.V : 0; v0 < p.V; v0 += p.piece) {
     const int n = std::min(p.piece, p.V - v0);
     LossGemm g;
     TRY(piece_logits(p, v0, n, LOSS_DZ, &g, s));
@@ -640,7 +619,16 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
     }
   }
   if (p.dx) {
-    if (p.splits > 1) TRY(launch_one(loss_sum_kernel, groups_for(p.R, 2, 8192), 256, s, p));
+    if (p.splits > 1 || few) {
+      LossParams q = p;
+      void* a[] = {&q};
+      const dim3 grid((unsigned)groups_for(p.R, 1, 8192), p.R < 1024 ? (unsigned)groups_for(p.D, 1024, 64) : 1u);
+      const hipError_t e = hipLaunchKernel((const void*)loss_sum_kernel, grid, dim3(256), a, 0, s);
+      if (e != hipSuccess) {
+        (void)hipGetLastError();
+        return e;
+      }
+    }
     TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0));
   }
   if (p.dw && p.mode == 1)

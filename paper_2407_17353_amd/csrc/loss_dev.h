@@ -1,0 +1,105 @@
+// Device helpers of the losses' kernels.
+#pragma once
+#include "attention_dev.h"
+#include "loss.h"
+
+namespace scalify {
+
+// Factor of a row's logits in base 2; past [2^-100, 2^64] it gives equal logits, or the
+// largest alone.
+__device__ __forceinline__ float logit_factor(const LossParams& p, int64_t row) {
+  const int e = pow2_exponent(p.s_x) + pow2_exponent(p.s_w) + (p.row_scale ? pow2_exponent(p.row_scale + row) : 0);
+  const float f = ldexpf(kLog2e / p.temp, e < -200 ? -200 : (e > 200 ? 200 : e));
+  return fminf(fmaxf(f, 0x1p-100f), 0x1p64f);
+}
+
+// Four values times inv = 2^-shift, inside the conversions' window, to F16 (round to nearest
+// even; the product is exact unless F16 overflows or is 0), two a word. NAN: some may be.
+template <bool NAN_>
+__device__ __forceinline__ u2 codes4_f16(const float* y, float inv, bool sat) {
+  u2 w;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float a = y[2 * i] * inv, b = y[2 * i + 1] * inv;
+    if (sat) {
+      a = __builtin_amdgcn_fmed3f(a, -65504.0f, 65504.0f);
+      b = __builtin_amdgcn_fmed3f(b, -65504.0f, 65504.0f);
+    }
+    asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(w[i]) : "v"(a), "v"(b));
+    if constexpr (NAN_) {
+      uint32_t lo = w[i] & 0xFFFFu, hi = w[i] >> 16;
+      if (y[2 * i] != y[2 * i]) lo = FmtTraits<kF16>::NANC | ((__float_as_uint(y[2 * i]) >> 16) & 0x8000u);
+      if (y[2 * i + 1] != y[2 * i + 1]) hi = FmtTraits<kF16>::NANC | ((__float_as_uint(y[2 * i + 1]) >> 16) & 0x8000u);
+      w[i] = lo | (hi << 16);
+    }
+  }
+  return w;
+}
+// The same to an 8-bit format, scale = 2^shift.
+template <int F, bool NAN_>
+__device__ __forceinline__ uint32_t codes4_fp8(const float* y, float scale, bool sat) {
+  uint32_t w = cast4_fp8_hw<F>(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]), scale, sat);
+  if constexpr (NAN_) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (y[i] != y[i]) {
+        const uint32_t c = FmtTraits<F>::NANC | ((__float_as_uint(y[i]) >> 24) & 0x80u);
+        w = (w & ~(0xFFu << (8 * i))) | (c << (8 * i));
+      }
+  }
+  return w;
+}
+// Two values as sticky16, a word.
+__device__ __forceinline__ uint32_t sticky2(float a, float b) {
+  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+  // (bit 16 is set if a lower one is)
+  return __builtin_amdgcn_perm(y | ((y & 0xFFFFu) + 0xFFFFu), x | ((x & 0xFFFFu) + 0xFFFFu), 0x07060302u);
+}
+
+// (m, n) and (mo, no), maxima (base 2; -Inf where there is nothing) and sums, as one. A NaN
+// is in the sums.
+__device__ __forceinline__ void join_sums(float& m, float& n, float mo, float no) {
+  const float t = fmaxf(m, mo);
+  const float a = m == -__builtin_inff() ? 0.f : n * exp2f(m - t);
+  const float c = mo == -__builtin_inff() ? 0.f : no * exp2f(mo - t);
+  n = a + c;
+  m = t;
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+
+__device__ __forceinline__ int hdr_exponent(const uint32_t* hdr, int word) {
+  return hdr[word] == 0u ? 0 : floor_log2_bits(hdr[word]);
+}
+
+// Unit of the products: a gradient's data in its propagated scale is the product times
+// 2^unit.
+__device__ __forceinline__ int unit_of(const LossParams& p, bool dw) {
+  const int u = hdr_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2;
+  return dw && p.row_scale ? u + hdr_exponent(p.hdr, LOSS_RMAX) : u;
+}
+__device__ __forceinline__ int base_of(const LossParams& p, bool dw) { return pow2_exponent(p.s_dloss) + pow2_exponent(dw ? p.s_x : p.s_w); }
+__device__ __forceinline__ int out_exponent(const LossParams& p, bool dw, int base, int unit) {
+  const uint32_t a = p.hdr[dw ? LOSS_AMAX_DW : LOSS_AMAX_DX];
+  const bool plain = p.mode != 1 || a == 0u || a >= 0x7F800000u;
+  return clamp_e8m0(base + (plain ? 0 : floor_log2_bits(a) + unit - p.target));
+}
+
+template <int F>
+__device__ __forceinline__ void store_codes(void* out, int64_t e, const uint32_t (&u)[16], int cols, int shift, bool sat) {
+  const bool fast = shift >= kFastShiftMinSub && shift <= kFastShiftMax;
+  uint32_t w[8];
+  encode16<F>(u, shift, fast ? pow2_float(shift) : 1.0f, fast, sat, w);
+  if (cols >= 16) {
+    store_words16<F>(out, e, w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 15; ++i)
+      if (i < cols) store1<F>(out, e + i, word_code<F>(w, i));
+  }
+}
+
+}  // namespace scalify

@@ -78,10 +78,7 @@ __device__ __forceinline__ int loss_exponent(const uint32_t* hdr, int word) {
 // else each stay in a register over the whole loop).
 __device__ __forceinline__ void held(uint32_t& x) { asm volatile("" : "+v"(x)); }
 
-// OF (LOSS_DW): what is stored: codes of a format, fp32, or the 16-bit form of fp32 that
-// keeps an 8-bit rounding (sticky16).
-enum LossForm : int { FORM_F32 = 8, FORM_STICKY = 9 };
-
+// OF: what LOSS_DW stores, a format's codes or a LossForm.
 template <bool A_MC, bool B_MC, int EPI, int OF>
 __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   using C = WaveCfg<4>;
@@ -384,14 +381,14 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
         float top = x[0];
 #pragma unroll
         for (int i = 1; i < 4 * NI; ++i) top = fmaxf(top, x[i]);
-        // (a factor is positive; a row of -Inf alone has the sum 0, one of NaN alone NaN)
+        // (a factor is positive; values of -Inf alone have the sum 0, and a NaN is in the sum)
         top = row4_max(top);
         const float m2 = top == -__builtin_inff() || top != top ? 0.f : top * f;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 4 * NI; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -m2));
         sum = row4_sum(sum);
-        if (lq == 0 && in) p.stats[(int64_t)((p.v0 + n0 + wn) / WTN) * p.R + m] = float2{top == -__builtin_inff() ? top : m2, sum};
+        if (lq == 0 && in) p.stats[(int64_t)((p.v0 + n0 + wn) / WTN) * p.R + m] = float2{sum == 0.f ? -__builtin_inff() : m2, sum};
         if constexpr (EPI == LOSS_STATS) {
           const int d = in ? r_i[mi] - (p.v0 + nb) : -1;
           // (the lane that has the label's column: d = 16 ni + i)

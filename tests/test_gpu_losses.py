@@ -88,7 +88,7 @@ class Case:
 
 
 SIZES = [(1, 1, 1), (1, 2, 8), (3, 130, 7), (2, 1000, 64), (17, 255, 65), (64, 256, 128), (65, 257, 100), (255, 513, 72),
-         (256, 384, 192), (257, 129, 1000), (600, 2000, 40), (40, 5003, 321)]
+         (256, 384, 192), (32, 700, 136), (33, 65, 1000), (100, 1003, 264), (128, 640, 1500), (129, 320, 72), (257, 129, 1000), (600, 2000, 40), (40, 5003, 321)]
 
 
 @pytest.mark.parametrize("R,V,D", SIZES)
@@ -147,17 +147,18 @@ def test_rows_that_do_not_count_hold_anything(top, bad):
     assert torch.equal(c.lse, lse0) and torch.equal(c.loss, loss0)
 
 
+@pytest.mark.parametrize("R,V", [(40, 300), (20, 30), (100, 100), (300, 700)])
 @pytest.mark.parametrize("top", [0, 4])
-def test_counted_nan(top):
+def test_counted_nan(top, R, V):
     """A NaN in a row that counts makes that row's results NaN, and no other's."""
-    c = Case(40, 300, 64, top=top, skip=0)
+    c = Case(R, V, 64, top=top, skip=0)
     c.forward()
     loss = c.loss.clone()
     i = 8
     c.x.data.view(torch.float16)[i, 5] = float("nan")
     c.forward()
     torch.cuda.synchronize()
-    others = torch.arange(40, device=DEV) != i
+    others = torch.arange(R, device=DEV) != i
     assert torch.isnan(c.loss[i]) and torch.isnan(c.lse[i]) and torch.equal(c.loss[others], loss[others])
 
 
@@ -217,10 +218,11 @@ def test_pieces_of_the_vocabulary(top):
     Case(2100, 131101, 24, E4M3, E4M3, False, top, seed=3).check(mode=sc.RESCALE_AMAX)
 
 
-def test_pieces_of_the_output_matrix():
-    """An 8-bit output matrix larger than its decoded piece."""
-    say("loss pieces of w")
-    Case(5, 40001, 7200, F16, E4M3, seed=4).check()
+@pytest.mark.parametrize("R", [5, 70])
+def test_pieces_of_the_output_matrix(R):
+    """An 8-bit output matrix larger than its decoded piece (few rows: read as it is)."""
+    say(f"loss pieces of w {R}")
+    Case(R, 40001, 7200, F16, E4M3, seed=4).check()
 
 
 @pytest.mark.parametrize("top", [0, 30])
