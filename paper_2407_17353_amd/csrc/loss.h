@@ -52,8 +52,8 @@ struct LossParams {
   float *factor;       // [R] logits in base 2 are factor * (x . w)
   float *lse2, *coef;  // [R] log-sum-exp in base 2; upstream gradient over 2^E, times 2^14
   float* picked2;      // [R] label's logit in base 2
-  int* top32;          // [R][topp] teacher's tokens, -1 where absent
-  int topp;
+  int *bins, *entries;  // forward: the teacher's entries of 16 places by groups of 128 tokens of a piece
+  int bin_columns;      // groups
   void *xc, *xw;       // F16 rows of x; times their row scale over the largest
   int64_t ldxc;
   void* w16;           // F16 rows of a piece of w (8 bits, or columns no multiple of 8)
@@ -70,7 +70,7 @@ struct LossParams {
 
 // Sizes that the host decides: pieces of w, splits of dx, and the bytes of a workspace.
 struct LossPlan {
-  int piece, splits, topp;
+  int piece, splits;
   bool copy_w;
   int64_t ldxc, ldw16, ldz, ldp;
   size_t bytes;
@@ -97,6 +97,12 @@ hipError_t launch_one(void (*kernel)(Args...), int64_t groups, int threads, hipS
   return e;
 }
 
+// An entry of the teacher among 16 rows and 128 columns.
+__device__ __forceinline__ int bin_pack(int row, int column, int entry) { return column | (row << 7) | (entry << 11); }
+__device__ __forceinline__ int bin_column(int e) { return e & 127; }
+__device__ __forceinline__ int bin_row(int e) { return (e >> 7) & 15; }
+__device__ __forceinline__ int bin_entry(int e) { return e >> 11; }
+
 // ---- one F16 product C[M][N] = sum_k A B of the losses (loss_gemm.h)
 
 enum LossEpi : int {
@@ -119,8 +125,8 @@ struct LossGemm {
   const float *factor, *lse2, *coef;
   const int* label;
   float* picked2;
-  const int* top32;
-  int topp, top;
+  const int *bins, *entries;
+  int bin_columns, top;
   const int* rows;
   float* picked;
   float2* stats;

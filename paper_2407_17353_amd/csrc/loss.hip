@@ -183,11 +183,6 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(LossParams p) {
         p.coef[i] = ldexpf(p.dloss ? p.dloss[row] * p.temp : p.temp, kLossGradLog2 - ec);
       }
     }
-    if (p.top32)
-      for (int j = threadIdx.x; j < p.topp; j += 256) {
-        const int64_t t = j < p.top ? p.index[row * p.top + j] : -1;
-        p.top32[i * p.topp + j] = t >= 0 && t < p.V ? (int)t : -1;
-      }
     const float rf = p.xw ? ldexpf(r, -er) : 1.0f;
     for (int c = threadIdx.x; c < chunks; c += 256) {
       const u4 v = load_tail8(p.x_fmt, p.x, row * p.ldx + 8 * c, p.D - 8 * c);
@@ -229,6 +224,56 @@ __global__ __launch_bounds__(256) void loss_copy_w_kernel(LossParams p, int v0, 
     }
     *(u4*)o = lo;
     if (c + 8 < cols) *(u4*)(o + 8) = hi;
+  }
+}
+
+// Distillation's forward: the entries of the teacher whose tokens lie in the piece of n rows
+// of w from v0 on, of 16 places (a workgroup), by groups of 128 tokens: the product's
+// epilogue has such rows and columns at hand. (Which of a group's entries comes first
+// changes nothing.) A piece has at most 2^20 tokens.
+constexpr int kMaxBins = (1 << 20) / 128;
+__global__ __launch_bounds__(256) void loss_bin_kernel(LossParams p, int v0, int n) {
+  __shared__ int at[kMaxBins];
+  __shared__ int sums[4];
+  const int count = (int)p.hdr[LOSS_COUNT], bins = p.bin_columns, tid = threadIdx.x;
+  const int per = (bins + 255) / 256, lo = min(tid * per, bins), hi = min(lo + per, bins);
+  for (int64_t g = blockIdx.x; 16 * g < count; g += gridDim.x) {
+    for (int i = tid; i < bins; i += 256) at[i] = 0;
+    __syncthreads();
+    const int all = (int)min((int64_t)16, count - 16 * g) * p.top;
+    auto token = [&](int e) {
+      const int64_t t = p.index[(int64_t)p.rows[16 * g + e / p.top] * p.top + e % p.top] - v0;
+      return t >= 0 && t < n ? (int)t : -1;
+    };
+    for (int e = tid; e < all; e += 256) {
+      const int t = token(e);
+      if (t >= 0) atomicAdd(at + t / 128, 1);
+    }
+    __syncthreads();
+    int mine = 0;
+    for (int i = lo; i < hi; ++i) mine += at[i];
+    int before = mine;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(before, o, 64);
+      if ((tid & 63) >= o) before += v;
+    }
+    if ((tid & 63) == 63) sums[tid >> 6] = before;
+    __syncthreads();
+    before -= mine;
+    for (int w = 0; w < tid >> 6; ++w) before += sums[w];
+    int* const bin = p.bins + g * (bins + 1);
+    for (int i = lo; i < hi; ++i) {
+      const int k = at[i];
+      at[i] = bin[i] = before;
+      before += k;
+    }
+    if (tid == 255) bin[bins] = before;
+    __syncthreads();
+    for (int e = tid; e < all; e += 256) {
+      const int t = token(e);
+      if (t >= 0) p.entries[g * 16 * p.top + atomicAdd(at + t / 128, 1)] = bin_pack(e / p.top, t % 128, e % p.top);
+    }
+    __syncthreads();
   }
 }
 
@@ -409,7 +454,6 @@ static int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool back, bool amax, LossParams* p, void* base) {
   LossPlan z = {};
   z.copy_w = w_fmt != kF16 || D % 8 != 0;
-  z.topp = (int)up(top, 16);
   // (a pitch of an odd number of 128 bytes: rows of a power of two would share memory channels)
   auto pitch = [](int64_t cols) { return up(cols, 64) + (up(cols, 64) / 64 % 2 == 0 ? 64 : 0); };
   z.ldxc = z.ldw16 = pitch(D);
@@ -454,7 +498,6 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
   take(&q.pos, 4 * r);
   take(&q.factor, 4 * r);
   take(&q.label, 4 * r);
-  if (top && (back || !few)) take(&q.top32, 4 * r * (size_t)z.topp);
   auto bytes_of = [](int64_t rows, int64_t ld, int64_t size) { return (size_t)rows * (size_t)ld * (size_t)size; };
   uint16_t *xc = nullptr, *xw = nullptr, *w16 = nullptr, *dz = nullptr;
   if (back || !few) take(&xc, bytes_of(R, z.ldxc, 2));
@@ -474,6 +517,12 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
       if (p && !p->lse) p->lse = lse;
       if (p && !p->picked) p->picked = picked;
     }
+    if (top && !few) {
+      const size_t groups = (size_t)((R + 15) / 16);
+      q.bin_columns = (int)((std::min<int64_t>(z.piece, V) + 127) / 128);
+      take(&q.bins, 4 * groups * (size_t)(q.bin_columns + 1));
+      take(&q.entries, 64 * groups * (size_t)top);
+    }
     take(&q.picked2, 4 * r);
     take(&q.stats, 8 * r * (size_t)(few ? (V + 63) / 64 : 2 * ((V + 255) / 256)));
   }
@@ -482,7 +531,6 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
     p->xw = back && p->row_scale ? xw : nullptr;
     p->w16 = few ? nullptr : w16;
     p->dz = dz;
-    p->topp = z.topp;
     p->ldxc = z.ldxc;
     p->ldw16 = z.ldw16;
     p->ldz = z.ldz;
@@ -534,8 +582,9 @@ static hipError_t piece_logits(const LossParams& p, int v0, int n, int epi, Loss
   g->coef = p.coef;
   g->label = p.labels ? p.label : nullptr;
   g->picked2 = p.picked2;
-  g->top32 = p.top32;
-  g->topp = p.topp;
+  g->bins = p.bins;
+  g->entries = p.entries;
+  g->bin_columns = p.bin_columns;
   g->top = p.top;
   g->rows = p.rows;
   g->picked = p.picked;
@@ -554,8 +603,11 @@ hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s) {
   }
   TRY(begin_loss(p, s));
   LossGemm g;
-  for (int v0 = 0; v0 < p.V; v0 += p.piece)
-    TRY(piece_logits(p, v0, std::min(p.piece, p.V - v0), p.labels ? LOSS_STATS : LOSS_PICK, &g, s));
+  for (int v0 = 0; v0 < p.V; v0 += p.piece) {
+    const int n = std::min(p.piece, p.V - v0);
+    if (!p.labels) TRY(launch_one(loss_bin_kernel, groups_for(p.R, 16, 16384), 256, s, p, v0, n));
+    TRY(piece_logits(p, v0, n, p.labels ? LOSS_STATS : LOSS_PICK, &g, s));
+  }
   TRY(launch_one(loss_join_kernel, groups_for(p.R, 64, 16384), 1024, s, p, 2 * ((p.V + 255) / 256)));
   if (!p.labels) TRY(launch_one(loss_top_kernel, groups_for(p.R, 4, 8192), 256, s, p));
   return hipSuccess;

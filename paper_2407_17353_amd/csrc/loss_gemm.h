@@ -286,6 +286,16 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   // A tile's numbers of a lane's rows, loaded while its last steps run.
   float r_f[MI], r_l[MI], r_c[MI];
   int r_i[MI];  // label; LOSS_PICK: row
+  int r_e[MI], bin_lo = 0, bin_hi = 0;  // LOSS_PICK: a lane's entry; lane mi: the rows' first entry and the end
+  auto load_bins = [&](int m0, int n0) {
+    if constexpr (EPI == LOSS_PICK) {
+      const int group = (m0 + wm) / 16 + (lane & (MI - 1));
+      const int* o = p.bins + (int64_t)group * (p.bin_columns + 1) + (n0 + wn) / WTN;
+      const bool there = 16 * group < M && n0 + wn < N;
+      bin_lo = there ? o[0] : 0;
+      bin_hi = there ? o[1] : 0;
+    }
+  };
   auto load_rows = [&](int m0) {
     if constexpr (EPI == LOSS_STATS || EPI == LOSS_PICK || EPI == LOSS_DZ) {
 #pragma unroll
@@ -293,9 +303,11 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
         const int m = min(m0 + wm + 16 * mi + lr, M - 1);
         r_f[mi] = p.factor[m];
         if constexpr (EPI == LOSS_DZ) r_l[mi] = p.lse2[m], r_c[mi] = p.coef[m];
-        if constexpr (EPI == LOSS_PICK)
+        if constexpr (EPI == LOSS_PICK) {
           r_i[mi] = p.rows[m];
-        else
+          const int at = __builtin_amdgcn_readlane(bin_lo, mi) + lane;
+          r_e[mi] = at < __builtin_amdgcn_readlane(bin_hi, mi) ? p.entries[(int64_t)((m0 + wm) / 16 + mi) * 16 * p.top + at] : 0;
+        } else
           r_i[mi] = p.label ? p.label[m] : -1;
       }
     }
@@ -401,26 +413,27 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
             if (mine) p.picked2[m] = z * f;
           }
         } else {
-          // the row's logits through LDS: the lanes of a row go through its tokens
-          static_for<0, NI>([&](auto Q) {
-            constexpr int ni = decltype(Q)::value;
-            *(v4f*)(st + lr * 512 + (((4 * ni + lq) ^ lr) * 16)) = v4f{x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
-          });
-          wait_lgkmcnt<0>();
-          if (in) {
-            const int64_t to = (int64_t)r_i[mi] * p.top;
+          // the teacher's tokens of these rows and columns (loss_bin_kernel), if any: the rows'
+          // logits through LDS, a lane an entry
+          const int lo = __builtin_amdgcn_readlane(bin_lo, mi), hi = __builtin_amdgcn_readlane(bin_hi, mi);
+          if (hi > lo) {
+            static_for<0, NI>([&](auto Q) {
+              constexpr int ni = decltype(Q)::value;
+              *(v4f*)(st + lr * 512 + (((4 * ni + lq) ^ lr) * 16)) = v4f{x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
+            });
+            wait_lgkmcnt<0>();
             const float fn = f * 0.69314718055994530942f;
-            for (int j = 4 * lq; j < p.topp; j += 16) {
-              const v4i t = *(const v4i*)(p.top32 + (int64_t)m * p.topp + j);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int d = t[i] - (p.v0 + n0 + wn);
-                if (t[i] >= 0 && d >= 0 && d < WTN)
-                  p.picked[to + j + i] = fn * *(const float*)(st + lr * 512 + (((d >> 2) ^ lr) * 16) + 4 * (d & 3));
-              }
+            for (int j = lo; j < hi; j += 64) {
+              int e = r_e[mi];
+              if (j > lo && j + lane < hi) e = p.entries[(int64_t)((m0 + wm) / 16 + mi) * 16 * p.top + j + lane];
+              const int row = bin_row(e), d = bin_column(e);
+              const float fe = __shfl(fn, row, 64);
+              const int to = __shfl(r_i[mi], row, 64);
+              if (j + lane < hi)
+                p.picked[(int64_t)to * p.top + bin_entry(e)] = fe * *(const float*)(st + row * 512 + (((d >> 2) ^ row) * 16) + 4 * (d & 3));
             }
+            wait_lgkmcnt<0>();
           }
-          wait_lgkmcnt<0>();
         }
       } else if constexpr (EPI == LOSS_DZ) {
         const float f = r_f[mi], l = r_l[mi], c = r_c[mi];
@@ -561,6 +574,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   using P1 = std::integral_constant<int, 1>;
   int c_r = 0, c_m0, c_n0, c_split;
   origin(0, c_m0, c_n0, c_split);
+  load_bins(c_m0, c_n0);
   head(P0{});
   for (int kt = 0;;) {
     kt += 2;
@@ -574,6 +588,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       store_tile(c_m0, c_n0, c_split);
       if (++c_r == ntiles) break;
       origin(c_r, c_m0, c_n0, c_split);
+      load_bins(c_m0, c_n0);
       mfma_drain();  // the zeroing writes before the next products read them
     }
     head(P0{});
