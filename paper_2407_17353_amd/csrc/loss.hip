@@ -110,22 +110,34 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
   __shared__ float cs[16], rs[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t per = (p.R + 1023) / 1024 * 64, lo = wave * per, hi = lo + per < p.R ? lo + per : p.R;
-  auto counts = [&](int64_t i) {
-    if (i >= hi) return false;
-    const bool has = p.labels ? p.labels[i] >= 0 && p.labels[i] < p.V : p.pos[i] >= 0;
-    return has && !(p.dloss && p.dloss[i] == 0.0f);
-  };
+  // (rows' numbers are loaded whether or not they count, four groups at a time)
   int n = 0;
   float c = 0.f, r = 0.f;
-#pragma unroll 4
-  for (int64_t at = lo; at < hi; at += 64) {
-    const int64_t i = at + lane;
-    const bool on = counts(i);
-    n += (int)__popcll(__ballot(on));
-    if (on) {
-      const float g = fabsf(p.dloss ? p.dloss[i] * p.temp : p.temp);
-      if (g < __builtin_inff()) c = fmaxf(c, g);
-      if (p.row_scale) r = fmaxf(r, p.row_scale[i]);
+  for (int64_t at = lo; at < hi; at += 256) {
+    bool on[4];
+    float g[4], rs_[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t i = at + 64 * j + lane;
+      const bool in = i < hi;
+      const int64_t label = p.labels && in ? p.labels[i] : -1;
+      const int flag = !p.labels && in ? p.pos[i] : -1;
+      g[j] = p.dloss && in ? p.dloss[i] : 1.0f;
+      rs_[j] = p.row_scale && in ? p.row_scale[i] : 0.0f;
+      on[j] = (p.labels ? label >= 0 && label < p.V : flag >= 0) && g[j] != 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t mask = __ballot(on[j]);
+      n += (int)__popcll(mask);
+      // what a row is, for the second pass: 0 counts
+      const int64_t i = at + 64 * j + lane;
+      if (i < hi) p.pos[i] = on[j] ? 0 : -1;
+      if (on[j]) {
+        const float a = fabsf(g[j] * p.temp);
+        if (a < __builtin_inff()) c = fmaxf(c, a);
+        r = fmaxf(r, rs_[j]);
+      }
     }
   }
   c = wave_max(c), r = wave_max(r);
@@ -136,15 +148,24 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
     if (w < wave) place += sums[w];
     all += sums[w];
   }
-#pragma unroll 4
-  for (int64_t at = lo; at < hi; at += 64) {
-    const int64_t i = at + lane;
-    const bool on = counts(i);
-    const uint64_t mask = __ballot(on);
-    const int to = place + (int)__popcll(mask & (((uint64_t)1 << lane) - 1));
-    if (i < hi) p.pos[i] = on ? to : -1;
-    if (on) p.rows[to] = (int)i;
-    place += (int)__popcll(mask);
+  for (int64_t at = lo; at < hi; at += 256) {
+    int flag[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t i = at + 64 * j + lane;
+      flag[j] = i < hi ? p.pos[i] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t i = at + 64 * j + lane;
+      const uint64_t mask = __ballot(flag[j] >= 0);
+      const int to = place + (int)__popcll(mask & (((uint64_t)1 << lane) - 1));
+      if (flag[j] >= 0) {
+        p.pos[i] = to;
+        p.rows[to] = (int)i;
+      }
+      place += (int)__popcll(mask);
+    }
   }
   if (tid == 0) {
     for (int w = 1; w < 16; ++w) c = fmaxf(c, cs[w]), r = fmaxf(r, rs[w]);
@@ -406,9 +427,19 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
   if (threadIdx.x == 0 && a > 0.f) atomicMax(p.hdr + LOSS_AMAX_DX, __float_as_uint(a));
 }
 
-// Rows of fp32 products cast to codes; dx: rows that do not count are 0.
-__global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw) {
+// The gradients' scales and statistics.
+__device__ __forceinline__ void write_scale(const LossParams& p, bool dw) {
+  if (!(dw ? p.dw : p.dx)) return;
+  const int unit = unit_of(p, dw), base = base_of(p, dw);
+  *(dw ? p.dw_scale : p.dx_scale) = pow2_float(out_exponent(p, dw, base, unit));
+  if (p.amax_out) p.amax_out[dw ? 1 : 0] = ldexpf(__uint_as_float(p.hdr[dw ? LOSS_AMAX_DW : LOSS_AMAX_DX]), unit);
+}
+__global__ void loss_scales_kernel(LossParams p) { write_scale(p, threadIdx.x == 1); }
+
+// Rows of fp32 products cast to codes (the first cast of a call writes the scales too); dx: rows that do not count are 0.
+__global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw, int scales) {
   const bool dw = is_dw != 0;
+  if (scales && blockIdx.x == 0 && threadIdx.x < 2) write_scale(p, threadIdx.x == 1);
   const int unit = unit_of(p, dw), base = base_of(p, dw), e_out = out_exponent(p, dw, base, unit);
   const int shift = e_out - base - unit, chunks = (p.D + 15) / 16;
   const int64_t all = (int64_t)(dw ? p.V : p.R) * chunks;
@@ -436,15 +467,6 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw)
     else if (fmt == kE4M3) store_codes<kE4M3>(out, e, u, cols, shift, p.sat);
     else store_codes<kE5M2>(out, e, u, cols, shift, p.sat);
   }
-}
-
-// The gradients' scales and statistics (threads 0 and 1: dx, dw).
-__global__ void loss_scales_kernel(LossParams p) {
-  const bool dw = threadIdx.x == 1;
-  if (!(dw ? p.dw : p.dx)) return;
-  const int unit = unit_of(p, dw), base = base_of(p, dw);
-  *(dw ? p.dw_scale : p.dx_scale) = pow2_float(out_exponent(p, dw, base, unit));
-  if (p.amax_out) p.amax_out[dw ? 1 : 0] = ldexpf(__uint_as_float(p.hdr[dw ? LOSS_AMAX_DW : LOSS_AMAX_DX]), unit);
 }
 
 // ---- host
@@ -681,11 +703,11 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
         return e;
       }
     }
-    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0));
+    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0, 1));
   }
   if (p.dw && p.mode == 1)
-    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1));
-  return launch_one(loss_scales_kernel, 1, 2, s, p);
+    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1, p.dx ? 0 : 1));
+  return p.dx || p.mode == 1 ? hipSuccess : launch_one(loss_scales_kernel, 1, 2, s, p);
 }
 
 }  // namespace scalify

@@ -183,16 +183,21 @@ def test_no_rows():
     assert (dw.data == 0).all() and lr.log2_of(dw) == c.ex
 
 
+@pytest.mark.parametrize("R", [20, 130])
 @pytest.mark.parametrize("top", [0, 7])
-def test_either_gradient_alone(top):
-    c = Case(130, 500, 96, E4M3, E4M3, True, top)
+def test_either_gradient_alone(top, R):
+    c = Case(R, 500, 96, E4M3, E4M3, True, top)
     dx, dw = c.check(mode=sc.RESCALE_AMAX)
-    a, b = lr.empty(130, 96, F16), lr.empty(500, 96, F16)
+    a, b = lr.empty(R, 96, F16), lr.empty(500, 96, F16)
     c.backward(a, None)
     c.backward(None, b)
     torch.cuda.synchronize()
     for x, y in ((a, dx), (b, dw)):
         assert torch.equal(x.data, y.data) and torch.equal(x.scale, y.scale)
+    dx, dw = c.check(mode=sc.RESCALE_NONE)
+    c.backward(None, b, rescale=sc.RESCALE_NONE)
+    torch.cuda.synchronize()
+    assert torch.equal(b.data, dw.data) and torch.equal(b.scale, dw.scale)
 
 
 def test_column_ranges():
@@ -218,11 +223,12 @@ def test_pieces_of_the_vocabulary(top):
     Case(2100, 131101, 24, E4M3, E4M3, False, top, seed=3).check(mode=sc.RESCALE_AMAX)
 
 
-@pytest.mark.parametrize("R", [5, 70])
-def test_pieces_of_the_output_matrix(R):
+@pytest.mark.parametrize("top", [0, 6])
+@pytest.mark.parametrize("R", [5, 140])
+def test_pieces_of_the_output_matrix(R, top):
     """An 8-bit output matrix larger than its decoded piece (few rows: read as it is)."""
-    say(f"loss pieces of w {R}")
-    Case(R, 40001, 7200, F16, E4M3, seed=4).check()
+    say(f"loss pieces of w {R} {top}")
+    Case(R, 40001, 7200, F16, E4M3, top=top, seed=4).check()
 
 
 @pytest.mark.parametrize("top", [0, 30])
