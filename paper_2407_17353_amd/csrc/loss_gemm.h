@@ -120,6 +120,14 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
     if (q < 2) kc[q] = 8 * c;
   }
 
+  // The call's operands, read anew by the scalar unit where a tile needs them: held over the
+  // loop they would not fit the scalar registers.
+  typedef const __attribute__((address_space(4))) LossGemm* Args;
+  auto fresh_args = [&]() {
+    Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(a));
+    return a;
+  };
   // Tile r of this workgroup: split and origin.
   auto origin = [&](int r, int& m0, int& n0, int& split) {
     const int t = (int)blockIdx.x + r * G;
@@ -143,6 +151,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
     return make_rsrc(base, n > 0 ? (uint32_t)(n - 1) * ld + width : 0u);
   };
   auto load_tile = [&]() {
+    const auto& p = *fresh_args();
     int m0, n0, split;
     origin(l_r, m0, n0, split);
     l_k = split * k_span;
@@ -289,6 +298,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   int r_e[MI], bin_lo = 0, bin_hi = 0;  // LOSS_PICK: a lane's entry; lane mi: the rows' first entry and the end
   auto load_bins = [&](int m0, int n0) {
     if constexpr (EPI == LOSS_PICK) {
+      const auto& p = *fresh_args();
       const int group = (m0 + wm) / 16 + (lane & (MI - 1));
       const int* o = p.bins + (int64_t)group * (p.bin_columns + 1) + (n0 + wn) / WTN;
       const bool there = 16 * group < M && n0 + wn < N;
@@ -298,6 +308,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   };
   auto load_rows = [&](int m0) {
     if constexpr (EPI == LOSS_STATS || EPI == LOSS_PICK || EPI == LOSS_DZ) {
+      const auto& p = *fresh_args();
 #pragma unroll
       for (int mi = 0; mi < MI; ++mi) {
         const int m = min(m0 + wm + 16 * mi + lr, M - 1);
@@ -368,11 +379,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   };
   auto store_tile = [&](int m0, int n0, int split) {
     stored = m0 + wm + WTM <= M && n0 + wn + WTN <= N;
-    // (the call's other operands are read here, by the scalar unit, not held over the loop)
-    typedef const __attribute__((address_space(4))) LossGemm* Args;
-    Args args = (Args)__builtin_amdgcn_kernarg_segment_ptr();
-    asm volatile("" : "+s"(args));
-    const auto& p = *args;
+    const auto& p = *fresh_args();
     uint32_t first_n = (uint32_t)(n0 + wn + 4 * lq);
     const bool all_n = n0 + wn + WTN <= N;
     static_for<0, MI>([&](auto J) {
