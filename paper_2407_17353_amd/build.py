@@ -20,7 +20,9 @@ residual codes and channel exponents at once and keeps some of them there.
 The loads of these kernels are inline asm too, so the compiler does not keep
 the distance their scalar operands need: the build fails if a vector memory
 instruction reads a scalar register that a vector instruction wrote less than
-five wait states before.
+five wait states before. The products of the losses' kernels read registers that
+vector instructions write (decoded codes): the build fails if one does less than
+two wait states later.
 """
 from __future__ import annotations
 
@@ -105,6 +107,37 @@ def scalar_distance_violations(insns) -> list:
     return bad
 
 
+def _vgprs(text: str) -> set:
+    """The vector registers a piece of an instruction names."""
+    regs = set()
+    for m in re.finditer(r"\bv(\d+)\b|\bv\[(\d+):(\d+)\]", text):
+        lo, hi = (m.group(1),) * 2 if m.group(1) else (m.group(2), m.group(3))
+        regs.update(range(int(lo), int(hi) + 1))
+    return regs
+
+
+def product_distance_violations(insns) -> list:
+    """Matrix products that read a vector register less than two wait states after a
+    vector instruction wrote it (straight-line scan): the compiler keeps that distance for
+    products that it knows, not for those of inline asm."""
+    bad, recent = [], []
+    for insn in insns:
+        if not insn:
+            continue
+        op = insn.split()[0]
+        if op.startswith("v_mfma") and "," in insn:
+            used = _vgprs(insn.split(",", 1)[1])
+            if any(age < 2 and used & regs for age, regs in recent):
+                bad.append(insn)
+        step = int(insn.split()[1]) + 1 if op == "s_nop" else 1
+        recent = [(age + step, regs) for age, regs in recent if age + step < 2]
+        if op.startswith("v_") and not op.startswith(("v_mfma", "v_cmp")) and " " in insn:
+            regs = _vgprs(insn.split(None, 1)[1].split(",")[0])
+            if regs:
+                recent.append((0, regs))
+    return bad
+
+
 def _agprs(insn: str) -> set:
     """The AGPR numbers an instruction names."""
     regs = set()
@@ -180,6 +213,9 @@ def check_functions(obj: str, kernels: dict) -> int:
             continue
         if not pinned_kernel(obj, name):
             continue
+        near = product_distance_violations(insns) if base.startswith("loss_") else []
+        if near:
+            raise RuntimeError(f"{obj}: {name} multiplies a register too soon: {near[:4]}")
         checked += 1
         held = set()
         for insn in insns:

@@ -116,6 +116,7 @@ enum LossEpi : int {
 struct LossGemm {
   const void *a, *b;
   int64_t lda, ldb;       // bytes
+  int b_fmt;              // of logits: F16, or 8 bits
   int M, N, K;
   int count_is;           // the dimension that is the number of rows that count: 0 M, 1 K
   const uint32_t* hdr;

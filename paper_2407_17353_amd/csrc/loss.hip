@@ -475,7 +475,9 @@ static int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool back, bool amax, LossParams* p, void* base) {
   LossPlan z = {};
-  z.copy_w = w_fmt != kF16 || D % 8 != 0;
+  // w is copied as F16 where its product cannot read it: rows of F16 that end inside 16 bytes, and
+  // 8 bits where they end inside 16 or dx's product, along the vocabulary, follows
+  z.copy_w = w_fmt == kF16 ? D % 8 != 0 : back || D % 16 != 0;
   // (a pitch of an odd number of 128 bytes: rows of a power of two would share memory channels)
   auto pitch = [](int64_t cols) { return up(cols, 64) + (up(cols, 64) / 64 % 2 == 0 ? 64 : 0); };
   z.ldxc = z.ldw16 = pitch(D);
@@ -591,8 +593,10 @@ static hipError_t piece_logits(const LossParams& p, int v0, int n, int epi, Loss
   if (p.w16) TRY(launch_one(loss_copy_w_kernel, groups_for((int64_t)n * ((p.D + 15) / 16), 1024, 16384), 256, s, p, v0, n));
   g->a = p.xc;
   g->lda = 2 * p.ldxc;
-  g->b = p.w16 ? p.w16 : (const void*)((const uint16_t*)p.w + (int64_t)v0 * p.ldw);
-  g->ldb = 2 * (p.w16 ? p.ldw16 : p.ldw);
+  const int64_t pitch = p.ldw * (p.w_fmt == kF16 ? 2 : 1);
+  g->b = p.w16 ? p.w16 : (const void*)((const uint8_t*)p.w + (int64_t)v0 * pitch);
+  g->ldb = p.w16 ? 2 * p.ldw16 : pitch;
+  g->b_fmt = p.w16 ? kF16 : p.w_fmt;
   g->M = p.R;
   g->N = n;
   g->K = p.D;

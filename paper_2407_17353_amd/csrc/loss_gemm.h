@@ -79,10 +79,16 @@ __device__ __forceinline__ int loss_exponent(const uint32_t* hdr, int word) {
 __device__ __forceinline__ void held(uint32_t& x) { asm volatile("" : "+v"(x)); }
 
 // OF: what LOSS_DW stores, a format's codes or a LossForm.
-template <bool A_MC, bool B_MC, int EPI, int OF>
+// BF: b's rows are F16 (kF16), or codes of 8 bits whose count along k is a multiple of 16:
+// they lie in LDS as they are (256 rows of 64 bytes) and are decoded between products, two a
+// product, while the group before theirs is multiplied.
+template <bool A_MC, bool B_MC, int EPI, int OF, int BF = kF16>
 __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   using C = WaveCfg<4>;
   constexpr int WTM = C::WTM, WTN = C::WTN, MI = C::MI, NI = C::NI, BPW = C::BPW;
+  constexpr bool B8 = BF != kF16;
+  static_assert(!B8 || !B_MC, "8 bits along k");
+  constexpr int BPB = B8 ? BPW / 2 : BPW;  // a wave's loads of b a step
   // bytes of an element that goes through LDS, and of a wave's 16 rows
   constexpr int ESZ = EPI == LOSS_DZ ? 2 : (EPI != LOSS_DW ? 4 : (OF == FORM_F32 ? 4 : (OF == kF16 || OF == FORM_STICKY ? 2 : 1)));
   constexpr int STAGE = EPI == LOSS_STATS || EPI == LOSS_DX ? 0 : 2048 * ESZ;
@@ -107,7 +113,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb;
 
   uint32_t qa[BPW], qb[BPW];
-  int kc[2];
+  int kc[2], kc8 = 0;
 #pragma unroll
   for (int q = 0; q < BPW; ++q) {
     const uint32_t blk = (uint32_t)(wave * BPW + q);
@@ -118,6 +124,11 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
     qa[q] = A_MC ? (uint32_t)kr * lda + 16u * cm : (blk * 8u + (uint32_t)(lane >> 3)) * lda + 16u * (uint32_t)c;
     qb[q] = B_MC ? (uint32_t)kr * ldb + 16u * cm : (blk * 8u + (uint32_t)(lane >> 3)) * ldb + 16u * (uint32_t)c;
     if (q < 2) kc[q] = 8 * c;
+    if (B8 && q < BPB) {  // 16 rows of 64 bytes a block
+      const int c8 = (lane & 3) ^ ((lane >> 4) & 3);
+      qb[q] = (uint32_t)((wave * BPB + q) * 16 + (lane >> 2)) * ldb + 16u * (uint32_t)c8;
+      kc8 = 16 * c8;
+    }
   }
 
   // The call's operands, read anew by the scalar unit where a tile needs them: held over the
@@ -142,9 +153,10 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   v4i ra, rb;
   const uint8_t *la, *lb;  // MC: the step's first row
   uint32_t wa, wb;         // MC: bytes of a row that are left (rows hold whole groups of 8)
-  auto rows_buffer = [&](const void* base, int64_t ld, int row0, int rows) {
+  auto rows_buffer = [&](const void* base, int64_t ld, int row0, int rows, bool codes) {
     const int n = min(rows - row0, 256);
-    return make_rsrc((const uint8_t*)base + (int64_t)row0 * ld, (uint32_t)((int64_t)(n - 1) * ld) + 2u * (uint32_t)((K + 7) & ~7));
+    const uint32_t width = codes ? (uint32_t)K : 2u * (uint32_t)((K + 7) & ~7);
+    return make_rsrc((const uint8_t*)base + (int64_t)row0 * ld, (uint32_t)((int64_t)(n - 1) * ld) + width);
   };
   auto k_buffer = [&](const uint8_t* base, uint32_t ld, uint32_t width) {
     const int n = min(l_end - l_k, LK);
@@ -161,14 +173,14 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       wa = 2u * (uint32_t)(((M + 7) & ~7) - m0);
       ra = k_buffer(la, lda, wa);
     } else {
-      ra = rows_buffer(p.a, p.lda, m0, M);
+      ra = rows_buffer(p.a, p.lda, m0, M, false);
     }
     if constexpr (B_MC) {
       lb = (const uint8_t*)p.b + (int64_t)l_k * p.ldb + 2 * (int64_t)n0;
       wb = 2u * (uint32_t)(((N + 7) & ~7) - n0);
       rb = k_buffer(lb, ldb, wb);
     } else {
-      rb = rows_buffer(p.b, p.ldb, n0, N);
+      rb = rows_buffer(p.b, p.ldb, n0, N, B8);
     }
   };
   load_tile();
@@ -196,23 +208,48 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
     const bool is_a = j < BPW;
     const int q = is_a ? j : j - BPW;
     uint32_t off = is_a ? qa[q] : qb[q];
-    if (!(is_a ? A_MC : B_MC)) {
+    if (!is_a && B8) {
+      off += (uint32_t)l_k;
+      if (l_k + kc8 >= l_end) off = 0x80000000u;
+    } else if (!(is_a ? A_MC : B_MC)) {
       off += 2u * (uint32_t)l_k;
       if (l_k + kc[q & 1] >= l_end) off = 0x80000000u;
     }
-    load_lds16(is_a ? ra : rb, off, smem + (is_a ? P : 2 + P) * TILE_BYTES + (wave * BPW + q) * 1024);
+    load_lds16(is_a ? ra : rb, off, smem + (is_a ? P : 2 + P) * TILE_BYTES + (wave * (is_a ? BPW : BPB) + q) * 1024);
   };
 
   const int wm = (wave / C::WAVES_N) * WTM;
   const int wn = (wave % C::WAVES_N) * WTN;
-  constexpr int DSA = A_MC ? 4 : 2, DSB = B_MC ? 4 : 2;
+  constexpr int DSA = A_MC ? 4 : 2, DSB = B8 ? 1 : (B_MC ? 4 : 2);
   constexpr int H = 6;
   constexpr int TS = (NI - H) * MI, AS = (H - 1) * MI, BP = 2 * DSB;
   constexpr int RX = MI < (NI - 2) * DSB ? MI : (NI - 2) * DSB;
   static_assert((NI - 2) * DSB <= H * MI, "head too short for its reads");
   v4i af[2][MI][2];
   v4i bf[NI][2];
-  uint32_t aa = operand_addr<A_MC>(wm, lane), ab = operand_addr<B_MC>(wn, lane);
+  v4i raw[B8 ? NI : 1];  // a group's 16 codes of a lane
+  uint32_t aa = operand_addr<A_MC>(wm, lane);
+  uint32_t ab = B8 ? (uint32_t)((wn + (lane & 15)) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4)) : operand_addr<B_MC>(wn, lane);
+  auto read_b = [&](auto group_tag, auto part_tag, const uint8_t* lds) {
+    constexpr int g = decltype(group_tag)::value;
+    if constexpr (B8)
+      raw[g] = *(const v4i*)(lds + ab + 1024 * g);
+    else
+      read_part<B_MC, g, decltype(part_tag)::value>(bf[g], lds, ab);
+  };
+  // Decodes pairs FIRST .. LAST - 1 of the codes of all groups, eight pairs a group.
+  auto decode = [&](auto first_tag, auto last_tag) {
+    static_for<decltype(first_tag)::value, decltype(last_tag)::value>([&](auto Q) {
+      constexpr int g = decltype(Q)::value / 8, c = decltype(Q)::value % 8;
+      const lh2 v = BF == kE4M3 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)raw[g][c >> 1], 1.0f, c & 1)
+                                : __builtin_amdgcn_cvt_scalef32_pk_f16_bf8((uint32_t)raw[g][c >> 1], 1.0f, c & 1);
+      int w = __builtin_bit_cast(int, v);
+      // (here and no later: a product may not follow what writes its operand at once, and the
+      // compiler does not see that the products are products)
+      asm volatile("" : "+v"(w));
+      bf[g][c >> 2][c & 3] = w;
+    });
+  };
 
   bool stored = false;  // the last thing done is an epilogue with all its stores
   // Schedule of a step: that of gemm4_kernel, with a pair of products in the place of
@@ -228,8 +265,10 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       AccTile<(mi + 1) * NI + ni>::mfma_f16(bf[ni][ks], af[P][mi + 1][ks]);
       if constexpr (i < (NI - 2) * DSB) {
         constexpr int g = 2 + i / DSB;
-        read_part<B_MC, g, i % DSB>(bf[g], cB, ab);
+        read_b(std::integral_constant<int, g>{}, std::integral_constant<int, i % DSB>{}, cB);
       }
+      // (groups 1 .. NI - 1, each done before its first product)
+      if constexpr (B8) decode(std::integral_constant<int, 8 + i * 8 * (NI - 1) / (H * MI)>{}, std::integral_constant<int, 8 + (i + 1) * 8 * (NI - 1) / (H * MI)>{});
       if constexpr (i == MI - 1) {
         wait_lgkmcnt<RX>();
         __builtin_amdgcn_s_barrier();
@@ -261,11 +300,17 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       constexpr int ks = i % 4 / 2, mi = 2 * (i / 4) + i % 2;
       AccTile<mi * NI + H>::mfma_f16(bf[H][ks], af[P][mi][ks]);
       AccTile<mi * NI + H + 1>::mfma_f16(bf[H + 1][ks], af[P][mi][ks]);
-      static_for<i * BPW / TS, (i + 1) * BPW / TS>([&](auto J) { issue_one(BPW + decltype(J)::value, P); });
-      static_for<i * BP / TS, (i + 1) * BP / TS>([&](auto Q) {
-        constexpr int q = decltype(Q)::value;
-        read_part<B_MC, q / DSB, q % DSB>(bf[q / DSB], nB, ab);
-      });
+      static_for<i * BPB / TS, (i + 1) * BPB / TS>([&](auto J) { issue_one(BPW + decltype(J)::value, P); });
+      if constexpr (B8) {
+        if constexpr (i < 2) read_b(I, I, nB);
+        constexpr int first = i - (TS - 10);  // (done two slots before the head's first product)
+        if constexpr (first >= 0 && first < 8) decode(std::integral_constant<int, first>{}, std::integral_constant<int, first + 1>{});
+      } else {
+        static_for<i * BP / TS, (i + 1) * BP / TS>([&](auto Q) {
+          constexpr int q = decltype(Q)::value;
+          read_b(std::integral_constant<int, q / DSB>{}, std::integral_constant<int, q % DSB>{}, nB);
+        });
+      }
       static_for<i * (MI * DSA) / TS, (i + 1) * (MI * DSA) / TS>([&](auto Q) {
         constexpr int q = decltype(Q)::value;
         read_part<A_MC, q / DSA, q % DSA>(af[P ^ 1][q / DSA], nA, aa);
@@ -559,13 +604,13 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
 
   // ---- the first two steps of the first tile
 #pragma unroll
-  for (int j = 0; j < 2 * BPW; ++j) issue_one(j, 0);
+  for (int j = 0; j < BPW + BPB; ++j) issue_one(j, 0);
   advance();
 #pragma unroll
-  for (int j = 0; j < 2 * BPW; ++j) issue_one(j, 1);
+  for (int j = 0; j < BPW + BPB; ++j) issue_one(j, 1);
   advance();
   static_for<0, MI * NI>([&](auto I) { AccTile<decltype(I)::value>::zero(); });
-  wait_vmcnt<2 * BPW>();
+  wait_vmcnt<BPW + BPB>();
   __syncthreads();
   static_for<0, MI * DSA>([&](auto Q) {
     constexpr int q = decltype(Q)::value;
@@ -573,8 +618,9 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   });
   static_for<0, BP>([&](auto Q) {
     constexpr int q = decltype(Q)::value;
-    read_part<B_MC, q / DSB, q % DSB>(bf[q / DSB], smem + 2 * TILE_BYTES, ab);
+    read_b(std::integral_constant<int, q / DSB>{}, std::integral_constant<int, q % DSB>{}, smem + 2 * TILE_BYTES);
   });
+  if constexpr (B8) decode(std::integral_constant<int, 0>{}, std::integral_constant<int, 8>{});
   mfma_drain();
 
   using P0 = std::integral_constant<int, 0>;
