@@ -56,7 +56,7 @@ struct LossParams {
   int bin_columns;      // groups
   void *xc, *xw;       // F16 rows of x; times their row scale over the largest
   int64_t ldxc;
-  void* w16;           // F16 rows of a piece of w (8 bits, or columns no multiple of 8)
+  void* w16;           // F16 rows of a piece of w, where its columns are no whole groups of 16 bytes
   int64_t ldw16;
   int piece;           // rows of w at a time
   float2* stats;       // [2 tiles of V][R] maximum (base 2) and sum
@@ -116,7 +116,7 @@ enum LossEpi : int {
 struct LossGemm {
   const void *a, *b;
   int64_t lda, ldb;       // bytes
-  int b_fmt;              // of logits: F16, or 8 bits
+  int b_fmt;              // of w
   int M, N, K;
   int count_is;           // the dimension that is the number of rows that count: 0 M, 1 K
   const uint32_t* hdr;

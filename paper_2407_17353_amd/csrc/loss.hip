@@ -475,9 +475,8 @@ static int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool back, bool amax, LossParams* p, void* base) {
   LossPlan z = {};
-  // w is copied as F16 where its product cannot read it: rows of F16 that end inside 16 bytes, and
-  // 8 bits where they end inside 16 or dx's product, along the vocabulary, follows
-  z.copy_w = w_fmt == kF16 ? D % 8 != 0 : back || D % 16 != 0;
+  // w is copied as F16 where its rows end inside a group of 16 bytes
+  z.copy_w = D % (w_fmt == kF16 ? 8 : 16) != 0;
   // (a pitch of an odd number of 128 bytes: rows of a power of two would share memory channels)
   auto pitch = [](int64_t cols) { return up(cols, 64) + (up(cols, 64) / 64 % 2 == 0 ? 64 : 0); };
   z.ldxc = z.ldw16 = pitch(D);

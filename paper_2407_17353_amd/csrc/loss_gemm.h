@@ -24,6 +24,9 @@ typedef short ls4 __attribute__((ext_vector_type(4)));
 // of a transposing read of 16 lanes, and those of its neighbour, meet distinct banks.
 __device__ __forceinline__ int swz_mc16(int k) { return 2 * ((k & 3) | (((k >> 4) & 1) << 2)); }
 
+// The same for 8 bits (rows of 256 bytes): eight rows of a transposing read, and their neighbour's.
+__device__ __forceinline__ int swz_mc8(int k) { return (k & 7) | (((k >> 4) & 1) << 3); }
+
 // A wave's operands in LDS. Part S (32 k of a step) of the operand of 16 rows or
 // columns 16 i .. of the wave's tile: lane l serves row or column l & 15, k = 16
 // (l >> 4) + 8 S .. + 7 (any order does that both operands share). A lane's address
@@ -79,15 +82,15 @@ __device__ __forceinline__ int loss_exponent(const uint32_t* hdr, int word) {
 __device__ __forceinline__ void held(uint32_t& x) { asm volatile("" : "+v"(x)); }
 
 // OF: what LOSS_DW stores, a format's codes or a LossForm.
-// BF: b's rows are F16 (kF16), or codes of 8 bits whose count along k is a multiple of 16:
-// they lie in LDS as they are (256 rows of 64 bytes) and are decoded between products, two a
-// product, while the group before theirs is multiplied.
+// BF: b's rows are F16 (kF16), or codes of 8 bits (whole groups of 16 of them): they lie in
+// LDS as they are (KC 256 rows of 64 bytes, MC 64 k-rows of 256, read with
+// ds_read_b64_tr_b8) and are decoded between products, two a product, while the group
+// before theirs is multiplied.
 template <bool A_MC, bool B_MC, int EPI, int OF, int BF = kF16>
 __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   using C = WaveCfg<4>;
   constexpr int WTM = C::WTM, WTN = C::WTN, MI = C::MI, NI = C::NI, BPW = C::BPW;
   constexpr bool B8 = BF != kF16;
-  static_assert(!B8 || !B_MC, "8 bits along k");
   constexpr int BPB = B8 ? BPW / 2 : BPW;  // a wave's loads of b a step
   // bytes of an element that goes through LDS, and of a wave's 16 rows
   constexpr int ESZ = EPI == LOSS_DZ ? 2 : (EPI != LOSS_DW ? 4 : (OF == FORM_F32 ? 4 : (OF == kF16 || OF == FORM_STICKY ? 2 : 1)));
@@ -124,7 +127,10 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
     qa[q] = A_MC ? (uint32_t)kr * lda + 16u * cm : (blk * 8u + (uint32_t)(lane >> 3)) * lda + 16u * (uint32_t)c;
     qb[q] = B_MC ? (uint32_t)kr * ldb + 16u * cm : (blk * 8u + (uint32_t)(lane >> 3)) * ldb + 16u * (uint32_t)c;
     if (q < 2) kc[q] = 8 * c;
-    if (B8 && q < BPB) {  // 16 rows of 64 bytes a block
+    if (B8 && B_MC && q < BPB) {  // 4 k-rows of 256 bytes a block
+      const int row = 4 * (wave * BPB + q) + (lane >> 4);
+      qb[q] = (uint32_t)row * ldb + 16u * (uint32_t)((lane & 15) ^ swz_mc8(row));
+    } else if (B8 && q < BPB) {  // 16 rows of 64 bytes a block
       const int c8 = (lane & 3) ^ ((lane >> 4) & 3);
       qb[q] = (uint32_t)((wave * BPB + q) * 16 + (lane >> 2)) * ldb + 16u * (uint32_t)c8;
       kc8 = 16 * c8;
@@ -176,8 +182,8 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       ra = rows_buffer(p.a, p.lda, m0, M, false);
     }
     if constexpr (B_MC) {
-      lb = (const uint8_t*)p.b + (int64_t)l_k * p.ldb + 2 * (int64_t)n0;
-      wb = 2u * (uint32_t)(((N + 7) & ~7) - n0);
+      lb = (const uint8_t*)p.b + (int64_t)l_k * p.ldb + (B8 ? 1 : 2) * (int64_t)n0;
+      wb = B8 ? (uint32_t)(((N + 15) & ~15) - n0) : 2u * (uint32_t)(((N + 7) & ~7) - n0);
       rb = k_buffer(lb, ldb, wb);
     } else {
       rb = rows_buffer(p.b, p.ldb, n0, N, B8);
@@ -208,7 +214,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
     const bool is_a = j < BPW;
     const int q = is_a ? j : j - BPW;
     uint32_t off = is_a ? qa[q] : qb[q];
-    if (!is_a && B8) {
+    if (!is_a && B8 && !B_MC) {
       off += (uint32_t)l_k;
       if (l_k + kc8 >= l_end) off = 0x80000000u;
     } else if (!(is_a ? A_MC : B_MC)) {
@@ -220,7 +226,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
 
   const int wm = (wave / C::WAVES_N) * WTM;
   const int wn = (wave % C::WAVES_N) * WTN;
-  constexpr int DSA = A_MC ? 4 : 2, DSB = B8 ? 1 : (B_MC ? 4 : 2);
+  constexpr int DSA = A_MC ? 4 : 2, DSB = (B_MC ? 4 : 2) / (B8 ? 2 : 1);
   constexpr int H = 6;
   constexpr int TS = (NI - H) * MI, AS = (H - 1) * MI, BP = 2 * DSB;
   constexpr int RX = MI < (NI - 2) * DSB ? MI : (NI - 2) * DSB;
@@ -229,10 +235,18 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   v4i bf[NI][2];
   v4i raw[B8 ? NI : 1];  // a group's 16 codes of a lane
   uint32_t aa = operand_addr<A_MC>(wm, lane);
-  uint32_t ab = B8 ? (uint32_t)((wn + (lane & 15)) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4)) : operand_addr<B_MC>(wn, lane);
+  const int t8 = lane & 15, k8 = 16 * (lane >> 4) + (t8 >> 1);
+  uint32_t ab = !B8    ? operand_addr<B_MC>(wn, lane)
+                : B_MC ? (uint32_t)(k8 * 256 + (((wn >> 4) ^ swz_mc8(k8)) << 4) + 8 * (t8 & 1))
+                       : (uint32_t)((wn + t8) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4));
   auto read_b = [&](auto group_tag, auto part_tag, const uint8_t* lds) {
     constexpr int g = decltype(group_tag)::value;
-    if constexpr (B8)
+    if constexpr (B8 && B_MC) {
+      constexpr int S = decltype(part_tag)::value;
+      const v2i v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS v2i*)(lds + (ab ^ (16 * g)) + 2048 * S));
+      raw[g][2 * S] = v.x;
+      raw[g][2 * S + 1] = v.y;
+    } else if constexpr (B8)
       raw[g] = *(const v4i*)(lds + ab + 1024 * g);
     else
       read_part<B_MC, g, decltype(part_tag)::value>(bf[g], lds, ab);
@@ -302,7 +316,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
       AccTile<mi * NI + H + 1>::mfma_f16(bf[H + 1][ks], af[P][mi][ks]);
       static_for<i * BPB / TS, (i + 1) * BPB / TS>([&](auto J) { issue_one(BPW + decltype(J)::value, P); });
       if constexpr (B8) {
-        if constexpr (i < 2) read_b(I, I, nB);
+        if constexpr (i < BP) read_b(std::integral_constant<int, i / DSB>{}, std::integral_constant<int, i % DSB>{}, nB);
         constexpr int first = i - (TS - 10);  // (done two slots before the head's first product)
         if constexpr (first >= 0 && first < 8) decode(std::integral_constant<int, first>{}, std::integral_constant<int, first + 1>{});
       } else {

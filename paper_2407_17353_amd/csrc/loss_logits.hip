@@ -13,7 +13,7 @@ static hipError_t launch_rows_of(const LossGemm& p, int grid, hipStream_t s) {
 hipError_t launch_loss_logits(const LossGemm& p, int epi, int grid, hipStream_t s) {
   if (epi == LOSS_STATS) return launch_rows_of<LOSS_STATS>(p, grid, s);
   if (epi == LOSS_PICK) return launch_rows_of<LOSS_PICK>(p, grid, s);
-  return launch_one(loss_gemm_kernel<false, false, LOSS_DZ, 0>, grid, 256, s, p);  // (w is decoded for dx's product)
+  return launch_rows_of<LOSS_DZ>(p, grid, s);
 }
 
 }  // namespace scalify

@@ -88,7 +88,7 @@ class Case:
 
 
 SIZES = [(1, 1, 1), (1, 2, 8), (3, 130, 7), (2, 1000, 64), (17, 255, 65), (64, 256, 128), (65, 257, 100), (255, 513, 72),
-         (256, 384, 192), (32, 700, 136), (33, 65, 1000), (100, 1003, 264), (128, 640, 1500), (129, 320, 72), (257, 129, 1000), (600, 2000, 40), (40, 5003, 321)]
+         (256, 384, 192), (32, 700, 136), (33, 65, 1000), (100, 1003, 264), (128, 640, 1500), (129, 320, 72), (300, 700, 480), (140, 600, 272), (257, 129, 1000), (600, 2000, 40), (40, 5003, 321)]
 
 
 @pytest.mark.parametrize("R,V,D", SIZES)
@@ -226,9 +226,10 @@ def test_pieces_of_the_vocabulary(top):
 @pytest.mark.parametrize("top", [0, 6])
 @pytest.mark.parametrize("R", [5, 140])
 def test_pieces_of_the_output_matrix(R, top):
-    """An 8-bit output matrix larger than its decoded piece (few rows: read as it is)."""
+    """An output matrix whose rows are copied as F16, larger than the copy's piece (few rows: read
+    as it is)."""
     say(f"loss pieces of w {R} {top}")
-    Case(R, 40001, 7200, F16, E4M3, top=top, seed=4).check()
+    Case(R, 40001, 7208, F16, E4M3, top=top, seed=4).check()
 
 
 @pytest.mark.parametrize("top", [0, 30])

@@ -99,9 +99,11 @@ def test_workspaces():
     assert f(-1, V, D, sc.F16) == 0 and f(R, 0, D, sc.F16) == 0 and f(R, V, 0, sc.F16) == 0 and f(R, V, D, sc.F32) == 0
     assert b(R, V, D, sc.F16, 2) == 0 and b(R, V, (1 << 20) + 1, sc.F16, 1) == 0
     assert kf(R, V, D, 0, sc.F16) == 0 and kf(R, V, D, 257, sc.F16) == 0 and kb(R, V, D, 8, sc.F16, 5) == 0
-    # an 8-bit matrix is decoded, at most 512 MiB at a time
-    assert f(4096, 32000, 2048, sc.E4M3) > f(4096, 32000, 2048, sc.F16)
-    assert f(1, 1 << 20, 4096, sc.E4M3) < 600 << 20
+    # a matrix whose rows are no whole groups of 16 bytes is copied as F16, at most 512 MiB at a time
+    assert f(4096, 32000, 2048, sc.E4M3) == f(4096, 32000, 2048, sc.F16) == f(4096, 32000, 2048, sc.E5M2)
+    assert f(4096, 32000, 2056, sc.E4M3) > f(4096, 32000, 2056, sc.F16) + 32000 * 2056 * 2
+    assert f(4096, 32000, 2049, sc.F16) == f(4096, 32000, 2049, sc.E4M3)
+    assert f(300, 1 << 20, 4100, sc.E4M3) < 700 << 20
     # the logits are not kept: 8 bytes for 128 of them forward, at most 512 MiB (of their gradient) backward
     assert f(16384, 131072, 64, sc.F16) < 16384 * 131072 * 4 / 50
     assert b(16384, 1 << 20, 64, sc.F16, 0) < 900 << 20
