@@ -7,8 +7,8 @@
 namespace scalify {
 
 // How dw is stored, beside a format's codes: fp32, or the 16-bit form of fp32 that keeps an
-// 8-bit rounding (sticky16).
-enum LossForm : int { FORM_F32 = 8, FORM_STICKY = 9 };
+// 8-bit rounding (sticky16); or not at all.
+enum LossForm : int { FORM_F32 = 8, FORM_STICKY = 9, FORM_NONE = 10 };
 
 // Words of the workspace header (kHeaderBytes):
 enum LossWord : int {

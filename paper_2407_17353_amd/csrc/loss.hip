@@ -531,7 +531,7 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
     take(&xw, bytes_of(R, z.ldxc, 2));
     take(&dz, bytes_of(R, z.ldz, 2));
     take(&q.part, bytes_of(R, z.ldp, 4 * (int64_t)z.splits));
-    if (amax) take(&q.dw32, bytes_of(V, z.ldp, 4));
+    if (amax && !few) take(&q.dw32, bytes_of(V, z.ldp, 4));
   } else {
     if (top) {
       float *lse = nullptr, *picked = nullptr;
@@ -708,9 +708,9 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
     }
     TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0, 1));
   }
-  if (p.dw && p.mode == 1)
+  if (p.dw && p.mode == 1 && !few)
     TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1, p.dx ? 0 : 1));
-  return p.dx || p.mode == 1 ? hipSuccess : launch_one(loss_scales_kernel, 1, 2, s, p);
+  return p.dx || (p.mode == 1 && !few) ? hipSuccess : launch_one(loss_scales_kernel, 1, 2, s, p);
 }
 
 }  // namespace scalify

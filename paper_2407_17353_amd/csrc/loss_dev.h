@@ -49,13 +49,6 @@ __device__ __forceinline__ uint32_t codes4_fp8(const float* y, float scale, bool
   }
   return w;
 }
-// Two values as sticky16, a word.
-__device__ __forceinline__ uint32_t sticky2(float a, float b) {
-  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-  // (bit 16 is set if a lower one is)
-  return __builtin_amdgcn_perm(y | ((y & 0xFFFFu) + 0xFFFFu), x | ((x & 0xFFFFu) + 0xFFFFu), 0x07060302u);
-}
-
 // (m, n) and (mo, no), maxima (base 2; -Inf where there is nothing) and sums, as one. A NaN
 // is in the sums.
 __device__ __forceinline__ void join_sums(float& m, float& n, float mo, float no) {

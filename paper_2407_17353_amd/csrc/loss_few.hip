@@ -404,15 +404,16 @@ __device__ __forceinline__ void wait_some() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// (OF: the codes' format, or FORM_NONE, the statistic alone: the dynamic rescale goes over the
+// products twice, which costs less than their bytes in between would.)
 // dw: 128 columns, whose x a workgroup keeps in registers, over a part of the vocabulary
 // (blockIdx.y, `per` tokens), 64 tokens' dz at a time through LDS. Bound: the bytes of
 // dw. A wave's 32 tokens x 64 columns go through its own LDS so that half a row (128 bytes of
 // F16) is stored at once.
 template <int NT, int OF>
 __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per) {
-  constexpr int ESZ = OF == FORM_F32 ? 4 : (OF == kF16 || OF == FORM_STICKY ? 2 : 1);
+  constexpr int ESZ = OF == kF16 ? 2 : 1;
   constexpr int PER = 16 / ESZ, LPR = 64 / PER;  // elements of a lane's store, lanes of a row
-  constexpr bool CODES = OF != FORM_F32 && OF != FORM_STICKY;
   constexpr int KS = 2 * NT;  // products of 16 places
   constexpr int ROW = 64 * ESZ, CH = ROW / 16;  // a token's bytes in a wave's LDS, and their chunks
   __shared__ __attribute__((aligned(1024))) uint8_t sd[3][32 * NT * 128], sx[8192 * NT > 8192 * ESZ ? 8192 * NT : 8192 * ESZ];
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
   const int col0 = blockIdx.x * 128, count = (int)p.hdr[LOSS_COUNT], cols = (p.D + 7) & ~7;
   const int first = blockIdx.y * per, end = min(p.V, first + per);
   if (first >= end) return;
-  const int base = base_of(p, true), shift = clamp_e8m0(base) - base - unit_of(p, true);
+  const int base = base_of(p, true), unit = unit_of(p, true), shift = out_exponent(p, true, base, unit) - base - unit;
   const bool fast = shift >= kFastShiftMinSub && shift <= kFastShiftMax;
   const float scale = fast ? pow2_float(shift) : 1.0f, inv = fast ? pow2_float(-shift) : 1.0f;
   auto begin = [&](int t0, int at) {
@@ -452,7 +453,7 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
   // dz is loaded two steps ahead. Vector memory is done in order: behind a step's loads there
   // are the next step's, and the stores of two steps, which so need not be waited for (each
   // step waiting for the last one's stores, 131 M elements of F16 took 95 us).
-  constexpr int STORES = 32 / PER;
+  constexpr int STORES = OF == FORM_NONE ? 0 : 32 / PER;
   const bool stores = col0 + 64 * cc + 64 <= p.D;  // all of them, in every step but the last
   begin(first, 0);
   if (first + 64 < end) begin(first + 64, 1);
@@ -480,12 +481,13 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
       for (int c = 0; c < 2; ++c) acc[c] = mfma(a[c][k], b, acc[c]);
     }
     // (columns past D are 0, as x's are)
-    if (p.mode == 1 || p.amax_out) {
+    if (OF == FORM_NONE || (p.mode != 1 && p.amax_out)) {
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) lmax = fmaxf(lmax, fabsf(acc[c][i]));
     }
+    if constexpr (OF == FORM_NONE) continue;
     const int r = lane & 31;
     wave_sync();
     auto stage = [&](auto nan_tag) {
@@ -496,34 +498,26 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
           const int o = (32 * c + 8 * g + 4 * h) * ESZ;  // of the row's bytes
           uint8_t* to = out + r * ROW + (((o >> 4) ^ (r & (CH - 1))) << 4) + (o & 15);
           const float y[4] = {acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
-          if constexpr (OF == FORM_F32) {
-            *(float4*)to = make_float4(y[0], y[1], y[2], y[3]);
-          } else if constexpr (OF == FORM_STICKY) {
-            *(u2*)to = u2{sticky2(y[0], y[1]), sticky2(y[2], y[3])};
-          } else if constexpr (OF == kF16) {
+          if constexpr (OF == kF16) {
             *(u2*)to = codes4_f16<decltype(nan_tag)::value>(y, inv, p.sat);
           } else {
-            *(uint32_t*)to = codes4_fp8<OF, decltype(nan_tag)::value>(y, scale, p.sat);
+            *(uint32_t*)to = codes4_fp8 < OF == kE4M3 ? kE4M3 : kE5M2, decltype(nan_tag)::value > (y, scale, p.sat);
           }
         }
     };
-    if constexpr (CODES) {
-      if (!fast) {  // exact wherever the result is normal, below it 0 either way
+    if (!fast) {  // exact wherever the result is normal, below it 0 either way
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < 2; ++c)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[c][i] = __builtin_amdgcn_ldexpf(acc[c][i], -shift);
-      }
-      float any = 0.f;  // (NaN if there is one, or two infinities)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) any += acc[0][i] + acc[1][i];
-      if (__builtin_expect(__ballot(any != any) != 0, 0))
-        stage(std::true_type{});
-      else
-        stage(std::false_type{});
-    } else {
-      stage(std::false_type{});
+        for (int i = 0; i < 16; ++i) acc[c][i] = __builtin_amdgcn_ldexpf(acc[c][i], -shift);
     }
+    float any = 0.f;  // (NaN if there is one, or two infinities)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) any += acc[0][i] + acc[1][i];
+    if (__builtin_expect(__ballot(any != any) != 0, 0))
+      stage(std::true_type{});
+    else
+      stage(std::false_type{});
     wave_sync();
     const int q = lane % LPR, c = col0 + 64 * cc + PER * q, n = p.D - c;
 #pragma unroll
@@ -531,8 +525,8 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
       const int row = PER * j + lane / LPR, t = t0 + 32 * tt + row;
       if (t < end && n > 0) {
         const u4 w = *(const u4*)(out + row * ROW + ((q ^ (row & (CH - 1))) << 4));
-        uint8_t* to = CODES ? (uint8_t*)p.dw + ((int64_t)t * p.lddw + c) * ESZ : (uint8_t*)p.dw32 + ((int64_t)t * p.ldp + c) * ESZ;
-        if (!CODES || n >= PER) {  // (ldp: whole groups of 16)
+        uint8_t* to = (uint8_t*)p.dw + ((int64_t)t * p.lddw + c) * ESZ;
+        if (n >= PER) {
           *(u4*)to = w;
         } else {
 #pragma unroll
@@ -610,7 +604,10 @@ hipError_t launch_loss_few_grads(const LossParams& p, hipStream_t s) {
     constexpr int OF = decltype(form)::value;
     return launch_parts(nt == 1 ? loss_few_dw_kernel<1, OF> : nt == 2 ? loss_few_dw_kernel<2, OF> : loss_few_dw_kernel<4, OF>, p, parts, s);
   };
-  if (p.mode == 1) return p.dw_fmt == kF16 ? launch(std::integral_constant<int, FORM_F32>{}) : launch(std::integral_constant<int, FORM_STICKY>{});
+  if (p.mode == 1) {
+    const hipError_t e = launch(std::integral_constant<int, FORM_NONE>{});
+    if (e != hipSuccess) return e;
+  }
   if (p.dw_fmt == kF16) return launch(std::integral_constant<int, kF16>{});
   return p.dw_fmt == kE4M3 ? launch(std::integral_constant<int, kE4M3>{}) : launch(std::integral_constant<int, kE5M2>{});
 }

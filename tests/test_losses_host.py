@@ -107,8 +107,9 @@ def test_workspaces():
     # the logits are not kept: 8 bytes for 128 of them forward, at most 512 MiB (of their gradient) backward
     assert f(16384, 131072, 64, sc.F16) < 16384 * 131072 * 4 / 50
     assert b(16384, 1 << 20, 64, sc.F16, 0) < 900 << 20
-    # the dynamic rescale keeps dw in fp32
-    assert b(R, V, D, sc.F16, 1) - b(R, V, D, sc.F16, 0) == 4 * V * D
+    # the dynamic rescale keeps dw in fp32, but for few rows
+    assert b(300, V, D, sc.F16, 1) - b(300, V, D, sc.F16, 0) == 4 * V * D
+    assert b(R, V, D, sc.F16, 1) == b(R, V, D, sc.F16, 0)
     # sums of byte counts past 32 bits
     assert b(1 << 20, 1 << 20, 8192, sc.F16, 1) > 1 << 35
 
