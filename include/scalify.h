@@ -15,6 +15,8 @@
  *     -> rebalance_scale (Section 3.3, Algorithm 4); the statistic is amax;
  *   - set_scaling and get_data_and_scale (Section 3.1);
  *   - casts act on the data component only (Appendix A, cast operators);
+ *   - the losses behind the last layer (softmax cross entropy, distillation) from its
+ *     operands, with their gradients and their rescale (Section 3.1, Section 3.3);
  *   - the scaled add and activation rules, fused into the matmul epilogue
  *     (Section 3.2, Algorithm 3; Appendix C.1), and the scaled LayerNorm with
  *     the dynamic rescale of its input gradient (Appendix C.2, Section 4);
@@ -581,15 +583,16 @@ scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
  * bytes), 1 <= D <= 2^20, rows of w below 2^23 bytes. row_scale (optional device fp32
  * [R], powers of two, 4-byte aligned): the a_channel_scale of x, as scalify_rmsnorm_fwd
  * gives it. The factor s_x s_w row_scale log2(e) / T is held to [2^-100, 2^64].
- * labels: device int64 [R]. Sizes: R and V at most 2^30, and at most 2^30 tiles of 256
+ * labels: device int64 [R]. Sizes: R and V at most 2^28, and at most 2^30 tiles of 256
  * x 256 (R x V and V x D; 2^24 of R x D) (SCALIFY_ERR_SHAPE).
  * Products are F16 with fp32 sums (8-bit values are F16 values), statistics fp32.
  * Deterministic on one device: every sum has a fixed order. No call synchronises;
  * which rows count is found on the device, and work goes by their number. */
 
-/* Bytes of device workspace scalify_cross_entropy_fwd needs: a copy of x in F16, 8 bytes
- * for each row and 128 columns of V, and up to 512 MiB of w in F16 where w has 8 bits or
- * D is no multiple of 8. 0 for invalid arguments. */
+/* Bytes of device workspace scalify_cross_entropy_fwd needs: 8 bytes for each row and 64
+ * tokens with up to 128 rows, else a copy of x in F16, 8 bytes for each row and 128
+ * tokens and, where the rows of w are no whole groups of 16 bytes, up to 512 MiB of w in
+ * F16. 0 for invalid arguments. */
 size_t scalify_cross_entropy_fwd_workspace_size(int64_t R, int64_t V, int64_t D, int32_t w_dtype);
 
 /* Softmax cross entropy of every row: loss, and lse (optional) for the backward; device
@@ -599,10 +602,11 @@ scalify_status scalify_cross_entropy_fwd(const scalify_scaled_array* x,
                                          const float* row_scale, float* loss, float* lse,
                                          void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of device workspace scalify_cross_entropy_bwd needs: two copies of x in F16,
- * up to 512 MiB each of the logits' gradient (of 256 tokens at least) and of w in F16,
- * fp32 products of dx for each part of the vocabulary that the device works on at once,
- * and with AMAX fp32 products of dw. 0 for invalid arguments. */
+/* Bytes of device workspace scalify_cross_entropy_bwd needs: two copies of x in F16, up
+ * to 512 MiB of the logits' gradient (of 256 tokens at least) and, where the rows of w are
+ * no whole groups of 16 bytes, of w in F16, fp32 products of dx for each part of the
+ * vocabulary that the device works on at once, and with AMAX and more than 128 rows fp32
+ * products of dw. 0 for invalid arguments. */
 size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D, int32_t w_dtype,
                                                 int32_t rescale);
 
@@ -629,8 +633,9 @@ scalify_status scalify_cross_entropy_bwd(const float* dloss, const float* dloss_
                                          float* amax_out, void* workspace, size_t workspace_bytes,
                                          void* stream);
 
-/* Workspace bytes of scalify_distillation_fwd: those of scalify_cross_entropy_fwd and 8
- * for each row and entry of the teacher (`top` entries a row, rounded up to 16). */
+/* Workspace bytes of scalify_distillation_fwd: those of scalify_cross_entropy_fwd, 8 for
+ * each row and entry of the teacher (`top` entries a row) and 4 for each 16 rows and 128
+ * tokens. */
 size_t scalify_distillation_fwd_workspace_size(int64_t R, int64_t V, int64_t D, int64_t top,
                                                int32_t w_dtype);
 
@@ -646,8 +651,7 @@ scalify_status scalify_distillation_fwd(const scalify_scaled_array* x,
                                         float* lse, float* picked, void* workspace,
                                         size_t workspace_bytes, void* stream);
 
-/* Workspace bytes of scalify_distillation_bwd: those of scalify_cross_entropy_bwd and 4
- * for each row and entry. */
+/* Workspace bytes of scalify_distillation_bwd: those of scalify_cross_entropy_bwd. */
 size_t scalify_distillation_bwd_workspace_size(int64_t R, int64_t V, int64_t D, int64_t top,
                                                int32_t w_dtype, int32_t rescale);
 

@@ -81,7 +81,9 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
 // Rows up to which a call goes by the bytes of w (loss_few.hip); the backward's dz is then
 // one piece.
 constexpr int kLossFewRows = 128;
-inline bool loss_few_bwd(int64_t R, int64_t V) { return R <= kLossFewRows && R * V <= ((int64_t)1 << 28); }
+inline bool loss_few_bwd(int64_t R, int64_t V) {
+  return R <= kLossFewRows && V <= ((int64_t)1 << 22) && R * V <= ((int64_t)1 << 28);
+}
 hipError_t launch_loss_few_dz(const LossParams& p, hipStream_t s);
 hipError_t launch_loss_few_grads(const LossParams& p, hipStream_t s);
 hipError_t launch_loss_few(const LossParams& p, hipStream_t s);

@@ -236,9 +236,10 @@ size_t rmsnorm_bwd_ws(int64_t R, int64_t D) {
   return kHeaderBytes + (size_t)rmsnorm_ws_floats(R, D) * sizeof(float);
 }
 
-// Sizes that the losses take: places and tiles are counted in 32 bits.
+// Sizes that the losses take: places, tiles and a launch's threads are counted in 32 bits.
+constexpr int64_t kMaxLoss = (int64_t)1 << 28;
 bool loss_sizes_ok(int64_t R, int64_t V, int64_t D) {
-  return R >= 0 && R <= kMaxDim && V >= 1 && V <= kMaxDim && D >= 1 && D <= ((int64_t)1 << 20) &&
+  return R >= 0 && R <= kMaxLoss && V >= 1 && V <= kMaxLoss && D >= 1 && D <= ((int64_t)1 << 20) &&
          ((R + 255) / 256) * ((V + 255) / 256) <= kMaxDim && ((R + 255) / 256) * ((D + 255) / 256) <= ((int64_t)1 << 24) &&
          ((V + 255) / 256) * ((D + 255) / 256) <= kMaxDim;
 }

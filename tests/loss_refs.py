@@ -108,12 +108,13 @@ def check_gradient(got, want, err, base, mode, target=0, amax=None):
     """A gradient's scale (base: the propagated one) and data."""
     e = lr.log2_of(got)
     top = want.abs().max().item() / 2.0 ** base if want.numel() else 0.0
-    if mode == sc.RESCALE_NONE:
-        assert e == base
-    elif amax is not None:
+    if amax is not None:
         a = amax.item()
         tol = (err.max().item() / 2.0 ** base if err.numel() else 0.0)
         assert abs(a - top) <= tol, (a, top, tol)
+    if mode == sc.RESCALE_NONE:
+        assert e == base
+    elif amax is not None:
         assert e == base + ((math.frexp(a)[1] - 1 - target) if a > 0 else 0)
     rel, sub = lr.HALF[got.fmt]
     d = (true(got) - want).abs()

@@ -365,6 +365,93 @@ def test_scales_of_any_size(ex, ew):
         assert (loss[~hit] >= 2.0 ** 60).all() and (loss[hit] >= 0).all()
 
 
+@pytest.mark.parametrize("ft,e", [(sc.F32, 3), (E4M3, -1), (E5M2, 0), (F16, None)])
+@pytest.mark.parametrize("R", [30, 150])
+def test_teachers_formats(R, ft, e):
+    """The teacher's logits in any format, with and without a scale, in rows of their own pitch."""
+    say(f"teacher {R} {ft}")
+    c = Case(R, 500, 72, top=11, T=1.5, seed=12)
+    t = lr.values(R, 11, ft, 40, 2.0)
+    c.teacher = lr.scaled(t, ft, e, ld=48)
+    c.check()
+
+
+@pytest.mark.parametrize("top", [0, 2])
+@pytest.mark.parametrize("R,V,D", [(70001, 130, 16), (140, 300, 9001), (20, 70, 20000), (3000, 600, 48)])
+def test_long_sides(R, V, D, top):
+    say(f"loss long {R} {V} {D} {top}")
+    Case(R, V, D, E4M3, F16, top=top, seed=13).check(mode=sc.RESCALE_AMAX)
+
+
+@pytest.mark.parametrize("R", [3, 130])
+def test_offsets_past_32_bits(R):
+    """An output matrix and its gradient of more than 2^32 bytes: zero but for its first and last
+    rows."""
+    say(f"loss offsets {R}")
+    V, D, f = 540000, 4104, torch.float64
+    g = torch.Generator().manual_seed(14)
+    x = torch.randn((R, D), generator=g).half()
+    ends = (torch.randn((2, D), generator=g) * 0.05).half()
+    w = torch.zeros((V, D), dtype=torch.float16, device=DEV)
+    w[0], w[V - 1] = ends[0].to(DEV), ends[1].to(DEV)
+    X = lr.scaled(x, F16, 0)
+    W = sc.ScaledArray(w.view(torch.int16), F16, sc.scale_tensor(0, DEV))
+    labels = torch.full((R,), V - 1)
+    labels[1::3] = 0
+    labels[2::3] = V // 2
+    loss, lse = torch.empty(R, device=DEV), torch.empty(R, device=DEV)
+    lab = labels.to(DEV)
+    sc.scalify_cross_entropy_fwd(X, W, lab, loss, lse=lse)
+    dx, dw = lr.empty(R, D, F16), lr.empty(V, D, F16)
+    sc.scalify_cross_entropy_bwd(X, W, lab, lse, dx=dx, dw=dw, rescale=sc.RESCALE_NONE)
+    torch.cuda.synchronize()
+    z = x.to(f) @ ends.to(f).t()
+    want = torch.log(V - 2 + z.exp().sum(1))
+    # (logits of magnitude up to 20: sums of 4104 products, 32 at a time; V terms of 1)
+    assert ((lse.cpu().to(f) - want).abs() < 1e-4).all()
+    zy = torch.where(labels == 0, z[:, 0], torch.where(labels == V - 1, z[:, 1], torch.zeros(R, dtype=f)))
+    assert ((loss.cpu().to(f) - (want - zy)).abs() < 2e-4).all()
+    p = (z - want[:, None]).exp()
+    dz = p - torch.stack([labels == 0, labels == V - 1], 1).to(f)
+    mid = torch.exp(-want) - (labels == V // 2).to(f)
+    rows = torch.stack([dz[:, 0], mid, dz[:, 1]])
+    at = torch.tensor([0, V // 2, V - 1], device=DEV)
+    for got, a, b in ((lr.data(dx), dz, ends.to(f)), (lr.data(sc.ScaledArray(dw.data[at], F16)), rows, x.to(f))):
+        # dz to F16, the sums and the output to F16: 2^-11 each, of the terms' magnitudes
+        assert ((got - a @ b).abs() <= 2.0 ** -9 * (a.abs() @ b.abs()) + 2.0 ** -24).all()
+    assert (lr.data(sc.ScaledArray(dw.data[at[1:2] + 1], F16)).abs() < 1e-2).all()
+
+
+@pytest.mark.parametrize("R", [20, 150])
+@pytest.mark.parametrize("fg", [E4M3, E5M2, F16])
+@pytest.mark.parametrize("sat", [True, False])
+def test_overflow(R, fg, sat):
+    """Gradients past their format: the largest value, or (not saturating) NaN and infinities."""
+    say(f"loss overflow {R} {NAMES[fg]} {sat}")
+    c = Case(R, 300, 96, skip=0, seed=15)
+    c.g = (torch.sign(torch.randn(R, generator=torch.Generator().manual_seed(1))) * {E4M3: 2.0 ** 10, E5M2: 2.0 ** 17, F16: 2.0 ** 17}[fg]).to(DEV)
+    c.forward()
+    r = c.reference()
+    wants = r.gradients(c.g.double(), c.lse)
+    dx, dw = lr.empty(R, 96, fg), lr.empty(300, 96, fg)
+    c.backward(dx, dw, eg=0, rescale=sc.RESCALE_NONE, saturate=sat)
+    torch.cuda.synchronize()
+    largest = {E4M3: 448.0, E5M2: 57344.0, F16: 65504.0}[fg]
+    rel = lr.HALF[fg][0]
+    for got, want, err, e in ((dx, wants[0], wants[2], c.ew), (dw, wants[1], wants[3], c.ex)):
+        d, w, tol = lr.data(got).to(DEV), want / 2.0 ** e, err / 2.0 ** e
+        over = w.abs() - tol > largest * (1 + rel)
+        under = w.abs() + tol < largest
+        assert over.any() and under.any()
+        if sat:
+            assert (d[over] == torch.sign(w[over]) * largest).all()
+        elif fg == E4M3:
+            assert torch.isnan(d[over]).all()
+        else:
+            assert (d[over] == torch.sign(w[over]) * math.inf).all()
+        assert ((d - w).abs() <= tol + (w.abs() + tol) * rel + lr.HALF[fg][1])[under].all()
+
+
 def test_against_differences():
     """Gradients against central differences of the forward's losses."""
     say("loss differences")
