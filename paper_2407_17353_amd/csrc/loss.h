@@ -48,6 +48,7 @@ struct LossParams {
   // workspace; rows that count stand in their order at 0 .. count - 1
   uint32_t* hdr;
   int *rows, *pos;     // [R] row of a place; place of a row, or -1
+  int* top_on;         // [R] distillation: whether the row's teacher says anything
   int* label;          // [R] of places
   float *factor;       // [R] logits in base 2 are factor * (x . w)
   float *lse2, *coef;  // [R] log-sum-exp in base 2; upstream gradient over 2^E, times 2^14

@@ -25,10 +25,6 @@ namespace scalify {
 
 // ---- which rows count
 
-// Distillation: pos[row] = 0 where the row has a token of the teacher with a logit
-// that is not -Inf, else -1. A wave a row.
-__global__ __launch_bounds__(256) void loss_flags_kernel(LossParams p);
-
 __device__ __forceinline__ float load_any(const void* base, int fmt, int64_t e) {
   if (fmt == kF32) return ((const float*)base)[e];
   if (fmt == kF16) return decode_hw<kF16>(((const uint16_t*)base)[e]);
@@ -93,12 +89,13 @@ __device__ __forceinline__ void teacher_softmax(const TeacherRow& r, float (&q)[
   }
 }
 
+// Distillation: whether a row has a token of the teacher with a logit above -Inf. A wave a row.
 __global__ __launch_bounds__(256) void loss_flags_kernel(LossParams p) {
   const int lane = threadIdx.x & 63;
   for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < p.R; row += (int64_t)gridDim.x * 4) {
     const TeacherRow r = load_teacher(p, row, lane);
     const bool some = teaches(r);
-    if (lane == 0) p.pos[row] = some ? 0 : -1;
+    if (lane == 0) p.top_on[row] = some;
   }
 }
 
@@ -121,10 +118,10 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
       const int64_t i = at + 64 * j + lane;
       const bool in = i < hi;
       const int64_t label = p.labels && in ? p.labels[i] : -1;
-      const int flag = !p.labels && in ? p.pos[i] : -1;
+      const int flag = !p.labels && in ? p.top_on[i] : 0;
       g[j] = p.dloss && in ? p.dloss[i] : 1.0f;
       rs_[j] = p.row_scale && in ? p.row_scale[i] : 0.0f;
-      on[j] = (p.labels ? label >= 0 && label < p.V : flag >= 0) && g[j] != 0.0f;
+      on[j] = (p.labels ? label >= 0 && label < p.V : flag != 0) && g[j] != 0.0f;
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -189,33 +186,76 @@ __device__ __forceinline__ u4 load_tail8(int fmt, const void* base, int64_t e, i
   return v;
 }
 
-// The rows that count: x in F16 (D rounded up to 8 columns), and its numbers.
-__global__ __launch_bounds__(256) void loss_gather_kernel(LossParams p) {
-  const int count = (int)p.hdr[LOSS_COUNT], chunks = (p.D + 7) / 8;
-  const int ec = hdr_exponent(p.hdr, LOSS_CMAX), er = hdr_exponent(p.hdr, LOSS_RMAX);
-  for (int64_t i = blockIdx.x; i < count; i += gridDim.x) {
-    const int64_t row = p.rows[i];
-    const float r = p.row_scale ? p.row_scale[row] : 1.0f;
-    if (threadIdx.x == 0) {
-      p.factor[i] = logit_factor(p, row);
-      if (p.labels) p.label[i] = (int)p.labels[row];
-      if (p.lse2) {
-        p.lse2[i] = p.lse[row] * kLog2e;
-        p.coef[i] = ldexpf(p.dloss ? p.dloss[row] * p.temp : p.temp, kLossGradLog2 - ec);
-      }
-    }
-    const float rf = p.xw ? ldexpf(r, -er) : 1.0f;
-    for (int c = threadIdx.x; c < chunks; c += 256) {
-      const u4 v = load_tail8(p.x_fmt, p.x, row * p.ldx + 8 * c, p.D - 8 * c);
-      *(u4*)((uint16_t*)p.xc + i * p.ldxc + 8 * c) = v;
-      if (p.xw) {
-        h8 h = __builtin_bit_cast(h8, v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[k] = (_Float16)((float)h[k] * rf);
-        *(h8*)((uint16_t*)p.xw + i * p.ldxc + 8 * c) = h;
-      }
+// A row that counts at its place: x in F16 (D rounded up to 8 columns), and its numbers. ec,
+// er: exponents of the largest upstream gradient and row scale. A workgroup.
+__device__ __forceinline__ void gather_row(const LossParams& p, int64_t i, int64_t row, int ec, int er) {
+  const int chunks = (p.D + 7) / 8;
+  const float r = p.row_scale ? p.row_scale[row] : 1.0f;
+  if (threadIdx.x == 0) {
+    p.factor[i] = logit_factor(p, row);
+    if (p.labels) p.label[i] = (int)p.labels[row];
+    if (p.lse2) {
+      p.lse2[i] = p.lse[row] * kLog2e;
+      p.coef[i] = ldexpf(p.dloss ? p.dloss[row] * p.temp : p.temp, kLossGradLog2 - ec);
     }
   }
+  const float rf = p.xw ? ldexpf(r, -er) : 1.0f;
+  for (int c = threadIdx.x; c < chunks; c += 256) {
+    const u4 v = load_tail8(p.x_fmt, p.x, row * p.ldx + 8 * c, p.D - 8 * c);
+    *(u4*)((uint16_t*)p.xc + i * p.ldxc + 8 * c) = v;
+    if (p.xw) {
+      h8 h = __builtin_bit_cast(h8, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) h[k] = (_Float16)((float)h[k] * rf);
+      *(h8*)((uint16_t*)p.xw + i * p.ldxc + 8 * c) = h;
+    }
+  }
+}
+__global__ __launch_bounds__(256) void loss_gather_kernel(LossParams p) {
+  const int count = (int)p.hdr[LOSS_COUNT];
+  const int ec = hdr_exponent(p.hdr, LOSS_CMAX), er = hdr_exponent(p.hdr, LOSS_RMAX);
+  for (int64_t i = blockIdx.x; i < count; i += gridDim.x) gather_row(p, i, p.rows[i], ec, er);
+}
+
+// loss_scan_kernel and loss_gather_kernel in one for at most 128 rows, which every workgroup
+// (a row's) scans for itself. The first one keeps what the scan found.
+__global__ __launch_bounds__(256) void loss_few_gather_kernel(LossParams p) {
+  __shared__ int rows[kLossFewRows], sums[2];
+  __shared__ float cs[2], rs[2];
+  const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
+  static_assert(kLossFewRows == 128, "two waves scan");
+  bool on = false;
+  uint64_t mask = 0;
+  if (i < 128) {
+    const bool in = i < p.R;
+    const int64_t label = p.labels && in ? p.labels[i] : -1;
+    const float g = p.dloss && in ? p.dloss[i] : 1.0f, r = p.row_scale && in ? p.row_scale[i] : 0.0f;
+    on = (p.labels ? label >= 0 && label < p.V : in && p.top_on[i] != 0) && g != 0.0f;
+    mask = __ballot(on);
+    const float a = fabsf(g * p.temp);
+    const float c = wave_max(on && a < __builtin_inff() ? a : 0.f), rm = wave_max(on ? r : 0.f);
+    if (lane == 0) sums[wave] = (int)__popcll(mask), cs[wave] = c, rs[wave] = rm;
+  }
+  __syncthreads();
+  const int count = sums[0] + sums[1];
+  const float c = fmaxf(cs[0], cs[1]), r = fmaxf(rs[0], rs[1]);
+  if (i < 128) {
+    const int to = (wave ? sums[0] : 0) + (int)__popcll(mask & (((uint64_t)1 << lane) - 1));
+    if (on) rows[to] = i;
+    if (blockIdx.x == 0 && i < p.R) {
+      p.pos[i] = on ? to : -1;
+      if (on) p.rows[to] = i;
+    }
+  }
+  if (blockIdx.x == 0 && i == 0) {
+    p.hdr[LOSS_COUNT] = (uint32_t)count;
+    p.hdr[LOSS_CMAX] = __float_as_uint(c);
+    p.hdr[LOSS_RMAX] = __float_as_uint(r);
+    p.hdr[LOSS_AMAX_DX] = p.hdr[LOSS_AMAX_DW] = 0u;
+  }
+  __syncthreads();
+  if ((int)blockIdx.x < count)
+    gather_row(p, blockIdx.x, rows[blockIdx.x], c > 0.f ? floor_log2_bits(__float_as_uint(c)) : 0, r > 0.f ? floor_log2_bits(__float_as_uint(r)) : 0);
 }
 
 // n rows of w from v0 on as F16, D rounded up to 8 columns.
@@ -436,8 +476,9 @@ __device__ __forceinline__ void write_scale(const LossParams& p, bool dw) {
 }
 __global__ void loss_scales_kernel(LossParams p) { write_scale(p, threadIdx.x == 1); }
 
-// Rows of fp32 products cast to codes (the first cast of a call writes the scales too); dx: rows that do not count are 0.
-__global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw, int scales) {
+// Rows of fp32 products (of dx, the sum of `splits` of them) cast to codes; the first cast of
+// a call writes the scales too where they are known by then; dx: rows that do not count are 0.
+__global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw, int scales, int splits) {
   const bool dw = is_dw != 0;
   if (scales && blockIdx.x == 0 && threadIdx.x < 2) write_scale(p, threadIdx.x == 1);
   const int unit = unit_of(p, dw), base = base_of(p, dw), e_out = out_exponent(p, dw, base, unit);
@@ -447,6 +488,9 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
   void* out = dw ? p.dw : p.dx;
   const int fmt = dw ? p.dw_fmt : p.dx_fmt;
   const int64_t ldo = dw ? p.lddw : p.lddx;
+  // (one product's statistic is its own kernel's, but for the few rows')
+  const bool stat = !dw && p.mode != 1 && p.amax_out && (splits > 1 || p.R <= kLossFewRows);
+  float lmax = 0.f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / chunks;
     const int c = 16 * (int)(i - r * chunks), cols = p.D - c;
@@ -458,6 +502,17 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
       for (int k = 0; k < 16; ++k) u[k] <<= 16;
     } else if (from >= 0) {
       load16<kF32>(src, from * p.ldp + c, u);
+      for (int k = 1; k < splits; ++k) {
+        uint32_t w[16];
+        load16<kF32>(src, ((int64_t)k * p.R + from) * p.ldp + c, w);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) + __uint_as_float(w[j]));
+      }
+      if (stat) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (j < cols) lmax = fmaxf(lmax, fabsf(__uint_as_float(u[j])));
+      }
     } else {
 #pragma unroll
       for (int k = 0; k < 16; ++k) u[k] = 0u;
@@ -466,6 +521,10 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
     if (fmt == kF16) store_codes<kF16>(out, e, u, cols, shift, p.sat);
     else if (fmt == kE4M3) store_codes<kE4M3>(out, e, u, cols, shift, p.sat);
     else store_codes<kE5M2>(out, e, u, cols, shift, p.sat);
+  }
+  if (stat) {
+    lmax = wave_max(lmax);
+    if ((threadIdx.x & 63) == 0 && lmax > 0.f) atomicMax(p.hdr + LOSS_AMAX_DX, __float_as_uint(lmax));
   }
 }
 
@@ -521,6 +580,7 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
   take(&q.pos, 4 * r);
   take(&q.factor, 4 * r);
   take(&q.label, 4 * r);
+  if (top) take(&q.top_on, 4 * r);
   auto bytes_of = [](int64_t rows, int64_t ld, int64_t size) { return (size_t)rows * (size_t)ld * (size_t)size; };
   uint16_t *xc = nullptr, *xw = nullptr, *w16 = nullptr, *dz = nullptr;
   if (back || !few) take(&xc, bytes_of(R, z.ldxc, 2));
@@ -582,6 +642,7 @@ static int grid_for(int64_t tiles) { return std::max(1, gemm4_grid((int)tiles));
 // Rows that count and their x.
 static hipError_t begin_loss(const LossParams& p, hipStream_t s) {
   if (!p.labels) TRY(launch_one(loss_flags_kernel, groups_for(p.R, 4, 8192), 256, s, p));
+  if (p.R > 0 && p.R <= kLossFewRows) return launch_one(loss_few_gather_kernel, p.R, 256, s, p);
   TRY(launch_one(loss_scan_kernel, 1, 1024, s, p));
   return launch_one(loss_gather_kernel, groups_for(p.R, 1, 16384), 256, s, p);
 }
@@ -695,8 +756,11 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
       TRY(launch_loss_grads(g, LOSS_DW, grid_for(tiles), s));
     }
   }
+  // The dynamic rescale needs dx's statistic before its cast, and so its sum; else the cast
+  // sums, and the statistic, if it is asked for, is written behind it.
+  const bool amax = p.mode == 1, late = !amax && p.amax_out;
   if (p.dx) {
-    if (p.splits > 1 || few) {
+    if (amax && (p.splits > 1 || few)) {
       LossParams q = p;
       void* a[] = {&q};
       const dim3 grid((unsigned)groups_for(p.R, 1, 8192), p.R < 1024 ? (unsigned)groups_for(p.D, 1024, 64) : 1u);
@@ -706,11 +770,12 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
         return e;
       }
     }
-    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0, 1));
+    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0, late ? 0 : 1, amax ? 1 : p.splits));
   }
-  if (p.dw && p.mode == 1 && !few)
-    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1, p.dx ? 0 : 1));
-  return p.dx || (p.mode == 1 && !few) ? hipSuccess : launch_one(loss_scales_kernel, 1, 2, s, p);
+  if (p.dw && amax && !few)
+    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1, p.dx ? 0 : 1, 1));
+  const bool written = !late && (p.dx || (amax && !few));
+  return written ? hipSuccess : launch_one(loss_scales_kernel, 1, 2, s, p);
 }
 
 }  // namespace scalify
