@@ -6,7 +6,7 @@
 // 64 rows of w (tokens) and its four waves share the columns, 128 bytes of each row at a
 // time in turn (512 contiguous bytes together); x comes from the L2 caches, where every
 // workgroup finds it, and the waves' sums meet in LDS in a fixed order. With more rows
-// that x would be several bytes for each of w (48 rows of 4096 columns: 79 us, with w's bytes
+// that x would be several bytes for each of w (48 rows of 4096 columns: 79 us, now 40, with w's bytes
 // alone 27): the waves then take 16 tokens each and go through x together, in LDS, the
 // columns of w and x loaded three chunks ahead.
 #include "attention_dev.h"
@@ -14,11 +14,11 @@
 #include "loss_dev.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace scalify {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
-
 
 constexpr int FEW_TOKENS = 64;
 
@@ -194,8 +194,10 @@ __global__ __launch_bounds__(256) void loss_few_kernel(LossParams p) {
   finish_few<16, 4, BACK>(p, &z[0][0][0], t0, R);
 }
 
-// Up to 16 NP rows, their columns in LDS.
-template <int FW, int NP, bool BACK>
+// Up to 16 NP rows, their columns in LDS. (X16 is a template's so that 8-bit rows of x wait in
+// half the registers: read in either form by a branch, 128 rows against 32000 x 4096 in E4M3
+// took 137 us, now 60.)
+template <int FW, int NP, bool X16, bool BACK>
 __global__ __launch_bounds__(256) void loss_rows_kernel(LossParams p) {
   constexpr int KL = few_k<FW>(), KC = 4 * KL, G8 = KL / 8, PLACES = 16 * NP, ROW = 2 * KC, CH = ROW / 16;
   constexpr int NG = PLACES * CH / 256;  // groups of eight of a chunk of x that a thread loads
@@ -207,7 +209,8 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossParams p) {
   constexpr int esz = FW == kF16 ? 2 : 1;
   const int R = BACK ? (int)p.hdr[LOSS_COUNT] : p.R;
   if (BACK && R == 0) return;
-  const int x_fmt = BACK ? kF16 : p.x_fmt, xsz = x_fmt == kF16 ? 2 : 1;
+  constexpr int xsz = X16 ? 2 : 1;
+  typedef std::conditional_t<X16, u4, u2> Group;  // eight columns of x
   const uint8_t* const x0 = (const uint8_t*)(BACK ? p.xc : p.x);
   const int64_t xpitch = (BACK ? p.ldxc : p.ldx) * xsz;
   const uint8_t* const wr = (const uint8_t*)p.w + (int64_t)min(t0 + 16 * wave + r, p.V - 1) * p.ldw * esz;
@@ -224,20 +227,13 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossParams p) {
   f4 acc[NP];
 #pragma unroll
   for (int n = 0; n < NP; ++n) acc[n] = f4{0.f, 0.f, 0.f, 0.f};
-  u4 w[3][2], x[3][NG];
-  auto load = [&](int k0, u4 (&wo)[2], u4 (&xo)[NG]) {
+  u4 w[3][2];
+  Group x[3][NG];
+  auto load = [&](int k0, u4 (&wo)[2], Group (&xo)[NG]) {
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
       const int at = k0 + xk[j];
-      xo[j] = u4{0u, 0u, 0u, 0u};
-      if (at < D) {
-        if (x_fmt == kF16) {
-          xo[j] = *(const u4*)(xr[j] + 2 * at);
-        } else {
-          const u2 v = *(const u2*)(xr[j] + at);
-          xo[j] = u4{v[0], v[1], 0u, 0u};
-        }
-      }
+      xo[j] = at < D ? *(const Group*)(xr[j] + xsz * at) : Group{};
     }
     const int k = k0 + KL * g;
 #pragma unroll
@@ -246,10 +242,16 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossParams p) {
       wo[h] = at < D ? *(const u4*)(wr + (int64_t)at * esz) : u4{0u, 0u, 0u, 0u};
     }
   };
-  auto put = [&](int k0, uint8_t* lds, const u4 (&xi)[NG]) {
+  auto put = [&](int k0, uint8_t* lds, const Group (&xi)[NG]) {
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-      u4 v = x_fmt == kF16 ? xi[j] : (x_fmt == kE4M3 ? to_f16x8(kE4M3, xi[j]) : to_f16x8(kE5M2, xi[j]));
+      u4 v;
+      if constexpr (X16) {
+        v = xi[j];
+      } else {
+        const u4 c = u4{xi[j][0], xi[j][1], 0u, 0u};
+        v = p.x_fmt == kE4M3 ? to_f16x8(kE4M3, c) : to_f16x8(kE5M2, c);
+      }
       if (k0 + KC > D) v = mask8(v, D - (k0 + xk[j]));
       *(u4*)(lds + xl[j]) = v;
     }
@@ -404,15 +406,16 @@ __device__ __forceinline__ void wait_some() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// (OF: the codes' format, or FORM_NONE, the statistic alone: the dynamic rescale goes over the
-// products twice, which costs less than their bytes in between would.)
 // dw: 128 columns, whose x a workgroup keeps in registers, over a part of the vocabulary
 // (blockIdx.y, `per` tokens), 64 tokens' dz at a time through LDS. Bound: the bytes of
 // dw. A wave's 32 tokens x 64 columns go through its own LDS so that half a row (128 bytes of
-// F16) is stored at once.
+// F16) is stored at once; they become codes before that (32000 x 4096 in F16, 48 rows: 56 us;
+// fp32 through LDS and cast on the way out, 100). OF: the codes' format, or FORM_NONE, the
+// statistic alone: the dynamic rescale goes over the products twice, which costs less than
+// their bytes in between would (64 rows, 50021 x 2048 in 8 bits: the backward 185 us, was 233).
 template <int NT, int OF>
 __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per) {
-  constexpr int ESZ = OF == kF16 ? 2 : 1;
+  constexpr int ESZ = OF == kF16 ? 2 : 1, F8 = OF == kE4M3 ? kE4M3 : kE5M2;
   constexpr int PER = 16 / ESZ, LPR = 64 / PER;  // elements of a lane's store, lanes of a row
   constexpr int KS = 2 * NT;  // products of 16 places
   constexpr int ROW = 64 * ESZ, CH = ROW / 16;  // a token's bytes in a wave's LDS, and their chunks
@@ -451,8 +454,7 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
   uint8_t* const out = sx + wave * 32 * ROW;  // [32 tokens][64 columns], the chunks of a row permuted by it
   float lmax = 0.f;
   // dz is loaded two steps ahead. Vector memory is done in order: behind a step's loads there
-  // are the next step's, and the stores of two steps, which so need not be waited for (each
-  // step waiting for the last one's stores, 131 M elements of F16 took 95 us).
+  // are the next step's, and the stores of two steps, which so need not be waited for.
   constexpr int STORES = OF == FORM_NONE ? 0 : 32 / PER;
   const bool stores = col0 + 64 * cc + 64 <= p.D;  // all of them, in every step but the last
   begin(first, 0);
@@ -501,7 +503,7 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
           if constexpr (OF == kF16) {
             *(u2*)to = codes4_f16<decltype(nan_tag)::value>(y, inv, p.sat);
           } else {
-            *(uint32_t*)to = codes4_fp8 < OF == kE4M3 ? kE4M3 : kE5M2, decltype(nan_tag)::value > (y, scale, p.sat);
+            *(uint32_t*)to = codes4_fp8<F8, decltype(nan_tag)::value>(y, scale, p.sat);
           }
         }
     };
@@ -547,33 +549,30 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
 
 // ---- host
 
-template <int FW, bool BACK>
+template <int FW, bool X16, bool BACK>
 static hipError_t launch_tokens(const LossParams& p, int groups, hipStream_t s) {
-  if (p.R <= 16) {
-    if (BACK || p.x_fmt == kF16) return launch_one(loss_few_kernel<FW, true, BACK>, groups, 256, s, p);
-    return launch_one(loss_few_kernel<FW, BACK, BACK>, groups, 256, s, p);
-  }
-  if (p.R <= 32) return launch_one(loss_rows_kernel<FW, 2, BACK>, groups, 256, s, p);
-  if (p.R <= 64) return launch_one(loss_rows_kernel<FW, 4, BACK>, groups, 256, s, p);
-  return launch_one(loss_rows_kernel<FW, 8, BACK>, groups, 256, s, p);
+  if (p.R <= 16) return launch_one(loss_few_kernel<FW, X16, BACK>, groups, 256, s, p);
+  if (p.R <= 32) return launch_one(loss_rows_kernel<FW, 2, X16, BACK>, groups, 256, s, p);
+  if (p.R <= 64) return launch_one(loss_rows_kernel<FW, 4, X16, BACK>, groups, 256, s, p);
+  return launch_one(loss_rows_kernel<FW, 8, X16, BACK>, groups, 256, s, p);
 }
 
-template <bool BACK>
+template <bool X16, bool BACK>
 static hipError_t launch_logits(const LossParams& p, int groups, hipStream_t s) {
-  if (p.w_fmt == kF16) return launch_tokens<kF16, BACK>(p, groups, s);
-  if (p.w_fmt == kE4M3) return launch_tokens<kE4M3, BACK>(p, groups, s);
-  return launch_tokens<kE5M2, BACK>(p, groups, s);
+  if (p.w_fmt == kF16) return launch_tokens<kF16, X16, BACK>(p, groups, s);
+  if (p.w_fmt == kE4M3) return launch_tokens<kE4M3, X16, BACK>(p, groups, s);
+  return launch_tokens<kE5M2, X16, BACK>(p, groups, s);
 }
 
 hipError_t launch_loss_few(const LossParams& p, hipStream_t s) {
   const int groups = (p.V + FEW_TOKENS - 1) / FEW_TOKENS;
-  const hipError_t e = launch_logits<false>(p, groups, s);
+  const hipError_t e = p.x_fmt == kF16 ? launch_logits<true, false>(p, groups, s) : launch_logits<false, false>(p, groups, s);
   if (e != hipSuccess) return e;
   return launch_one(loss_few_join_kernel, p.R, 256, s, p, groups);
 }
 
 hipError_t launch_loss_few_dz(const LossParams& p, hipStream_t s) {
-  return launch_logits<true>(p, (p.V + FEW_TOKENS - 1) / FEW_TOKENS, s);
+  return launch_logits<true, true>(p, (p.V + FEW_TOKENS - 1) / FEW_TOKENS, s);
 }
 
 // A workgroup 128 columns and a part of the vocabulary, of whole tiles of 64 tokens.

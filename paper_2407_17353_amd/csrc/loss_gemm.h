@@ -12,7 +12,7 @@
 // the others ("MC", 64 k-rows of 512 bytes) with the transposing ds_read_b64_tr_b16.
 #pragma once
 #include "gemm4_kernel.h"
-#include "loss.h"
+#include "loss_dev.h"
 
 namespace scalify {
 
@@ -69,12 +69,6 @@ __device__ __forceinline__ float row4_max(float v) {
 }
 __device__ __forceinline__ float row4_sum(float v) {
   return row4(v, [](float a, float b) { return a + b; });
-}
-
-// Exponent of the largest |upstream gradient| (0 where there is none).
-__device__ __forceinline__ int loss_exponent(const uint32_t* hdr, int word) {
-  const uint32_t u = hdr[word];
-  return u == 0u ? 0 : floor_log2_bits(u);
 }
 
 // A value that the compiler forms anew from here on (the flipped addresses would
@@ -343,7 +337,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   float d_scale = 1.0f, d_inv = 1.0f;
   if constexpr (EPI == LOSS_DW) {
     if constexpr (OF != FORM_F32 && OF != FORM_STICKY) {  // the scale is known: codes at once
-      const int unit = loss_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2 + (p.rowscaled ? loss_exponent(p.hdr, LOSS_RMAX) : 0);
+      const int unit = hdr_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2 + (p.rowscaled ? hdr_exponent(p.hdr, LOSS_RMAX) : 0);
       const int base = pow2_exponent(p.s0) + pow2_exponent(p.s1);
       e_out = clamp_e8m0(base);
       d_shift = e_out - base - unit;
