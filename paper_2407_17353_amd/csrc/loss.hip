@@ -464,7 +464,7 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
   __syncthreads();
   a = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  if (threadIdx.x == 0 && a > 0.f) atomicMax(p.hdr + LOSS_AMAX_DX, __float_as_uint(a));
+  if (threadIdx.x == 0) raise_amax(p.hdr + LOSS_AMAX_DX, a);
 }
 
 // The gradients' scales and statistics.
@@ -478,6 +478,8 @@ __global__ void loss_scales_kernel(LossParams p) { write_scale(p, threadIdx.x ==
 
 // Rows of fp32 products (of dx, the sum of `splits` of them) cast to codes; the first cast of
 // a call writes the scales too where they are known by then; dx: rows that do not count are 0.
+// SUM: there are splits to add.
+template <bool SUM>
 __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw, int scales, int splits) {
   const bool dw = is_dw != 0;
   if (scales && blockIdx.x == 0 && threadIdx.x < 2) write_scale(p, threadIdx.x == 1);
@@ -488,8 +490,7 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
   void* out = dw ? p.dw : p.dx;
   const int fmt = dw ? p.dw_fmt : p.dx_fmt;
   const int64_t ldo = dw ? p.lddw : p.lddx;
-  // (one product's statistic is its own kernel's, but for the few rows')
-  const bool stat = !dw && p.mode != 1 && p.amax_out && (splits > 1 || p.R <= kLossFewRows);
+  const bool stat = SUM && p.mode != 1 && p.amax_out;  // (one product's is its own kernel's)
   float lmax = 0.f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / chunks;
@@ -502,7 +503,8 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
       for (int k = 0; k < 16; ++k) u[k] <<= 16;
     } else if (from >= 0) {
       load16<kF32>(src, from * p.ldp + c, u);
-      for (int k = 1; k < splits; ++k) {
+#pragma unroll 4
+      for (int k = 1; k < (SUM ? splits : 1); ++k) {
         uint32_t w[16];
         load16<kF32>(src, ((int64_t)k * p.R + from) * p.ldp + c, w);
 #pragma unroll
@@ -524,7 +526,61 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
   }
   if (stat) {
     lmax = wave_max(lmax);
-    if ((threadIdx.x & 63) == 0 && lmax > 0.f) atomicMax(p.hdr + LOSS_AMAX_DX, __float_as_uint(lmax));
+    if ((threadIdx.x & 63) == 0) raise_amax(p.hdr + LOSS_AMAX_DX, lmax);
+  }
+}
+
+// The few rows' dx from its many parts: 256 columns of a row a workgroup, whose waves share
+// the parts (a thread for 16 columns, as above: 22 us for 16 rows of 2048 columns and 64
+// parts, now 5). KEEP: the sums take the place of the first part (the statistic of the dynamic
+// rescale is due before its cast); else they are cast at once.
+template <bool KEEP>
+__global__ __launch_bounds__(256) void loss_few_sum_kernel(LossParams p, int scales) {
+  __shared__ __attribute__((aligned(16))) float sums[4][256], most[4];
+  const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
+  const int col0 = 256 * blockIdx.y, c4 = col0 + 4 * lane, col = col0 + i;
+  if (scales && blockIdx.x == 0 && blockIdx.y == 0 && i < 2) write_scale(p, i == 1);
+  const int unit = unit_of(p, false), base = base_of(p, false), shift = out_exponent(p, false, base, unit) - base - unit;
+  float lmax = 0.f;
+  for (int64_t row = blockIdx.x; row < p.R; row += gridDim.x) {
+    const int64_t from = p.pos[row];
+    if (KEEP && from < 0) continue;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (from >= 0 && c4 < p.D) {
+      const float* o = p.part + from * p.ldp + c4;
+#pragma unroll 8
+      for (int s = wave; s < p.splits; s += 4) {
+        const float4 w = *(const float4*)(o + (int64_t)s * p.R * p.ldp);
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+      }
+    }
+    __syncthreads();
+    *(float4*)&sums[wave][4 * lane] = v;
+    __syncthreads();
+    const float t = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+    if (col < p.D) lmax = fmaxf(lmax, fabsf(t));
+    if constexpr (KEEP) {
+      if (col < p.D) p.part[from * p.ldp + col] = t;
+    } else {
+      sums[0][i] = t;  // (its own column's alone)
+      __syncthreads();
+      const int c = col0 + 16 * i, cols = p.D - c;
+      if (i < 16 && cols > 0) {
+        uint32_t u[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) u[k] = __float_as_uint(sums[0][16 * i + k]);
+        const int64_t e = row * p.lddx + c;
+        if (p.dx_fmt == kF16) store_codes<kF16>(p.dx, e, u, cols, shift, p.sat);
+        else if (p.dx_fmt == kE4M3) store_codes<kE4M3>(p.dx, e, u, cols, shift, p.sat);
+        else store_codes<kE5M2>(p.dx, e, u, cols, shift, p.sat);
+      }
+    }
+  }
+  if (KEEP || p.amax_out) {
+    lmax = wave_max(lmax);
+    if (lane == 0) most[wave] = lmax;
+    __syncthreads();
+    if (i == 0) raise_amax(p.hdr + LOSS_AMAX_DX, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
   }
 }
 
@@ -760,20 +816,26 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
   // sums, and the statistic, if it is asked for, is written behind it.
   const bool amax = p.mode == 1, late = !amax && p.amax_out;
   if (p.dx) {
-    if (amax && (p.splits > 1 || few)) {
+    auto launch2 = [&](auto kernel, int64_t x, unsigned y, auto... args) {
       LossParams q = p;
-      void* a[] = {&q};
-      const dim3 grid((unsigned)groups_for(p.R, 1, 8192), p.R < 1024 ? (unsigned)groups_for(p.D, 1024, 64) : 1u);
-      const hipError_t e = hipLaunchKernel((const void*)loss_sum_kernel, grid, dim3(256), a, 0, s);
-      if (e != hipSuccess) {
-        (void)hipGetLastError();
-        return e;
-      }
+      void* a[] = {&q, &args...};
+      const hipError_t e = hipLaunchKernel((const void*)kernel, dim3((unsigned)x, y), dim3(256), a, 0, s);
+      if (e != hipSuccess) (void)hipGetLastError();
+      return e;
+    };
+    // (512 workgroups: more of them wait for each other at the statistic's word)
+    const unsigned wide = (unsigned)((p.D + 255) / 256);
+    const int64_t rows = groups_for(p.R, 1, std::max<int64_t>(1, 512 / wide));
+    if (few && !amax) {
+      TRY(launch2(loss_few_sum_kernel<false>, rows, wide, late ? 0 : 1));
+    } else {
+      if (few) TRY(launch2(loss_few_sum_kernel<true>, rows, wide, 0));
+      else if (amax && p.splits > 1) TRY(launch2(loss_sum_kernel, groups_for(p.R, 1, 8192), p.R < 1024 ? (unsigned)groups_for(p.D, 1024, 64) : 1u));
+      TRY(launch_one(amax || p.splits == 1 ? loss_cast_kernel<false> : loss_cast_kernel<true>, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0, late ? 0 : 1, amax ? 1 : p.splits));
     }
-    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0, late ? 0 : 1, amax ? 1 : p.splits));
   }
   if (p.dw && amax && !few)
-    TRY(launch_one(loss_cast_kernel, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1, p.dx ? 0 : 1, 1));
+    TRY(launch_one(loss_cast_kernel<false>, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1, p.dx ? 0 : 1, 1));
   const bool written = !late && (p.dx || (amax && !few));
   return written ? hipSuccess : launch_one(loss_scales_kernel, 1, 2, s, p);
 }

@@ -49,6 +49,12 @@ __device__ __forceinline__ uint32_t codes4_fp8(const float* y, float scale, bool
   }
   return w;
 }
+// A statistic is raised to `a`. Most are below it already, and one read is cheaper than an
+// atomic on the word that all share (8192 of them: 80 us); a read that is late is too low.
+__device__ __forceinline__ void raise_amax(uint32_t* word, float a) {
+  const uint32_t u = __float_as_uint(a);
+  if (a > 0.f && u > __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(word, u);
+}
 // (m, n) and (mo, no), maxima (base 2; -Inf where there is nothing) and sums, as one. A NaN
 // is in the sums.
 __device__ __forceinline__ void join_sums(float& m, float& n, float mo, float no) {

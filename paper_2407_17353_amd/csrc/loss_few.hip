@@ -543,8 +543,13 @@ __global__ __launch_bounds__(256) void loss_few_dw_kernel(LossParams p, int per)
       }
     }
   }
+  if (OF != FORM_NONE && (p.mode == 1 || !p.amax_out)) return;
   lmax = wave_max(lmax);
-  if (lane == 0 && lmax > 0.f) atomicMax(p.hdr + LOSS_AMAX_DW, __float_as_uint(lmax));
+  __syncthreads();
+  float* const most = (float*)sx;
+  if (lane == 0) most[wave] = lmax;
+  __syncthreads();
+  if (threadIdx.x == 0) raise_amax(p.hdr + LOSS_AMAX_DW, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
 }
 
 // ---- host

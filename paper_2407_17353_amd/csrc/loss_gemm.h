@@ -658,7 +658,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   if constexpr (EPI == LOSS_DW || EPI == LOSS_DX) {
     if (!p.amax) return;
     for (int off = 32; off > 0; off >>= 1) lmax = fmaxf(lmax, __shfl_xor(lmax, off, 64));
-    if (lane == 0 && lmax > 0.f) atomicMax(p.amax, __float_as_uint(lmax));
+    if (lane == 0) raise_amax(p.amax, lmax);
   }
 }
 
