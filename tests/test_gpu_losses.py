@@ -223,6 +223,20 @@ def test_pieces_of_the_vocabulary(top):
     Case(2100, 131101, 24, E4M3, E4M3, False, top, seed=3).check(mode=sc.RESCALE_AMAX)
 
 
+@pytest.mark.parametrize("mode", [sc.RESCALE_NONE, sc.RESCALE_AMAX])
+@pytest.mark.parametrize("top", [0, 5])
+@pytest.mark.parametrize("R,V,D,counted", [(300, 3000, 72, 150), (600, 2000, 40, 5), (600, 2000, 40, 256), (1025, 5000, 264, 257),
+                                           (1025, 5000, 264, 513), (3000, 700, 40, 1), (2100, 131101, 24, 300)])
+def test_fewer_rows_count_than_there_are(R, V, D, counted, top, mode):
+    """Tiles of rows that nothing fills: what counts is known on the device alone."""
+    say(f"loss rows that count {R} {V} {D} {counted} {top} {mode}")
+    c = Case(R, V, D, E4M3, F16, top=top, skip=0, seed=6)
+    g = torch.Generator().manual_seed(7)
+    out = torch.randperm(R, generator=g)[counted:].to(DEV)
+    (c.index if top else c.labels)[out] = -1
+    c.check(mode=mode)
+
+
 @pytest.mark.parametrize("top", [0, 6])
 @pytest.mark.parametrize("R", [5, 140])
 def test_pieces_of_the_output_matrix(R, top):
