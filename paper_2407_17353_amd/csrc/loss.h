@@ -87,6 +87,7 @@ inline bool loss_few_bwd(int64_t R, int64_t V) {
 }
 hipError_t launch_loss_few_dz(const LossParams& p, hipStream_t s);
 hipError_t launch_loss_few_grads(const LossParams& p, hipStream_t s);
+int loss_few_groups(const LossParams& p);  // of tokens, each with statistics of its own
 hipError_t launch_loss_few(const LossParams& p, hipStream_t s);
 hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s);
 hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s);

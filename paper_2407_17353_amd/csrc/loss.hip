@@ -101,7 +101,9 @@ __global__ __launch_bounds__(256) void loss_flags_kernel(LossParams p) {
 
 // Rows that count, in order, their number, and the largest upstream gradient and row
 // scale among them. One workgroup of 16 waves, each with consecutive rows, 64 at a time:
-// a first pass counts, a second one places them.
+// a first pass counts, a second one places them. Bound: the latency of a wave's chain of
+// loads (5 us for 300 rows, 22 for 16384, under 1 % of such a call; grids of more workgroups
+// would have to meet in between).
 __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
   __shared__ int sums[16];
   __shared__ float cs[16], rs[16];
@@ -211,6 +213,7 @@ __device__ __forceinline__ void gather_row(const LossParams& p, int64_t i, int64
     }
   }
 }
+// Bound: the bytes (16384 x 4096, 8 bits to F16: 201 MB in 51 us).
 __global__ __launch_bounds__(256) void loss_gather_kernel(LossParams p) {
   const int count = (int)p.hdr[LOSS_COUNT];
   const int ec = hdr_exponent(p.hdr, LOSS_CMAX), er = hdr_exponent(p.hdr, LOSS_RMAX);
@@ -218,7 +221,8 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(LossParams p) {
 }
 
 // loss_scan_kernel and loss_gather_kernel in one for at most 128 rows, which every workgroup
-// (a row's) scans for itself. The first one keeps what the scan found.
+// (a row's) scans for itself: 5 us, where two launches took 9. The first one keeps what the
+// scan found.
 __global__ __launch_bounds__(256) void loss_few_gather_kernel(LossParams p) {
   __shared__ int rows[kLossFewRows], sums[2];
   __shared__ float cs[2], rs[2];
@@ -258,7 +262,8 @@ __global__ __launch_bounds__(256) void loss_few_gather_kernel(LossParams p) {
     gather_row(p, blockIdx.x, rows[blockIdx.x], c > 0.f ? floor_log2_bits(__float_as_uint(c)) : 0, r > 0.f ? floor_log2_bits(__float_as_uint(r)) : 0);
 }
 
-// n rows of w from v0 on as F16, D rounded up to 8 columns.
+// n rows of w from v0 on as F16, D rounded up to 8 columns: where 8-bit rows, or those of F16,
+// end inside 16 bytes, which the products' loads cannot mask. Bound: the bytes.
 __global__ __launch_bounds__(256) void loss_copy_w_kernel(LossParams p, int v0, int n) {
   const int chunks = (p.D + 15) / 16, cols = (p.D + 7) & ~7;
   const int64_t all = (int64_t)n * chunks;
@@ -291,7 +296,8 @@ __global__ __launch_bounds__(256) void loss_copy_w_kernel(LossParams p, int v0, 
 // Distillation's forward: the entries of the teacher whose tokens lie in the piece of n rows
 // of w from v0 on, of 16 places (a workgroup), by groups of 128 tokens: the product's
 // epilogue has such rows and columns at hand. (Which of a group's entries comes first
-// changes nothing.) A piece has at most 2^20 tokens.
+// changes nothing.) A piece has at most 2^20 tokens. 7 us for 4096 rows of 64 entries; each tile
+// searching its rows' lists instead cost the product 38.
 constexpr int kMaxBins = (1 << 20) / 128;
 __global__ __launch_bounds__(256) void loss_bin_kernel(LossParams p, int v0, int n) {
   __shared__ int at[kMaxBins];
@@ -340,7 +346,8 @@ __global__ __launch_bounds__(256) void loss_bin_kernel(LossParams p, int v0, int
 
 // Joins the maxima and sums of a row's column groups: log-sum-exp, and the cross
 // entropy. 64 places a workgroup, the groups dealt to its 16 waves (a fixed order).
-// Rows that do not count get 0.
+// Rows that do not count get 0. Bound: the bytes, 8 for each row and 128 tokens (16384 rows,
+// 32000 tokens: 33 MB in 10 us).
 __global__ __launch_bounds__(1024) void loss_join_kernel(LossParams p, int groups) {
   __shared__ float sm[16][64], ss[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -375,37 +382,68 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossParams p, int group
   }
 }
 
-// Distillation's loss; rows that do not count, and logits of tokens that are not there,
-// get 0. A wave a row.
+// Distillation's loss of a row, from its log-sum-exp l; rows that do not count, and logits of
+// tokens that are not there, get 0. A wave.
+__device__ __forceinline__ void top_row(const LossParams& p, int64_t row, const TeacherRow& r, float l, int lane) {
+  const bool on = teaches(r);
+  float q[kTopRegs], logq[kTopRegs], sum = 0.f;
+  teacher_softmax(r, q, logq);
+#pragma unroll
+  for (int j = 0; j < kTopRegs; ++j) {
+    const int e = lane + 64 * j;
+    if (e >= p.top) continue;
+    float* z = p.picked + row * p.top + e;
+    if (!on || r.token[j] < 0)
+      *z = 0.f;
+    else if (q[j] != 0.f)
+      sum += q[j] * (logq[j] - (*z - l));
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) {
+    p.loss[row] = on ? p.temp * p.temp * sum : 0.f;
+    p.lse[row] = on ? l : 0.f;
+  }
+}
+// A wave a row (5 us for 4096 rows of 64 entries).
 __global__ __launch_bounds__(256) void loss_top_kernel(LossParams p) {
   const int lane = threadIdx.x & 63;
-  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < p.R; row += (int64_t)gridDim.x * 4) {
-    const TeacherRow r = load_teacher(p, row, lane);
-    const bool on = teaches(r);
-    float q[kTopRegs], logq[kTopRegs], sum = 0.f;
-    teacher_softmax(r, q, logq);
-    const float l = p.lse[row];
-#pragma unroll
-    for (int j = 0; j < kTopRegs; ++j) {
-      const int e = lane + 64 * j;
-      if (e >= p.top) continue;
-      float* z = p.picked + row * p.top + e;
-      if (!on || r.token[j] < 0)
-        *z = 0.f;
-      else if (q[j] != 0.f)
-        sum += q[j] * (logq[j] - (*z - l));
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) {
-      p.loss[row] = on ? p.temp * p.temp * sum : 0.f;
-      if (!on) p.lse[row] = 0.f;
-    }
+  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < p.R; row += (int64_t)gridDim.x * 4)
+    top_row(p, row, load_teacher(p, row, lane), p.lse[row], lane);
+}
+
+// The few rows' end: a row's parts joined to its log-sum-exp, and its loss; rows that do not
+// count get 0. A workgroup a row. Bound: latency (4 us; the distillation's part in a launch of
+// its own took 4 more).
+__global__ __launch_bounds__(256) void loss_few_join_kernel(LossParams p, int groups) {
+  __shared__ float sm[4], ss[4];
+  const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  TeacherRow r;
+  if (!p.labels && wave == 0) r = load_teacher(p, row, lane);
+  float m = -__builtin_inff(), n = 0.f;
+  for (int g = threadIdx.x; g < groups; g += 256) {
+    const float2 v = p.stats[(int64_t)row * groups + g];
+    join_sums(m, n, v.x, v.y);
+  }
+  for (int o = 1; o < 64; o <<= 1) join_sums(m, n, __shfl_xor(m, o, 64), __shfl_xor(n, o, 64));
+  if (lane == 0) sm[wave] = m, ss[wave] = n;
+  __syncthreads();
+  if (wave != 0) return;
+  m = sm[0], n = ss[0];  // (one value in all lanes)
+  for (int w = 1; w < 4; ++w) join_sums(m, n, sm[w], ss[w]);
+  const float l2 = m + log2f(n);
+  if (!p.labels) {
+    top_row(p, row, r, kLn2 * l2, lane);
+  } else if (lane == 0) {
+    const bool on = p.labels[row] >= 0 && p.labels[row] < p.V;
+    p.loss[row] = on ? kLn2 * (l2 - p.picked2[row]) : 0.f;
+    if (p.lse) p.lse[row] = on ? kLn2 * l2 : 0.f;
   }
 }
 
 // Distillation's backward: dz of the teacher's tokens in the piece of n rows of w from
 // v0 on, from their stored logits: c (p - q), q the sum over a token's entries. A wave
-// a place.
+// a place. Bound: 2 bytes of every entry's own cache line of dz (8192 rows of 128 entries:
+// 48 us, 1 % of the call).
 __global__ __launch_bounds__(256) void loss_fix_kernel(LossParams p, int v0, int n) {
   const int lane = threadIdx.x & 63;
   const int count = (int)p.hdr[LOSS_COUNT];
@@ -440,7 +478,8 @@ __global__ __launch_bounds__(256) void loss_fix_kernel(LossParams p, int v0, int
 // ---- the gradients' rescale and cast
 
 // dx: the splits' sum into the first of them, and its statistic (one split's is the
-// product's own). A workgroup a row at a time, or with few rows 1024 columns of it.
+// product's own). A workgroup a row at a time, or with few rows 1024 columns of it. Bound: the
+// bytes (4096 x 2048, two parts: 100 MB in 27 us).
 __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
   const int count = (int)p.hdr[LOSS_COUNT];
   float a = 0.f;
@@ -478,7 +517,7 @@ __global__ void loss_scales_kernel(LossParams p) { write_scale(p, threadIdx.x ==
 
 // Rows of fp32 products (of dx, the sum of `splits` of them) cast to codes; the first cast of
 // a call writes the scales too where they are known by then; dx: rows that do not count are 0.
-// SUM: there are splits to add.
+// SUM: there are splits to add. Bound: the bytes (4.7 TB/s for 32000 x 4096 to F16).
 template <bool SUM>
 __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw, int scales, int splits) {
   const bool dw = is_dw != 0;
@@ -741,7 +780,7 @@ static hipError_t piece_logits(const LossParams& p, int v0, int n, int epi, Loss
 hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s) {
   if (p.R <= kLossFewRows) {
     TRY(launch_loss_few(p, s));
-    return p.labels ? hipSuccess : launch_one(loss_top_kernel, groups_for(p.R, 4, 8192), 256, s, p);
+    return launch_one(loss_few_join_kernel, p.R, 256, s, p, loss_few_groups(p));
   }
   TRY(begin_loss(p, s));
   LossGemm g;
