@@ -605,8 +605,9 @@ scalify_status scalify_cross_entropy_fwd(const scalify_scaled_array* x,
 /* Bytes of device workspace scalify_cross_entropy_bwd needs: two copies of x in F16, up
  * to 512 MiB of the logits' gradient (of 256 tokens at least) and, where the rows of w are
  * no whole groups of 16 bytes, of w in F16, fp32 products of dx for each part of the
- * vocabulary that the device works on at once, and with AMAX and more than 128 rows fp32
- * products of dw. 0 for invalid arguments. */
+ * vocabulary that the device works on at once, and with more than 128 rows fp32 products
+ * of dw with AMAX, or for each of up to 64 parts of the rows where V x D is too small to
+ * fill the device. 0 for invalid arguments. */
 size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D, int32_t w_dtype,
                                                 int32_t rescale);
 

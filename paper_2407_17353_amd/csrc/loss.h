@@ -64,14 +64,14 @@ struct LossParams {
   void* dz;            // F16 [R][ldz]
   int64_t ldz;
   float* part;         // [splits][R][ldp] products of dx
-  float* dw32;         // [V][ldp] (dynamic rescale)
+  float* dw32;         // [dw_splits][V][ldp] products of dw (dynamic rescale, or more than one split)
   int64_t ldp;
-  int splits;
+  int splits, dw_splits;
 };
 
 // Sizes that the host decides: pieces of w, splits of dx, and the bytes of a workspace.
 struct LossPlan {
-  int piece, splits;
+  int piece, splits, dw_splits;
   bool copy_w;
   int64_t ldxc, ldw16, ldz, ldp;
   size_t bytes;
@@ -124,7 +124,7 @@ struct LossGemm {
   int M, N, K;
   int count_is;           // the dimension that is the number of rows that count: 0 M, 1 K
   const uint32_t* hdr;
-  int splits, k_split;    // k of a split (a multiple of 128)
+  int splits;             // parts of k, of whole groups of 128
   int v0;                 // first row of w
   // logits
   const float *factor, *lse2, *coef;
@@ -139,8 +139,8 @@ struct LossGemm {
   void* dz;
   int64_t ldz;
   // gradients
-  float* part;
-  int64_t ldp;
+  float* part;            // fp32 products, [splits][part_rows][ldp]
+  int64_t ldp, part_rows;
   int accumulate;
   void* out;
   int64_t ldo;

@@ -477,19 +477,21 @@ __global__ __launch_bounds__(256) void loss_fix_kernel(LossParams p, int v0, int
 
 // ---- the gradients' rescale and cast
 
-// dx: the splits' sum into the first of them, and its statistic (one split's is the
-// product's own). A workgroup a row at a time, or with few rows 1024 columns of it. Bound: the
+// The splits' sum into the first of them, and its statistic (one split's is the product's
+// own), of dx or dw. A workgroup a row at a time, or with few rows 1024 columns of it. Bound: the
 // bytes (4096 x 2048, two parts: 100 MB in 27 us).
-__global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
-  const int count = (int)p.hdr[LOSS_COUNT];
+__global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p, int is_dw) {
+  const bool dw = is_dw != 0;
+  const int count = dw ? p.V : (int)p.hdr[LOSS_COUNT], splits = dw ? p.dw_splits : p.splits;
+  const int64_t stride = (int64_t)(dw ? p.V : p.R) * p.ldp;
   float a = 0.f;
   for (int64_t r = blockIdx.x; r < count; r += gridDim.x)
     for (int c = 4 * (int)(blockIdx.y * 256 + threadIdx.x); c < p.D; c += 1024 * gridDim.y) {
-      float* o = p.part + r * p.ldp + c;
+      float* o = (dw ? p.dw32 : p.part) + r * p.ldp + c;
       float4 v = *(const float4*)o;
 #pragma unroll 4
-      for (int s = 1; s < p.splits; ++s) {
-        const float4 w = *(const float4*)(o + (int64_t)s * p.R * p.ldp);
+      for (int s = 1; s < splits; ++s) {
+        const float4 w = *(const float4*)(o + s * stride);
         v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
       }
       *(float4*)o = v;
@@ -503,7 +505,7 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p) {
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
   __syncthreads();
   a = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  if (threadIdx.x == 0) raise_amax(p.hdr + LOSS_AMAX_DX, a);
+  if (threadIdx.x == 0) raise_amax(p.hdr + (dw ? LOSS_AMAX_DW : LOSS_AMAX_DX), a);
 }
 
 // The gradients' scales and statistics.
@@ -515,7 +517,7 @@ __device__ __forceinline__ void write_scale(const LossParams& p, bool dw) {
 }
 __global__ void loss_scales_kernel(LossParams p) { write_scale(p, threadIdx.x == 1); }
 
-// Rows of fp32 products (of dx, the sum of `splits` of them) cast to codes; the first cast of
+// Rows of fp32 products (the sum of `splits` of them) cast to codes; the first cast of
 // a call writes the scales too where they are known by then; dx: rows that do not count are 0.
 // SUM: there are splits to add. Bound: the bytes (4.7 TB/s for 32000 x 4096 to F16).
 template <bool SUM>
@@ -529,6 +531,7 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
   void* out = dw ? p.dw : p.dx;
   const int fmt = dw ? p.dw_fmt : p.dx_fmt;
   const int64_t ldo = dw ? p.lddw : p.lddx;
+  const int64_t stride = (int64_t)(dw ? p.V : p.R) * p.ldp;
   const bool stat = SUM && p.mode != 1 && p.amax_out;  // (one product's is its own kernel's)
   float lmax = 0.f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
     const int c = 16 * (int)(i - r * chunks), cols = p.D - c;
     const int64_t from = dw ? r : p.pos[r];
     uint32_t u[16];
-    if (dw && fmt != kF16) {
+    if (dw && fmt != kF16 && p.dw_splits == 1) {
       load16<kF16>(src, from * p.ldp + c, u);  // (16 bits of each fp32, sticky16)
 #pragma unroll
       for (int k = 0; k < 16; ++k) u[k] <<= 16;
@@ -545,7 +548,7 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
 #pragma unroll 4
       for (int k = 1; k < (SUM ? splits : 1); ++k) {
         uint32_t w[16];
-        load16<kF32>(src, ((int64_t)k * p.R + from) * p.ldp + c, w);
+        load16<kF32>(src, k * stride + from * p.ldp + c, w);
 #pragma unroll
         for (int j = 0; j < 16; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) + __uint_as_float(w[j]));
       }
@@ -565,7 +568,7 @@ __global__ __launch_bounds__(256) void loss_cast_kernel(LossParams p, int is_dw,
   }
   if (stat) {
     lmax = wave_max(lmax);
-    if ((threadIdx.x & 63) == 0) raise_amax(p.hdr + LOSS_AMAX_DX, lmax);
+    if ((threadIdx.x & 63) == 0) raise_amax(p.hdr + (dw ? LOSS_AMAX_DW : LOSS_AMAX_DX), lmax);
   }
 }
 
@@ -643,17 +646,25 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
   const int64_t pieces = (V + most - 1) / most;
   z.piece = (int)up((V + pieces - 1) / pieces, 256);
   z.ldz = pitch(z.piece);
-  z.splits = 1;
+  z.splits = z.dw_splits = 1;
   if (back) {
     // dx has few tiles: its k is split where that fills the device's rounds of tiles (4.9e12
     // operations a second and CU) for more than the sums' bytes cost (4e12 a second)
-    const int64_t cus = gemm4_grid(1 << 30), tiles = ((R + 255) / 256) * ((D + 255) / 256);
-    double best = 1e300;
-    for (int s = 1; s <= 64 && (s == 1 || z.piece / s >= 256); ++s) {
-      const double t = (double)((tiles * s + cus - 1) / cus) / s * 2.0 * 65536.0 * z.piece / 4.9e12 +
-                       8.0 * s * (double)R * (double)D / 4e12;
-      if (t < best * 0.98) best = t, z.splits = s;
-    }
+    const int64_t cus = gemm4_grid(1 << 30), columns = (D + 255) / 256;
+    auto best_of = [&](int64_t rows, int64_t k, auto bytes) {
+      double best = 1e300;
+      int splits = 1;
+      for (int s = 1; s <= 64 && (s == 1 || k / s >= 256); ++s) {
+        const int64_t tiles = (rows + 255) / 256 * columns * s;
+        const double t = (double)((tiles + cus - 1) / cus) / s * 2.0 * 65536.0 * (double)k / 4.9e12 + bytes(s) / 4e12;
+        if (t < best * 0.98) best = t, splits = s;
+      }
+      return splits;
+    };
+    z.splits = best_of(R, z.piece, [&](int s) { return 8.0 * s * (double)R * (double)D; });
+    // dw likewise over the rows, where V and D are small (one part leaves as codes, or as its own
+    // fp32; 16384 rows, 4096 x 512: 326 us, was 532)
+    z.dw_splits = best_of(std::min<int64_t>(z.piece, V), R, [&](int s) { return s == 1 ? 0.0 : (8.0 * s + 8.0) * (double)V * (double)D; });
   }
   const bool few = back ? loss_few_bwd(R, V) : R <= kLossFewRows;
   if (back && few) {
@@ -686,7 +697,7 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
     take(&xw, bytes_of(R, z.ldxc, 2));
     take(&dz, bytes_of(R, z.ldz, 2));
     take(&q.part, bytes_of(R, z.ldp, 4 * (int64_t)z.splits));
-    if (amax && !few) take(&q.dw32, bytes_of(V, z.ldp, 4));
+    if ((amax || z.dw_splits > 1) && !few) take(&q.dw32, bytes_of(V, z.ldp, 4 * (int64_t)z.dw_splits));
   } else {
     if (top) {
       float *lse = nullptr, *picked = nullptr;
@@ -715,6 +726,7 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
     p->ldp = z.ldp;
     p->piece = z.piece;
     p->splits = z.splits;
+    p->dw_splits = z.dw_splits;
   }
   z.bytes = at;
   return z;
@@ -796,7 +808,7 @@ hipError_t launch_loss_fwd(const LossParams& p, hipStream_t s) {
 
 hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
   TRY(begin_loss(p, s));
-  const bool few = loss_few_bwd(p.R, p.V);
+  const bool few = loss_few_bwd(p.R, p.V), parts_dw = !few && p.dw_splits > 1;
   if (few) {
     TRY(launch_loss_few_dz(p, s));
     if (!p.labels) TRY(launch_one(loss_fix_kernel, groups_for(p.R, 4, 8192), 256, s, p, 0, p.V));
@@ -818,7 +830,7 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
       g.N = p.D;
       g.K = n;
       g.splits = p.splits;
-      g.k_split = (int)up((n + p.splits - 1) / p.splits, 128);
+      g.part_rows = p.R;
       g.part = p.part;
       g.ldp = p.ldp;
       g.accumulate = v0 > 0;
@@ -835,48 +847,56 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
       g.N = p.D;
       g.K = 0;
       g.count_is = 1;
-      g.splits = 1;
+      g.splits = p.dw_splits;
       g.part = p.dw32;
+      g.part_rows = p.V;
       g.ldp = p.ldp;
       g.out = p.dw;
       g.ldo = p.lddw;
-      g.out_fmt = p.dw_fmt;
+      g.out_fmt = parts_dw ? kF16 : p.dw_fmt;  // (parts: as the dynamic rescale's F16, in fp32)
       g.sat = p.sat;
-      g.mode = p.mode;
-      g.amax = p.hdr + LOSS_AMAX_DW;
+      g.mode = parts_dw ? 1 : p.mode;
+      g.amax = parts_dw ? nullptr : p.hdr + LOSS_AMAX_DW;
       g.s0 = p.s_dloss;
       g.s1 = p.s_x;
       g.rowscaled = p.row_scale != nullptr;
-      const int64_t tiles = (int64_t)((n + 255) / 256) * ((p.D + 255) / 256);
+      const int64_t tiles = (int64_t)((n + 255) / 256) * ((p.D + 255) / 256) * p.dw_splits;
       TRY(launch_loss_grads(g, LOSS_DW, grid_for(tiles), s));
     }
   }
-  // The dynamic rescale needs dx's statistic before its cast, and so its sum; else the cast
+  // The dynamic rescale needs a statistic before its cast, and so the parts' sum; else the cast
   // sums, and the statistic, if it is asked for, is written behind it.
   const bool amax = p.mode == 1, late = !amax && p.amax_out;
-  if (p.dx) {
-    auto launch2 = [&](auto kernel, int64_t x, unsigned y, auto... args) {
-      LossParams q = p;
-      void* a[] = {&q, &args...};
-      const hipError_t e = hipLaunchKernel((const void*)kernel, dim3((unsigned)x, y), dim3(256), a, 0, s);
-      if (e != hipSuccess) (void)hipGetLastError();
-      return e;
-    };
-    // (512 and 1024 workgroups: more of them wait for each other at the statistic's word; 4096 rows
-    // of 2048 columns, a workgroup each, took 48 us, now 27)
+  auto launch2 = [&](auto kernel, int64_t x, unsigned y, auto... args) {
+    LossParams q = p;
+    void* a[] = {&q, &args...};
+    const hipError_t e = hipLaunchKernel((const void*)kernel, dim3((unsigned)x, y), dim3(256), a, 0, s);
+    if (e != hipSuccess) (void)hipGetLastError();
+    return e;
+  };
+  // (512 and 1024 workgroups: more of them wait for each other at the statistic's word; 4096 rows
+  // of 2048 columns, a workgroup each, took 48 us, now 27)
+  auto sum_and_cast = [&](int is_dw, int rows, int splits, int scales) {
+    if (amax && splits > 1) TRY(launch2(loss_sum_kernel, groups_for(rows, 1, 1024), rows < 1024 ? (unsigned)groups_for(p.D, 1024, 64) : 1u, is_dw));
+    const int parts = amax ? 1 : splits;
+    return launch_one(parts > 1 ? loss_cast_kernel<true> : loss_cast_kernel<false>, groups_for((int64_t)rows * ((p.D + 15) / 16), 256, 16384), 256, s, p, is_dw,
+                      scales, parts);
+  };
+  if (p.dx && few) {
     const unsigned wide = (unsigned)((p.D + 255) / 256);
     const int64_t rows = groups_for(p.R, 1, std::max<int64_t>(1, 512 / wide));
-    if (few && !amax) {
-      TRY(launch2(loss_few_sum_kernel<false>, rows, wide, late ? 0 : 1));
+    if (amax) {
+      TRY(launch2(loss_few_sum_kernel<true>, rows, wide, 0));
+      TRY(sum_and_cast(0, p.R, 1, 1));
     } else {
-      if (few) TRY(launch2(loss_few_sum_kernel<true>, rows, wide, 0));
-      else if (amax && p.splits > 1) TRY(launch2(loss_sum_kernel, groups_for(p.R, 1, 1024), p.R < 1024 ? (unsigned)groups_for(p.D, 1024, 64) : 1u));
-      TRY(launch_one(amax || p.splits == 1 ? loss_cast_kernel<false> : loss_cast_kernel<true>, groups_for((int64_t)p.R * ((p.D + 15) / 16), 256, 16384), 256, s, p, 0, late ? 0 : 1, amax ? 1 : p.splits));
+      TRY(launch2(loss_few_sum_kernel<false>, rows, wide, late ? 0 : 1));
     }
   }
-  if (p.dw && amax && !few)
-    TRY(launch_one(loss_cast_kernel<false>, groups_for((int64_t)p.V * ((p.D + 15) / 16), 256, 16384), 256, s, p, 1, p.dx ? 0 : 1, 1));
-  const bool written = !late && (p.dx || (amax && !few));
+  // (the scales need both statistics: dw's parts are summed before the first cast)
+  const bool cast_dw = p.dw && !few && (amax || parts_dw);
+  if (cast_dw) TRY(sum_and_cast(1, p.V, p.dw_splits, 0));
+  if (p.dx && !few) TRY(sum_and_cast(0, p.R, p.splits, late ? 0 : 1));
+  const bool written = !late && p.dx;
   return written ? hipSuccess : launch_one(loss_scales_kernel, 1, 2, s, p);
 }
 

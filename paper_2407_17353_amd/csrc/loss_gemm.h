@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   const int T1 = tiles_m * tiles_n, T = T1 * p.splits;
   const int ntiles = (T - (int)blockIdx.x + G - 1) / G;
   if (ntiles <= 0) return;
-  const int k_span = p.splits > 1 ? p.k_split : K;
+  const int k_span = p.splits > 1 ? ((K + p.splits - 1) / p.splits + 127) / 128 * 128 : K;
   const int KT = (k_span + LK - 1) / LK;
   const int KTe = KT < 2 ? 2 : KT + (KT & 1);  // steps a tile, even
   const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb;
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
         store_rows(p.dz, p.ldz, m0 + wm + 16 * mi, n0 + wn, (int)p.ldz);
       } else if constexpr (EPI == LOSS_DX) {
         if (in) {
-          float* o = p.part + ((int64_t)split * p.R + m) * p.ldp + nb;
+          float* o = p.part + ((int64_t)split * p.part_rows + m) * p.ldp + nb;
           static_for<0, NI>([&](auto Q) {
             constexpr int ni = decltype(Q)::value;
             if (nb + 16 * ni < p.ldp) {
@@ -554,7 +554,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
             constexpr int ni = decltype(Q)::value;
             return v4f{x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
           });
-          store_rows(p.part + (int64_t)p.v0 * p.ldp, p.ldp, m0 + wm + 16 * mi, n0 + wn, (int)p.ldp);
+          store_rows(p.part + ((int64_t)split * p.part_rows + p.v0) * p.ldp, p.ldp, m0 + wm + 16 * mi, n0 + wn, (int)p.ldp);
         } else if constexpr (OF == FORM_STICKY) {
           stage_rows([&](auto Q) {
             constexpr int ni = decltype(Q)::value;

@@ -237,6 +237,23 @@ def test_fewer_rows_count_than_there_are(R, V, D, counted, top, mode):
     c.check(mode=mode)
 
 
+@pytest.mark.parametrize("mode", [sc.RESCALE_NONE, sc.RESCALE_AMAX])
+@pytest.mark.parametrize("fg", [F16, E4M3, E5M2])
+@pytest.mark.parametrize("R,V,D,top,rows", [(3000, 700, 72, 0, True), (5000, 300, 264, 5, False), (1037, 1, 1, 0, False), (9001, 513, 24, 3, True)])
+def test_many_rows_of_a_small_matrix(R, V, D, top, rows, fg, mode):
+    """dw has few tiles: its product is split over the rows. Alone, and without statistics, the
+    same."""
+    say(f"loss many rows {R} {V} {D} {top} {fg} {mode}")
+    c = Case(R, V, D, E4M3, F16, rows, top=top, seed=8)
+    dx, dw = c.check(fg, mode)
+    a, b = lr.empty(R, D, fg), lr.empty(V, D, fg)
+    c.backward(a, None, rescale=mode)
+    c.backward(None, b, rescale=mode)
+    torch.cuda.synchronize()
+    for x, y in ((a, dx), (b, dw)):
+        assert torch.equal(x.data.view(torch.uint8), y.data.view(torch.uint8)) and torch.equal(x.scale, y.scale)
+
+
 @pytest.mark.parametrize("top", [0, 6])
 @pytest.mark.parametrize("R", [5, 140])
 def test_pieces_of_the_output_matrix(R, top):
