@@ -11,10 +11,10 @@
 // Operands whose k is contiguous ("KC", 128-byte rows) are read with ds_read_b128,
 // the others ("MC", 64 k-rows of 512 bytes) with the transposing ds_read_b64_tr_b16.
 //
-// Measured, 16384 x 32000 x 4096 with 8-bit w: logits and statistics 2880 us (1490 TFLOP/s;
-// library products of F16 reach 1366-1415 with both operands along k), dz 3170 (1355), dx 3120
-// (1378; library 1199-1344), dw in fp32 3000 (1432; library 1062-1071). The matrix cores
-// wait for the epilogues (of three products about 7 % of the time) and run at the power limit.
+// Measured, 16384 x 32000 x 4096 with 8-bit w: logits and statistics 2830-2880 us (1490-1520
+// TFLOP/s; library products of F16 reach 1366-1415 with both operands along k), dz 3160 (1357),
+// dx 3100 (1384; library 1199-1344), dw in fp32 2950 (1457; library 1062-1071). The epilogues
+// stop the matrix cores (about 7 % of the three products), which else run at the power limit.
 // 256 x 256 tiles need 256 of them to fill the device: 125 (150 rows against 32000) leave
 // half of it idle, 55 us for 2048 columns.
 #pragma once
