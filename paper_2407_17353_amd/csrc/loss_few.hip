@@ -9,7 +9,7 @@
 // that x would be several bytes for each of w (48 rows of 4096 columns: 79 us, now 40, with w's bytes
 // alone 27): the waves then take 16 tokens each and go through x together, in LDS, the
 // columns of w and x loaded three chunks ahead. Measured (131 MB of w: 27 us at the rate of a
-// large copy): logits of 16 rows, 2048 columns in F16, 26 us; 48 rows, 4096 in 8 bits, 37, of 128
+// large copy): logits of 16 rows, 2048 columns in F16, 26 us; 48 rows, 4096 in 8 bits, 31, of 128
 // rows 56 (LDS reads and the products, 25 us each, meet the bytes).
 #include "attention_dev.h"
 #include "kernels.h"
@@ -196,7 +196,9 @@ __global__ __launch_bounds__(256) void loss_few_kernel(LossParams p) {
   finish_few<16, 4, BACK>(p, &z[0][0][0], t0, R);
 }
 
-// Up to 16 NP rows, their columns in LDS. (X16 is a template's so that 8-bit rows of x wait in
+// Up to 16 NP rows, their columns in LDS. Products go by groups of 16 rows, as do LDS reads: NP
+// 3 and 6 beside 2, 4 and 8 (4096 columns in 8 bits, 48 rows: 41 us as 64, 35 as 48; 96 rows 62
+// and 52). (X16 is a template's so that 8-bit rows of x wait in
 // half the registers: read in either form by a branch, 128 rows against 32000 x 4096 in E4M3
 // took 137 us, now 60.)
 template <int FW, int NP, bool X16, bool BACK>
@@ -204,7 +206,9 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossParams p) {
   constexpr int KL = few_k<FW>(), KC = 4 * KL, G8 = KL / 8, PLACES = 16 * NP, ROW = 2 * KC, CH = ROW / 16;
   constexpr int NG = PLACES * CH / 256;  // groups of eight of a chunk of x that a thread loads
   constexpr int BUF = PLACES * ROW;
-  constexpr int BYTES = 2 * BUF > FEW_TOKENS * PLACES * 4 ? 2 * BUF : FEW_TOKENS * PLACES * 4;
+  constexpr int ZP = NP <= 2 ? 32 : (NP <= 4 ? 64 : 128);  // places of a token's logits (those past PLACES hold anything)
+  constexpr int BYTES = 2 * BUF > FEW_TOKENS * ZP * 4 ? 2 * BUF : FEW_TOKENS * ZP * 4;
+  static_assert(PLACES * CH % 256 == 0, "whole groups a thread");
   __shared__ __attribute__((aligned(16))) uint8_t smem[BYTES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
   const int t0 = blockIdx.x * FEW_TOKENS, D = p.D;
@@ -296,10 +300,10 @@ __global__ __launch_bounds__(256) void loss_rows_kernel(LossParams p) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = 16 * wave + 4 * g + i;
-      z[t * PLACES + few_at(t, 16 * n + r)] = acc[n][i];
+      z[t * ZP + few_at(t, 16 * n + r)] = acc[n][i];
     }
   __syncthreads();
-  finish_few<PLACES, 1, BACK>(p, z, t0, R);
+  finish_few<ZP, 1, BACK>(p, z, t0, R);
 }
 
 // ---- the gradients' products of few rows, from their dz
@@ -537,7 +541,11 @@ template <int FW, bool X16, bool BACK>
 static hipError_t launch_tokens(const LossParams& p, int groups, hipStream_t s) {
   if (p.R <= 16) return launch_one(loss_few_kernel<FW, X16, BACK>, groups, 256, s, p);
   if (p.R <= 32) return launch_one(loss_rows_kernel<FW, 2, X16, BACK>, groups, 256, s, p);
+  if constexpr (FW != kF16) {
+    if (p.R <= 48) return launch_one(loss_rows_kernel<FW, 3, X16, BACK>, groups, 256, s, p);
+  }
   if (p.R <= 64) return launch_one(loss_rows_kernel<FW, 4, X16, BACK>, groups, 256, s, p);
+  if (p.R <= 96) return launch_one(loss_rows_kernel<FW, 6, X16, BACK>, groups, 256, s, p);
   return launch_one(loss_rows_kernel<FW, 8, X16, BACK>, groups, 256, s, p);
 }
 
