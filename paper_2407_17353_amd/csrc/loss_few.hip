@@ -6,7 +6,7 @@
 // 64 rows of w (tokens) and its four waves share the columns, 128 bytes of each row at a
 // time in turn (512 contiguous bytes together); x comes from the L2 caches, where every
 // workgroup finds it, and the waves' sums meet in LDS in a fixed order. With more rows
-// that x would be several bytes for each of w (48 rows of 4096 columns: 79 us, now 40, with w's bytes
+// that x would be several bytes for each of w (48 rows of 4096 columns: 79 us, now 35, with w's bytes
 // alone 27): the waves then take 16 tokens each and go through x together, in LDS, the
 // columns of w and x loaded three chunks ahead. Measured (131 MB of w: 27 us at the rate of a
 // large copy): logits of 16 rows, 2048 columns in F16, 26 us; 48 rows, 4096 in 8 bits, 31, of 128
