@@ -622,9 +622,10 @@ size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D,
  * dx (R x D), dw (V x D): E4M3, E5M2 or F16, layouts as x; either may be NULL, not both.
  * They must not overlap x, w or each other, nor their scales those of x, w, dloss or each
  * other (SCALIFY_ERR_LAYOUT). amax_out: optional device fp32 [2], the statistics of dx and
- * dw. dz is rounded to F16 as 2^14 dz / 2^E, 2^E <= max |g| the power of two below it
- * (normal numbers down to 2^-28 of 2^E); for dw, x times row_scale over the largest
- * row_scale to F16 (exact where that is a normal number of F16). */
+ * dw. dz_ij is rounded to F16, off by at most 2^-11 of it or 2^-31 |g_i|, each row with a
+ * power of two of its own; for dw, x times row_scale over the largest row_scale to F16
+ * (exact where that is a normal number of F16), further down by what |g_i| lies below
+ * 2^-8 of the largest. */
 scalify_status scalify_cross_entropy_bwd(const float* dloss, const float* dloss_scale,
                                          const scalify_scaled_array* x,
                                          const scalify_scaled_array* w, const int64_t* labels,
@@ -658,7 +659,7 @@ size_t scalify_distillation_bwd_workspace_size(int64_t R, int64_t V, int64_t D, 
 
 /* Gradients of scalify_distillation_fwd with respect to x and w, from its stored lse and
  * picked: dz_ij = g_i T (p_ij - q_ij), q_ij the sum over the row's entries of token j;
- * everything else as in scalify_cross_entropy_bwd (2^E goes by max |g T|). */
+ * everything else as in scalify_cross_entropy_bwd (its bounds with |g T|). */
 scalify_status scalify_distillation_bwd(const float* dloss, const float* dloss_scale,
                                         const scalify_scaled_array* x,
                                         const scalify_scaled_array* w,

@@ -20,9 +20,13 @@ enum LossWord : int {
 };
 
 constexpr int kLossMaxTop = 256;  // teacher's entries of a row
-// The gradient of the logits is kept in F16 as 2^14 c (p - q) with c at most 1 in
-// magnitude (below 2^15): normal numbers down to |c (p - q)| = 2^-28.
-constexpr int kLossGradLog2 = 14;
+// The gradient of the logits is kept in F16 as 2^14 c (p - q) with c = g T / 2^h below 2 in
+// magnitude (so below 2^15): normal numbers down to |c (p - q)| = 2^-28. The 2^h is a row's own,
+// its product's in dx is taken out again there, and x carries it into dw. A row whose |g T| lies
+// 2^s below the largest leaves min(s, 8) of that to dz and the rest to x: dz then is normal down
+// to 2^-20 |g T| at the least, and x, of magnitude 1, as long as s is at most 22. (One power of
+// two for all rows cost a row 2^-24 below the largest, of 32768 tokens, all its probabilities.)
+constexpr int kLossGradLog2 = 14, kLossShare = 8;
 
 struct LossParams {
   // the call's operands
@@ -51,11 +55,12 @@ struct LossParams {
   int* top_on;         // [R] distillation: whether the row's teacher says anything
   int* label;          // [R] of places
   float *factor;       // [R] logits in base 2 are factor * (x . w)
-  float *lse2, *coef;  // [R] log-sum-exp in base 2; upstream gradient over 2^E, times 2^14
+  float *lse2, *coef;  // [R] log-sum-exp in base 2; upstream gradient over 2^h, times 2^14
+  float* dx_factor;    // [R] 2^h over the largest row's
   float* picked2;      // [R] label's logit in base 2
   int *bins, *entries;  // forward: the teacher's entries of 16 places by groups of 128 tokens of a piece
   int bin_columns;      // groups
-  void *xc, *xw;       // F16 rows of x; times their row scale over the largest
+  void *xc, *xw;       // F16 rows of x; times their row scale over the largest and what dz leaves to them
   int64_t ldxc;
   void* w16;           // F16 rows of a piece of w, where its columns are no whole groups of 16 bytes
   int64_t ldw16;
@@ -127,7 +132,7 @@ struct LossGemm {
   int splits;             // parts of k, of whole groups of 128
   int v0;                 // first row of w
   // logits
-  const float *factor, *lse2, *coef;
+  const float *factor, *lse2, *coef, *dx_factor;
   const int* label;
   float* picked2;
   const int *bins, *entries;

@@ -193,15 +193,18 @@ __device__ __forceinline__ u4 load_tail8(int fmt, const void* base, int64_t e, i
 __device__ __forceinline__ void gather_row(const LossParams& p, int64_t i, int64_t row, int ec, int er) {
   const int chunks = (p.D + 7) / 8;
   const float r = p.row_scale ? p.row_scale[row] : 1.0f;
+  const float g = p.dloss ? p.dloss[row] * p.temp : p.temp;
+  const RowUnit unit = row_unit(g, ec);
   if (threadIdx.x == 0) {
     p.factor[i] = logit_factor(p, row);
     if (p.labels) p.label[i] = (int)p.labels[row];
     if (p.lse2) {
       p.lse2[i] = p.lse[row] * kLog2e;
-      p.coef[i] = ldexpf(p.dloss ? p.dloss[row] * p.temp : p.temp, kLossGradLog2 - ec);
+      p.coef[i] = ldexpf(g, kLossGradLog2 - unit.dz);
+      p.dx_factor[i] = ldexpf(1.0f, unit.dz - ec);
     }
   }
-  const float rf = p.xw ? ldexpf(r, -er) : 1.0f;
+  const float rf = p.xw ? ldexpf(r, unit.x - er) : 1.0f;
   for (int c = threadIdx.x; c < chunks; c += 256) {
     const u4 v = load_tail8(p.x_fmt, p.x, row * p.ldx + 8 * c, p.D - 8 * c);
     *(u4*)((uint16_t*)p.xc + i * p.ldxc + 8 * c) = v;
@@ -694,6 +697,7 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
   if (back) {
     take(&q.lse2, 4 * r);
     take(&q.coef, 4 * r);
+    take(&q.dx_factor, 4 * r);
     take(&xw, bytes_of(R, z.ldxc, 2));
     take(&dz, bytes_of(R, z.ldz, 2));
     take(&q.part, bytes_of(R, z.ldp, 4 * (int64_t)z.splits));
@@ -717,7 +721,7 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
   }
   if (p) {
     p->xc = xc;
-    p->xw = back && p->row_scale ? xw : nullptr;
+    p->xw = back && (p->row_scale || p->dloss) ? xw : nullptr;  // (else x as it is)
     p->w16 = few ? nullptr : w16;
     p->dz = dz;
     p->ldxc = z.ldxc;
@@ -773,6 +777,7 @@ static hipError_t piece_logits(const LossParams& p, int v0, int n, int epi, Loss
   g->factor = p.factor;
   g->lse2 = p.lse2;
   g->coef = p.coef;
+  g->dx_factor = p.dx_factor;
   g->label = p.labels ? p.label : nullptr;
   g->picked2 = p.picked2;
   g->bins = p.bins;

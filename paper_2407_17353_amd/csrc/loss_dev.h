@@ -74,6 +74,18 @@ __device__ __forceinline__ int hdr_exponent(const uint32_t* hdr, int word) {
   return hdr[word] == 0u ? 0 : floor_log2_bits(hdr[word]);
 }
 
+// The powers of two of a row with the upstream gradient g (times T): out of dz, and on x for dw.
+// top: the exponent of the largest of them. (What is 0 or not finite loses nothing.)
+struct RowUnit {
+  int dz, x;
+};
+__device__ __forceinline__ RowUnit row_unit(float g, int top) {
+  const uint32_t a = __float_as_uint(fabsf(g));
+  if (a == 0u || a >= 0x7F800000u) return {top, 0};
+  const int e = floor_log2_bits(a), below = top - e, share = min(below, kLossShare);
+  return {e + share, share - below};
+}
+
 // Unit of the products: a gradient's data in its propagated scale is the product times
 // 2^unit.
 __device__ __forceinline__ int unit_of(const LossParams& p, bool dw) {

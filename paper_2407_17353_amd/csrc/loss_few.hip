@@ -373,11 +373,12 @@ __global__ __launch_bounds__(256) void loss_few_dx_kernel(LossParams p, int per)
   for (int n = 0; n < NT; ++n) {
     const int place = 32 * n + (lane & 31);
     if (place < count) {
+      const float f = p.dx_factor[place];
       float* o = p.part + ((int64_t)blockIdx.y * p.R + place) * p.ldp;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int c = col0 + 32 * wave + 8 * g + 4 * h;
-        if (c < p.ldp) *(float4*)(o + c) = make_float4(acc[n][4 * g], acc[n][4 * g + 1], acc[n][4 * g + 2], acc[n][4 * g + 3]);
+        if (c < p.ldp) *(float4*)(o + c) = make_float4(acc[n][4 * g] * f, acc[n][4 * g + 1] * f, acc[n][4 * g + 2] * f, acc[n][4 * g + 3] * f);
       }
     }
   }

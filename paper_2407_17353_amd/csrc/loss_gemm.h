@@ -367,12 +367,13 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
     }
   };
   auto load_rows = [&](int m0) {
-    if constexpr (EPI == LOSS_STATS || EPI == LOSS_PICK || EPI == LOSS_DZ) {
+    if constexpr (EPI != LOSS_DW) {
       const auto& p = *fresh_args();
 #pragma unroll
       for (int mi = 0; mi < MI; ++mi) {
         const int m = min(m0 + wm + 16 * mi + lr, M - 1);
-        r_f[mi] = p.factor[m];
+        r_f[mi] = EPI == LOSS_DX ? p.dx_factor[m] : p.factor[m];
+        if constexpr (EPI == LOSS_DX) continue;
         if constexpr (EPI == LOSS_DZ) r_l[mi] = p.lse2[m], r_c[mi] = p.coef[m];
         if constexpr (EPI == LOSS_PICK) {
           r_i[mi] = p.rows[m];
@@ -526,11 +527,12 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
         store_rows(p.dz, p.ldz, m0 + wm + 16 * mi, n0 + wn, (int)p.ldz);
       } else if constexpr (EPI == LOSS_DX) {
         if (in) {
+          const float f = r_f[mi];
           float* o = p.part + ((int64_t)split * p.part_rows + m) * p.ldp + nb;
           static_for<0, NI>([&](auto Q) {
             constexpr int ni = decltype(Q)::value;
             if (nb + 16 * ni < p.ldp) {
-              v4f v = {x[4 * ni], x[4 * ni + 1], x[4 * ni + 2], x[4 * ni + 3]};
+              v4f v = {x[4 * ni] * f, x[4 * ni + 1] * f, x[4 * ni + 2] * f, x[4 * ni + 3] * f};
               if (p.accumulate) v += *(const v4f*)(o + 16 * ni);
               *(v4f*)(o + 16 * ni) = v;
 #pragma unroll
