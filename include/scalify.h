@@ -623,9 +623,9 @@ size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D,
  * They must not overlap x, w or each other, nor their scales those of x, w, dloss or each
  * other (SCALIFY_ERR_LAYOUT). amax_out: optional device fp32 [2], the statistics of dx and
  * dw. dz_ij is rounded to F16, off by at most 2^-11 of it or 2^-31 |g_i|, each row with a
- * power of two of its own; for dw, x times row_scale over the largest row_scale to F16
- * (exact where that is a normal number of F16), further down by what |g_i| lies below
- * 2^-8 of the largest. */
+ * power of two of its own; for dw, x_i to F16, times a power of two where |g_i|
+ * row_scale[i] lies 2^8 or more below the largest of them (exact but where that leaves F16's
+ * normal numbers: off by at most what 2^-33 of the largest makes of it). */
 scalify_status scalify_cross_entropy_bwd(const float* dloss, const float* dloss_scale,
                                          const scalify_scaled_array* x,
                                          const scalify_scaled_array* w, const int64_t* labels,

@@ -14,7 +14,7 @@ enum LossForm : int { FORM_F32 = 8, FORM_STICKY = 9, FORM_NONE = 10 };
 enum LossWord : int {
   LOSS_COUNT = 0,   // rows that count
   LOSS_CMAX = 1,    // largest finite |upstream gradient| of them, fp32 bits
-  LOSS_RMAX = 2,    // largest row scale of them, fp32 bits
+  LOSS_WEIGHT = 2,  // largest exponent of |g T| times row scale among them, plus kWeightBias (0: none)
   LOSS_AMAX_DX = 3, // statistics of the gradients' data, in the products' units
   LOSS_AMAX_DW = 4,
 };
@@ -24,9 +24,11 @@ constexpr int kLossMaxTop = 256;  // teacher's entries of a row
 // magnitude (so below 2^15): normal numbers down to |c (p - q)| = 2^-28. The 2^h is a row's own,
 // its product's in dx is taken out again there, and x carries it into dw. A row whose |g T| lies
 // 2^s below the largest leaves min(s, 8) of that to dz and the rest to x: dz then is normal down
-// to 2^-20 |g T| at the least, and x, of magnitude 1, as long as s is at most 22. (One power of
-// two for all rows cost a row 2^-24 below the largest, of 32768 tokens, all its probabilities.)
-constexpr int kLossGradLog2 = 14, kLossShare = 8;
+// to 2^-20 |g T| at the least, and x, of magnitude 1, as long as s is at most 22. What s counts
+// is |g T| times the row scale, a row's weight in dw. (One power of two for all rows cost a row
+// 2^-24 below the largest, of 32768 tokens, all its probabilities; one for all row scales cost
+// a row of 2^-26 of the largest its part of dw.)
+constexpr int kLossGradLog2 = 14, kLossShare = 8, kWeightBias = 1024;
 
 struct LossParams {
   // the call's operands
@@ -56,11 +58,11 @@ struct LossParams {
   int* label;          // [R] of places
   float *factor;       // [R] logits in base 2 are factor * (x . w)
   float *lse2, *coef;  // [R] log-sum-exp in base 2; upstream gradient over 2^h, times 2^14
-  float* dx_factor;    // [R] 2^h over the largest row's
+  float* dx_factor;    // [R] 2^h over the power of two of the largest |g T|
   float* picked2;      // [R] label's logit in base 2
   int *bins, *entries;  // forward: the teacher's entries of 16 places by groups of 128 tokens of a piece
   int bin_columns;      // groups
-  void *xc, *xw;       // F16 rows of x; times their row scale over the largest and what dz leaves to them
+  void *xc, *xw;       // F16 rows of x; times the powers of two that dz leaves to them
   int64_t ldxc;
   void* w16;           // F16 rows of a piece of w, where its columns are no whole groups of 16 bytes
   int64_t ldw16;
@@ -152,7 +154,6 @@ struct LossGemm {
   int out_fmt, sat, mode;
   uint32_t* amax;         // statistic of the products, or NULL
   const float *s0, *s1;   // factors of the propagated scale
-  int rowscaled;          // a factor of the largest row scale is due
 };
 hipError_t launch_loss_logits(const LossGemm& p, int epi, int grid, hipStream_t s);
 hipError_t launch_loss_grads(const LossGemm& p, int epi, int grid, hipStream_t s);

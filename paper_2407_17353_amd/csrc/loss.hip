@@ -99,22 +99,24 @@ __global__ __launch_bounds__(256) void loss_flags_kernel(LossParams p) {
   }
 }
 
-// Rows that count, in order, their number, and the largest upstream gradient and row
-// scale among them. One workgroup of 16 waves, each with consecutive rows, 64 at a time:
+// Rows that count, in order, their number, and the largest upstream gradient and weight in
+// dw among them. One workgroup of 16 waves, each with consecutive rows, 64 at a time:
 // a first pass counts, a second one places them. Bound: the latency of a wave's chain of
 // loads (5 us for 300 rows, 22 for 16384, under 1 % of such a call; grids of more workgroups
 // would have to meet in between).
 __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
   __shared__ int sums[16];
-  __shared__ float cs[16], rs[16];
+  __shared__ float cs[16];
+  __shared__ int ws[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t per = (p.R + 1023) / 1024 * 64, lo = wave * per, hi = lo + per < p.R ? lo + per : p.R;
   // (rows' numbers are loaded whether or not they count, four groups at a time)
-  int n = 0;
-  float c = 0.f, r = 0.f;
+  int n = 0, most = 0;
+  float c = 0.f;
   for (int64_t at = lo; at < hi; at += 256) {
     bool on[4];
-    float g[4], rs_[4];
+    float g[4];
+    int w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t i = at + 64 * j + lane;
@@ -122,7 +124,7 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
       const int64_t label = p.labels && in ? p.labels[i] : -1;
       const int flag = !p.labels && in ? p.top_on[i] : 0;
       g[j] = p.dloss && in ? p.dloss[i] : 1.0f;
-      rs_[j] = p.row_scale && in ? p.row_scale[i] : 0.0f;
+      w[j] = in ? row_weight(p, i, g[j] * p.temp) : 0;
       on[j] = (p.labels ? label >= 0 && label < p.V : flag != 0) && g[j] != 0.0f;
     }
 #pragma unroll
@@ -135,12 +137,12 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
       if (on[j]) {
         const float a = fabsf(g[j] * p.temp);
         if (a < __builtin_inff()) c = fmaxf(c, a);
-        r = fmaxf(r, rs_[j]);
+        most = max(most, w[j]);
       }
     }
   }
-  c = wave_max(c), r = wave_max(r);
-  if (lane == 0) sums[wave] = n, cs[wave] = c, rs[wave] = r;
+  c = wave_max(c), most = wave_max(most);
+  if (lane == 0) sums[wave] = n, cs[wave] = c, ws[wave] = most;
   __syncthreads();
   int place = 0, all = 0;
   for (int w = 0; w < 16; ++w) {
@@ -167,10 +169,10 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
     }
   }
   if (tid == 0) {
-    for (int w = 1; w < 16; ++w) c = fmaxf(c, cs[w]), r = fmaxf(r, rs[w]);
+    for (int w = 1; w < 16; ++w) c = fmaxf(c, cs[w]), most = max(most, ws[w]);
     p.hdr[LOSS_COUNT] = (uint32_t)all;
     p.hdr[LOSS_CMAX] = __float_as_uint(c);
-    p.hdr[LOSS_RMAX] = __float_as_uint(r);
+    p.hdr[LOSS_WEIGHT] = (uint32_t)most;
     p.hdr[LOSS_AMAX_DX] = p.hdr[LOSS_AMAX_DW] = 0u;
   }
 }
@@ -188,13 +190,12 @@ __device__ __forceinline__ u4 load_tail8(int fmt, const void* base, int64_t e, i
   return v;
 }
 
-// A row that counts at its place: x in F16 (D rounded up to 8 columns), and its numbers. ec,
-// er: exponents of the largest upstream gradient and row scale. A workgroup.
-__device__ __forceinline__ void gather_row(const LossParams& p, int64_t i, int64_t row, int ec, int er) {
+// A row that counts at its place: x in F16 (D rounded up to 8 columns), and its numbers. ec:
+// exponent of the largest upstream gradient; most: the largest row_weight. A workgroup.
+__device__ __forceinline__ void gather_row(const LossParams& p, int64_t i, int64_t row, int ec, int most) {
   const int chunks = (p.D + 7) / 8;
-  const float r = p.row_scale ? p.row_scale[row] : 1.0f;
   const float g = p.dloss ? p.dloss[row] * p.temp : p.temp;
-  const RowUnit unit = row_unit(g, ec);
+  const RowUnit unit = row_unit(p, row, g, most, ec);
   if (threadIdx.x == 0) {
     p.factor[i] = logit_factor(p, row);
     if (p.labels) p.label[i] = (int)p.labels[row];
@@ -204,7 +205,7 @@ __device__ __forceinline__ void gather_row(const LossParams& p, int64_t i, int64
       p.dx_factor[i] = ldexpf(1.0f, unit.dz - ec);
     }
   }
-  const float rf = p.xw ? ldexpf(r, unit.x - er) : 1.0f;
+  const float rf = ldexpf(1.0f, unit.x);
   for (int c = threadIdx.x; c < chunks; c += 256) {
     const u4 v = load_tail8(p.x_fmt, p.x, row * p.ldx + 8 * c, p.D - 8 * c);
     *(u4*)((uint16_t*)p.xc + i * p.ldxc + 8 * c) = v;
@@ -219,16 +220,16 @@ __device__ __forceinline__ void gather_row(const LossParams& p, int64_t i, int64
 // Bound: the bytes (16384 x 4096, 8 bits to F16: 201 MB in 51 us).
 __global__ __launch_bounds__(256) void loss_gather_kernel(LossParams p) {
   const int count = (int)p.hdr[LOSS_COUNT];
-  const int ec = hdr_exponent(p.hdr, LOSS_CMAX), er = hdr_exponent(p.hdr, LOSS_RMAX);
-  for (int64_t i = blockIdx.x; i < count; i += gridDim.x) gather_row(p, i, p.rows[i], ec, er);
+  const int ec = hdr_exponent(p.hdr, LOSS_CMAX), most = (int)p.hdr[LOSS_WEIGHT];
+  for (int64_t i = blockIdx.x; i < count; i += gridDim.x) gather_row(p, i, p.rows[i], ec, most);
 }
 
 // loss_scan_kernel and loss_gather_kernel in one for at most 128 rows, which every workgroup
 // (a row's) scans for itself: 5 us, where two launches took 9. The first one keeps what the
 // scan found.
 __global__ __launch_bounds__(256) void loss_few_gather_kernel(LossParams p) {
-  __shared__ int rows[kLossFewRows], sums[2];
-  __shared__ float cs[2], rs[2];
+  __shared__ int rows[kLossFewRows], sums[2], ws[2];
+  __shared__ float cs[2];
   const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
   static_assert(kLossFewRows == 128, "two waves scan");
   bool on = false;
@@ -236,16 +237,18 @@ __global__ __launch_bounds__(256) void loss_few_gather_kernel(LossParams p) {
   if (i < 128) {
     const bool in = i < p.R;
     const int64_t label = p.labels && in ? p.labels[i] : -1;
-    const float g = p.dloss && in ? p.dloss[i] : 1.0f, r = p.row_scale && in ? p.row_scale[i] : 0.0f;
+    const float g = p.dloss && in ? p.dloss[i] : 1.0f;
     on = (p.labels ? label >= 0 && label < p.V : in && p.top_on[i] != 0) && g != 0.0f;
     mask = __ballot(on);
     const float a = fabsf(g * p.temp);
-    const float c = wave_max(on && a < __builtin_inff() ? a : 0.f), rm = wave_max(on ? r : 0.f);
-    if (lane == 0) sums[wave] = (int)__popcll(mask), cs[wave] = c, rs[wave] = rm;
+    const float c = wave_max(on && a < __builtin_inff() ? a : 0.f);
+    const int most = wave_max(on ? row_weight(p, i, g * p.temp) : 0);
+    if (lane == 0) sums[wave] = (int)__popcll(mask), cs[wave] = c, ws[wave] = most;
   }
   __syncthreads();
   const int count = sums[0] + sums[1];
-  const float c = fmaxf(cs[0], cs[1]), r = fmaxf(rs[0], rs[1]);
+  const float c = fmaxf(cs[0], cs[1]);
+  const int most = max(ws[0], ws[1]);
   if (i < 128) {
     const int to = (wave ? sums[0] : 0) + (int)__popcll(mask & (((uint64_t)1 << lane) - 1));
     if (on) rows[to] = i;
@@ -257,12 +260,12 @@ __global__ __launch_bounds__(256) void loss_few_gather_kernel(LossParams p) {
   if (blockIdx.x == 0 && i == 0) {
     p.hdr[LOSS_COUNT] = (uint32_t)count;
     p.hdr[LOSS_CMAX] = __float_as_uint(c);
-    p.hdr[LOSS_RMAX] = __float_as_uint(r);
+    p.hdr[LOSS_WEIGHT] = (uint32_t)most;
     p.hdr[LOSS_AMAX_DX] = p.hdr[LOSS_AMAX_DW] = 0u;
   }
   __syncthreads();
   if ((int)blockIdx.x < count)
-    gather_row(p, blockIdx.x, rows[blockIdx.x], c > 0.f ? floor_log2_bits(__float_as_uint(c)) : 0, r > 0.f ? floor_log2_bits(__float_as_uint(r)) : 0);
+    gather_row(p, blockIdx.x, rows[blockIdx.x], c > 0.f ? floor_log2_bits(__float_as_uint(c)) : 0, most);
 }
 
 // n rows of w from v0 on as F16, D rounded up to 8 columns: where 8-bit rows, or those of F16,
@@ -864,7 +867,6 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
       g.amax = parts_dw ? nullptr : p.hdr + LOSS_AMAX_DW;
       g.s0 = p.s_dloss;
       g.s1 = p.s_x;
-      g.rowscaled = p.row_scale != nullptr;
       const int64_t tiles = (int64_t)((n + 255) / 256) * ((p.D + 255) / 256) * p.dw_splits;
       TRY(launch_loss_grads(g, LOSS_DW, grid_for(tiles), s));
     }

@@ -69,28 +69,39 @@ __device__ __forceinline__ float wave_max(float v) {
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
 }
+__device__ __forceinline__ int wave_max(int v) {
+  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+  return v;
+}
 
 __device__ __forceinline__ int hdr_exponent(const uint32_t* hdr, int word) {
   return hdr[word] == 0u ? 0 : floor_log2_bits(hdr[word]);
 }
 
+// Exponent of a row's weight in dw, biased; 0 where g (times T) is 0 or not finite.
+__device__ __forceinline__ int row_weight(const LossParams& p, int64_t row, float g) {
+  const uint32_t a = __float_as_uint(fabsf(g));
+  if (a == 0u || a >= 0x7F800000u) return 0;
+  return floor_log2_bits(a) + pow2_exponent(p.row_scale ? p.row_scale + row : nullptr) + kWeightBias;
+}
 // The powers of two of a row with the upstream gradient g (times T): out of dz, and on x for dw.
-// top: the exponent of the largest of them. (What is 0 or not finite loses nothing.)
+// most: the largest row_weight. (Rows whose g is 0 or not finite keep x.)
 struct RowUnit {
   int dz, x;
 };
-__device__ __forceinline__ RowUnit row_unit(float g, int top) {
-  const uint32_t a = __float_as_uint(fabsf(g));
-  if (a == 0u || a >= 0x7F800000u) return {top, 0};
-  const int e = floor_log2_bits(a), below = top - e, share = min(below, kLossShare);
-  return {e + share, share - below};
+__device__ __forceinline__ RowUnit row_unit(const LossParams& p, int64_t row, float g, int most, int ec) {
+  const int w = row_weight(p, row, g);
+  if (w == 0) return {ec, 0};
+  const int below = most - w, share = min(below, kLossShare);
+  return {floor_log2_bits(__float_as_uint(fabsf(g))) + share, share - below};
 }
+// Unit of dw's products less that of dz.
+__device__ __forceinline__ int hdr_weight(const uint32_t* hdr) { return hdr[LOSS_WEIGHT] == 0u ? 0 : (int)hdr[LOSS_WEIGHT] - kWeightBias; }
 
 // Unit of the products: a gradient's data in its propagated scale is the product times
 // 2^unit.
 __device__ __forceinline__ int unit_of(const LossParams& p, bool dw) {
-  const int u = hdr_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2;
-  return dw && p.row_scale ? u + hdr_exponent(p.hdr, LOSS_RMAX) : u;
+  return (dw ? hdr_weight(p.hdr) : hdr_exponent(p.hdr, LOSS_CMAX)) - kLossGradLog2;
 }
 __device__ __forceinline__ int base_of(const LossParams& p, bool dw) { return pow2_exponent(p.s_dloss) + pow2_exponent(dw ? p.s_x : p.s_w); }
 __device__ __forceinline__ int out_exponent(const LossParams& p, bool dw, int base, int unit) {

@@ -344,7 +344,7 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
   float d_scale = 1.0f, d_inv = 1.0f;
   if constexpr (EPI == LOSS_DW) {
     if constexpr (OF != FORM_F32 && OF != FORM_STICKY) {  // the scale is known: codes at once
-      const int unit = hdr_exponent(p.hdr, LOSS_CMAX) - kLossGradLog2 + (p.rowscaled ? hdr_exponent(p.hdr, LOSS_RMAX) : 0);
+      const int unit = hdr_weight(p.hdr) - kLossGradLog2;
       const int base = pow2_exponent(p.s0) + pow2_exponent(p.s1);
       e_out = clamp_e8m0(base);
       d_shift = e_out - base - unit;

@@ -83,3 +83,28 @@ def test_upstream_gradients_of_many_magnitudes(R, top, fx):
     want = bounds(ref.Loss(X, W, None, *case), g, None, lse, -5)
     ref.check_gradient(dx, want[0], want[2], 0, sc.RESCALE_AMAX, 14)
     ref.check_gradient(dw, want[1], want[3], -5, sc.RESCALE_AMAX, 14)
+
+
+@pytest.mark.parametrize("fx", [F16, E4M3])
+@pytest.mark.parametrize("top", [0, 5])
+@pytest.mark.parametrize("R", [24, 90, 160])
+def test_row_scales_of_many_magnitudes(R, top, fx):
+    """Rows of small scales, alone with their tokens: the others, sure of a token of their own
+    (and wrong), leave those no gradient."""
+    say(f"loss row scales {R} {top} {fx}")
+    V, D = 300, 64
+    e = torch.tensor([0.0, -10.0, -20.0, -26.0])[torch.arange(R) % 4]
+    w = lr.values(V, D, F16, 5)
+    x = lr.values(R, D, F16, 6).float()
+    sure = e == 0
+    x[sure] = w[:R][sure].float()            # (z of about D, where the others' are of about 8)
+    labels, teacher, index = inputs(R, 100, top, 7)
+    what = labels if labels is not None else index
+    what += 200                              # (no row is sure of these)
+    what[sure.to(DEV)] = (torch.arange(R) % 100 + 100).to(DEV)[sure.to(DEV)].reshape(-1, *([1] * (what.dim() - 1)))
+    X, W, row = lr.scaled(x.to(lr.TORCH[fx]), fx, 0), lr.scaled(w, F16, 0), torch.exp2(e).to(DEV)
+    g = torch.ones(R, device=DEV)
+    lse, dx, dw = run(X, W, row, labels, teacher, index, g, 14)
+    want = bounds(ref.Loss(X, W, row, labels, teacher, index), g, row, lse, 0)
+    ref.check_gradient(dx, want[0], want[2], 0, sc.RESCALE_AMAX, 14)
+    ref.check_gradient(dw, want[1], want[3], 0, sc.RESCALE_AMAX, 14)
