@@ -55,6 +55,12 @@ __device__ __forceinline__ void raise_amax(uint32_t* word, float a) {
   const uint32_t u = __float_as_uint(a);
   if (a > 0.f && u > __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(word, u);
 }
+// A sum's terms 2^(x f - m2) are taken with one rounding, that of x f left out; it may come to
+// half a step of m2, the rounded largest x f, which m2 + log2(sum) so makes good. From here on
+// that could end fp32's exponents: such a row's differences are formed first.
+constexpr float kLargeLogit = 0x1p28f;
+__device__ __forceinline__ bool is_large(float m2) { return fabsf(m2) >= kLargeLogit; }
+
 // (m, n) and (mo, no), maxima (base 2; -Inf where there is nothing) and sums, as one. A NaN
 // is in the sums.
 __device__ __forceinline__ void join_sums(float& m, float& n, float mo, float no) {

@@ -96,9 +96,10 @@ __device__ __forceinline__ void finish_few(const LossParams& p, const float* z, 
   for (int o = 1; o < SH; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   const float f = in ? logit_factor(p, place) : 0.f;
   const float m2 = top == -__builtin_inff() || top != top ? 0.f : top * f;
+  const bool large = is_large(m2);
   float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[i], f, -m2));
+  for (int i = 0; i < PER; ++i) sum += __builtin_amdgcn_exp2f(large ? (v[i] - top) * f : __builtin_fmaf(v[i], f, -m2));
 #pragma unroll
   for (int o = 1; o < SH; o <<= 1) sum += __shfl_xor(sum, o, 64);
   if (in && share == 0) p.stats[(int64_t)place * gridDim.x + blockIdx.x] = float2{sum == 0.f ? -__builtin_inff() : m2, sum};

@@ -458,17 +458,6 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
           for (int i = 0; i < 4 * NI; ++i)
             if (nb + 16 * (i >> 2) + (i & 3) >= N) x[i] = -__builtin_inff();
         }
-        float top = x[0];
-#pragma unroll
-        for (int i = 1; i < 4 * NI; ++i) top = fmaxf(top, x[i]);
-        // (a factor is positive; values of -Inf alone have the sum 0, and a NaN is in the sum)
-        top = row4_max(top);
-        const float m2 = top == -__builtin_inff() || top != top ? 0.f : top * f;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4 * NI; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -m2));
-        sum = row4_sum(sum);
-        if (lq == 0 && in) p.stats[(int64_t)((p.v0 + n0 + wn) / WTN) * p.R + m] = float2{sum == 0.f ? -__builtin_inff() : m2, sum};
         if constexpr (EPI == LOSS_STATS) {
           const int d = in ? r_i[mi] - (p.v0 + nb) : -1;
           // (the lane that has the label's column: d = 16 ni + i)
@@ -503,6 +492,24 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
             wait_lgkmcnt<0>();
           }
         }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < 4 * NI; ++i) top = fmaxf(top, x[i]);
+        // (a factor is positive; values of -Inf alone have the sum 0, and a NaN is in the sum)
+        top = row4_max(top);
+        const float m2 = top == -__builtin_inff() || top != top ? 0.f : top * f;
+        float less = m2;
+        if (__builtin_expect(__ballot(is_large(m2)) != 0, 0)) {
+          const bool large = is_large(m2);
+          less = large ? 0.f : m2;
+#pragma unroll
+          for (int i = 0; i < 4 * NI; ++i) x[i] = large ? x[i] - top : x[i];
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * NI; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -less));
+        sum = row4_sum(sum);
+        if (lq == 0 && in) p.stats[(int64_t)((p.v0 + n0 + wn) / WTN) * p.R + m] = float2{sum == 0.f ? -__builtin_inff() : m2, sum};
       } else if constexpr (EPI == LOSS_DZ) {
         const float f = r_f[mi], l = r_l[mi], c = r_c[mi];
 #pragma unroll
