@@ -622,7 +622,8 @@ size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D,
  * dx (R x D), dw (V x D): E4M3, E5M2 or F16, layouts as x; either may be NULL, not both.
  * They must not overlap x, w or each other, nor their scales those of x, w, dloss or each
  * other (SCALIFY_ERR_LAYOUT). amax_out: optional device fp32 [2], the statistics of dx and
- * dw. dz_ij is rounded to F16, off by at most 2^-11 of it or 2^-31 |g_i|, each row with a
+ * dw. p has the fp32 rounding of the stored lse, a factor of up to 2^(2^-21 |lse|), and is held
+ * to 1 where that would matter. dz_ij is rounded to F16, off by at most 2^-11 of it or 2^-31 |g_i|, each row with a
  * power of two of its own; for dw, x_i to F16, times a power of two where |g_i|
  * row_scale[i] lies 2^8 or more below the largest of them (exact but where that leaves F16's
  * normal numbers: off by at most what 2^-33 of the largest makes of it). */

@@ -474,7 +474,7 @@ __global__ __launch_bounds__(256) void loss_fix_kernel(LossParams p, int v0, int
     for (int j = 0; j < kTopRegs; ++j) {
       const int e = lane + 64 * j, d = r.token[j] - v0;
       if (e < p.top && r.token[j] >= 0 && d >= 0 && d < n) {
-        const float prob = exp2f(p.picked[row * p.top + e] * kLog2e - l2);
+        const float prob = exp2f(held_log(p.picked[row * p.top + e] * kLog2e - l2, l2));
         ((_Float16*)p.dz)[i * p.ldz + d] = (_Float16)(c * (prob - want[j]));
       }
     }

@@ -61,6 +61,11 @@ __device__ __forceinline__ void raise_amax(uint32_t* word, float a) {
 constexpr float kLargeLogit = 0x1p28f;
 __device__ __forceinline__ bool is_large(float m2) { return fabsf(m2) >= kLargeLogit; }
 
+// A probability 2^(z - l) is at most 1, but l has the roundings of a stored log-sum-exp, 2^-22 of
+// it in all: from here on dz is held to that (F16 would end at 2; a NaN stays).
+constexpr float kLargeSum = 0x1p20f;
+__device__ __forceinline__ float held_log(float arg, float l) { return fabsf(l) >= kLargeSum && arg > 0.f ? 0.f : arg; }
+
 // (m, n) and (mo, no), maxima (base 2; -Inf where there is nothing) and sums, as one. A NaN
 // is in the sums.
 __device__ __forceinline__ void join_sums(float& m, float& n, float mo, float no) {

@@ -76,7 +76,7 @@ __device__ __forceinline__ void finish_few(const LossParams& p, const float* z, 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int t = share * PER + 4 * b + i;
-        float v = c * __builtin_amdgcn_exp2f(__builtin_fmaf(sum_at(t, place), f, -l));
+        float v = c * __builtin_amdgcn_exp2f(held_log(__builtin_fmaf(sum_at(t, place), f, -l), l));
         if (t == label) v -= c;
         y[i] = (_Float16)(t0 + t < p.V ? v : 0.f);
       }

@@ -511,7 +511,13 @@ __global__ __launch_bounds__(256, 1) void loss_gemm_kernel(LossGemm p) {
         sum = row4_sum(sum);
         if (lq == 0 && in) p.stats[(int64_t)((p.v0 + n0 + wn) / WTN) * p.R + m] = float2{sum == 0.f ? -__builtin_inff() : m2, sum};
       } else if constexpr (EPI == LOSS_DZ) {
-        const float f = r_f[mi], l = r_l[mi], c = r_c[mi];
+        float f = r_f[mi], l = r_l[mi];
+        const float c = r_c[mi];
+        if (__builtin_expect(__ballot(fabsf(l) >= kLargeSum) != 0, 0)) {
+#pragma unroll
+          for (int i = 0; i < 4 * NI; ++i) x[i] = held_log(__builtin_fmaf(x[i], f, -l), l);
+          f = 1.f, l = 0.f;
+        }
 #pragma unroll
         for (int i = 0; i < 4 * NI; ++i) x[i] = c * __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -l));
         const int d = r_i[mi] - (p.v0 + nb);  // (no label: below 0)
