@@ -620,8 +620,9 @@ size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D,
  * scalify_layernorm_bwd (AMAX, or NONE: the propagated scales). A row that does not
  * count, or whose g_i is 0, gives 0 and adds nothing, whatever it holds.
  * dx (R x D), dw (V x D): E4M3, E5M2 or F16, layouts as x; either may be NULL, not both.
- * They must not overlap x, w or each other, nor their scales those of x, w, dloss or each
- * other (SCALIFY_ERR_LAYOUT). amax_out: optional device fp32 [2], the statistics of dx and
+ * They must not overlap an operand (x, w, labels, row_scale, lse, dloss; a teacher's) or each
+ * other, nor their scales those of the operands, dloss_scale or each other
+ * (SCALIFY_ERR_LAYOUT). amax_out: optional device fp32 [2], the statistics of dx and
  * dw. p has the fp32 rounding of the stored lse, a factor of up to 2^(2^-21 |lse|), and is held
  * to 1 where that would matter. dz_ij is rounded to F16, off by at most 2^-11 of it or 2^-31 |g_i|, each row with a
  * power of two of its own; for dw, x_i to F16, times a power of two where |g_i|

@@ -343,6 +343,13 @@ bool tokens_overlap(const scalify_scaled_array* a, const scalify_scaled_array* b
   return !(d >= aw && d + bw <= ap);
 }
 
+// Whether a contiguous vector's bytes meet those between a matrix's first and last.
+bool vector_overlaps(const scalify_scaled_array* a, const void* v, int64_t bytes) {
+  if (!v || bytes <= 0 || a->rows == 0 || a->cols == 0) return false;
+  const uint64_t a0 = (uintptr_t)a->data, a1 = a0 + (uint64_t)(((a->rows - 1) * a->ld + a->cols) * elem_bytes(a->dtype));
+  return a0 < (uintptr_t)v + (uint64_t)bytes && (uintptr_t)v < a1;
+}
+
 // ---- losses
 
 // x [R][D], w [V][D] and the optional row scales of x; the numbers of either loss.
@@ -404,9 +411,10 @@ scalify_status loss_forward(LossParams* p, void* workspace, size_t workspace_byt
   return launch_loss_fwd(*p, (hipStream_t)stream) == hipSuccess ? SCALIFY_OK : SCALIFY_ERR_HIP;
 }
 
-// The backward's outputs, and the rest of its call.
+// The backward's outputs, and the rest of its call. A piece of dw is written before the next
+// one reads the operands, so no output may lie over any of them.
 scalify_status loss_backward(LossParams* p, const scalify_scaled_array* x, const scalify_scaled_array* w,
-                             scalify_scaled_array* dx, scalify_scaled_array* dw, int32_t rescale, int32_t target_log2,
+                             const scalify_scaled_array* teacher, scalify_scaled_array* dx, scalify_scaled_array* dw, int32_t rescale, int32_t target_log2,
                              int32_t saturate, float* amax_out, void* workspace, size_t workspace_bytes, void* stream) {
   if (!dx && !dw) return SCALIFY_ERR_NULL;
   if ((dx && !dx->scale) || (dw && !dw->scale)) return SCALIFY_ERR_NULL;
@@ -421,6 +429,13 @@ scalify_status loss_backward(LossParams* p, const scalify_scaled_array* x, const
     if (!y) continue;
     if (tokens_overlap(y, x) || tokens_overlap(y, w)) return SCALIFY_ERR_LAYOUT;
     if (y->scale == x->scale || y->scale == w->scale || y->scale == p->s_dloss) return SCALIFY_ERR_LAYOUT;
+    if (teacher && (tokens_overlap(y, teacher) || y->scale == teacher->scale)) return SCALIFY_ERR_LAYOUT;
+    for (const void* v : {(const void*)p->dloss, (const void*)p->lse, (const void*)p->row_scale})
+      if (vector_overlaps(y, v, 4 * (int64_t)p->R)) return SCALIFY_ERR_LAYOUT;
+    const int64_t entries = (int64_t)p->R * p->top;
+    if (vector_overlaps(y, p->labels, 8 * (int64_t)p->R) || vector_overlaps(y, p->index, 8 * entries) ||
+        vector_overlaps(y, p->picked, 4 * entries))
+      return SCALIFY_ERR_LAYOUT;
   }
   if (dx && dw && (tokens_overlap(dx, dw) || dx->scale == dw->scale)) return SCALIFY_ERR_LAYOUT;
   const bool amax = rescale == SCALIFY_RESCALE_AMAX;
@@ -1214,7 +1229,7 @@ scalify_status scalify_cross_entropy_bwd(const float* dloss, const float* dloss_
   p.s_dloss = dloss_scale;
   p.labels = labels;
   p.lse = (float*)lse;
-  return loss_backward(&p, x, w, dx, dw, rescale, target_log2, saturate, amax_out, workspace, workspace_bytes, stream);
+  return loss_backward(&p, x, w, nullptr, dx, dw, rescale, target_log2, saturate, amax_out, workspace, workspace_bytes, stream);
 }
 
 size_t scalify_distillation_fwd_workspace_size(int64_t R, int64_t V, int64_t D, int64_t top, int32_t w_dtype) {
@@ -1267,7 +1282,7 @@ scalify_status scalify_distillation_bwd(const float* dloss, const float* dloss_s
   p.s_dloss = dloss_scale;
   p.lse = (float*)lse;
   p.picked = (float*)picked;
-  return loss_backward(&p, x, w, dx, dw, rescale, target_log2, saturate, amax_out, workspace, workspace_bytes, stream);
+  return loss_backward(&p, x, w, teacher, dx, dw, rescale, target_log2, saturate, amax_out, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"
