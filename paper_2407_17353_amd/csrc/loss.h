@@ -49,7 +49,7 @@ struct LossParams {
   void *dx, *dw;
   int64_t lddx, lddw;
   int dx_fmt, dw_fmt;
-  float *dx_scale, *dw_scale, *amax_out;
+  float *dx_scale, *dw_scale, *amax_out;  // (a gradient that is asked for has a scale, if maybe no rows)
   int mode, target, sat;
   // workspace; rows that count stand in their order at 0 .. count - 1
   uint32_t* hdr;

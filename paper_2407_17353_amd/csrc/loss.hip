@@ -516,7 +516,7 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(LossParams p, int is_dw) 
 
 // The gradients' scales and statistics.
 __device__ __forceinline__ void write_scale(const LossParams& p, bool dw) {
-  if (!(dw ? p.dw : p.dx)) return;
+  if (!(dw ? p.dw_scale : p.dx_scale)) return;
   const int unit = unit_of(p, dw), base = base_of(p, dw);
   *(dw ? p.dw_scale : p.dx_scale) = pow2_float(out_exponent(p, dw, base, unit));
   if (p.amax_out) p.amax_out[dw ? 1 : 0] = ldexpf(__uint_as_float(p.hdr[dw ? LOSS_AMAX_DW : LOSS_AMAX_DX]), unit);
@@ -829,7 +829,7 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
     if (!p.labels) TRY(launch_one(loss_fix_kernel, groups_for(p.R, 4, 8192), 256, s, p, v0, n));
     const void* w = g.b;
     const int64_t ldw = g.ldb;
-    if (p.dx) {
+    if (p.dx_scale) {
       g.a = p.dz;
       g.lda = 2 * p.ldz;
       g.b = w;
@@ -846,7 +846,7 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
       const int64_t tiles = (int64_t)((p.R + 255) / 256) * ((p.D + 255) / 256) * p.splits;
       TRY(launch_loss_grads(g, LOSS_DX, grid_for(tiles), s));
     }
-    if (p.dw) {
+    if (p.dw_scale) {
       g.a = p.dz;
       g.lda = 2 * p.ldz;
       g.b = p.xw ? p.xw : p.xc;
@@ -889,7 +889,7 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
     return launch_one(parts > 1 ? loss_cast_kernel<true> : loss_cast_kernel<false>, groups_for((int64_t)rows * ((p.D + 15) / 16), 256, 16384), 256, s, p, is_dw,
                       scales, parts);
   };
-  if (p.dx && few) {
+  if (p.dx_scale && few) {
     const unsigned wide = (unsigned)((p.D + 255) / 256);
     const int64_t rows = groups_for(p.R, 1, std::max<int64_t>(1, 512 / wide));
     if (amax) {
@@ -900,10 +900,10 @@ hipError_t launch_loss_bwd(const LossParams& p, hipStream_t s) {
     }
   }
   // (the scales need both statistics: dw's parts are summed before the first cast)
-  const bool cast_dw = p.dw && !few && (amax || parts_dw);
+  const bool cast_dw = p.dw_scale && !few && (amax || parts_dw);
   if (cast_dw) TRY(sum_and_cast(1, p.V, p.dw_splits, 0));
-  if (p.dx && !few) TRY(sum_and_cast(0, p.R, p.splits, late ? 0 : 1));
-  const bool written = !late && p.dx;
+  if (p.dx_scale && !few) TRY(sum_and_cast(0, p.R, p.splits, late ? 0 : 1));
+  const bool written = !late && p.dx_scale;
   return written ? hipSuccess : launch_one(loss_scales_kernel, 1, 2, s, p);
 }
 

@@ -581,7 +581,7 @@ static hipError_t launch_parts(void (*kernel)(LossParams, int), const LossParams
 
 hipError_t launch_loss_few_grads(const LossParams& p, hipStream_t s) {
   const int nt = p.R <= 32 ? 1 : (p.R <= 64 ? 2 : 4);
-  if (p.dx) {
+  if (p.dx_scale) {
     const bool w16 = p.w_fmt == kF16;
     const hipError_t e = launch_parts(nt == 1   ? (w16 ? loss_few_dx_kernel<true, 1> : loss_few_dx_kernel<false, 1>)
                                       : nt == 2 ? (w16 ? loss_few_dx_kernel<true, 2> : loss_few_dx_kernel<false, 2>)
@@ -589,7 +589,7 @@ hipError_t launch_loss_few_grads(const LossParams& p, hipStream_t s) {
                                       p, p.splits, s);
     if (e != hipSuccess) return e;
   }
-  if (!p.dw) return hipSuccess;
+  if (!p.dw_scale) return hipSuccess;
   // parts: 4 workgroups for each CU
   const int tiles = (p.D + 127) / 128;
   const int parts = std::max(1, std::min((p.V + 63) / 64, 4 * gemm4_grid(1 << 30) / tiles));
