@@ -115,8 +115,7 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
   float c = 0.f;
   for (int64_t at = lo; at < hi; at += 256) {
     bool on[4];
-    float g[4];
-    int w[4];
+    float g[4], r[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t i = at + 64 * j + lane;
@@ -124,7 +123,7 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
       const int64_t label = p.labels && in ? p.labels[i] : -1;
       const int flag = !p.labels && in ? p.top_on[i] : 0;
       g[j] = p.dloss && in ? p.dloss[i] : 1.0f;
-      w[j] = in ? row_weight(p, i, g[j] * p.temp) : 0;
+      r[j] = p.row_scale && in ? p.row_scale[i] : 1.0f;
       on[j] = (p.labels ? label >= 0 && label < p.V : flag != 0) && g[j] != 0.0f;
     }
 #pragma unroll
@@ -137,7 +136,7 @@ __global__ __launch_bounds__(1024) void loss_scan_kernel(LossParams p) {
       if (on[j]) {
         const float a = fabsf(g[j] * p.temp);
         if (a < __builtin_inff()) c = fmaxf(c, a);
-        most = max(most, w[j]);
+        most = max(most, row_weight(g[j] * p.temp, r[j]));
       }
     }
   }
@@ -195,7 +194,7 @@ __device__ __forceinline__ u4 load_tail8(int fmt, const void* base, int64_t e, i
 __device__ __forceinline__ void gather_row(const LossParams& p, int64_t i, int64_t row, int ec, int most) {
   const int chunks = (p.D + 7) / 8;
   const float g = p.dloss ? p.dloss[row] * p.temp : p.temp;
-  const RowUnit unit = row_unit(p, row, g, most, ec);
+  const RowUnit unit = row_unit(g, p.row_scale ? p.row_scale[row] : 1.0f, most, ec);
   if (threadIdx.x == 0) {
     p.factor[i] = logit_factor(p, row);
     if (p.labels) p.label[i] = (int)p.labels[row];
@@ -237,12 +236,12 @@ __global__ __launch_bounds__(256) void loss_few_gather_kernel(LossParams p) {
   if (i < 128) {
     const bool in = i < p.R;
     const int64_t label = p.labels && in ? p.labels[i] : -1;
-    const float g = p.dloss && in ? p.dloss[i] : 1.0f;
+    const float g = p.dloss && in ? p.dloss[i] : 1.0f, r = p.row_scale && in ? p.row_scale[i] : 1.0f;
     on = (p.labels ? label >= 0 && label < p.V : in && p.top_on[i] != 0) && g != 0.0f;
     mask = __ballot(on);
     const float a = fabsf(g * p.temp);
     const float c = wave_max(on && a < __builtin_inff() ? a : 0.f);
-    const int most = wave_max(on ? row_weight(p, i, g * p.temp) : 0);
+    const int most = wave_max(on ? row_weight(g * p.temp, r) : 0);
     if (lane == 0) sums[wave] = (int)__popcll(mask), cs[wave] = c, ws[wave] = most;
   }
   __syncthreads();

@@ -89,19 +89,20 @@ __device__ __forceinline__ int hdr_exponent(const uint32_t* hdr, int word) {
   return hdr[word] == 0u ? 0 : floor_log2_bits(hdr[word]);
 }
 
-// Exponent of a row's weight in dw, biased; 0 where g (times T) is 0 or not finite.
-__device__ __forceinline__ int row_weight(const LossParams& p, int64_t row, float g) {
+// Exponent of a row's weight in dw, biased; 0 where g (times T) is 0 or not finite. r: its row
+// scale.
+__device__ __forceinline__ int row_weight(float g, float r) {
   const uint32_t a = __float_as_uint(fabsf(g));
-  if (a == 0u || a >= 0x7F800000u) return 0;
-  return floor_log2_bits(a) + pow2_exponent(p.row_scale ? p.row_scale + row : nullptr) + kWeightBias;
+  const int w = floor_log2_bits(a) + pow2_exponent(&r) + kWeightBias;
+  return a == 0u || a >= 0x7F800000u ? 0 : w;
 }
-// The powers of two of a row with the upstream gradient g (times T): out of dz, and on x for dw.
-// most: the largest row_weight. (Rows whose g is 0 or not finite keep x.)
+// The powers of two of such a row: out of dz, and on x for dw. most: the largest row_weight.
+// (Rows whose g is 0 or not finite keep x.)
 struct RowUnit {
   int dz, x;
 };
-__device__ __forceinline__ RowUnit row_unit(const LossParams& p, int64_t row, float g, int most, int ec) {
-  const int w = row_weight(p, row, g);
+__device__ __forceinline__ RowUnit row_unit(float g, float r, int most, int ec) {
+  const int w = row_weight(g, r);
   if (w == 0) return {ec, 0};
   const int below = most - w, share = min(below, kLossShare);
   return {floor_log2_bits(__float_as_uint(fabsf(g))) + share, share - below};
