@@ -576,9 +576,9 @@ scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
  *   distillation:  q_i = softmax_k(s_t t_ik / T) over the teacher's entries of the row,
  *     loss_i = T^2 sum_k q_ik (log q_ik - z_i,index[i][k] + lse_i)
  * A row counts if its label lies in [0, V), for distillation if one of its tokens does
- * with a teacher's logit above -Inf. The others' loss, lse and logits are 0, and of them
- * nothing else is read. Entries of the teacher whose token lies outside [0, V) are not
- * there; those of one token add up.
+ * with a teacher's logit above -Inf. The others' loss, lse and logits are 0, and whatever
+ * their rows of x hold reaches nothing. Entries of the teacher whose token lies outside [0,
+ * V) are not there; those of one token add up.
  * x, w: E4M3, E5M2 or F16, any mix; trans = 0, rows 16-byte aligned (ld a multiple of 16
  * bytes), 1 <= D <= 2^20, rows of w below 2^23 bytes. row_scale (optional device fp32
  * [R], powers of two, 4-byte aligned): the a_channel_scale of x, as scalify_rmsnorm_fwd
@@ -587,7 +587,8 @@ scalify_status scalify_attention_bwd(const scalify_scaled_array* dout,
  * x 256 (R x V and V x D; 2^24 of R x D) (SCALIFY_ERR_SHAPE).
  * Products are F16 with fp32 sums (8-bit values are F16 values), statistics fp32.
  * Deterministic on one device: every sum has a fixed order. No call synchronises;
- * which rows count is found on the device, and work goes by their number. */
+ * which rows count is found on the device, and the products go by their number (with up
+ * to 128 rows, by R: they cost the bytes of w). */
 
 /* Bytes of device workspace scalify_cross_entropy_fwd needs: 8 bytes for each row and 64
  * tokens with up to 128 rows, else a copy of x in F16, 8 bytes for each row and 128
@@ -623,11 +624,11 @@ size_t scalify_cross_entropy_bwd_workspace_size(int64_t R, int64_t V, int64_t D,
  * They must not overlap an operand (x, w, labels, row_scale, lse, dloss; a teacher's) or each
  * other, nor their scales those of the operands, dloss_scale or each other
  * (SCALIFY_ERR_LAYOUT). amax_out: optional device fp32 [2], the statistics of dx and
- * dw. p has the fp32 rounding of the stored lse, a factor of up to 2^(2^-21 |lse|), and is held
- * to 1 where that would matter. dz_ij is rounded to F16, off by at most 2^-11 of it or 2^-31 |g_i|, each row with a
- * power of two of its own; for dw, x_i to F16, times a power of two where |g_i|
- * row_scale[i] lies 2^8 or more below the largest of them (exact but where that leaves F16's
- * normal numbers: off by at most what 2^-33 of the largest makes of it). */
+ * dw. p has the fp32 roundings of the stored lse, a factor of up to 2^(2^-21 |lse|), and is
+ * held to 1 where that would matter. dz_ij is rounded to F16, with a power of two of its row's
+ * own: off by at most 2^-11 of it or 2^-31 |g_i|. For dw, row_scale[i] x_i is F16 as well, exact
+ * where |g_i| row_scale[i] is at least 2^-8 of the largest of them, else off by at most 2^-32 of
+ * that over |g_i|. */
 scalify_status scalify_cross_entropy_bwd(const float* dloss, const float* dloss_scale,
                                          const scalify_scaled_array* x,
                                          const scalify_scaled_array* w, const int64_t* labels,

@@ -87,7 +87,10 @@ struct LossPlan {
 LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool back, bool amax, LossParams* p, void* base);
 
 // Rows up to which a call goes by the bytes of w (loss_few.hip); the backward's dz is then
-// one piece.
+// one piece. This is where those kernels end, not where the tiles begin to win: 128 rows
+// take 0.6 to 0.7 of the time of 129 (32000 x 2048 in F16: forward 36 and 61 us, backward 129
+// and 201; 32000 x 4096 in E4M3 60 and 98, 215 and 300). The host knows the rows, not how many
+// of them count, so a call of more rows takes the tiles however few count.
 constexpr int kLossFewRows = 128;
 inline bool loss_few_bwd(int64_t R, int64_t V) {
   return R <= kLossFewRows && V <= ((int64_t)1 << 22) && R * V <= ((int64_t)1 << 28);

@@ -9,8 +9,13 @@
 // that x would be several bytes for each of w (48 rows of 4096 columns: 79 us, now 35, with w's bytes
 // alone 27): the waves then take 16 tokens each and go through x together, in LDS, the
 // columns of w and x loaded three chunks ahead. Measured (131 MB of w: 27 us at the rate of a
-// large copy): logits of 16 rows, 2048 columns in F16, 26 us; 48 rows, 4096 in 8 bits, 31, of 128
-// rows 56 (LDS reads and the products, 25 us each, meet the bytes).
+// large copy): logits of 16 rows, 2048 columns in F16, 26 us; 48 rows, 4096 in 8 bits, 32, of 128
+// rows 56 (LDS reads and the products, 25 us each, meet the bytes). So with w in the last-level
+// cache from the call before; with another w of six in turn, the calls take 39 us for 30 (16
+// rows) and 44 for 34 (48).
+// The forward goes over every row, those that do not count too (their results are 0, and
+// nothing of them reaches another's); the backward over those that count. Either picks its
+// kernels by the number of rows, all that the host knows.
 #include "attention_dev.h"
 #include "kernels.h"
 #include "loss_dev.h"
@@ -109,6 +114,8 @@ __device__ __forceinline__ void finish_few(const LossParams& p, const float* z, 
       if (d >= share * PER && d < (share + 1) * PER && d + t0 < p.V) p.picked2[place] = sum_at((int)d, place) * f;
     }
   } else {
+    // (the whole list, whose numbers are in the L2 caches: it costs by its length. 128 rows against
+    // 32000 x 2048 in 8 bits 38 us with 8 entries a row, 45 with 64, 76 with 256)
     for (int e = threadIdx.x; e < p.R * p.top; e += 256) {
       const int64_t d = p.index[e] - t0;
       if (d >= 0 && d < FEW_TOKENS && d + t0 < p.V) p.picked[e] = sum_at((int)d, e / p.top) * (logit_factor(p, e / p.top) * kLn2);
@@ -199,7 +206,8 @@ __global__ __launch_bounds__(256) void loss_few_kernel(LossParams p) {
 
 // Up to 16 NP rows, their columns in LDS. Products go by groups of 16 rows, as do LDS reads: NP
 // 3 and 6 beside 2, 4 and 8 (4096 columns in 8 bits, 48 rows: 41 us as 64, 35 as 48; 96 rows 62
-// and 52). (X16 is a template's so that 8-bit rows of x wait in
+// and 52). F16's chunks of 64 columns need an even NP, a whole number of loads a thread; 5 and 7,
+// for 80 and 112 rows of 8 bits, have not been tried. (X16 is a template's so that 8-bit rows of x wait in
 // half the registers: read in either form by a branch, 128 rows against 32000 x 4096 in E4M3
 // took 137 us, now 60.)
 template <int FW, int NP, bool X16, bool BACK>
