@@ -724,7 +724,7 @@ LossPlan loss_plan(int64_t R, int64_t V, int64_t D, int w_fmt, int top, bool bac
   }
   if (p) {
     p->xc = xc;
-    p->xw = back && (p->row_scale || p->dloss) ? xw : nullptr;  // (else x as it is)
+    p->xw = back && p->dw_scale && (p->row_scale || p->dloss) ? xw : nullptr;  // (else x as it is)
     p->w16 = few ? nullptr : w16;
     p->dz = dz;
     p->ldxc = z.ldxc;
